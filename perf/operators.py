@@ -106,8 +106,8 @@ def _pack(x):
     v = v.view(rows, -1, 32)
     m, e = torch.frexp(v.abs().amax(2))
     e = torch.where(m > 0, e - 7 + (m > 127 / 128).int(), torch.full_like(e, -126)).clamp(min=-126)
-    q = torch.round(v * torch.exp2(-e.float())[:, :, None]).view(rows, -1)[:, :cols]
-    return q.to(torch.int8).contiguous(), (e + 127).to(torch.uint8)
+    q = torch.round(v * torch.exp2(-e.float())[:, :, None]).view(rows, -1).to(torch.int8)[:, :cols]
+    return q, (e + 127).to(torch.uint8)   # q's rows lie a multiple of 32 apart
 
 
 def _unpack(q, s):
