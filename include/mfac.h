@@ -372,6 +372,147 @@ mfac_status mfac_static_set_stream(mfac_static s, hipStream_t stream);
 mfac_status mfac_static_status(mfac_static s);
 mfac_status mfac_static_destroy(mfac_static s);
 
+/* ======================================================================
+ * Training operators: layer norm, linear layers, 8-bit activation copies
+ * ======================================================================
+ * The forward and backward passes of a transformer's feed-forward block, for
+ * the models whose gradients the window above takes, with the activations
+ * that the backward pass needs kept in 8 bits next to a window that fills
+ * most of the card's memory. These calls have no handle: each one checks its
+ * arguments on the host (MFAC_EINVAL, MFAC_EWORKSPACE; nothing is enqueued
+ * then), enqueues its kernels on the given stream and returns. Nothing is
+ * allocated, nothing is kept between calls, and a call may be captured into a
+ * HIP graph. Results do not depend on the order in which work-groups run: sums
+ * are joined in a fixed order, without atomics. Infinities and NaN pass through
+ * by the rules of the arithmetic and are not latched as errors.
+ *
+ * Matrices are row-major with unit stride along a row and a leading dimension
+ * (elements between rows) of at least the row's length; pointers are aligned to
+ * the element. The products take 16-bit matrices as they are where the rows
+ * start 16-byte aligned and their length is a multiple of 8 elements, and lay
+ * others out in the workspace first, as they do with fp32 and with 8-bit copies.
+ * Their *_bytes queries therefore take the matrices' addresses (which are not
+ * read) and leading dimensions; x NULL means an 8-bit copy. A query returns 0 on
+ * invalid sizes and where no workspace is needed. Workspaces are 256-byte aligned.
+ * Sizes are at least 0 (rows) or 1 (columns) and at most 2^30, the widths of linear
+ * layers at most 2^21; offsets are 64-bit. rows == 0 is valid: the gradients of
+ * weights are then zero. Inputs and outputs must not overlap unless a call says
+ * so. */
+
+/* Element types. Sums, statistics and the arithmetic between them are fp32 in
+ * every type; a result is rounded once, when it is stored. */
+typedef enum {
+    MFAC_F32 = 0,
+    MFAC_BF16 = 1,
+    MFAC_F16 = 2,
+    MFAC_DTYPE_INT32_ = 0x7fffffff /* not a type: widens the enum to int32 */
+} mfac_dtype;
+
+/* Activations: z, max(z, 0), z Phi(z) (Phi the normal distribution function),
+ * 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))), z / (1 + exp(-z)). */
+typedef enum {
+    MFAC_ACT_NONE = 0,
+    MFAC_ACT_RELU = 1,
+    MFAC_ACT_GELU = 2,
+    MFAC_ACT_GELU_TANH = 3,
+    MFAC_ACT_SILU = 4,
+    MFAC_ACT_INT32_ = 0x7fffffff /* not an activation: widens the enum to int32 */
+} mfac_act;
+
+/* 8-bit copies. Row r of a rows x cols matrix is cut into ceil(cols / 32) groups
+ * of 32 neighbouring columns (the last may be shorter). Group j has the power
+ * 2^e, e >= -126 the smallest with max |x| <= 127 * 2^e; s[r * ceil(cols/32) + j]
+ * = e + 127 and q[r * ldq + c] = x * 2^-e rounded to the nearest integer, ties to
+ * even (for e = 122 at most 63 in magnitude: 64 * 2^122 is no fp32 value). The copy
+ * stands for q * 2^e, off by at most 2^(e-1) (2^e for e = 122). A value with 8 bits
+ * times a power of two is a bf16 value, so bf16 products of it need no second
+ * rounding. A group with an infinity or a NaN has s = 255 and q = 0 and stands
+ * for NaN throughout. Rows of q lie ldq >= cols bytes apart; what is past the cols
+ * of a row is neither read nor written. */
+#define MFAC_PACK8_GROUP 32
+
+/* q, s <- the 8-bit copy of x. */
+mfac_status mfac_pack8(mfac_dtype type, int64_t rows, int64_t cols, const void* x, int64_t ldx, int8_t* q, int64_t ldq,
+                       uint8_t* s, hipStream_t stream);
+
+/* y <- the values a copy stands for, rounded to y's type (exact in fp32 and
+ * bf16; in fp16 values past 65504 become 65504). */
+mfac_status mfac_unpack8(mfac_dtype type, int64_t rows, int64_t cols, const int8_t* q, int64_t ldq, const uint8_t* s,
+                         void* y, int64_t ldy, hipStream_t stream);
+
+/* Layer norm of each row: mean, rstd = 1 / sqrt(mean((x - mean)^2) + eps), xhat =
+ * (x - mean) rstd, y = xhat w + b. w and b (cols values of type wtype: fp32 or x's
+ * type) may be NULL (1 and 0). mean_out and rstd_out (rows fp32 values) may be
+ * NULL. q and s: the 8-bit copy of xhat, or both NULL. eps >= 0, finite. y may
+ * be x. */
+mfac_status mfac_layer_norm(mfac_dtype type, mfac_dtype wtype, int64_t rows, int64_t cols, const void* x, int64_t ldx,
+                            const void* w, const void* b, double eps, void* y, int64_t ldy, float* mean_out,
+                            float* rstd_out, int8_t* q, int64_t ldq, uint8_t* s, hipStream_t stream);
+
+/* Gradients of layer norm: with h = dy w,
+ *   dx = rstd (h - mean(h) - xhat mean(h xhat)) + add,
+ *   dw = sum over rows of dy xhat, db = sum over rows of dy.
+ * xhat is (x - mean) rstd, or the 8-bit copy (q, s), for which x and mean are
+ * NULL. add (type, rows of ldadd) may be NULL: the gradient of a skip connection
+ * around the norm. dw and db (cols values of wtype) may be NULL. dx may be dy
+ * or add. */
+size_t mfac_layer_norm_bwd_workspace_bytes(int64_t rows, int64_t cols);
+mfac_status mfac_layer_norm_bwd(mfac_dtype type, mfac_dtype wtype, int64_t rows, int64_t cols, const void* dy,
+                                int64_t lddy, const void* x, int64_t ldx, const float* mean, const float* rstd,
+                                const int8_t* q, int64_t ldq, const uint8_t* s, const void* w, const void* add,
+                                int64_t ldadd, void* dx, int64_t lddx, void* dw, void* db, void* workspace,
+                                size_t workspace_bytes, hipStream_t stream);
+
+/* Linear layer: z = x W^T + b, y = act(z) + res, for x (rows x cin), W (cout x cin),
+ * y (rows x cout). bias (cout values of btype: fp32 or x's type) and res may be
+ * NULL. z_out (type) or the 8-bit copy of z (q, s) keep the pre-activation for
+ * the backward pass; at most one of the two, both optional. y may be res.
+ * Products: fp16 and bf16 values on the matrix cores with fp32 sums; fp32 values
+ * as three bf16 parts each, of whose nine products the six largest are taken
+ * (what is left out is at most 2^-26 of the product); the parts of a value
+ * above 3.39e38 or an infinite one are not finite together, and its products
+ * come out NaN. Layers of few rows in fp32 multiply in fp32. */
+size_t mfac_linear_workspace_bytes(mfac_dtype type, int64_t rows, int64_t cin, int64_t cout, const void* x,
+                                   int64_t ldx, const void* w, int64_t ldw);
+mfac_status mfac_linear(mfac_dtype type, mfac_dtype btype, mfac_act act, int64_t rows, int64_t cin, int64_t cout,
+                        const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, const void* res,
+                        int64_t ldres, void* y, int64_t ldy, void* z_out, int64_t ldz, int8_t* q, int64_t ldq,
+                        uint8_t* s, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* The activation's part of a backward pass over a rows x cols pre-activation z
+ * (type, or its 8-bit copy):
+ *   dz = dy act'(z) rounded to type, a = act(z) (NULL: not wanted),
+ *   db[c] = sum over rows of dy act'(z) in fp32, before the rounding (NULL: not wanted).
+ * With MFAC_ACT_NONE z, q, s are NULL, and dz may be NULL (it equals dy). dz may
+ * be dy. */
+size_t mfac_act_bwd_workspace_bytes(int64_t rows, int64_t cols);
+mfac_status mfac_act_bwd(mfac_dtype type, mfac_act act, int64_t rows, int64_t cols, const void* dy, int64_t lddy,
+                         const void* z, int64_t ldz, const int8_t* q, int64_t ldq, const uint8_t* s, void* dz,
+                         int64_t lddz, void* a, int64_t lda, float* db, void* workspace, size_t workspace_bytes,
+                         hipStream_t stream);
+
+/* Gradient of a linear layer's input: dx = dz W + add, for dz (rows x cout), W
+ * (cout x cin), dx (rows x cin); add (type) may be NULL. dx may be add. */
+size_t mfac_linear_bwd_input_workspace_bytes(mfac_dtype type, int64_t rows, int64_t cin, int64_t cout, const void* dz,
+                                             int64_t lddz, const void* w, int64_t ldw);
+mfac_status mfac_linear_bwd_input(mfac_dtype type, int64_t rows, int64_t cin, int64_t cout, const void* dz,
+                                  int64_t lddz, const void* w, int64_t ldw, const void* add, int64_t ldadd, void* dx,
+                                  int64_t lddx, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Gradient of a linear layer's weight: dW = dz^T x (cout x cin, type gtype: fp32
+ * or the inputs' type). x (rows x cin) is given in `type`, or as an 8-bit copy (q,
+ * s; x NULL). gamma and beta (cin fp32 values each, or both NULL) say that the
+ * layer's input was gamma x + beta, the affine part of a layer norm whose xhat
+ * is x: dW = (dz^T x) diag(gamma) + db beta^T, for which db (cout fp32 values, the
+ * column sums of dz) is needed; it may be NULL otherwise. */
+size_t mfac_linear_bwd_weight_workspace_bytes(mfac_dtype type, int64_t rows, int64_t cin, int64_t cout,
+                                              const void* dz, int64_t lddz, const void* x, int64_t ldx);
+mfac_status mfac_linear_bwd_weight(mfac_dtype type, mfac_dtype gtype, int64_t rows, int64_t cin, int64_t cout,
+                                   const void* dz, int64_t lddz, const void* x, int64_t ldx, const int8_t* q,
+                                   int64_t ldq, const uint8_t* s, const float* gamma, const float* beta,
+                                   const float* db, void* dw, int64_t lddw, void* workspace, size_t workspace_bytes,
+                                   hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

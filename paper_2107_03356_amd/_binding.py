@@ -25,6 +25,8 @@ MFAC_ESTATE = -5
 MFAC_EPRECISION = -6
 MFAC_STATIC_TRACE = 1
 MFAC_STATIC_FP32 = 2
+MFAC_F32, MFAC_BF16, MFAC_F16 = 0, 1, 2
+MFAC_ACT_NONE, MFAC_ACT_RELU, MFAC_ACT_GELU, MFAC_ACT_GELU_TANH, MFAC_ACT_SILU = range(5)
 
 _c = ctypes
 _VP, _I32, _I64, _SZ, _F32, _F64 = _c.c_void_p, _c.c_int32, _c.c_int64, _c.c_size_t, _c.c_float, _c.c_double
@@ -68,6 +70,25 @@ SIGNATURES = {
     "mfac_static_set_stream": (_c.c_int, [_VP, _VP]),
     "mfac_static_status": (_c.c_int, [_VP]),
     "mfac_static_destroy": (_c.c_int, [_VP]),
+    "mfac_pack8": (_c.c_int, [_I32, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _VP]),
+    "mfac_unpack8": (_c.c_int, [_I32, _I64, _I64, _VP, _I64, _VP, _VP, _I64, _VP]),
+    "mfac_layer_norm": (_c.c_int, [_I32, _I32, _I64, _I64, _VP, _I64, _VP, _VP, _F64, _VP, _I64, _VP, _VP, _VP, _I64,
+                                   _VP, _VP]),
+    "mfac_layer_norm_bwd_workspace_bytes": (_SZ, [_I64, _I64]),
+    "mfac_layer_norm_bwd": (_c.c_int, [_I32, _I32, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _VP, _I64, _VP, _VP,
+                                       _VP, _I64, _VP, _I64, _VP, _VP, _VP, _SZ, _VP]),
+    "mfac_linear_workspace_bytes": (_SZ, [_I32, _I64, _I64, _I64, _VP, _I64, _VP, _I64]),
+    "mfac_linear": (_c.c_int, [_I32, _I32, _I32, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _I64, _VP, _I64,
+                               _VP, _I64, _VP, _I64, _VP, _VP, _SZ, _VP]),
+    "mfac_act_bwd_workspace_bytes": (_SZ, [_I64, _I64]),
+    "mfac_act_bwd": (_c.c_int, [_I32, _I32, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _I64, _VP, _I64,
+                                _VP, _VP, _SZ, _VP]),
+    "mfac_linear_bwd_input_workspace_bytes": (_SZ, [_I32, _I64, _I64, _I64, _VP, _I64, _VP, _I64]),
+    "mfac_linear_bwd_input": (_c.c_int, [_I32, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _SZ,
+                                         _VP]),
+    "mfac_linear_bwd_weight_workspace_bytes": (_SZ, [_I32, _I64, _I64, _I64, _VP, _I64, _VP, _I64]),
+    "mfac_linear_bwd_weight": (_c.c_int, [_I32, _I32, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _VP,
+                                          _VP, _VP, _I64, _VP, _SZ, _VP]),
 }
 
 _lib = None

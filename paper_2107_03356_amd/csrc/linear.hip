@@ -1,0 +1,557 @@
+// Matrix products of a linear layer and its gradients, C (M x N) = A B^T over K:
+//
+//   forward   y = act(x W^T + b) + res     A = x [m][k],   B = W [n][k]
+//   input     dx = dz W + add              A = dz [m][k],  B = W [k][n]
+//   weight    dW = dz^T x                  A = dz [k][m],  B = x [k][n]
+//
+// Three kernels share one epilogue:
+//   k_product  16-bit operands on v_mfma_f32_16x16x32, tiles of C in registers,
+//              operand tiles copied from memory straight into LDS;
+//   k_skinny   few rows of C: W streams through registers once, no LDS;
+//   k_finish   joins the K parts of a product that was split over work-groups.
+// Operands that the copies into LDS cannot take as they are (rows that do not start
+// 16-byte aligned, 8-bit copies, fp32) are laid out first in the workspace: fp32 as
+// three bf16 planes, hi + mid + lo, of whose nine products six are summed (the
+// others are at most 2^-26 of |a b| together).
+#include <algorithm>
+
+#include "internal.h"
+#include "train.h"
+#include "train_util.h"
+
+namespace mfac {
+namespace {
+
+typedef float v4 __attribute__((ext_vector_type(4)));
+typedef int i4 __attribute__((ext_vector_type(4)));
+
+// ---------------------------------------------------------------- epilogue
+__device__ __forceinline__ f8 load8_dt(const void* p, int dt, int64_t off, int64_t c, int64_t cols) {
+    if (dt == DT_F32) return load8((const float*)p + off, c, cols);
+    if (dt == DT_BF16) return load8((const bf16*)p + off, c, cols);
+    return load8((const f16*)p + off, c, cols);
+}
+__device__ __forceinline__ void store8_dt(void* p, int dt, int64_t off, int64_t c, int64_t cols, f8 v) {
+    if (dt == DT_F32) store8((float*)p + off, c, cols, v);
+    else if (dt == DT_BF16) store8((bf16*)p + off, c, cols, v);
+    else store8((f16*)p + off, c, cols, v);
+}
+
+// The sums c at (m, n .. n + 7) become outputs. Four neighbouring lanes hold 32
+// neighbouring n of one row; every lane of a wave takes part (in: whether m is a row).
+__device__ __forceinline__ void finish8(const Epilogue& e, int64_t N, bool in, int64_t m, int64_t n, f8 c) {
+    if (!in) n = N;
+    if (e.bias) c += load8_dt(e.bias, e.bias_dt, 0, n, N);
+    if (e.gamma) {
+        const float d = in ? e.db[m] : 0.f;
+        c = c * load8(e.gamma, n, N) + d * load8(e.beta, n, N);
+    }
+    if (e.p.q) {
+        f8 v = c;
+        if (n + 8 > N)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (n + i >= N) v[i] = 0.f;
+        pack_group(e.p.q + m * e.p.ldq, e.p.s + m * ((N + 31) / 32), n, N, v);
+    }
+    if (n >= N) return;
+    if (e.z) store8_dt(e.z, e.io_dt, m * e.ldz, n, N, c);
+    with_act(e.act, [&](auto tag) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = act_of<decltype(tag)::value>(c[i]);
+    });
+    if (e.add) c += load8_dt(e.add, e.io_dt, m * e.ldadd, n, N);
+    store8_dt(e.out, e.out_dt, m * e.ldo, n, N, c);
+}
+
+// ---------------------------------------------------------------- large products
+// Operand tile of R rows (of C's m or n) by 64 k in LDS, 16-byte pieces.
+// [row][k] in memory: row r at piece 8 r, its piece p at p ^ (r & 7): the 16 rows that a
+// fragment read touches at one p then lie in all banks. [k][row] in memory: k at piece
+// k R/8, its piece p at p ^ 2 f(k), f(k) = (k & 3) | (k >> 1 & 4): the eight k that
+// half a wave's transposing read touches lie in all banks.
+constexpr int BK = 64;
+constexpr unsigned OUT_OF_RANGE = 0x80000000u;   // past every buffer's size: the copy writes zeros
+
+__device__ __forceinline__ int col_swizzle(int k) { return ((k & 3) | (k >> 1 & 4)) << 1; }
+
+struct GemmArgs {
+    const char *A, *B;       // 16-bit elements
+    int64_t lda, ldb;        // bytes
+    int64_t apl, bpl;        // bytes between planes
+    int M, N, K;
+    int ksteps, nseg;        // 64-wide steps over K, and how often K is gone over (pairs of planes)
+    unsigned pa, pb;         // planes of the pairs, 4 bits each
+    int tiles_m, tiles_n, splits;
+    float* part;             // [splits][M][N] sums, where splits > 1
+    Epilogue e;
+};
+
+// What a thread copies of an operand tile: NI pieces, NT * 16 bytes apart in LDS.
+template <int R, int NT, bool COL>
+struct Copier {
+    static constexpr int NI = R * BK / 8 / NT;
+    unsigned off[NI];
+    int k[COL ? NI : 1];
+    int64_t step;   // bytes from one K step to the next
+    __device__ __forceinline__ void init(int t, int row0, int rows, int64_t ld) {
+        if constexpr (COL) {
+            step = BK * ld;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int l = i * NT + t, kk = l / (R / 8), c = ((l % (R / 8)) ^ col_swizzle(kk)) * 8;
+                k[i] = kk;
+                off[i] = row0 + c < rows ? (unsigned)(kk * ld + c * 2) : OUT_OF_RANGE;
+            }
+        } else {
+            step = BK * 2;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int l = i * NT + t, r = l >> 3;
+                const int kc = ((l & 7) ^ (r & 7)) * 8;
+                k[0] = kc;   // the same for every i
+                // a row past the end reads the last one: its sums are not stored
+                off[i] = (unsigned)(min(r, rows - 1 - row0) * ld + kc * 2);
+            }
+        }
+    }
+    // base: the tile's first element at this step; left: K's elements from there on
+    __device__ __forceinline__ void issue(const char* base, int left, char* lds, int wave) const {
+        const __amdgpu_buffer_rsrc_t r =
+            __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)OUT_OF_RANGE, 0x00020000);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const unsigned o = k[COL ? i : 0] < left ? off[i] : OUT_OF_RANGE;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                r, (__attribute__((address_space(3))) void*)(lds + (i * NT + wave * 64) * 16), 16, (int)o, 0, 0, 0);
+        }
+    }
+};
+
+template <typename T>
+struct Frag {
+    typedef typename VecOf<T, 8>::plain type;
+};
+__device__ __forceinline__ v4 mma(VecOf<bf16, 8>::plain a, VecOf<bf16, 8>::plain b, v4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ v4 mma(VecOf<f16, 8>::plain a, VecOf<f16, 8>::plain b, v4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// Fragment of 16 rows (from row0) and k 32 kk .. + 31: lane l holds row l % 16 and eight
+// k from 8 (l / 16).
+template <typename T, int R, bool COL>
+__device__ __forceinline__ typename Frag<T>::type read_frag(const char* lds, int row0, int kk, int lane) {
+    if constexpr (COL) {
+        typedef short s4 __attribute__((ext_vector_type(4)));
+        typedef short s8 __attribute__((ext_vector_type(8)));
+        const int k = kk * 32 + (lane >> 4) * 8 + ((lane & 15) >> 2), r = row0 + 4 * (lane & 3);
+        const int at = k * R * 2 + ((r >> 3) ^ col_swizzle(k)) * 16 + (r & 4) * 2;
+        typedef __attribute__((address_space(3))) s4* P;
+        const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds + at));
+        const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds + at + 4 * R * 2));
+        const s8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        return __builtin_bit_cast(typename Frag<T>::type, v);
+    } else {
+        const int r = row0 + (lane & 15), p = kk * 4 + (lane >> 4);
+        return *reinterpret_cast<const typename Frag<T>::type*>(lds + r * (BK * 2) + (p ^ (r & 7)) * 16);
+    }
+}
+
+// A work-group's TM x TN tile of C, one part of K; each wave (TM/WM) x (TN/WN) of it. The
+// MFMA's rows are n and its columns m, so that a lane's four sums are neighbours in a
+// row of C. FRESH: the sums of a step start from zero and reach the accumulator by
+// fp32 additions; the MFMA cuts what lies below a larger accumulator's last bits,
+// which is too much for fp32 results.
+template <typename T, bool ACOL, bool BCOL, int TM, int TN, int WM, int WN, bool FRESH>
+__global__ __launch_bounds__(WM* WN * 64) void k_product(GemmArgs g) {
+    constexpr int NT = WM * WN * 64, MT = TM / WM / 16, NTL = TN / WN / 16;
+    constexpr int STAGE = (TM + TN) * BK * 2;
+    constexpr int EP_LD = TN + 4, EP_ROWS = 32 * WM;
+    static_assert(EP_ROWS * EP_LD * 4 <= 2 * STAGE, "the epilogue's rows fit the staging buffers");
+    __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+
+    // tile of this work-group: neighbours share an XCD, and go over bands of 8 tile rows
+    const int ntile = g.tiles_m * g.tiles_n;
+    int p = blockIdx.x;
+    if (ntile % 8 == 0) p = (p % 8) * (ntile / 8) + p / 8;
+    constexpr int BAND = 8;
+    const int band = p / (BAND * g.tiles_n), in_band = p % (BAND * g.tiles_n);
+    const int height = min(BAND, g.tiles_m - band * BAND);
+    const int m0 = (band * BAND + in_band % height) * TM, n0 = in_band / height * TN;
+
+    Copier<TM, NT, ACOL> ca;
+    Copier<TN, NT, BCOL> cb;
+    ca.init(t, m0, g.M, g.lda);
+    cb.init(t, n0, g.N, g.ldb);
+    const int64_t a0 = ACOL ? (int64_t)m0 * 2 : m0 * g.lda, b0 = BCOL ? (int64_t)n0 * 2 : n0 * g.ldb;
+
+    const int total = g.ksteps * g.nseg;
+    const int s_begin = (int)((int64_t)total * blockIdx.y / g.splits);
+    const int s_end = (int)((int64_t)total * (blockIdx.y + 1) / g.splits);
+    int seg = s_begin / g.ksteps, ks = s_begin % g.ksteps;
+    auto issue = [&](int stage) {
+        const char* a = g.A + (g.pa >> (4 * seg) & 15) * g.apl + a0 + ks * ca.step;
+        const char* b = g.B + (g.pb >> (4 * seg) & 15) * g.bpl + b0 + ks * cb.step;
+        ca.issue(a, g.K - ks * BK, lds + stage * STAGE, wave);
+        cb.issue(b, g.K - ks * BK, lds + stage * STAGE + TM * BK * 2, wave);
+        if (++ks == g.ksteps) {
+            ks = 0;
+            ++seg;
+        }
+    };
+
+    v4 acc[MT][NTL];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NTL; ++j) acc[i][j] = v4{0.f, 0.f, 0.f, 0.f};
+
+    issue(0);
+    for (int s = s_begin; s < s_end; ++s) {
+        const int stage = (s - s_begin) & 1;
+        // this step's copies have landed for every wave, and every wave has read the other stage
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (s + 1 < s_end) issue(stage ^ 1);
+        const char* la = lds + stage * STAGE;
+        const char* lb = la + TM * BK * 2;
+        v4 fresh[FRESH ? MT : 1][FRESH ? NTL : 1];
+#pragma unroll
+        for (int kk = 0; kk < BK / 32; ++kk) {
+            typename Frag<T>::type fa[MT], fb[NTL];
+#pragma unroll
+            for (int j = 0; j < NTL; ++j) fb[j] = read_frag<T, TN, BCOL>(lb, wn * (TN / WN) + j * 16, kk, lane);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) fa[i] = read_frag<T, TM, ACOL>(la, wm * (TM / WM) + i * 16, kk, lane);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NTL; ++j) {
+                    if constexpr (FRESH) {
+                        const v4 zero = {0.f, 0.f, 0.f, 0.f};
+                        acc[i][j] += mma(fb[j], fa[i], zero);
+                    } else {
+                        acc[i][j] = mma(fb[j], fa[i], acc[i][j]);
+                    }
+                }
+        }
+    }
+
+    // 32 rows of each wave's tile at a time through LDS, so that a row's pieces are stored together
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    float* ep = reinterpret_cast<float*>(lds);
+    float* part = g.splits > 1 ? g.part + (int64_t)blockIdx.y * g.M * g.N : nullptr;
+#pragma unroll
+    for (int q = 0; q < MT / 2; ++q) {
+        if (q) __syncthreads();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < NTL; ++j)
+                *reinterpret_cast<v4*>(&ep[(wm * 32 + h * 16 + (lane & 15)) * EP_LD + wn * (TN / WN) + j * 16 +
+                                           4 * (lane >> 4)]) = acc[2 * q + h][j];
+        __syncthreads();
+        constexpr int PIECES = TN / 8;
+#pragma unroll 1
+        for (int u = t; u < EP_ROWS * PIECES; u += NT) {
+            const int r = u / PIECES, c = (u % PIECES) * 8;
+            const int64_t m = m0 + (r >> 5) * (TM / WM) + q * 32 + (r & 31), n = n0 + c;
+            const f8 v = *reinterpret_cast<const f8*>(&ep[r * EP_LD + c]);
+            if (part) {
+                if (m < g.M) store8(part + m * g.N, n, (int64_t)g.N, v);
+            } else {
+                finish8(g.e, g.N, m < g.M, m, n, v);
+            }
+        }
+    }
+}
+
+// Joins the K parts in order and finishes.
+__global__ __launch_bounds__(256) void k_finish(const float* __restrict__ part, int splits, int64_t M, int64_t N,
+                                                Epilogue e) {
+    const int64_t pieces = (N + 31) / 32 * 4, total = M * pieces;
+    // whole waves go around together (the exchanges of an 8-bit copy)
+    for (int64_t u0 = (int64_t)blockIdx.x * 256; u0 < total; u0 += (int64_t)gridDim.x * 256) {
+        const int64_t u = u0 + threadIdx.x, m = u / pieces, n = (u - m * pieces) * 8;
+        const bool in = m < M;
+        f8 v = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (in)
+            for (int z = 0; z < splits; ++z) v += load8(part + (z * M + m) * N, n, N);
+        finish8(e, N, in, m, n, v);
+    }
+}
+
+// ---------------------------------------------------------------- few rows
+// C (M <= 16 rows) = x W^T. A work-group of 8 waves takes 32 rows of W and one part of K,
+// which its waves share out in pieces of 16 bytes a row; lane l holds row l % 16 of x
+// and of a half of the W rows, and the k of piece l / 16. The waves' sums are joined
+// through LDS. 16-bit types on v_mfma_f32_16x16x32, fp32 on v_mfma_f32_16x16x4.
+template <typename T>
+struct Piece {
+    static constexpr int K = 16 / sizeof(T);   // values in 16 bytes
+    typedef typename VecOf<T, K>::plain type;
+};
+__device__ __forceinline__ v4 mma_piece(VecOf<bf16, 8>::plain a, VecOf<bf16, 8>::plain b, v4 c) { return mma(a, b, c); }
+__device__ __forceinline__ v4 mma_piece(VecOf<f16, 8>::plain a, VecOf<f16, 8>::plain b, v4 c) { return mma(a, b, c); }
+__device__ __forceinline__ v4 mma_piece(VecOf<float, 4>::plain a, VecOf<float, 4>::plain b, v4 c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+}
+
+template <typename T>
+__device__ __forceinline__ typename Piece<T>::type load_piece(const T* __restrict__ row, int64_t k, int64_t K) {
+    constexpr int N = Piece<T>::K;
+    if (k + N <= K) return *reinterpret_cast<const typename VecOf<T, N>::type*>(row + k);
+    typename Piece<T>::type r;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = k + i < K ? row[k + i] : (T)0.f;
+    return r;
+}
+
+struct SkinnyArgs {
+    const void *x, *w;
+    int64_t ldx, ldw, M, N, K;
+    int splits;
+    float* part;
+    Epilogue e;
+};
+
+template <typename T>
+__global__ __launch_bounds__(512) void k_skinny(SkinnyArgs g) {
+    constexpr int KP = 4 * Piece<T>::K;   // k of one MFMA step
+    constexpr int U = 8;                  // steps in flight
+    __shared__ float red[8][32][17];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t n0 = (int64_t)blockIdx.x * 32;
+    const int64_t nsteps = (g.K + KP - 1) / KP;
+    const int64_t nw = 8 * (int64_t)g.splits, me = (int64_t)blockIdx.y * 8 + wave;
+    const int64_t s0 = nsteps * me / nw, s1 = nsteps * (me + 1) / nw;
+    const T* x = (const T*)g.x + min((int64_t)(lane & 15), g.M - 1) * g.ldx;
+    const T* w0 = (const T*)g.w + min(n0 + (lane & 15), g.N - 1) * g.ldw;
+    const T* w1 = (const T*)g.w + min(n0 + 16 + (lane & 15), g.N - 1) * g.ldw;
+    const int64_t kl = (lane >> 4) * Piece<T>::K;
+    v4 c0 = {0.f, 0.f, 0.f, 0.f}, c1 = c0;
+    for (int64_t s = s0; s < s1; s += U) {
+        typename Piece<T>::type xv[U], a[U], b[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t k = s + u < s1 ? (s + u) * KP + kl : g.K;   // past K: zeros
+            a[u] = load_piece(w0, k, g.K);
+            b[u] = load_piece(w1, k, g.K);
+            xv[u] = load_piece(x, k, g.K);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            c0 = mma_piece(a[u], xv[u], c0);
+            c1 = mma_piece(b[u], xv[u], c1);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        red[wave][4 * (lane >> 4) + i][lane & 15] = c0[i];
+        red[wave][16 + 4 * (lane >> 4) + i][lane & 15] = c1[i];
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    const int m = lane >> 2;
+    const int64_t n = n0 + (lane & 3) * 8;
+    f8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float s = 0.f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s += red[q][(lane & 3) * 8 + i][m];
+        v[i] = s;
+    }
+    if (g.splits > 1) {
+        if (m < g.M) store8(g.part + ((int64_t)blockIdx.y * g.M + m) * g.N, n, g.N, v);
+        return;
+    }
+    finish8(g.e, g.N, m < g.M, m, n, v);
+}
+
+// ---------------------------------------------------------------- operands into the workspace
+// dst (rows of ld elements, ld a multiple of 8) <- src, zeros past cols.
+template <typename T>
+__global__ __launch_bounds__(256) void k_lay_out(const T* __restrict__ src, int64_t lds, int64_t rows, int64_t cols,
+                                                 T* __restrict__ dst, int64_t ld) {
+    const int64_t pieces = ld / 8, total = rows * pieces;
+    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
+        const int64_t r = u / pieces, c = (u - r * pieces) * 8;
+        store8(dst + r * ld, c, ld, load8(src + r * lds, c, cols));
+    }
+}
+// The same from fp32 into three bf16 planes, `plane` elements apart.
+__global__ __launch_bounds__(256) void k_lay_out_split(const float* __restrict__ src, int64_t lds, int64_t rows,
+                                                       int64_t cols, bf16* __restrict__ dst, int64_t ld, int64_t plane) {
+    typedef VecOf<bf16, 8>::plain b8;
+    const int64_t pieces = ld / 8, total = rows * pieces;
+    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
+        const int64_t r = u / pieces, c = (u - r * pieces) * 8;
+        f8 x = load8(src + r * lds, c, cols);
+        bf16* d = dst + r * ld + c;
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            const b8 h = __builtin_convertvector(x, b8);
+            *reinterpret_cast<b8*>(d + p * plane) = h;
+            x -= __builtin_convertvector(h, f8);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- host
+constexpr int64_t SKINNY_ROWS = 16;
+constexpr int64_t CUS = 256;
+
+// Rows of `cols` elements that the copies into LDS take as they are.
+bool plain16(const void* p, int64_t ld, int64_t cols) {
+    return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && cols % 8 == 0 && ld <= (int64_t(1) << 21);
+}
+
+struct Operand {
+    bool planes, lay_out;
+    int64_t rows, cols, ld;   // as laid out in memory
+    size_t bytes;             // in the workspace
+};
+Operand operand_of(int dt, const void* p, int64_t ld, bool packed, int64_t rows, int64_t cols) {
+    Operand o{dt == DT_F32 && !packed, true, rows, cols, round_up(cols, 8), 0};
+    o.lay_out = o.planes || packed || !plain16(p, ld, cols);
+    if (!o.lay_out) o.ld = ld;
+    else o.bytes = (size_t)round_up(rows * o.ld * 2 * (o.planes ? 3 : 1), 256);
+    return o;
+}
+
+struct Plan {
+    bool skinny;
+    Operand a, b;
+    int tile, ksteps, nseg, splits;
+    int64_t tiles_m, tiles_n;
+    size_t part_bytes;
+};
+Plan plan_of(int dt, const Product& p) {
+    Plan q{};
+    q.skinny = p.M <= SKINNY_ROWS && !p.a_col && !p.b_col;
+    if (q.skinny) {
+        // parts of K until two work-groups share a CU, each wave with 8 steps at least
+        const int64_t n = ceil_div(p.N, 32), kp = dt == DT_F32 ? 16 : 32;
+        q.splits = (int)std::max<int64_t>(1, std::min(ceil_div(CUS, n), p.K / (kp * 64)));
+    } else {
+        q.a = p.a_col ? operand_of(dt, p.A, p.lda, false, p.K, p.M) : operand_of(dt, p.A, p.lda, false, p.M, p.K);
+        const bool packed = p.bp.q != nullptr;
+        q.b = p.b_col ? operand_of(dt, p.B, p.ldb, packed, p.K, p.N) : operand_of(dt, p.B, p.ldb, packed, p.N, p.K);
+        q.ksteps = (int)ceil_div(p.K, BK);
+        q.nseg = q.a.planes ? (q.b.planes ? 6 : 3) : 1;
+        const int64_t total = (int64_t)q.ksteps * q.nseg;
+        const int64_t t256 = ceil_div(p.M, 256) * ceil_div(p.N, 256);
+        q.tile = t256 >= 160 ? 256 : 128;
+        q.tiles_m = ceil_div(p.M, q.tile);
+        q.tiles_n = ceil_div(p.N, q.tile);
+        q.splits = 1;
+        if (q.tile == 128)
+            q.splits = (int)std::max<int64_t>(1, std::min<int64_t>(2 * CUS / (q.tiles_m * q.tiles_n), total / 4));
+    }
+    q.splits = std::min(q.splits, 64);
+    if (q.splits > 1) q.part_bytes = (size_t)round_up(p.M * p.N * q.splits * 4, 256);
+    return q;
+}
+
+hipError_t lay_out(int dt, const Operand& o, const void* src, int64_t ld, Packed p, void* dst, hipStream_t st) {
+    if (p.q) return launch_unpack8(dt == DT_F16 ? DT_F16 : DT_BF16, o.rows, o.cols, p, dst, o.ld, st);
+    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(o.rows * (o.ld / 8), 256), 4096);
+    if (o.planes)
+        k_lay_out_split<<<grid, 256, 0, st>>>((const float*)src, ld, o.rows, o.cols, (bf16*)dst, o.ld, o.rows * o.ld);
+    else if (dt == DT_BF16)
+        k_lay_out<bf16><<<grid, 256, 0, st>>>((const bf16*)src, ld, o.rows, o.cols, (bf16*)dst, o.ld);
+    else
+        k_lay_out<f16><<<grid, 256, 0, st>>>((const f16*)src, ld, o.rows, o.cols, (f16*)dst, o.ld);
+    return hipGetLastError();
+}
+
+template <typename T, bool ACOL, bool BCOL, bool FRESH>
+hipError_t run_product(const Plan& q, const GemmArgs& g, hipStream_t st) {
+    const dim3 grid((unsigned)(q.tiles_m * q.tiles_n), (unsigned)q.splits);
+    if (q.tile == 256) k_product<T, ACOL, BCOL, 256, 256, 2, 4, FRESH><<<grid, 512, 0, st>>>(g);
+    else k_product<T, ACOL, BCOL, 128, 128, 2, 2, FRESH><<<grid, 256, 0, st>>>(g);
+    return hipGetLastError();
+}
+template <typename T, bool FRESH>
+hipError_t run_product(const Product& p, const Plan& q, const GemmArgs& g, hipStream_t st) {
+    if (p.a_col) return run_product<T, true, true, FRESH>(q, g, st);
+    return p.b_col ? run_product<T, false, true, FRESH>(q, g, st) : run_product<T, false, false, FRESH>(q, g, st);
+}
+
+hipError_t run_finish(const float* part, int splits, int64_t M, int64_t N, const Epilogue& e, hipStream_t st) {
+    const int64_t pieces = ceil_div(N, 32) * 4;
+    k_finish<<<(unsigned)std::min<int64_t>(ceil_div(M * pieces, 256), 8192), 256, 0, st>>>(part, splits, M, N, e);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t product_workspace_bytes(int dt, const Product& p) {
+    const Plan q = plan_of(dt, p);
+    return q.a.bytes + q.b.bytes + q.part_bytes;
+}
+
+hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws, hipStream_t st) {
+    const Plan q = plan_of(dt, p);
+    char* w = (char*)ws;
+    hipError_t err;
+    if (q.skinny) {
+        SkinnyArgs g{p.A, p.B, p.lda, p.ldb, p.M, p.N, p.K, q.splits, (float*)w, e};
+        const dim3 grid((unsigned)ceil_div(p.N, 32), (unsigned)q.splits);
+        if (dt == DT_F32) k_skinny<float><<<grid, 512, 0, st>>>(g);
+        else if (dt == DT_BF16) k_skinny<bf16><<<grid, 512, 0, st>>>(g);
+        else k_skinny<f16><<<grid, 512, 0, st>>>(g);
+        err = hipGetLastError();
+    } else {
+        GemmArgs g{};
+        g.A = (const char*)p.A;
+        g.B = (const char*)p.B;
+        if (q.a.lay_out) {
+            if ((err = lay_out(dt, q.a, p.A, p.lda, Packed{}, w, st)) != hipSuccess) return err;
+            g.A = w;
+            w += q.a.bytes;
+        }
+        if (q.b.lay_out) {
+            if ((err = lay_out(dt, q.b, p.B, p.ldb, p.bp, w, st)) != hipSuccess) return err;
+            g.B = w;
+            w += q.b.bytes;
+        }
+        g.lda = q.a.ld * 2;
+        g.ldb = q.b.ld * 2;
+        g.apl = q.a.rows * q.a.ld * 2;
+        g.bpl = q.b.rows * q.b.ld * 2;
+        g.M = (int)p.M;
+        g.N = (int)p.N;
+        g.K = (int)p.K;
+        g.ksteps = q.ksteps;
+        g.nseg = q.nseg;
+        // pairs of planes, the small products first
+        if (q.nseg == 6) {   // hi mid lo = 0 1 2; (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
+            g.pa = 2u | 0u << 4 | 1u << 8 | 1u << 12 | 0u << 16 | 0u << 20;
+            g.pb = 0u | 2u << 4 | 1u << 8 | 0u << 12 | 1u << 16 | 0u << 20;
+        } else if (q.nseg == 3) {
+            g.pa = 2u | 1u << 4 | 0u << 8;
+        }
+        g.tiles_m = (int)q.tiles_m;
+        g.tiles_n = (int)q.tiles_n;
+        g.splits = q.splits;
+        g.part = (float*)w;
+        g.e = e;
+        const bool fresh = e.out_dt == DT_F32;
+        if (dt == DT_F16) err = fresh ? run_product<f16, true>(p, q, g, st) : run_product<f16, false>(p, q, g, st);
+        else err = fresh ? run_product<bf16, true>(p, q, g, st) : run_product<bf16, false>(p, q, g, st);
+    }
+    if (err != hipSuccess || q.splits == 1) return err;
+    return run_finish((const float*)w, q.splits, p.M, p.N, e, st);
+}
+
+}  // namespace mfac

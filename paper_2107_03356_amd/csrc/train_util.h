@@ -1,0 +1,233 @@
+// Device helpers shared by the training operators (norm.hip, pack8.hip,
+// linear.hip): eight values at a time in and out of fp32, bf16 and fp16 rows,
+// 8-bit copies, activations and sums over a wave.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+namespace mfac {
+namespace {
+
+typedef float f8 __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16;
+typedef __bf16 bf16;
+
+// Vectors with the alignment of their element: global accesses need no more, so
+// rows of any leading dimension take 128-bit accesses.
+template <typename T, int N>
+struct VecOf {
+    typedef T plain __attribute__((ext_vector_type(N)));
+    typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    typedef float wide __attribute__((ext_vector_type(N)));
+};
+
+// Elements c .. c + 7 of a row of `cols`; zeros past its end.
+template <typename T>
+__device__ __forceinline__ f8 load8(const T* __restrict__ row, int64_t c, int64_t cols) {
+    if (c + 8 <= cols) {
+        const typename VecOf<T, 8>::plain v = *reinterpret_cast<const typename VecOf<T, 8>::type*>(row + c);
+        return __builtin_convertvector(v, f8);
+    }
+    f8 r = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c + i < cols) r[i] = (float)row[c + i];
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(T* __restrict__ row, int64_t c, int64_t cols, f8 v) {
+    typedef typename VecOf<T, 8>::plain V;
+    const V w = __builtin_convertvector(v, V);
+    if (c + 8 <= cols) {
+        *reinterpret_cast<typename VecOf<T, 8>::type*>(row + c) = w;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c + i < cols) row[c + i] = w[i];
+}
+
+// ---------------------------------------------------------------- 8-bit copies
+// The byte s = e + 127 of a group whose largest magnitude has these bits: e is the
+// exponent less 6, one more where the significand passes 127/64; at least -126,
+// so that 2^e and 2^-e are normal. Bits are compared as integers, by which a NaN is
+// the largest: a group with an infinity or a NaN has s = 255.
+__device__ __forceinline__ unsigned pack_scale(unsigned amax_bits) {
+    const int ex = (int)(amax_bits >> 23);
+    if (ex == 255) return 255u;
+    const int s = ex - 6 + ((amax_bits & 0x7fffffu) > 0x7e0000u ? 1 : 0);
+    return (unsigned)(s < 1 ? 1 : s);
+}
+// 2^-e, or 0 for s = 255 (every q of the group is then 0 by the caller's select).
+__device__ __forceinline__ float pack_inverse(unsigned s) { return __uint_as_float((254u - s) << 23); }
+// 2^e; NaN for s = 255.
+__device__ __forceinline__ float unpack_scale(unsigned s) {
+    return s == 255u ? __uint_as_float(0x7fc00000u) : s == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(s << 23);
+}
+__device__ __forceinline__ unsigned abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+__device__ __forceinline__ unsigned max_bits8(f8 v) {
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, abs_bits(v[i]));
+    return m;
+}
+
+// Four values as int8 in a word, the lowest first; scaled by 2^-e. With e = 122 a value may
+// round to 64, and 64 * 2^122 is no fp32 value: 63 then.
+__device__ __forceinline__ unsigned quant4(float a, float b, float c, float d, unsigned s) {
+    if (s == 255u) return 0u;
+    const float r = pack_inverse(s);
+    int ia = (int)__builtin_rintf(a * r), ib = (int)__builtin_rintf(b * r);
+    int ic = (int)__builtin_rintf(c * r), id = (int)__builtin_rintf(d * r);
+    if (s == 249u) {
+        ia = max(-63, min(63, ia));
+        ib = max(-63, min(63, ib));
+        ic = max(-63, min(63, ic));
+        id = max(-63, min(63, id));
+    }
+    return (unsigned)(ia & 255) | (unsigned)(ib & 255) << 8 | (unsigned)(ic & 255) << 16 | (unsigned)id << 24;
+}
+
+struct __attribute__((packed, aligned(1))) Bytes8 {
+    unsigned lo, hi;
+};
+
+// Columns c .. c + 7 of a copy's row: q * 2^e.
+__device__ __forceinline__ f8 load_packed8(const int8_t* __restrict__ qrow, const uint8_t* __restrict__ srow, int64_t c,
+                                           int64_t cols) {
+    f8 r = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (c >= cols) return r;
+    const float sc = unpack_scale(srow[c >> 5]);
+    if (c + 8 <= cols) {
+        const Bytes8 b = *reinterpret_cast<const Bytes8*>(qrow + c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            r[i] = (float)(int8_t)(b.lo >> (8 * i)) * sc;
+            r[4 + i] = (float)(int8_t)(b.hi >> (8 * i)) * sc;
+        }
+        return r;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c + i < cols) r[i] = (float)qrow[c + i] * sc;
+    return r;
+}
+
+// Eight values of a group whose scale byte is s, columns c .. c + 7.
+__device__ __forceinline__ void store_packed8(int8_t* __restrict__ qrow, int64_t c, int64_t cols, f8 v, unsigned s) {
+    Bytes8 b;
+    b.lo = quant4(v[0], v[1], v[2], v[3], s);
+    b.hi = quant4(v[4], v[5], v[6], v[7], s);
+    if (c + 8 <= cols) {
+        *reinterpret_cast<Bytes8*>(qrow + c) = b;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (c + i < cols) qrow[c + i] = (int8_t)((i < 4 ? b.lo : b.hi) >> (8 * (i & 3)));
+}
+
+// The copy of 32 values held by four neighbouring lanes, eight each (zeros past
+// the row's end). Every lane of the four takes part.
+__device__ __forceinline__ void pack_group(int8_t* __restrict__ qrow, uint8_t* __restrict__ srow, int64_t c, int64_t cols,
+                                           f8 v) {
+    unsigned m = max_bits8(v);
+    m = max(m, (unsigned)__shfl_xor((int)m, 1));
+    m = max(m, (unsigned)__shfl_xor((int)m, 2));
+    const unsigned s = pack_scale(m);
+    if (c >= cols) return;
+    store_packed8(qrow, c, cols, v, s);
+    if ((c & 31) == 0) srow[c >> 5] = (uint8_t)s;
+}
+
+// ---------------------------------------------------------------- activations
+// exp(x) through the hardware's 2^x (1 ulp); the arguments here are at most 0 or
+// saturate to 0 and infinity as the formulas want.
+__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+
+// 1 - erf(y) for y >= 0 as poly(t) exp(-y^2), t = 1 / (1 + p y): Abramowitz and
+// Stegun, Handbook of Mathematical Functions, 7.1.26 (absolute error 1.5e-7);
+// ex = exp(-y^2) is passed in, since the slope of z Phi(z) needs it too.
+__device__ __forceinline__ float erfc_pos(float y, float ex) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, y, 1.f));
+    float p = fmaf(1.061405429f, t, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f);
+    return p * t * ex;
+}
+
+template <int ACT>
+__device__ __forceinline__ float act_of(float z) {
+    if constexpr (ACT == 1) return z > 0.f || z != z ? z : 0.f;
+    if constexpr (ACT == 2) {
+        const float h = 0.5f * erfc_pos(fabsf(z) * 0.70710678118654752f, exp_fast(-0.5f * z * z));
+        return z * (z < 0.f ? h : 1.f - h);
+    }
+    if constexpr (ACT == 3) {   // (1 + tanh u) / 2 = 1 / (1 + exp(-2u))
+        const float u = z * fmaf(0.044715f * z, z, 1.f);
+        return z * __builtin_amdgcn_rcpf(1.f + exp_fast(-1.59576912160573072f * u));
+    }
+    if constexpr (ACT == 4) return z * __builtin_amdgcn_rcpf(1.f + exp_fast(-z));
+    return z;
+}
+
+// act'(z), and act(z) in *a.
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z, float* a) {
+    if constexpr (ACT == 1) {
+        *a = z > 0.f || z != z ? z : 0.f;
+        return z > 0.f ? 1.f : z != z ? z : 0.f;
+    }
+    if constexpr (ACT == 2) {
+        const float ex = exp_fast(-0.5f * z * z);
+        const float h = 0.5f * erfc_pos(fabsf(z) * 0.70710678118654752f, ex);
+        const float p = z < 0.f ? h : 1.f - h;
+        *a = z * p;
+        return fmaf(z * 0.39894228040143268f, ex, p);
+    }
+    if constexpr (ACT == 3) {
+        const float z2 = z * z;
+        const float p = __builtin_amdgcn_rcpf(1.f + exp_fast(-1.59576912160573072f * z * fmaf(0.044715f, z2, 1.f)));
+        *a = z * p;
+        return fmaf(p * (1.f - p) * z, 1.59576912160573072f * fmaf(0.134145f, z2, 1.f), p);
+    }
+    if constexpr (ACT == 4) {
+        const float p = __builtin_amdgcn_rcpf(1.f + exp_fast(-z));
+        *a = z * p;
+        return fmaf(p * (1.f - p), z, p);
+    }
+    *a = z;
+    return 1.f;
+}
+
+// f(integral constant of the activation): one uniform branch around the code of each.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
+    switch (act) {
+        case 1: f(std::integral_constant<int, 1>()); break;
+        case 2: f(std::integral_constant<int, 2>()); break;
+        case 3: f(std::integral_constant<int, 3>()); break;
+        case 4: f(std::integral_constant<int, 4>()); break;
+        default: f(std::integral_constant<int, 0>()); break;
+    }
+}
+
+// ---------------------------------------------------------------- sums over a wave
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+__device__ __forceinline__ float sum8(f8 v) {
+    return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+}
+
+}  // namespace
+}  // namespace mfac

@@ -1,0 +1,600 @@
+"""Layer norm, linear layers and 8-bit copies on the GPU against their definitions in 64 bits."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_common import require_gpu, say
+from train_ref import E32, TINY, U, act64, act_error, growth, off, pack64, unpack64
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+TYPES = [F32, BF16, F16]
+ACTS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
+
+
+@pytest.fixture(scope="module")
+def dev():
+    return require_gpu()
+
+
+def rand(dev, seed, *shape, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g, dtype=torch.float64) * scale).to(dev)
+
+
+def strided(x, dtype, pad):
+    """x in `dtype` with `pad` elements after each row, which hold NaN."""
+    wide = torch.full((x.shape[0], x.shape[1] + pad), float("nan"), dtype=dtype, device=x.device)
+    wide[:, :x.shape[1]] = x.to(dtype)
+    return wide[:, :x.shape[1]]
+
+
+def holds(got, want, bound, what):
+    o = off(got, want, bound)
+    assert o <= 1, (what, o)
+
+
+# ---------------------------------------------------------------- 8-bit copies
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,pad", [(1, 1, 0), (1, 33, 0), (3, 31, 1), (5, 64, 0), (67, 100, 3), (9, 513, 7),
+                                           (130, 1024, 8), (2, 20000, 0), (4097, 8, 0)])
+def test_pack8_is_the_definition_bit_for_bit(dev, dtype, rows, cols, pad):
+    from paper_2107_03356_amd import nn
+    say("pack8", dtype, rows, cols, pad)
+    x = strided(rand(dev, rows + cols, rows, cols) * torch.exp(3 * rand(dev, 7, cols)), dtype, pad)
+    p = nn.pack8(x)
+    q, s = pack64(x)
+    assert torch.equal(p.q, q) and torch.equal(p.s, s)
+    want = unpack64(q, s)   # NaN in the groups of an fp16 infinity
+
+    def equal(a, b):
+        return torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(torch.nan_to_num(a), torch.nan_to_num(b))
+
+    for t in (F32, BF16):   # 8 bits times a power of two: exact in both
+        assert equal(nn.unpack8(p, t).double(), want)
+    assert equal(nn.unpack8(p, F16).double(), want.clamp(-65504, 65504).to(F16).double())
+    err = torch.nan_to_num((x.double() - want).abs(), nan=0.0)
+    assert (err <= torch.exp2(s.double() - 128).repeat_interleave(32, 1)[:, :cols]).all()
+
+
+def test_pack8_edges(dev):
+    """Zeros, subnormals, the largest values, halves, the power's boundary 127/64, infinities and NaN."""
+    from paper_2107_03356_amd import nn
+    say("pack8 edges")
+    big = 3.4028234663852886e38
+    groups = [[0.0] * 32, [1e-45, -1e-40] + [0.0] * 30, [big, -big] + [1.0] * 30, [127.0, 0.5, 1.5, 2.5, -0.5] + [0.0] * 27,
+              [1.984375, 0.1] + [0.0] * 30, [1.98437511920929, 0.1] + [0.0] * 30, [float("inf")] + [1.0] * 31,
+              [1.0] * 31 + [float("nan")], [float("-inf"), float("nan")] + [0.0] * 30, [2.0 ** -126 * 127] + [2.0 ** -127] * 31,
+              [-0.0] * 32]
+    x = torch.tensor(groups, dtype=F32, device=dev).reshape(1, -1)
+    p = nn.pack8(x)
+    q, s = pack64(x)
+    assert torch.equal(p.q, q) and torch.equal(p.s, s)
+    back = nn.unpack8(p, F32)[0].view(-1, 32)
+    want = unpack64(q, s)[0].view(-1, 32)
+    for g in range(len(groups)):
+        if int(s[0, g]) == 255:
+            assert torch.isnan(back[g]).all()
+        else:
+            assert torch.equal(back[g].double(), want[g])
+    h = torch.tensor([[65504.0, -65504.0, 65440.0] + [1.0] * 29], dtype=F16, device=dev)
+    y = nn.unpack8(nn.pack8(h), F16)   # 64 * 1024 is past fp16's largest: saturated, not infinite
+    assert y[0, 0].item() == 65504 and y[0, 1].item() == -65504 and torch.isfinite(y).all()
+
+
+# ---------------------------------------------------------------- layer norm
+NORM_SIZES = [(1, 1, 0), (1, 7, 0), (1, 4096, 0), (3, 512, 0), (5, 513, 1), (600, 64, 0), (37, 1000, 3), (33, 1025, 0),
+              (7, 2048, 8), (9, 2051, 0), (3, 4097, 1), (2, 8192, 0), (5, 9000, 0), (2, 16384, 0), (3, 16385, 2), (2, 40001, 0),
+              (2500, 96, 0)]
+
+
+def norm_inputs(dev, rows, cols, dtype, pad, seed=0):
+    x = strided(rand(dev, seed + 1, rows, cols) + 0.3 * rand(dev, seed + 2, cols) + 0.5, dtype, pad)
+    w, b = (1 + 0.2 * rand(dev, seed + 3, cols)).to(F32), (0.1 * rand(dev, seed + 4, cols)).to(F32)
+    return x, w, b
+
+
+def norm64(x, w, b, eps):
+    x = x.double()
+    mean = x.mean(1, keepdim=True)
+    var = (x - mean).square().mean(1, keepdim=True)
+    rstd = 1 / torch.sqrt(var + eps)
+    xh = (x - mean) * rstd
+    return xh * w.double() + b.double(), mean, rstd, xh
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,pad", NORM_SIZES)
+def test_layer_norm_forward(dev, dtype, rows, cols, pad):
+    from paper_2107_03356_amd import nn
+    say("layer_norm fwd", dtype, rows, cols, pad)
+    x, w, b = norm_inputs(dev, rows, cols, dtype, pad)
+    eps = 1e-5
+    y64, mean64, rstd64, xh64 = norm64(x, w, b, eps)
+    # the mean's error is a few units of the largest partial sum's, and moves every x - mean; with few columns the
+    # variance may be as small as eps, hence rstd in it
+    moved = E32 * 16 * x.double().abs().amax(1, keepdim=True)
+    xh_err = moved * rstd64 + E32 * 16 * (xh64.abs() + 1)
+    y, mean, rstd = nn.layer_norm_forward(x, w, b, eps)
+    holds(y, y64, U[dtype] * y64.abs() + 2 * (xh_err * w.double().abs() + E32 * b.double().abs()) + TINY[dtype], "y")
+    holds(mean[:, None], mean64, moved, "mean")
+    holds(rstd[:, None], rstd64, rstd64 * (E32 * 16 + moved * rstd64), "rstd")
+    y8, p, rstd8 = nn.layer_norm_forward(x, w, b, eps, pack=True)
+    assert torch.equal(y8, y) and torch.equal(rstd8, rstd)
+    step = torch.exp2(p.s.double() - 127).repeat_interleave(32, 1)[:, :cols]
+    holds(nn.unpack8(p), xh64, step / 2 + xh_err, "copy")
+    # the step is no larger than the definition's for values moved by their error
+    most = xh64.abs() + xh_err
+    most = torch.nn.functional.pad(most, (0, -cols % 32)).view(rows, -1, 32).amax(2)
+    assert (torch.exp2(p.s.double() - 127) <= torch.clamp(2 * most / 127, min=2.0 ** -126)).all()
+    # no parameters; in place through the C call's rules is left to its own test
+    y0, _, _ = nn.layer_norm_forward(x, eps=eps)
+    holds(y0, xh64, U[dtype] * xh64.abs() + 2 * xh_err + TINY[dtype], "no parameters")
+
+
+def norm_bwd64(dy, xh, rstd, w):
+    h = dy * w
+    dx = rstd * (h - h.mean(1, keepdim=True) - xh * (h * xh).mean(1, keepdim=True))
+    return dx, (dy * xh).sum(0), dy.sum(0)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,pad", NORM_SIZES)
+def test_layer_norm_backward(dev, dtype, rows, cols, pad):
+    from paper_2107_03356_amd import nn
+    say("layer_norm bwd", dtype, rows, cols, pad)
+    x, w, b = norm_inputs(dev, rows, cols, dtype, pad)
+    dy = strided(rand(dev, 11, rows, cols), dtype, pad)
+    add = strided(rand(dev, 12, rows, cols), dtype, pad)
+    _, mean, rstd = nn.layer_norm_forward(x, w, b)
+    r = rstd.double()[:, None]
+    p = nn.pack8(((x.double() - mean.double()[:, None]) * r).to(F32))
+    for xin, m, xh in ((x, mean, (x.double() - mean.double()[:, None]) * r), (p, None, unpack64(p.q, p.s))):
+        d = dy.double()
+        dx64, dw64, db64 = norm_bwd64(d, xh, r, w.double())
+        h = (d * w.double()).abs()
+        err = E32 * 24 * r * (h + h.mean(1, keepdim=True) + xh.abs() * (h * xh.abs()).mean(1, keepdim=True))
+        # x - mean loses what mean's units are worth
+        err = err + E32 * 4 * r * (x.double().abs().amax(1, keepdim=True) * r) * (h * xh.abs() + h).mean(1, keepdim=True)
+        dx, dw, db = nn.layer_norm_backward(dy, xin, m, rstd, w)
+        holds(dx, dx64, U[dtype] * dx64.abs() + err + TINY[dtype], "dx")
+        sums = E32 * growth(rows)
+        xh_err = xh.abs() + x.double().abs().amax(1, keepdim=True) * r
+        holds(dw, dw64, sums * (d.abs() * xh_err).sum(0) + TINY[F32], "dw")
+        holds(db, db64, sums * d.abs().sum(0) + TINY[F32], "db")
+        dxa, dwa, dba = nn.layer_norm_backward(dy, xin, m, rstd, w, add=add)
+        want = dx64 + add.double()
+        holds(dxa, want, U[dtype] * want.abs() + err + E32 * add.double().abs() + TINY[dtype], "dx + add")
+        assert torch.equal(dwa, dw) and torch.equal(dba, db)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_layer_norm_parameters_in_16_bits(dev, dtype):
+    from paper_2107_03356_amd import nn
+    say("layer_norm 16-bit parameters", dtype)
+    x, w, b = norm_inputs(dev, 100, 777, dtype, 0)
+    dy = rand(dev, 5, 100, 777).to(dtype)
+    y, mean, rstd = nn.layer_norm_forward(x, w.to(dtype), b.to(dtype))
+    yf, _, _ = nn.layer_norm_forward(x, w.to(dtype).float(), b.to(dtype).float())
+    assert torch.equal(y, yf)
+    dx, dw, db = nn.layer_norm_backward(dy, x, mean, rstd, w.to(dtype))
+    dxf, dwf, dbf = nn.layer_norm_backward(dy, x, mean, rstd, w.to(dtype).float())
+    assert dw.dtype == dtype and torch.equal(dx, dxf) and torch.equal(dw, dwf.to(dtype)) and torch.equal(db, dbf.to(dtype))
+
+
+def test_layer_norm_equal_values_infinities_and_rows_apart(dev):
+    """A row of one value has xhat = 0; a row with an infinity is NaN and leaves the others as they are."""
+    from paper_2107_03356_amd import nn
+    say("layer_norm special rows")
+    x = rand(dev, 3, 6, 300).to(F32)
+    x[1] = 4.25
+    clean, _, _ = nn.layer_norm_forward(x)
+    assert torch.equal(clean[1], torch.zeros_like(clean[1]))
+    x[3, 17] = float("inf")
+    x[5, 0] = float("nan")
+    y, p, rstd = nn.layer_norm_forward(x, pack=True)
+    for r in (0, 1, 2, 4):
+        assert torch.equal(y[r], clean[r])
+    assert torch.isnan(y[5]).all() and torch.isnan(y[3]).any()
+    assert (p.s[5] == 255).all() and torch.isnan(nn.unpack8(p)[5]).all()
+
+
+# ---------------------------------------------------------------- linear layers
+# (rows, cin, cout, pad): one row to many; odd and tiny sizes; K past several steps; tiles of both sizes
+LINEAR_SIZES = [(1, 1, 1, 0), (1, 2048, 1024, 0), (2, 40, 33, 0), (7, 129, 65, 1), (16, 1000, 520, 0), (17, 64, 64, 0),
+                (31, 333, 129, 3), (100, 8, 8, 0), (128, 128, 128, 0), (129, 520, 264, 8), (300, 777, 200, 5),
+                (1000, 72, 1016, 0), (513, 1030, 515, 0)]
+
+
+def linear_inputs(dev, rows, cin, cout, dtype, pad):
+    x = strided(rand(dev, 21, rows, cin), dtype, pad)
+    w = strided(rand(dev, 22, cout, cin) / math.sqrt(cin), dtype, pad)
+    b = (0.5 * rand(dev, 23, cout)).to(F32)
+    res = strided(rand(dev, 24, rows, cout), dtype, pad)
+    return x, w, b, res
+
+
+def z_error(x, w, b):
+    """fp32 sums of products, and for fp32 operands what the six products leave out."""
+    return E32 * (growth(x.shape[1]) * (x.double().abs() @ w.double().abs().t()) + 2 * b.double().abs())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cin,cout,pad", LINEAR_SIZES)
+def test_linear_forward(dev, dtype, rows, cin, cout, pad):
+    from paper_2107_03356_amd import nn
+    x, w, b, res = linear_inputs(dev, rows, cin, cout, dtype, pad)
+    z64 = x.double() @ w.double().t() + b.double()
+    ze = z_error(x, w, b)
+    for act in ACTS:
+        say("linear fwd", dtype, rows, cin, cout, pad, act)
+        a64, _ = act64(act, z64)
+        err = 1.2 * ze + act_error(z64) * (act != "none")
+        y = nn.linear_forward(x, w, b, act)
+        holds(y, a64, U[dtype] * a64.abs() + err + TINY[dtype], "y")
+        yr, z = nn.linear_forward(x, w, b, act, residual=res, keep="z")
+        want = a64 + res.double()
+        holds(yr, want, U[dtype] * want.abs() + err + E32 * want.abs() + TINY[dtype], "y + res")
+        holds(z, z64, U[dtype] * z64.abs() + ze + TINY[dtype], "z")
+        y8, p = nn.linear_forward(x, w, b, act, keep="pack8")
+        assert torch.equal(y8, y)
+        step = torch.exp2(p.s.double() - 127).repeat_interleave(32, 1)[:, :cout]
+        holds(nn.unpack8(p), z64, step / 2 + ze, "copy of z")
+    y0 = nn.linear_forward(x, w)
+    want = x.double() @ w.double().t()
+    holds(y0, want, U[dtype] * want.abs() + z_error(x, w, 0 * b) + TINY[dtype], "no bias")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cin,cout,pad", LINEAR_SIZES)
+def test_linear_backward(dev, dtype, rows, cin, cout, pad):
+    from paper_2107_03356_amd import nn
+    x, w, b, _ = linear_inputs(dev, rows, cin, cout, dtype, pad)
+    z = strided(rand(dev, 31, rows, cout, scale=1.5), dtype, pad)
+    dy = strided(rand(dev, 32, rows, cout), dtype, pad)
+    gamma, beta = (1 + 0.2 * rand(dev, 33, cin)).to(F32), (0.3 * rand(dev, 34, cin)).to(F32)
+    xp, zp = nn.pack8(x), nn.pack8(z)
+    for act in ACTS:
+        for packed in (False, True):
+            for gtype in {dtype, F32}:
+                say("linear bwd", dtype, rows, cin, cout, pad, act, packed, gtype)
+                zz = unpack64(zp.q, zp.s) if packed else z.double()
+                slope = act64(act, zz)[1]
+                dz64 = dy.double() * slope
+                # dz is rounded to the operands' type before the products, except without an activation
+                dz_err = (dz64.abs() * (U[dtype] + 2 * E32) + TINY[dtype]) * (act != "none") + dy.double().abs() * (
+                    act_error(zz) * (act != "none"))
+                x64 = unpack64(xp.q, xp.s) * gamma.double() + beta.double() if packed else x.double()
+                xmag = unpack64(xp.q, xp.s).abs() * gamma.double().abs() + beta.double().abs() if packed else x64.abs()
+                dx, dw, db = nn.linear_backward(dy, xp if packed else x, w, None if act == "none" else zp if packed else z,
+                                                act, affine=(gamma, beta) if packed else None, grad_dtype=gtype)
+                dzm = dz64.abs() + dz_err
+                wm = w.double().abs()
+                want = dz64 @ w.double()
+                holds(dx, want, U[dtype] * want.abs() + dz_err @ wm + E32 * growth(cout) * (dzm @ wm) + 2 * TINY[dtype], "dx")
+                want = dz64.t() @ x64
+                holds(dw, want, U[gtype] * want.abs() + dz_err.t() @ xmag + E32 * 2 * growth(rows) * (dzm.t() @ xmag)
+                      + TINY[gtype], "dw")
+                holds(db, dz64.sum(0), (dy.double().abs() * act_error(zz) * (act != "none")).sum(0)
+                      + E32 * growth(rows) * dz64.abs().sum(0) + TINY[F32], "db")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_large_tiles_against_64_bits(dev, dtype):
+    """Sizes that take the large tiles, ragged at every edge, through all three products."""
+    from paper_2107_03356_amd import nn
+    rows, cin, cout = 4100, 1048, 4056
+    x, w, b, res = linear_inputs(dev, rows, cin, cout, dtype, 0)
+    dy = rand(dev, 32, rows, cout).to(dtype)
+    z64 = x.double() @ w.double().t() + b.double()
+    say("large tiles fwd", dtype)
+    a64, _ = act64("silu", z64)
+    want = a64 + res.double()
+    y = nn.linear_forward(x, w, b, "silu", res)
+    holds(y, want, U[dtype] * want.abs() + 1.2 * z_error(x, w, b) + act_error(z64) + E32 * want.abs(), "y")
+    say("large tiles bwd", dtype)
+    dx, dw, db = nn.linear_backward(dy, x, w, grad_dtype=F32)
+    d, wd = dy.double(), w.double()
+    want = d @ wd
+    holds(dx, want, U[dtype] * want.abs() + E32 * growth(cout) * (d.abs() @ wd.abs()), "dx")
+    want = d.t() @ x.double()
+    holds(dw, want, U[F32] * want.abs() + E32 * growth(rows) * (d.abs().t() @ x.double().abs()), "dw")
+
+
+def test_skip_connection_joins_the_input_gradient_and_outputs_may_be_their_addend(dev):
+    from paper_2107_03356_amd import _binding as B
+    from paper_2107_03356_amd import nn
+    say("linear_backward_input add, in place")
+    dz, w = rand(dev, 1, 200, 96).to(BF16), rand(dev, 2, 96, 136, scale=0.1).to(BF16)
+    add = rand(dev, 3, 200, 136).to(BF16)
+    want = dz.double() @ w.double() + add.double()
+    dx = nn.linear_backward_input(dz, w, add=add)
+    holds(dx, want, U[BF16] * want.abs() + E32 * growth(96) * (dz.double().abs() @ w.double().abs() + add.double().abs()), "dx")
+    buf = add.clone()
+    st = torch.cuda.current_stream().cuda_stream
+    n = B.mfac_linear_bwd_input_workspace_bytes(B.MFAC_BF16, 200, 136, 96, dz.data_ptr(), 96, w.data_ptr(), 136)
+    ws = torch.empty(max(n, 1), dtype=torch.uint8, device=dev)
+    assert B.mfac_linear_bwd_input(B.MFAC_BF16, 200, 136, 96, dz.data_ptr(), 96, w.data_ptr(), 136, buf.data_ptr(), 136,
+                                   buf.data_ptr(), 136, ws.data_ptr(), n, st) == B.MFAC_OK
+    assert torch.equal(buf, dx)
+    # layer norm in place, forward and backward
+    x = rand(dev, 4, 50, 700).to(BF16)
+    y, mean, rstd = nn.layer_norm_forward(x)
+    z = x.clone()
+    assert B.mfac_layer_norm(B.MFAC_BF16, B.MFAC_F32, 50, 700, z.data_ptr(), 700, None, None, 1e-5, z.data_ptr(), 700, None,
+                             None, None, 0, None, st) == B.MFAC_OK
+    assert torch.equal(z, y)
+    for cols in (700, 20000):
+        x, dy = rand(dev, 6, 20, cols).to(BF16), rand(dev, 5, 20, cols).to(BF16)
+        y, mean, rstd = nn.layer_norm_forward(x)
+        dx, dw, db = nn.layer_norm_backward(dy, x, mean, rstd)
+        g = torch.empty(2, cols, device=dev)
+        d = dy.clone()
+        n = B.mfac_layer_norm_bwd_workspace_bytes(20, cols)
+        ws = torch.empty(n, dtype=torch.uint8, device=dev)
+        assert B.mfac_layer_norm_bwd(B.MFAC_BF16, B.MFAC_F32, 20, cols, d.data_ptr(), cols, x.data_ptr(), cols,
+                                     mean.data_ptr(), rstd.data_ptr(), None, 0, None, None, None, 0, d.data_ptr(), cols,
+                                     g[0].data_ptr(), g[1].data_ptr(), ws.data_ptr(), n, st) == B.MFAC_OK
+        assert torch.equal(d, dx) and torch.equal(g[0], dw) and torch.equal(g[1], db)
+
+
+def test_rows_of_zero_and_row_of_infinities(dev):
+    from paper_2107_03356_amd import nn
+    say("no rows")
+    w, b = rand(dev, 1, 24, 40).to(BF16), rand(dev, 2, 24).to(F32)
+    x = torch.empty(0, 40, dtype=BF16, device=dev)
+    y, z = nn.linear_forward(x, w, b, "gelu", keep="z")
+    assert y.shape == (0, 24) and z.shape == (0, 24)
+    dx, dw, db = nn.linear_backward(y, x, w, z, "gelu", grad_dtype=F32)
+    assert dx.shape == (0, 40) and not dw.any() and not db.any() and dw.shape == (24, 40)
+    y, mean, rstd = nn.layer_norm_forward(x)
+    dx, dw, db = nn.layer_norm_backward(y, x, mean, rstd)
+    assert dx.shape == (0, 40) and not dw.any() and not db.any()
+    p = nn.pack8(x)
+    assert p.shape == (0, 40) and nn.unpack8(p).shape == (0, 40)
+    for rows in (5, 40):
+        say("infinities", rows)
+        x = rand(dev, 3, rows, 40).to(BF16)
+        clean = nn.linear_forward(x, w, b)
+        x[2, 3] = float("inf")
+        x[4, 39] = float("nan")
+        y = nn.linear_forward(x, w, b)
+        assert torch.equal(y[:2], clean[:2]) and torch.equal(y[3], clean[3]) and torch.equal(y[5:], clean[5:])
+        assert not torch.isfinite(y[2]).any() and torch.isnan(y[4]).all()
+        want = (x.double() @ w.double().t())[2]
+        assert torch.equal(y[2].double(), want)
+        # rows and columns past the ends hold NaN: nothing of them is read
+        xs, ws = strided(rand(dev, 3, rows, 41), BF16, 7), strided(rand(dev, 1, 24, 41), BF16, 7)
+        assert torch.isfinite(nn.linear_forward(xs, ws, b)).all()
+
+
+@pytest.mark.parametrize("act", ACTS[1:])
+def test_activation_ends(dev, act):
+    """Far out on both sides, zero, and the infinities that the formulas have values for."""
+    from paper_2107_03356_amd import nn
+    say("activation ends", act)
+    z = torch.tensor([[0.0, -0.0, 1e-30, -1e-30, 5.0, -5.0, 12.0, -12.0, 30.0, -30.0, 88.0, -88.0, 300.0, -300.0, 1e4, -1e4]],
+                     dtype=F32, device=dev)
+    eye = torch.eye(16, device=dev)
+    y = nn.linear_forward(z, eye, None, act)
+    a64, s64 = act64(act, z.double())
+    holds(y, a64, act_error(z.double()) * torch.clamp(a64.abs() * 1e9, max=1.0) + 1e-30 + E32 * a64.abs(), "act")
+    dz, a, db = nn.act_backward(torch.ones_like(z), z, act, want_a=True)
+    holds(dz, s64, act_error(z.double()).clamp(max=1e-4) + 0 * s64, "slope")
+    holds(a, a64, act_error(z.double()) + 0 * a64, "a")
+    assert torch.equal(db, dz[0])
+
+
+# ---------------------------------------------------------------- gradients against differences
+@pytest.mark.parametrize("copy8", [False, True])
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+def test_feed_forward_gradients_against_differences(dev, act, copy8):
+    """The block's gradients along random directions against central differences of its definition in
+    64 bits (which with copy8 they meet up to the copies' steps)."""
+    from paper_2107_03356_amd import nn
+    say("feed_forward gradients", act, copy8)
+    rows, dim, hid = 96, 72, 200
+    names = ["x", "lw", "lb", "w1", "b1", "w2", "b2"]
+    p = [rand(dev, 1, rows, dim), 1 + 0.2 * rand(dev, 2, dim), 0.1 * rand(dev, 3, dim), rand(dev, 4, hid, dim, scale=dim ** -0.5),
+         0.1 * rand(dev, 5, hid), rand(dev, 6, dim, hid, scale=hid ** -0.5), 0.1 * rand(dev, 7, dim)]
+    p = [t.float().double() for t in p]
+    c = rand(dev, 8, rows, dim).float().double()
+
+    def f(x, lw, lb, w1, b1, w2, b2):
+        h = norm64(x, lw, lb, 1e-5)[0]
+        return ((x + act64(act, h @ w1.t() + b1)[0] @ w2.t() + b2) * c).sum()
+
+    q = [t.float().requires_grad_() for t in p]
+    y = nn.feed_forward(*q, act=act, copy8=copy8)
+    (y * c.float()).sum().backward()
+    for i, name in enumerate(names):
+        v = rand(dev, 20 + i, *p[i].shape)
+        h = 1e-5
+        at = [list(p), list(p)]
+        at[0][i] = p[i] + h * v
+        at[1][i] = p[i] - h * v
+        want = float((f(*at[0]) - f(*at[1])) / (2 * h))
+        got = float((q[i].grad.double() * v).sum())
+        scale = float(q[i].grad.double().norm())   # what the sum's size is for a random direction
+        # differences: h^2 times third derivatives, about 1e-9; fp32 kernels 1e-5; copies: a step of 2 / 127 of a
+        # group's largest value (about 2.5 deviations) at most, so 0.012 of a deviation (rms) on each value, of which
+        # the slope and the products take their mean
+        assert abs(got - want) <= (0.1 if copy8 else 1e-4) * scale, (name, got, want, scale)
+
+
+def test_autograd_of_layers_in_mixed_types(dev):
+    """float32 parameters with 16-bit data: gradients come in the parameters' type and agree with the
+    passes called by hand."""
+    from paper_2107_03356_amd import nn
+    say("autograd mixed types")
+    x = rand(dev, 1, 4, 10, 64).to(BF16).requires_grad_()
+    lin, norm = nn.Linear(64, 48, act="gelu_tanh", device=dev), nn.LayerNorm(64, device=dev)
+    res = rand(dev, 2, 4, 10, 48).to(BF16).requires_grad_()
+    y = lin(norm(x), residual=res)
+    assert y.shape == (4, 10, 48) and y.dtype == BF16
+    dy = rand(dev, 3, 4, 10, 48).to(BF16)
+    y.backward(dy)
+    assert lin.weight.grad.dtype == F32 and lin.bias.grad.dtype == F32 and norm.weight.grad.dtype == F32
+    assert torch.equal(res.grad, dy)
+    h, mean, rstd = nn.layer_norm_forward(x.detach(), norm.weight, norm.bias)
+    w = lin.weight.to(BF16)
+    yy, z = nn.linear_forward(h, w, lin.bias, "gelu_tanh", res.detach(), keep="z")
+    dh, dw, db = nn.linear_backward(dy, h, w, z, "gelu_tanh", grad_dtype=F32)
+    dx, dlw, dlb = nn.layer_norm_backward(dh, x.detach(), mean, rstd, norm.weight)
+    assert torch.equal(yy, y) and torch.equal(lin.weight.grad, dw) and torch.equal(lin.bias.grad, db)
+    assert torch.equal(x.grad, dx) and torch.equal(norm.weight.grad, dlw) and torch.equal(norm.bias.grad, dlb)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_copies_change_gradients_by_their_steps_only(dev, dtype):
+    """copy8 leaves the forward pass as it is, and the gradients are those of the passes on the copies."""
+    from paper_2107_03356_amd import nn
+    say("copy8 layers", dtype)
+    outs = []
+    for copy8 in (False, True):
+        torch.manual_seed(3)
+        block = nn.FeedForward(96, 352, act="gelu", copy8=copy8, device=dev)
+        x = rand(dev, 1, 200, 96).to(dtype).requires_grad_()
+        y = block(x)
+        y.backward(rand(dev, 2, 200, 96).to(dtype))
+        outs.append([y.detach(), x.grad] + [p.grad for p in block.parameters()])
+    assert torch.equal(outs[0][0], outs[1][0])
+    for a, b in zip(outs[0][1:], outs[1][1:]):
+        d = float((a.double() - b.double()).norm() / a.double().norm())
+        assert d < 0.03, d   # a step's rms (2.5 / 127 / sqrt 12 to twice that) on x and z, and bf16 roundings
+    say("copy8 linear")
+    lin = nn.Linear(96, 64, act="relu", copy8=True, device=dev)
+    x = rand(dev, 5, 50, 96).to(dtype)
+    lin(x).backward(rand(dev, 6, 50, 64).to(dtype))
+    w = lin.weight.detach().to(dtype)
+    _, z = nn.linear_forward(x, w, lin.bias.detach(), "relu", keep="pack8")
+    _, dw, db = nn.linear_backward(rand(dev, 6, 50, 64).to(dtype), nn.pack8(x), w, z, "relu", grad_dtype=F32)
+    assert torch.equal(lin.weight.grad, dw) and torch.equal(lin.bias.grad, db)
+
+
+# ---------------------------------------------------------------- streams, graphs, repeats
+def block_pass(nn, t):
+    h, p, rstd = nn.layer_norm_forward(t["x"], t["lw"], t["lb"], pack=True)
+    a, z = nn.linear_forward(h, t["w1"], t["b1"], "gelu", keep="pack8")
+    y = nn.linear_forward(a, t["w2"], residual=t["x"])
+    da = nn.linear_backward_input(y, t["w2"])
+    dz, a2, db1 = nn.act_backward(da, z, "gelu", want_a=True)
+    dw2 = nn.linear_backward_weight(y, a2, grad_dtype=torch.float32)
+    dw1 = nn.linear_backward_weight(dz, p, (t["lw"], t["lb"]), db1)
+    dx, dlw, dlb = nn.layer_norm_backward(nn.linear_backward_input(dz, t["w1"]), p, None, rstd, t["lw"], add=y)
+    return [y, db1, dw2, dw1, dx, dlw, dlb]
+
+
+def block_inputs(dev, rows, dim, hid, seed):
+    return dict(x=rand(dev, seed, rows, dim).to(BF16), lw=(1 + 0.1 * rand(dev, 2, dim)).to(F32), lb=(0.1 * rand(dev, 3, dim)).to(F32),
+                w1=rand(dev, 4, hid, dim, scale=dim ** -0.5).to(BF16), b1=(0.1 * rand(dev, 5, hid)).to(F32),
+                w2=rand(dev, 6, dim, hid, scale=hid ** -0.5).to(BF16))
+
+
+@pytest.mark.parametrize("rows,dim,hid", [(300, 128, 512), (12, 264, 1000), (130, 100, 70)])
+def test_other_stream_and_graph_replays_equal_the_first_pass(dev, rows, dim, hid):
+    from paper_2107_03356_amd import nn
+    say("stream and graph", rows, dim, hid)
+    t = block_inputs(dev, rows, dim, hid, 1)
+    first = block_pass(nn, t)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        other = block_pass(nn, t)
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, other))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        held = block_pass(nn, t)
+    for k in range(4):   # new inputs each time, with eager work and a wait between the replays
+        t["x"].copy_(rand(dev, 30 + k, rows, dim).to(BF16))
+        eager = block_pass(nn, t)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, held)), k
+
+
+def test_long_rows_of_offsets_past_32_bits(dev):
+    """A row stride that puts the last rows past 2^31 elements."""
+    from paper_2107_03356_amd import nn
+    say("offsets past 32 bits")
+    ld, rows, cols = 300_000_000, 9, 136
+    buf = torch.empty(ld * (rows - 1) + cols, dtype=BF16, device=dev)
+    x = buf.as_strided((rows, cols), (ld, 1))
+    src = rand(dev, 1, rows, cols).to(BF16)
+    x.copy_(src)
+    w, b = rand(dev, 2, 72, cols, scale=0.1).to(BF16), rand(dev, 3, 72).to(F32)
+    assert torch.equal(nn.layer_norm_forward(x)[0], nn.layer_norm_forward(src)[0])
+    p, ps = nn.pack8(x), nn.pack8(src)
+    assert torch.equal(p.q, ps.q) and torch.equal(p.s, ps.s)
+    assert torch.equal(nn.linear_forward(x, w, b, "silu"), nn.linear_forward(src, w, b, "silu"))
+    dz = rand(dev, 4, rows, 72).to(BF16)
+    assert torch.equal(nn.linear_backward_weight(dz, x), nn.linear_backward_weight(dz, src))
+
+
+def test_training_with_the_optimizer(dev):
+    """A stack of blocks with 8-bit copies trained by M-FAC on a regression task: the loss falls as far as
+    with the activations kept whole."""
+    from paper_2107_03356_amd import nn
+    from paper_2107_03356_amd.optim import MFAC
+    say("feed-forward blocks under M-FAC")
+    ends = []
+    for copy8 in (False, True):
+        torch.manual_seed(0)
+        net = torch.nn.Sequential(nn.FeedForward(32, 128, copy8=copy8, device=dev), nn.FeedForward(32, 128, copy8=copy8, device=dev),
+                                  nn.LayerNorm(32, copy8=copy8, device=dev), nn.Linear(32, 8, copy8=copy8, device=dev))
+        x, t = rand(dev, 1, 256, 32).float(), rand(dev, 2, 256, 8).float()
+        opt = MFAC(net.parameters(), lr=0.02, m=16, damp=1e-2)
+        losses = []
+        for _ in range(40):
+            opt.zero_grad()
+            loss = (net(x) - t).square().mean()
+            loss.backward()
+            opt.step()
+            losses.append(loss.item())
+        assert opt.status() == 0
+        ends.append(losses)
+    assert all(np.isfinite(e).all() and e[-1] < 0.8 * e[0] for e in ends), ends
+    assert abs(ends[1][-1] - ends[0][-1]) < 0.1 * ends[0][0], ends
+
+
+# ---------------------------------------------------------------- refusals
+def test_refusals(dev):
+    from paper_2107_03356_amd import nn
+    say("refusals")
+    x, w, b = rand(dev, 1, 8, 64).to(BF16), rand(dev, 2, 32, 64).to(BF16), rand(dev, 3, 32).to(F32)
+    bad = [
+        lambda: nn.linear_forward(x.double(), w),
+        lambda: nn.linear_forward(x, w.float()),
+        lambda: nn.linear_forward(x, w[:, :60]),
+        lambda: nn.linear_forward(x, w, b[:31]),
+        lambda: nn.linear_forward(x, w, b.to(F16)),
+        lambda: nn.linear_forward(x, w, b, act="tanh"),
+        lambda: nn.linear_forward(x, w, b, keep="all"),
+        lambda: nn.linear_forward(x, w, b, residual=x),
+        lambda: nn.linear_forward(x.cpu(), w, b),
+        lambda: nn.linear_backward(x[:, :32], x, w, act="gelu"),
+        lambda: nn.linear_backward_weight(x, nn.pack8(x), affine=(x[0], x[0])),
+        lambda: nn.linear_backward_weight(x, x, grad_dtype=F16),
+        lambda: nn.layer_norm_forward(x, b),
+        lambda: nn.layer_norm_backward(x, x, None, None),
+        lambda: nn.layer_norm_backward(x, nn.pack8(x), b, b),
+        lambda: nn.Packed8(x, x),
+        lambda: nn.feed_forward(x, b, b, w, b, w.t(), b, act="none"),
+        lambda: nn.pack8(torch.empty(3, 0, device=dev)),
+    ]
+    for i, f in enumerate(bad):
+        with pytest.raises(ValueError):
+            f()
+            raise AssertionError(f"call {i} was taken")
+    with pytest.raises(nn.MfacError):
+        nn.layer_norm_forward(x, eps=-1.0)
+    with pytest.raises(nn.MfacError):
+        nn.layer_norm_forward(x, eps=float("nan"))
