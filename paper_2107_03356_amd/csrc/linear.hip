@@ -14,6 +14,7 @@
 // three bf16 planes, hi + mid + lo, of whose nine products six are summed (the
 // others are at most 2^-26 of |a b| together).
 #include <algorithm>
+#include <utility>
 
 #include "internal.h"
 #include "train.h"
@@ -23,7 +24,11 @@ namespace mfac {
 namespace {
 
 typedef float v4 __attribute__((ext_vector_type(4)));
-typedef int i4 __attribute__((ext_vector_type(4)));
+
+template <int... I, typename F>
+__device__ __forceinline__ void for_each_index(std::integer_sequence<int, I...>, F f) {
+    (f(std::integral_constant<int, I>()), ...);
+}
 
 // ---------------------------------------------------------------- epilogue
 __device__ __forceinline__ f8 load8_dt(const void* p, int dt, int64_t off, int64_t c, int64_t cols) {
@@ -37,42 +42,183 @@ __device__ __forceinline__ void store8_dt(void* p, int dt, int64_t off, int64_t 
     else store8((f16*)p + off, c, cols, v);
 }
 
+// The three products' epilogues; the fields of the others are unused.
+enum : int { FORWARD = 0, INPUT = 1, WEIGHT = 2 };
+
+// What an epilogue reads for columns n .. n + 7, whichever the row.
+struct OfColumn {
+    f8 bias, beta;   // bias, or gamma
+};
+template <int KIND>
+__device__ __forceinline__ OfColumn of_column(const Epilogue& e, int64_t N, int64_t n) {
+    OfColumn o{};
+    if (KIND == FORWARD && e.bias) o.bias = load8_dt(e.bias, e.bias_dt, 0, n, N);
+    if (KIND == WEIGHT && e.gamma) {
+        o.bias = load8(e.gamma, n, N);
+        o.beta = load8(e.beta, n, N);
+    }
+    return o;
+}
+// And for (m, n .. n + 7).
+struct OfPlace {
+    f8 add;
+    float db;
+};
+template <int KIND>
+__device__ __forceinline__ OfPlace of_place(const Epilogue& e, int64_t N, bool in, int64_t m, int64_t n) {
+    OfPlace o{};
+    if (KIND != WEIGHT && e.add && in) o.add = load8_dt(e.add, e.io_dt, m * e.ldadd, n, N);
+    if (KIND == WEIGHT && e.gamma && in) o.db = e.db[m];
+    return o;
+}
+
 // The sums c at (m, n .. n + 7) become outputs. Four neighbouring lanes hold 32
 // neighbouring n of one row; every lane of a wave takes part (in: whether m is a row).
-__device__ __forceinline__ void finish8(const Epilogue& e, int64_t N, bool in, int64_t m, int64_t n, f8 c) {
+template <int KIND>
+__device__ __forceinline__ void finish8(const Epilogue& e, int64_t N, bool in, int64_t m, int64_t n, f8 c,
+                                        const OfColumn& col, const OfPlace& at) {
     if (!in) n = N;
-    if (e.bias) c += load8_dt(e.bias, e.bias_dt, 0, n, N);
-    if (e.gamma) {
-        const float d = in ? e.db[m] : 0.f;
-        c = c * load8(e.gamma, n, N) + d * load8(e.beta, n, N);
-    }
-    if (e.p.q) {
-        f8 v = c;
-        if (n + 8 > N)
+    if constexpr (KIND == FORWARD) {
+        c += col.bias;
+        if (e.p.q) {
+            f8 v = c;
+            if (n + 8 > N)
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (n + i >= N) v[i] = 0.f;
-        pack_group(e.p.q + m * e.p.ldq, e.p.s + m * ((N + 31) / 32), n, N, v);
+                for (int i = 0; i < 8; ++i)
+                    if (n + i >= N) v[i] = 0.f;
+            pack_group(e.p.q + m * e.p.ldq, e.p.s + m * ((N + 31) / 32), n, N, v);
+        }
+        if (e.z && n < N) store8_dt(e.z, e.io_dt, m * e.ldz, n, N, c);
+        f8 one[1] = {c};
+        act_apply(act_forward(e.act), one);
+        c = one[0];
     }
-    if (n >= N) return;
-    if (e.z) store8_dt(e.z, e.io_dt, m * e.ldz, n, N, c);
-    with_act(e.act, [&](auto tag) {
+    if constexpr (KIND == WEIGHT)
+        if (e.gamma) c = c * col.bias + at.db * col.beta;
+    if constexpr (KIND != WEIGHT) c += at.add;
+    if (n < N) store8_dt(e.out, e.out_dt, m * e.ldo, n, N, c);
+}
+template <int KIND>
+__device__ __forceinline__ void finish8(const Epilogue& e, int64_t N, bool in, int64_t m, int64_t n, f8 c) {
+    finish8<KIND>(e, N, in, m, n, c, of_column<KIND>(e, N, n), of_place<KIND>(e, N, in, m, n));
+}
+
+// Four sums at a time, as the matrix cores leave them: lane l has columns n .. n + 3, n = 4 (l / 16)
+// of 16, of row l % 16. EDGE: columns past N are possible; tiles without them run code
+// without their checks, which would be most of it (and more than the instruction
+// cache holds). Values are fp32 or of the operands' type T.
+template <bool EDGE, typename T>
+__device__ __forceinline__ v4 load4(const T* row, int64_t n, int64_t N) {
+    if (!EDGE || n + 4 <= N) {
+        const typename VecOf<T, 4>::plain v = *reinterpret_cast<const typename VecOf<T, 4>::type*>(row + n);
+        return __builtin_convertvector(v, v4);
+    }
+    v4 r = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = act_of<decltype(tag)::value>(c[i]);
-    });
-    if (e.add) c += load8_dt(e.add, e.io_dt, m * e.ldadd, n, N);
-    store8_dt(e.out, e.out_dt, m * e.ldo, n, N, c);
+    for (int i = 0; i < 4; ++i)
+        if (n + i < N) r[i] = (float)row[n + i];
+    return r;
+}
+template <bool EDGE, typename T>
+__device__ __forceinline__ v4 load4_dt(const void* p, int dt, int64_t off, int64_t n, int64_t N) {
+    return dt == DT_F32 ? load4<EDGE>((const float*)p + off, n, N) : load4<EDGE>((const T*)p + off, n, N);
+}
+// STREAM: nontemporal stores, which leave the caches to the operands but take longer
+// (see LAST_LEVEL_CACHE).
+template <bool STREAM, typename V, typename P>
+__device__ __forceinline__ void put(V v, P* p) {
+    if constexpr (STREAM) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+template <bool EDGE, bool STREAM>
+__device__ __forceinline__ void store4(float* row, int64_t n, int64_t N, v4 v) {
+    if (!EDGE || n + 4 <= N) {
+        put<STREAM>(v, reinterpret_cast<VecOf<float, 4>::type*>(row + n));
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (n + i < N) row[n + i] = v[i];
+}
+// Of two tiles of 16 columns, a in the first and b in the second: lanes with an even l / 16
+// get their neighbour's a beside their own, those with an odd one their neighbour's b.
+__device__ __forceinline__ void swap_rows(unsigned& a, unsigned& b) {
+    const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = r[0];
+    b = r[1];
+}
+template <bool EDGE, bool STREAM, typename T>
+__device__ __forceinline__ void store_pair16(T* row, int64_t n, int64_t N, int lane, v4 a, v4 b) {
+    typedef typename VecOf<T, 4>::plain V;
+    typedef unsigned u2 __attribute__((ext_vector_type(2)));
+    typedef unsigned u4 __attribute__((ext_vector_type(4)));
+    u2 x = __builtin_bit_cast(u2, __builtin_convertvector(a, V)), y = __builtin_bit_cast(u2, __builtin_convertvector(b, V));
+    unsigned x0 = x[0], x1 = x[1], y0 = y[0], y1 = y[1];
+    swap_rows(x0, y0);
+    swap_rows(x1, y1);
+    n += (lane >> 4 & 1) * 12;   // an odd l / 16: 16 further, less 4
+    const u4 v = {x0, x1, y0, y1};
+    const auto w = __builtin_bit_cast(typename VecOf<T, 8>::plain, v);
+    if (!EDGE || n + 8 <= N) {
+        put<STREAM>(w, reinterpret_cast<typename VecOf<T, 8>::type*>(row + n));
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (n + i < N) row[n + i] = w[i];
+}
+template <bool EDGE, bool STREAM, typename T, int NTL>
+__device__ __forceinline__ void store_quads(void* p, int dt, int64_t off, int64_t n, int64_t N, int lane,
+                                            const v4 (&c)[NTL]) {
+    if (dt == DT_F32) {
+#pragma unroll
+        for (int j = 0; j < NTL; ++j) store4<EDGE, STREAM>((float*)p + off, n + j * 16, N, c[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < NTL; j += 2)
+            store_pair16<EDGE, STREAM>((T*)p + off, n + j * 16, N, lane, c[j], c[j + 1]);
+    }
+}
+// The 8-bit copy of a row's 32 columns from two such tiles, a and b.
+template <bool EDGE>
+__device__ __forceinline__ void pack_quads(int8_t* qrow, uint8_t* srow, int64_t n, int64_t N, int lane, v4 a, v4 b) {
+    if constexpr (EDGE)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (n + i >= N) a[i] = 0.f;
+            if (n + 16 + i >= N) b[i] = 0.f;
+        }
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = max(m, max(abs_bits(a[i]), abs_bits(b[i])));
+    unsigned o = m;
+    swap_rows(m, o);
+    m = o = max(m, o);
+    const auto r = __builtin_amdgcn_permlane32_swap(m, o, false, false);
+    const unsigned s = pack_scale(max(r[0], r[1]));
+    unsigned x = quant4(a[0], a[1], a[2], a[3], s), y = quant4(b[0], b[1], b[2], b[3], s);
+    swap_rows(x, y);
+    if (lane < 16 && (!EDGE || n < N)) srow[n >> 5] = (uint8_t)s;
+    n += (lane >> 4 & 1) * 12;
+    if (!EDGE || n + 8 <= N) {
+        *reinterpret_cast<Bytes8*>(qrow + n) = Bytes8{x, y};
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (n + i < N) qrow[n + i] = (int8_t)((i < 4 ? x : y) >> (8 * (i & 3)));
 }
 
 // ---------------------------------------------------------------- large products
-// Operand tile of R rows (of C's m or n) by 64 k in LDS, 16-byte pieces.
-// [row][k] in memory: row r at piece 8 r, its piece p at p ^ (r & 7): the 16 rows that a
-// fragment read touches at one p then lie in all banks. [k][row] in memory: k at piece
+// Operand tile of R rows (of C's m or n) by BK = 64 k in LDS, in pieces of 16 bytes.
+// [row][k] in memory: row r at piece 8 r, its piece p at p ^ (r % 8): the 16 rows that a
+// fragment read touches at one p lie in all banks. [k][row] in memory: k at piece
 // k R/8, its piece p at p ^ 2 f(k), f(k) = (k & 3) | (k >> 1 & 4): the eight k that
 // half a wave's transposing read touches lie in all banks.
 constexpr int BK = 64;
 constexpr unsigned OUT_OF_RANGE = 0x80000000u;   // past every buffer's size: the copy writes zeros
 
+__device__ __forceinline__ int row_swizzle(int r) { return r & 7; }
 __device__ __forceinline__ int col_swizzle(int k) { return ((k & 3) | (k >> 1 & 4)) << 1; }
 
 struct GemmArgs {
@@ -80,7 +226,7 @@ struct GemmArgs {
     int64_t lda, ldb;        // bytes
     int64_t apl, bpl;        // bytes between planes
     int M, N, K;
-    int ksteps, nseg;        // 64-wide steps over K, and how often K is gone over (pairs of planes)
+    int ksteps, nseg;        // BK-wide steps over K, and how often K is gone over (pairs of planes)
     unsigned pa, pb;         // planes of the pairs, 4 bits each
     int tiles_m, tiles_n, splits;
     float* part;             // [splits][M][N] sums, where splits > 1
@@ -108,7 +254,7 @@ struct Copier {
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
                 const int l = i * NT + t, r = l >> 3;
-                const int kc = ((l & 7) ^ (r & 7)) * 8;
+                const int kc = ((l & 7) ^ row_swizzle(r)) * 8;
                 k[0] = kc;   // the same for every i
                 // a row past the end reads the last one: its sums are not stored
                 off[i] = (unsigned)(min(r, rows - 1 - row0) * ld + kc * 2);
@@ -121,7 +267,7 @@ struct Copier {
             __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)OUT_OF_RANGE, 0x00020000);
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            const unsigned o = k[COL ? i : 0] < left ? off[i] : OUT_OF_RANGE;
+            const unsigned o = left >= BK || k[COL ? i : 0] < left ? off[i] : OUT_OF_RANGE;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 r, (__attribute__((address_space(3))) void*)(lds + (i * NT + wave * 64) * 16), 16, (int)o, 0, 0, 0);
         }
@@ -139,8 +285,8 @@ __device__ __forceinline__ v4 mma(VecOf<f16, 8>::plain a, VecOf<f16, 8>::plain b
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-// Fragment of 16 rows (from row0) and k 32 kk .. + 31: lane l holds row l % 16 and eight
-// k from 8 (l / 16).
+// Fragment of 16 rows (from row0) and k 32 kk .. + 31: lane l holds row l % 16 and eight k
+// from 8 (l / 16).
 template <typename T, int R, bool COL>
 __device__ __forceinline__ typename Frag<T>::type read_frag(const char* lds, int row0, int kk, int lane) {
     if constexpr (COL) {
@@ -155,21 +301,78 @@ __device__ __forceinline__ typename Frag<T>::type read_frag(const char* lds, int
         return __builtin_bit_cast(typename Frag<T>::type, v);
     } else {
         const int r = row0 + (lane & 15), p = kk * 4 + (lane >> 4);
-        return *reinterpret_cast<const typename Frag<T>::type*>(lds + r * (BK * 2) + (p ^ (r & 7)) * 16);
+        return *reinterpret_cast<const typename Frag<T>::type*>(lds + r * (BK * 2) + (p ^ row_swizzle(r)) * 16);
     }
+}
+
+// The sums of a wave's tile into outputs; (m, n): this lane's first place. Straight from the
+// registers: through LDS, whole rows of a tile stored together, it took 11 us a tile of
+// 256 x 256, this way 7, of which 5 are the memory's (bf16, every CU at once).
+template <typename T, int KIND, bool EDGE, bool STREAM, int MT, int NTL>
+__device__ __forceinline__ void epilogue(const GemmArgs& g, float* part, int lane, int64_t m0, int64_t n,
+                                         v4 (&acc)[MT][NTL]) {
+    constexpr bool FWD = KIND == FORWARD, WGT = KIND == WEIGHT;
+    const Epilogue& e = g.e;
+    const int64_t N = g.N;
+    v4 bias[NTL], beta[WGT ? NTL : 1];   // bias, or gamma
+    ActForward act{};
+    if constexpr (FWD) act = act_forward(e.act);
+#pragma unroll
+    for (int j = 0; j < NTL; ++j) {
+        bias[j] = v4{0.f, 0.f, 0.f, 0.f};
+        if (FWD && e.bias) bias[j] = load4_dt<EDGE, T>(e.bias, e.bias_dt, 0, n + j * 16, N);
+        if constexpr (WGT)
+            if (e.gamma) {
+                bias[j] = load4<EDGE>(e.gamma, n + j * 16, N);
+                beta[j] = load4<EDGE>(e.beta, n + j * 16, N);
+            }
+    }
+    // by templates: the body is past what the compiler unrolls, and acc must stay in registers
+    for_each_index(std::make_integer_sequence<int, MT>(), [&](auto tag) {
+        constexpr int i = decltype(tag)::value;
+        const int64_t m = m0 + i * 16;
+        if (m >= g.M) return;   // the four lanes of a row leave together
+        if (part) {
+#pragma unroll
+            for (int j = 0; j < NTL; ++j) store4<EDGE, false>(part + m * N, n + j * 16, N, acc[i][j]);
+            return;
+        }
+        if constexpr (FWD) {
+#pragma unroll
+            for (int j = 0; j < NTL; ++j) acc[i][j] += bias[j];
+            if (e.p.q)
+#pragma unroll
+                for (int j = 0; j < NTL; j += 2)
+                    pack_quads<EDGE>(e.p.q + m * e.p.ldq, e.p.s + m * ((N + 31) / 32), n + j * 16, N, lane, acc[i][j],
+                                     acc[i][j + 1]);
+            if (e.z) store_quads<EDGE, STREAM, T>(e.z, e.io_dt, m * e.ldz, n, N, lane, acc[i]);
+            act_apply(act, acc[i]);
+        }
+        if constexpr (WGT)
+            if (e.gamma) {
+                const float db = e.db[m];
+#pragma unroll
+                for (int j = 0; j < NTL; ++j) acc[i][j] = acc[i][j] * bias[j] + db * beta[j];
+            }
+        if constexpr (!WGT)
+            if (e.add)
+#pragma unroll
+                for (int j = 0; j < NTL; ++j)
+                    acc[i][j] += load4_dt<EDGE, T>(e.add, e.io_dt, m * e.ldadd, n + j * 16, N);
+        store_quads<EDGE, STREAM, T>(e.out, e.out_dt, m * e.ldo, n, N, lane, acc[i]);
+    });
 }
 
 // A work-group's TM x TN tile of C, one part of K; each wave (TM/WM) x (TN/WN) of it. The
 // MFMA's rows are n and its columns m, so that a lane's four sums are neighbours in a
-// row of C. FRESH: the sums of a step start from zero and reach the accumulator by
-// fp32 additions; the MFMA cuts what lies below a larger accumulator's last bits,
-// which is too much for fp32 results.
-template <typename T, bool ACOL, bool BCOL, int TM, int TN, int WM, int WN, bool FRESH>
-__global__ __launch_bounds__(WM* WN * 64) void k_product(GemmArgs g) {
+// row of C.
+// The sums stay in the MFMA's accumulators over all of K: against 64 bits an fp32 dW of
+// random bf16 operands is off by 1.9e-7 (relative, 2-norm) over 8192 rows, 2.8e-7
+// over 16384.
+template <typename T, bool ACOL, bool BCOL, int TM, int TN, int WM, int WN, bool STREAM>
+__global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
     constexpr int NT = WM * WN * 64, MT = TM / WM / 16, NTL = TN / WN / 16;
-    constexpr int STAGE = (TM + TN) * BK * 2;
-    constexpr int EP_LD = TN + 4, EP_ROWS = 32 * WM;
-    static_assert(EP_ROWS * EP_LD * 4 <= 2 * STAGE, "the epilogue's rows fit the staging buffers");
+    constexpr int STAGE = (TM + TN) * BK * 2, KIND = ACOL ? WEIGHT : BCOL ? INPUT : FORWARD;
     __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int wm = wave / WN, wn = wave % WN;
@@ -210,69 +413,64 @@ __global__ __launch_bounds__(WM* WN * 64) void k_product(GemmArgs g) {
 #pragma unroll
         for (int j = 0; j < NTL; ++j) acc[i][j] = v4{0.f, 0.f, 0.f, 0.f};
 
-    issue(0);
-    for (int s = s_begin; s < s_end; ++s) {
-        const int stage = (s - s_begin) & 1;
-        // this step's copies have landed for every wave, and every wave has read the other stage
+    // Two halves of a step, 32 k each. While the matrix cores work on one half's fragments,
+    // the other's are read from LDS. Between the halves, the next step's copies have
+    // landed, and this step's buffer is free for those of the step after it.
+    typename Frag<T>::type fa[2][MT], fb[2][NTL];
+    auto read = [&](int stage, int kk) {
+        const char* la = lds + stage * STAGE;
+        const char* lb = la + TM * BK * 2;
+#pragma unroll
+        for (int j = 0; j < NTL; ++j) fb[kk][j] = read_frag<T, TN, BCOL>(lb, wn * (TN / WN) + j * 16, kk, lane);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) fa[kk][i] = read_frag<T, TM, ACOL>(la, wm * (TM / WM) + i * 16, kk, lane);
+    };
+    auto multiply = [&](int kk) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NTL; ++j) acc[i][j] = mma(fb[kk][j], fa[kk][i], acc[i][j]);
+        // one LDS read, then two products, and so on
+        constexpr int READS = MT * (ACOL ? 2 : 1) + NTL * (BCOL ? 2 : 1), PER = MT * NTL / READS;
+#pragma unroll
+        for (int i = 0; i < READS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, MT * NTL - READS * PER, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // this wave's copies have landed and its LDS reads are in registers; then every wave's
+    auto wait_all = [&]() {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (s + 1 < s_end) issue(stage ^ 1);
-        const char* la = lds + stage * STAGE;
-        const char* lb = la + TM * BK * 2;
-        v4 fresh[FRESH ? MT : 1][FRESH ? NTL : 1];
-#pragma unroll
-        for (int kk = 0; kk < BK / 32; ++kk) {
-            typename Frag<T>::type fa[MT], fb[NTL];
-#pragma unroll
-            for (int j = 0; j < NTL; ++j) fb[j] = read_frag<T, TN, BCOL>(lb, wn * (TN / WN) + j * 16, kk, lane);
-#pragma unroll
-            for (int i = 0; i < MT; ++i) fa[i] = read_frag<T, TM, ACOL>(la, wm * (TM / WM) + i * 16, kk, lane);
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NTL; ++j) {
-                    if constexpr (FRESH) {
-                        const v4 zero = {0.f, 0.f, 0.f, 0.f};
-                        acc[i][j] += mma(fb[j], fa[i], zero);
-                    } else {
-                        acc[i][j] = mma(fb[j], fa[i], acc[i][j]);
-                    }
-                }
-        }
+    };
+
+    issue(0);
+    wait_all();
+    if (s_begin + 1 < s_end) issue(1);
+    read(0, 0);
+    for (int s = s_begin; s < s_end; ++s) {
+        const int stage = (s - s_begin) & 1;
+        __builtin_amdgcn_sched_barrier(0);
+        read(stage, 1);
+        multiply(0);
+        wait_all();
+        if (s + 2 < s_end) issue(stage);
+        __builtin_amdgcn_sched_barrier(0);
+        if (s + 1 < s_end) read(stage ^ 1, 0);
+        multiply(1);
     }
 
-    // 32 rows of each wave's tile at a time through LDS, so that a row's pieces are stored together
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    float* ep = reinterpret_cast<float*>(lds);
     float* part = g.splits > 1 ? g.part + (int64_t)blockIdx.y * g.M * g.N : nullptr;
-#pragma unroll
-    for (int q = 0; q < MT / 2; ++q) {
-        if (q) __syncthreads();
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < NTL; ++j)
-                *reinterpret_cast<v4*>(&ep[(wm * 32 + h * 16 + (lane & 15)) * EP_LD + wn * (TN / WN) + j * 16 +
-                                           4 * (lane >> 4)]) = acc[2 * q + h][j];
-        __syncthreads();
-        constexpr int PIECES = TN / 8;
-#pragma unroll 1
-        for (int u = t; u < EP_ROWS * PIECES; u += NT) {
-            const int r = u / PIECES, c = (u % PIECES) * 8;
-            const int64_t m = m0 + (r >> 5) * (TM / WM) + q * 32 + (r & 31), n = n0 + c;
-            const f8 v = *reinterpret_cast<const f8*>(&ep[r * EP_LD + c]);
-            if (part) {
-                if (m < g.M) store8(part + m * g.N, n, (int64_t)g.N, v);
-            } else {
-                finish8(g.e, g.N, m < g.M, m, n, v);
-            }
-        }
-    }
+    const int m = m0 + wm * (TM / WM) + (lane & 15), n = n0 + wn * (TN / WN) + 4 * (lane >> 4);
+    if (n0 + TN <= g.N) epilogue<T, KIND, false, STREAM>(g, part, lane, m, n, acc);
+    else epilogue<T, KIND, true, STREAM>(g, part, lane, m, n, acc);
 }
 
 // Joins the K parts in order and finishes.
+template <int KIND>
 __global__ __launch_bounds__(256) void k_finish(const float* __restrict__ part, int splits, int64_t M, int64_t N,
                                                 Epilogue e) {
     const int64_t pieces = (N + 31) / 32 * 4, total = M * pieces;
@@ -283,7 +481,7 @@ __global__ __launch_bounds__(256) void k_finish(const float* __restrict__ part, 
         f8 v = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (in)
             for (int z = 0; z < splits; ++z) v += load8(part + (z * M + m) * N, n, N);
-        finish8(e, N, in, m, n, v);
+        finish8<KIND>(e, N, in, m, n, v);
     }
 }
 
@@ -374,7 +572,7 @@ __global__ __launch_bounds__(512) void k_skinny(SkinnyArgs g) {
         if (m < g.M) store8(g.part + ((int64_t)blockIdx.y * g.M + m) * g.N, n, g.N, v);
         return;
     }
-    finish8(g.e, g.N, m < g.M, m, n, v);
+    finish8<FORWARD>(g.e, g.N, m < g.M, m, n, v);
 }
 
 // ---------------------------------------------------------------- operands into the workspace
@@ -409,6 +607,10 @@ __global__ __launch_bounds__(256) void k_lay_out_split(const float* __restrict__
 // ---------------------------------------------------------------- host
 constexpr int64_t SKINNY_ROWS = 16;
 constexpr int64_t CUS = 256;
+// Past the 256 MB of the last-level cache, outputs written through the caches push the operands
+// out: 8192^3, dx and dW 1003 and 1030 us, with nontemporal stores 915 and 943. Below, those
+// are slower: dx of 8192 x 8192 over K = 2048 takes 248 us, with them 271.
+constexpr int64_t LAST_LEVEL_CACHE = int64_t(256) << 20;
 
 // Rows of `cols` elements that the copies into LDS take as they are.
 bool plain16(const void* p, int64_t ld, int64_t cols) {
@@ -474,22 +676,27 @@ hipError_t lay_out(int dt, const Operand& o, const void* src, int64_t ld, Packed
     return hipGetLastError();
 }
 
-template <typename T, bool ACOL, bool BCOL, bool FRESH>
-hipError_t run_product(const Plan& q, const GemmArgs& g, hipStream_t st) {
+template <typename T, bool ACOL, bool BCOL>
+hipError_t run_product(const Product& p, const Plan& q, const GemmArgs& g, hipStream_t st) {
     const dim3 grid((unsigned)(q.tiles_m * q.tiles_n), (unsigned)q.splits);
-    if (q.tile == 256) k_product<T, ACOL, BCOL, 256, 256, 2, 4, FRESH><<<grid, 512, 0, st>>>(g);
-    else k_product<T, ACOL, BCOL, 128, 128, 2, 2, FRESH><<<grid, 256, 0, st>>>(g);
+    const int64_t bytes = (p.M * p.K + p.N * p.K) * 2 * (q.nseg > 1 ? 3 : 1) + p.M * p.N * dtype_bytes(g.e.out_dt);
+    if (q.tile == 128) k_product<T, ACOL, BCOL, 128, 128, 2, 2, false><<<grid, 256, 0, st>>>(g);
+    else if (bytes <= LAST_LEVEL_CACHE) k_product<T, ACOL, BCOL, 256, 256, 2, 4, false><<<grid, 512, 0, st>>>(g);
+    else k_product<T, ACOL, BCOL, 256, 256, 2, 4, true><<<grid, 512, 0, st>>>(g);
     return hipGetLastError();
 }
-template <typename T, bool FRESH>
+template <typename T>
 hipError_t run_product(const Product& p, const Plan& q, const GemmArgs& g, hipStream_t st) {
-    if (p.a_col) return run_product<T, true, true, FRESH>(q, g, st);
-    return p.b_col ? run_product<T, false, true, FRESH>(q, g, st) : run_product<T, false, false, FRESH>(q, g, st);
+    if (p.a_col) return run_product<T, true, true>(p, q, g, st);
+    return p.b_col ? run_product<T, false, true>(p, q, g, st) : run_product<T, false, false>(p, q, g, st);
 }
 
-hipError_t run_finish(const float* part, int splits, int64_t M, int64_t N, const Epilogue& e, hipStream_t st) {
-    const int64_t pieces = ceil_div(N, 32) * 4;
-    k_finish<<<(unsigned)std::min<int64_t>(ceil_div(M * pieces, 256), 8192), 256, 0, st>>>(part, splits, M, N, e);
+hipError_t run_finish(const Product& p, const float* part, int splits, const Epilogue& e, hipStream_t st) {
+    const int64_t pieces = ceil_div(p.N, 32) * 4;
+    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(p.M * pieces, 256), 8192);
+    if (p.a_col) k_finish<WEIGHT><<<grid, 256, 0, st>>>(part, splits, p.M, p.N, e);
+    else if (p.b_col) k_finish<INPUT><<<grid, 256, 0, st>>>(part, splits, p.M, p.N, e);
+    else k_finish<FORWARD><<<grid, 256, 0, st>>>(part, splits, p.M, p.N, e);
     return hipGetLastError();
 }
 
@@ -546,12 +753,10 @@ hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws,
         g.splits = q.splits;
         g.part = (float*)w;
         g.e = e;
-        const bool fresh = e.out_dt == DT_F32;
-        if (dt == DT_F16) err = fresh ? run_product<f16, true>(p, q, g, st) : run_product<f16, false>(p, q, g, st);
-        else err = fresh ? run_product<bf16, true>(p, q, g, st) : run_product<bf16, false>(p, q, g, st);
+        err = dt == DT_F16 ? run_product<f16>(p, q, g, st) : run_product<bf16>(p, q, g, st);
     }
     if (err != hipSuccess || q.splits == 1) return err;
-    return run_finish((const float*)w, q.splits, p.M, p.N, e, st);
+    return run_finish(p, (const float*)w, q.splits, e, st);
 }
 
 }  // namespace mfac

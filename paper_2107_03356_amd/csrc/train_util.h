@@ -78,20 +78,19 @@ __device__ __forceinline__ unsigned max_bits8(f8 v) {
     return m;
 }
 
-// Four values as int8 in a word, the lowest first; scaled by 2^-e. With e = 122 a value may
-// round to 64, and 64 * 2^122 is no fp32 value: 63 then.
+// Four values as int8 in a word, the lowest first; scaled by 2^-e. Added to 3 * 2^22 a value
+// is rounded to an integer (ties to even), whose low byte is the sum's. With e = 122 a
+// value may round to 64, and 64 * 2^122 is no fp32 value: 63 then.
 __device__ __forceinline__ unsigned quant4(float a, float b, float c, float d, unsigned s) {
-    if (s == 255u) return 0u;
-    const float r = pack_inverse(s);
-    int ia = (int)__builtin_rintf(a * r), ib = (int)__builtin_rintf(b * r);
-    int ic = (int)__builtin_rintf(c * r), id = (int)__builtin_rintf(d * r);
-    if (s == 249u) {
-        ia = max(-63, min(63, ia));
-        ib = max(-63, min(63, ib));
-        ic = max(-63, min(63, ic));
-        id = max(-63, min(63, id));
+    const float r = pack_inverse(s), big = 12582912.f;
+    unsigned ia = __float_as_uint(fmaf(a, r, big)), ib = __float_as_uint(fmaf(b, r, big));
+    unsigned ic = __float_as_uint(fmaf(c, r, big)), id = __float_as_uint(fmaf(d, r, big));
+    if (s >= 249u) {
+        auto least = [](unsigned v) { return (unsigned)max(-63, min(63, (int)(int8_t)v)); };
+        ia = least(ia), ib = least(ib), ic = least(ic), id = least(id);
     }
-    return (unsigned)(ia & 255) | (unsigned)(ib & 255) << 8 | (unsigned)(ic & 255) << 16 | (unsigned)id << 24;
+    const unsigned lo = __builtin_amdgcn_perm(ib, ia, 0x0c0c0400u), hi = __builtin_amdgcn_perm(id, ic, 0x04000c0cu);
+    return s == 255u ? 0u : lo | hi;
 }
 
 struct __attribute__((packed, aligned(1))) Bytes8 {
@@ -163,19 +162,45 @@ __device__ __forceinline__ float erfc_pos(float y, float ex) {
     return p * t * ex;
 }
 
-template <int ACT>
-__device__ __forceinline__ float act_of(float z) {
-    if constexpr (ACT == 1) return z > 0.f || z != z ? z : 0.f;
-    if constexpr (ACT == 2) {
-        const float h = 0.5f * erfc_pos(fabsf(z) * 0.70710678118654752f, exp_fast(-0.5f * z * z));
-        return z * (z < 0.f ? h : 1.f - h);
+// The forward activations as three formulas, so that a kernel holds three and not five:
+// max(z, lo), lo = -inf or 0; z / (1 + 2^(z (p + q z^2))), for x / (1 + exp(-x)) and
+// (1 + tanh u) / 2 = 1 / (1 + exp(-2u)); z Phi(z).
+struct ActForward {
+    int formula;
+    float p, q;
+};
+__device__ __forceinline__ ActForward act_forward(int act) {
+    if (act == 4) return {1, -1.44269504088896341f, 0.f};
+    if (act == 3) return {1, -2.30220819813644130f, -0.10294323980544930f};   // -2 log2(e) sqrt(2/pi) (1, 0.044715)
+    return {act == 2 ? 2 : 0, act == 1 ? 0.f : -__builtin_inff(), 0.f};
+}
+// N values of one formula under one uniform branch.
+template <typename V, int N>
+__device__ __forceinline__ void act_apply(const ActForward& f, V (&z)[N]) {
+    constexpr int W = sizeof(V) / 4;
+    if (f.formula == 1) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const float x = z[j][i];
+                z[j][i] = x * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * fmaf(f.q * x, x, f.p)));
+            }
+    } else if (f.formula == 2) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const float x = z[j][i];
+                const float h = 0.5f * erfc_pos(fabsf(x) * 0.70710678118654752f, exp_fast(-0.5f * x * x));
+                z[j][i] = x * (x < 0.f ? h : 1.f - h);
+            }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int i = 0; i < W; ++i) z[j][i] = z[j][i] < f.p ? f.p : z[j][i];   // a NaN stays one
     }
-    if constexpr (ACT == 3) {   // (1 + tanh u) / 2 = 1 / (1 + exp(-2u))
-        const float u = z * fmaf(0.044715f * z, z, 1.f);
-        return z * __builtin_amdgcn_rcpf(1.f + exp_fast(-1.59576912160573072f * u));
-    }
-    if constexpr (ACT == 4) return z * __builtin_amdgcn_rcpf(1.f + exp_fast(-z));
-    return z;
 }
 
 // act'(z), and act(z) in *a.

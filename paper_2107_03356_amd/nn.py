@@ -85,6 +85,10 @@ def _type(t, what):
 
 def _rows(t, what):
     """t as a matrix of rows with unit stride (a copy where it has none)."""
+    if t.dim() == 2 and t.is_cuda:   # most calls: nothing to do
+        (rows, cols), (ld, unit) = t.shape, t.stride()
+        if unit == 1 and ld >= cols > 0:
+            return t
     if not t.is_cuda:
         raise ValueError(f"{what}: a CUDA tensor, not one on {t.device}")
     if t.dim() == 0 or t.shape[-1] == 0:
@@ -131,15 +135,18 @@ def _act(name):
 
 def _call(name, device, *args):
     """The C call of this name on the current stream of `device`."""
-    fn = getattr(load(), name)
-    stream = torch.cuda.current_stream(device).cuda_stream
-    if device.index is not None and device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            status = fn(*args, stream)
+    if device.index == torch._C._cuda_getDevice():
+        status = getattr(load(), name)(*args, torch._C._cuda_getCurrentRawStream(device.index))
     else:
-        status = fn(*args, stream)
+        with torch.cuda.device(device):
+            status = getattr(load(), name)(*args, torch.cuda.current_stream(device).cuda_stream)
     if status != B.MFAC_OK:
         raise MfacError(name, status)
+
+
+def _like(t):
+    """Room for a result of t's shape and type, its rows contiguous."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _workspace(nbytes, device):
@@ -175,7 +182,7 @@ def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, pack=False):
     x2 = _rows(x, "layer_norm: x")
     rows, cols = x2.shape
     w, b, wt = _norm_params(weight, bias, x2)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = _like(x)
     rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
     mean = None if pack else torch.empty_like(rstd)
     p = Packed8.empty(rows, cols, x.device) if pack else None
@@ -218,12 +225,12 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, add=None, params=True):
     if add is not None:
         add = _rows(add, "layer_norm: add")
         _same("layer_norm: add", add, dy2, dy2.shape)
-    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
+    dx = _like(dy)
     dw = db = None
     ws = (None, 0, None)
     if params:
         grads = torch.empty((2, cols), dtype=torch.float32 if w is None else w.dtype, device=dy.device)
-        dw, db = grads[0], grads[1]
+        dw, db = grads.unbind(0)
         ws = _workspace(load().mfac_layer_norm_bwd_workspace_bytes(rows, cols), dy.device)
     _call("mfac_layer_norm_bwd", dy.device, _type(dy2, "layer_norm: dy"), wt, rows, cols, *_mat(dy2), *xm, _ptr(mean),
           rstd.data_ptr(), *packed, _ptr(w), *_mat(add), dx.data_ptr(), cols, _ptr(dw), _ptr(db), ws[0], ws[1])
@@ -276,8 +283,8 @@ def act_backward(dy, z=None, act="none", want_a=False, want_db=True):
         z = _rows(z, "act: z")
         _same("act: z", z, dy2, dy2.shape)
         zm = _mat(z)
-    dz = dy if z is None else torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
-    a = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device) if want_a else None
+    dz = dy if z is None else _like(dy)
+    a = _like(dy) if want_a else None
     db = torch.empty(cols, dtype=torch.float32, device=dy.device) if want_db else None
     if z is None and not want_db:
         return dz, None, None
