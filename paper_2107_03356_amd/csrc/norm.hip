@@ -89,21 +89,21 @@ __global__ __launch_bounds__(norm_block(NT)) void k_norm_fwd(NormArgs<T, TW> g) 
     }
     const int64_t step = (int64_t)gridDim.x * RPB;
     int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / NT;
-    f8 next[NCH];
+    Raw8<T> next[NCH];
     if (row < g.rows)
 #pragma unroll
-        for (int j = 0; j < NCH; ++j) next[j] = load8(g.x + row * g.ldx, (int64_t)(j * NT + t) * 8, g.cols);
+        for (int j = 0; j < NCH; ++j) next[j].load(g.x + row * g.ldx, (int64_t)(j * NT + t) * 8, g.cols);
     for (; row < g.rows; row += step) {
         f8 x[NCH];
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
-            x[j] = next[j];
+            x[j] = next[j].get();
             sum += sum8(x[j]);
         }
         if (row + step < g.rows)
 #pragma unroll
-            for (int j = 0; j < NCH; ++j) next[j] = load8(g.x + (row + step) * g.ldx, (int64_t)(j * NT + t) * 8, g.cols);
+            for (int j = 0; j < NCH; ++j) next[j].load(g.x + (row + step) * g.ldx, (int64_t)(j * NT + t) * 8, g.cols);
         const float mean = row_sum<NT>(sum, red, turn) / g.ncols;
         float sq = 0.f;
 #pragma unroll
@@ -201,34 +201,72 @@ __device__ __forceinline__ f8 load_xhat(const NormBwdArgs<T, TW>& g, int64_t row
     return x;
 }
 
-template <typename T, typename TW, int NT, int NCH>
+// What a row's pass takes, loaded while the row before it is worked on.
+template <typename T, typename TW, int NT, int NCH, bool PACKED>
+struct NormBwdRow {
+    static constexpr bool ADD = NT < 1024;   // add too; without room for it it is loaded when it is used
+    Raw8<T> dy[NCH], add[NCH];
+    std::conditional_t<PACKED, RawPacked8, Raw8<T>> x[NCH];
+    float mean, rstd;
+    __device__ __forceinline__ void load(const NormBwdArgs<T, TW>& g, int64_t row, int t) {
+        rstd = g.rstd[row];
+        if constexpr (!PACKED) mean = g.mean[row];
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            const int64_t c = (int64_t)(j * NT + t) * 8;
+            dy[j].load(g.dy + row * g.lddy, c, g.cols);
+            if constexpr (PACKED) x[j].load(g.p.q + row * g.p.ldq, g.p.s + row * g.ngroups, c, g.cols);
+            else x[j].load(g.x + row * g.ldx, c, g.cols);
+            if (ADD && g.add) add[j].load(g.add + row * g.ldadd, c, g.cols);
+        }
+    }
+};
+
+template <typename T, typename TW, int NT, int NCH, bool PACKED>
 __global__ __launch_bounds__(norm_block(NT)) void k_norm_bwd(NormBwdArgs<T, TW> g) {
     constexpr int RPB = norm_block(NT) / NT;
     __shared__ float red[4 * (NT / 64)];
     __shared__ float cols_of[RPB > 1 ? RPB * NT * 8 : 1];
     int turn = 0;
     const int t = threadIdx.x % NT;
+    // 1024 threads have 128 registers each: no room for the next row, nor for w
+    constexpr bool AHEAD = NT < 1024;
     f8 w[NCH], sw[NCH], sb[NCH];
+    auto load_w = [&]() {
 #pragma unroll
-    for (int j = 0; j < NCH; ++j) {
-        w[j] = sw[j] = sb[j] = f8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (g.w) w[j] = load8(g.w, (int64_t)(j * NT + t) * 8, g.cols);
-        else w[j] += 1.f;
-    }
+        for (int j = 0; j < NCH; ++j) {
+            w[j] = f8{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+            if (g.w) w[j] = load8(g.w, (int64_t)(j * NT + t) * 8, g.cols);
+        }
+    };
+    if (AHEAD) load_w();
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) sw[j] = sb[j] = f8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const int64_t step = (int64_t)gridDim.x * RPB;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / NT; row < g.rows; row += step) {
-        const float rstd = g.rstd[row], mean = g.mean ? g.mean[row] : 0.f;
-        f8 h[NCH], xh[NCH], ad[NCH];
+    int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / NT;
+    NormBwdRow<T, TW, NT, NCH, PACKED> next;
+    if (AHEAD && row < g.rows) next.load(g, row, t);
+    for (; row < g.rows; row += step) {
+        if (!AHEAD) {
+            next.load(g, row, t);
+            load_w();
+        }
+        const auto now = next;
+        if (AHEAD && row + step < g.rows) next.load(g, row + step, t);
+        f8 h[NCH], xh[NCH];
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
-            const int64_t c = (int64_t)(j * NT + t) * 8;
-            h[j] = load8(g.dy + row * g.lddy, c, g.cols);
-            xh[j] = load_xhat(g, row, c, mean, rstd);
-            if (g.add) ad[j] = load8(g.add + row * g.ldadd, c, g.cols);
-        }
+            h[j] = now.dy[j].get();
+            xh[j] = now.x[j].get();
+            if constexpr (!PACKED) {
+                const int64_t c = (int64_t)(j * NT + t) * 8;
+                xh[j] = (xh[j] - now.mean) * now.rstd;
+                if (c + 8 > g.cols)
 #pragma unroll
-        for (int j = 0; j < NCH; ++j) {
+                    for (int i = 0; i < 8; ++i)
+                        if (c + i >= g.cols) xh[j][i] = 0.f;
+            }
             sb[j] += h[j];
             sw[j] += h[j] * xh[j];
             h[j] *= w[j];
@@ -240,8 +278,12 @@ __global__ __launch_bounds__(norm_block(NT)) void k_norm_bwd(NormBwdArgs<T, TW> 
         s2 *= g.inv_cols;
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
-            f8 d = (h[j] - s1 - xh[j] * s2) * rstd;
-            if (g.add) d += ad[j];
+            f8 d = (h[j] - s1 - xh[j] * s2) * now.rstd;
+            if (AHEAD) {
+                if (g.add) d += now.add[j].get();
+            } else if (g.add) {
+                d += load8(g.add + row * g.ldadd, (int64_t)(j * NT + t) * 8, g.cols);
+            }
             store8(g.dx + row * g.lddx, (int64_t)(j * NT + t) * 8, g.cols, d);
         }
     }
@@ -312,7 +354,7 @@ __global__ __launch_bounds__(256) void k_norm_bwd_cols(NormBwdArgs<T, TW> g) {
 }
 
 constexpr int64_t NORM_MAX_COLS = 16384;   // 1024 threads of two chunks
-constexpr int64_t NORM_FWD_GRID = 2048, NORM_BWD_GRID = 512, NORM_LONG_PARTS = 64;
+constexpr int64_t NORM_FWD_GRID = 2048, NORM_LONG_PARTS = 64;
 
 int64_t rows_per_block(int64_t cols) { return cols <= 1024 ? 4 : 1; }
 
@@ -356,7 +398,13 @@ hipError_t norm_bwd(int64_t rows, int64_t cols, const void* dy, int64_t lddy, co
         return hipGetLastError();
     }
     const int64_t grid = norm_bwd_parts(rows, cols);
-#define LAUNCH(NT, NCH) k_norm_bwd<T, TW, NT, NCH><<<(unsigned)grid, norm_block(NT), 0, st>>>(g);
+#define LAUNCH(NT, NCH) k_norm_bwd<T, TW, NT, NCH, true><<<(unsigned)grid, norm_block(NT), 0, st>>>(g);
+    if (p.q) {
+        NORM_SHAPES(LAUNCH)
+        return hipGetLastError();
+    }
+#undef LAUNCH
+#define LAUNCH(NT, NCH) k_norm_bwd<T, TW, NT, NCH, false><<<(unsigned)grid, norm_block(NT), 0, st>>>(g);
     NORM_SHAPES(LAUNCH)
 #undef LAUNCH
     return hipGetLastError();
@@ -371,10 +419,12 @@ hipError_t by_types(int dt, int wt, F f) {
 
 }  // namespace
 
-// Partial column sums that the backward pass writes: one a work-group.
+// Partial column sums that the backward pass writes, one a work-group: as many as keep 8 waves
+// on a CU, since they are written and read again (at 16384 x 4096 in bf16 7% of the traffic).
 int64_t norm_bwd_parts(int64_t rows, int64_t cols) {
     if (cols > NORM_MAX_COLS) return std::min(rows, NORM_LONG_PARTS);
-    return std::min(ceil_div(rows, rows_per_block(cols)), NORM_BWD_GRID);
+    const int64_t grid = cols <= 1024 ? 512 : cols <= 2048 ? 1024 : cols <= 4096 ? 512 : 256;
+    return std::min(ceil_div(rows, rows_per_block(cols)), grid);
 }
 
 hipError_t launch_layer_norm(int dt, int wt, int64_t rows, int64_t cols, const void* x, int64_t ldx, const void* w,

@@ -78,6 +78,17 @@ __global__ __launch_bounds__(256) void k_zero_matrix(Strips s, T* __restrict__ y
 }
 
 // ---------------------------------------------------------------- activation, backward
+template <typename T>
+__device__ __forceinline__ void load_z(Raw8<T>& v, const T* z, int64_t ldz, Packed, int64_t, int64_t r, int64_t c,
+                                       int64_t cols) {
+    v.load(z + r * ldz, c, cols);
+}
+template <typename T>
+__device__ __forceinline__ void load_z(RawPacked8& v, const T*, int64_t, Packed p, int64_t ngroups, int64_t r, int64_t c,
+                                       int64_t cols) {
+    v.load(p.q + r * p.ldq, p.s + r * ngroups, c, cols);
+}
+
 // Work-group (strip blockIdx.x, part blockIdx.y): its rows part, part + nparts, ... of
 // the strip's columns, by wave and sub-row; the column sums in registers, joined
 // over the waves and sub-rows at the end.
@@ -94,12 +105,21 @@ __global__ __launch_bounds__(256) void k_act_bwd(Strips s, int act, const T* dy,
     with_act(ZP ? act : 0, [&](auto tag) {
         constexpr int ACT = decltype(tag)::value;
         if (c >= s.cols) return;
-        for (int64_t row = blockIdx.y * nsub + sub; row < s.rows; row += gridDim.y * nsub) {
-            f8 d = load8(dy + row * lddy, c, s.cols);
+        const int64_t step = gridDim.y * nsub;
+        int64_t row = blockIdx.y * nsub + sub;
+        // the next row is on its way while this one is worked on
+        Raw8<T> d_next;
+        std::conditional_t<ZP == 2, RawPacked8, Raw8<T>> z_next;
+        auto load = [&](int64_t r) {
+            d_next.load(dy + r * lddy, c, s.cols);
+            if constexpr (ACT != 0) load_z(z_next, z, ldz, p, ngroups, r, c, s.cols);
+        };
+        if (row < s.rows) load(row);
+        for (; row < s.rows; row += step) {
+            f8 d = d_next.get(), v{};
+            if constexpr (ACT != 0) v = z_next.get();
+            if (row + step < s.rows) load(row + step);
             if constexpr (ACT != 0) {
-                f8 v;
-                if constexpr (ZP == 2) v = load_packed8(p.q + row * p.ldq, p.s + row * ngroups, c, s.cols);
-                else v = load8(z + row * ldz, c, s.cols);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     float av;

@@ -25,6 +25,14 @@ struct VecOf {
     typedef float wide __attribute__((ext_vector_type(N)));
 };
 
+// Values of other lanes of a row of 16, without a trip through LDS.
+constexpr int DPP_XOR1 = 0xB1, DPP_XOR2 = 0x4E;               // quad_perm
+constexpr int DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140;    // lane i of 8, of 16: 7 - i, 15 - i
+template <int CTRL>
+__device__ __forceinline__ unsigned dpp(unsigned v) {
+    return (unsigned)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, true);
+}
+
 // Elements c .. c + 7 of a row of `cols`; zeros past its end.
 template <typename T>
 __device__ __forceinline__ f8 load8(const T* __restrict__ row, int64_t c, int64_t cols) {
@@ -38,6 +46,21 @@ __device__ __forceinline__ f8 load8(const T* __restrict__ row, int64_t c, int64_
         if (c + i < cols) r[i] = (float)row[c + i];
     return r;
 }
+
+// The same in two halves: the load, and what waits for it.
+template <typename T>
+struct Raw8 {
+    typename VecOf<T, 8>::plain v;
+    __device__ __forceinline__ void load(const T* __restrict__ row, int64_t c, int64_t cols) {
+        if (c + 8 <= cols) {
+            v = *reinterpret_cast<const typename VecOf<T, 8>::type*>(row + c);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? row[c + i] : (T)0.f;
+    }
+    __device__ __forceinline__ f8 get() const { return __builtin_convertvector(v, f8); }
+};
 
 template <typename T>
 __device__ __forceinline__ void store8(T* __restrict__ row, int64_t c, int64_t cols, f8 v) {
@@ -97,14 +120,26 @@ struct __attribute__((packed, aligned(1))) Bytes8 {
     unsigned lo, hi;
 };
 
-// Columns c .. c + 7 of a copy's row: q * 2^e.
-__device__ __forceinline__ f8 load_packed8(const int8_t* __restrict__ qrow, const uint8_t* __restrict__ srow, int64_t c,
-                                           int64_t cols) {
-    f8 r = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (c >= cols) return r;
-    const float sc = unpack_scale(srow[c >> 5]);
-    if (c + 8 <= cols) {
-        const Bytes8 b = *reinterpret_cast<const Bytes8*>(qrow + c);
+struct RawPacked8 {
+    Bytes8 b;
+    unsigned s;
+    __device__ __forceinline__ void load(const int8_t* __restrict__ qrow, const uint8_t* __restrict__ srow, int64_t c,
+                                         int64_t cols) {
+        b = Bytes8{0, 0};
+        s = 127;
+        if (c >= cols) return;
+        s = srow[c >> 5];
+        if (c + 8 <= cols) {
+            b = *reinterpret_cast<const Bytes8*>(qrow + c);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i < cols) (i < 4 ? b.lo : b.hi) |= (unsigned)(uint8_t)qrow[c + i] << (8 * (i & 3));
+    }
+    __device__ __forceinline__ f8 get() const {
+        f8 r;
+        const float sc = unpack_scale(s);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             r[i] = (float)(int8_t)(b.lo >> (8 * i)) * sc;
@@ -112,10 +147,14 @@ __device__ __forceinline__ f8 load_packed8(const int8_t* __restrict__ qrow, cons
         }
         return r;
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (c + i < cols) r[i] = (float)qrow[c + i] * sc;
-    return r;
+};
+
+// Columns c .. c + 7 of a copy's row: q * 2^e.
+__device__ __forceinline__ f8 load_packed8(const int8_t* __restrict__ qrow, const uint8_t* __restrict__ srow, int64_t c,
+                                           int64_t cols) {
+    RawPacked8 r;
+    r.load(qrow, srow, c, cols);
+    return r.get();
 }
 
 // Eight values of a group whose scale byte is s, columns c .. c + 7.
@@ -137,8 +176,8 @@ __device__ __forceinline__ void store_packed8(int8_t* __restrict__ qrow, int64_t
 __device__ __forceinline__ void pack_group(int8_t* __restrict__ qrow, uint8_t* __restrict__ srow, int64_t c, int64_t cols,
                                            f8 v) {
     unsigned m = max_bits8(v);
-    m = max(m, (unsigned)__shfl_xor((int)m, 1));
-    m = max(m, (unsigned)__shfl_xor((int)m, 2));
+    m = max(m, dpp<DPP_XOR1>(m));
+    m = max(m, dpp<DPP_XOR2>(m));
     const unsigned s = pack_scale(m);
     if (c >= cols) return;
     store_packed8(qrow, c, cols, v, s);
@@ -246,9 +285,14 @@ __device__ __forceinline__ void with_act(int act, F f) {
 
 // ---------------------------------------------------------------- sums over a wave
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    return v;
+    v += __uint_as_float(dpp<DPP_XOR1>(__float_as_uint(v)));
+    v += __uint_as_float(dpp<DPP_XOR2>(__float_as_uint(v)));
+    v += __uint_as_float(dpp<DPP_HALF_MIRROR>(__float_as_uint(v)));
+    v += __uint_as_float(dpp<DPP_MIRROR>(__float_as_uint(v)));
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(h[0]) + __uint_as_float(h[1]);
 }
 __device__ __forceinline__ float sum8(f8 v) {
     return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
