@@ -219,7 +219,10 @@ constexpr int BK = 64;
 constexpr unsigned OUT_OF_RANGE = 0x80000000u;   // past every buffer's size: the copy writes zeros
 
 __device__ __forceinline__ int row_swizzle(int r) { return r & 7; }
-__device__ __forceinline__ int col_swizzle(int k) { return ((k & 3) | (k >> 1 & 4)) << 1; }
+template <int R>
+__device__ __forceinline__ int col_swizzle(int k) {
+    return ((k & 3) | (k >> 1 & 4)) << 1 & (R / 8 - 1);   // 64 rows: four of the eight k
+}
 
 struct GemmArgs {
     const char *A, *B;       // 16-bit elements
@@ -245,7 +248,7 @@ struct Copier {
             step = BK * ld;
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
-                const int l = i * NT + t, kk = l / (R / 8), c = ((l % (R / 8)) ^ col_swizzle(kk)) * 8;
+                const int l = i * NT + t, kk = l / (R / 8), c = ((l % (R / 8)) ^ col_swizzle<R>(kk)) * 8;
                 k[i] = kk;
                 off[i] = row0 + c < rows ? (unsigned)(kk * ld + c * 2) : OUT_OF_RANGE;
             }
@@ -293,7 +296,7 @@ __device__ __forceinline__ typename Frag<T>::type read_frag(const char* lds, int
         typedef short s4 __attribute__((ext_vector_type(4)));
         typedef short s8 __attribute__((ext_vector_type(8)));
         const int k = kk * 32 + (lane >> 4) * 8 + ((lane & 15) >> 2), r = row0 + 4 * (lane & 3);
-        const int at = k * R * 2 + ((r >> 3) ^ col_swizzle(k)) * 16 + (r & 4) * 2;
+        const int at = k * R * 2 + ((r >> 3) ^ col_swizzle<R>(k)) * 16 + (r & 4) * 2;
         typedef __attribute__((address_space(3))) s4* P;
         const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds + at));
         const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds + at + 4 * R * 2));
@@ -432,12 +435,14 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
             for (int j = 0; j < NTL; ++j) acc[i][j] = mma(fb[kk][j], fa[kk][i], acc[i][j]);
         // one LDS read, then two products, and so on
         constexpr int READS = MT * (ACOL ? 2 : 1) + NTL * (BCOL ? 2 : 1), PER = MT * NTL / READS;
+        if constexpr (PER > 0) {
 #pragma unroll
-        for (int i = 0; i < READS; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
+            for (int i = 0; i < READS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, PER, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, MT * NTL - READS * PER, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, MT * NTL - READS * PER, 0);
         __builtin_amdgcn_sched_barrier(0);
     };
     // this wave's copies have landed and its LDS reads are in registers; then every wave's
@@ -486,10 +491,12 @@ __global__ __launch_bounds__(256) void k_finish(const float* __restrict__ part, 
 }
 
 // ---------------------------------------------------------------- few rows
-// C (M <= 16 rows) = x W^T. A work-group of 8 waves takes 32 rows of W and one part of K,
-// which its waves share out in pieces of 16 bytes a row; lane l holds row l % 16 of x
-// and of a half of the W rows, and the k of piece l / 16. The waves' sums are joined
-// through LDS. 16-bit types on v_mfma_f32_16x16x32, fp32 on v_mfma_f32_16x16x4.
+// C (M <= 16 rows) = x W^T. A work-group takes 16 NH rows of W and all of K, which its NW waves
+// share out in pieces of 16 bytes a row; lane l holds row l % 16 of x and of W, and the k
+// of piece l / 16. The waves' sums are joined through LDS. 16-bit types on
+// v_mfma_f32_16x16x32, fp32 on v_mfma_f32_16x16x4. Bound by reading W. All of K in one
+// work-group, because joining parts of it would be a launch more: 5 us, where a CU reads
+// W's share of a 4 MB layer in 2.
 template <typename T>
 struct Piece {
     static constexpr int K = 16 / sizeof(T);   // values in 16 bytes
@@ -516,63 +523,61 @@ __device__ __forceinline__ typename Piece<T>::type load_piece(const T* __restric
 struct SkinnyArgs {
     const void *x, *w;
     int64_t ldx, ldw, M, N, K;
-    int splits;
-    float* part;
     Epilogue e;
 };
 
-template <typename T>
-__global__ __launch_bounds__(512) void k_skinny(SkinnyArgs g) {
+constexpr int NW = 16;   // whatever NH, so that a sum's order does not depend on it
+template <typename T, int NH>
+__global__ __launch_bounds__(NW * 64) void k_skinny(SkinnyArgs g) {
     constexpr int KP = 4 * Piece<T>::K;   // k of one MFMA step
-    constexpr int U = 8;                  // steps in flight
-    __shared__ float red[8][32][17];
+    constexpr int U = 8 / NH;             // steps in flight
+    __shared__ float red[NW][16 * NH][17];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t n0 = (int64_t)blockIdx.x * 32;
+    const int64_t n0 = (int64_t)blockIdx.x * 16 * NH;
     const int64_t nsteps = (g.K + KP - 1) / KP;
-    const int64_t nw = 8 * (int64_t)g.splits, me = (int64_t)blockIdx.y * 8 + wave;
-    const int64_t s0 = nsteps * me / nw, s1 = nsteps * (me + 1) / nw;
+    const int64_t s0 = nsteps * wave / NW, s1 = nsteps * (wave + 1) / NW;
     const T* x = (const T*)g.x + min((int64_t)(lane & 15), g.M - 1) * g.ldx;
-    const T* w0 = (const T*)g.w + min(n0 + (lane & 15), g.N - 1) * g.ldw;
-    const T* w1 = (const T*)g.w + min(n0 + 16 + (lane & 15), g.N - 1) * g.ldw;
+    const T* w[NH];
+    v4 c[NH];
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+        w[h] = (const T*)g.w + min(n0 + 16 * h + (lane & 15), g.N - 1) * g.ldw;
+        c[h] = v4{0.f, 0.f, 0.f, 0.f};
+    }
     const int64_t kl = (lane >> 4) * Piece<T>::K;
-    v4 c0 = {0.f, 0.f, 0.f, 0.f}, c1 = c0;
     for (int64_t s = s0; s < s1; s += U) {
-        typename Piece<T>::type xv[U], a[U], b[U];
+        typename Piece<T>::type xv[U], a[U][NH];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t k = s + u < s1 ? (s + u) * KP + kl : g.K;   // past K: zeros
-            a[u] = load_piece(w0, k, g.K);
-            b[u] = load_piece(w1, k, g.K);
+#pragma unroll
+            for (int h = 0; h < NH; ++h) a[u][h] = load_piece(w[h], k, g.K);
             xv[u] = load_piece(x, k, g.K);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            c0 = mma_piece(a[u], xv[u], c0);
-            c1 = mma_piece(b[u], xv[u], c1);
-        }
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < NH; ++h) c[h] = mma_piece(a[u][h], xv[u], c[h]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        red[wave][4 * (lane >> 4) + i][lane & 15] = c0[i];
-        red[wave][16 + 4 * (lane >> 4) + i][lane & 15] = c1[i];
-    }
+    for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) red[wave][16 * h + 4 * (lane >> 4) + i][lane & 15] = c[h][i];
     __syncthreads();
-    if (wave > 0) return;
-    const int m = lane >> 2;
-    const int64_t n = n0 + (lane & 3) * 8;
-    f8 v;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    if (threadIdx.x < 256 * NH) {   // a thread to a sum
+        const int n = threadIdx.x >> 4, m = threadIdx.x & 15;
         float s = 0.f;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) s += red[q][(lane & 3) * 8 + i][m];
-        v[i] = s;
+        for (int q = 0; q < NW; ++q) s += red[q][n][m];
+        red[0][n][m] = s;
     }
-    if (g.splits > 1) {
-        if (m < g.M) store8(g.part + ((int64_t)blockIdx.y * g.M + m) * g.N, n, g.N, v);
-        return;
-    }
-    finish8<FORWARD>(g.e, g.N, m < g.M, m, n, v);
+    __syncthreads();
+    if (threadIdx.x >= 32 * NH) return;
+    const int m = lane / (2 * NH), n = lane % (2 * NH) * 8;
+    f8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = red[0][n + i][m];
+    finish8<FORWARD>(g.e, g.N, m < g.M, m, n0 + n, v);
 }
 
 // ---------------------------------------------------------------- operands into the workspace
@@ -637,29 +642,48 @@ struct Plan {
     int64_t tiles_m, tiles_n;
     size_t part_bytes;
 };
+
+// What a product takes in tiles of `tile`, its `total` K steps in `splits` parts: us, fitted to
+// launches of 64 to 16384 rows (within 15% of most). A K step of a CU's work-groups (one of
+// 256 x 256, up to two of 128 x 128, up to four of 64 x 64) takes step[their number]; dx and dW, whose
+// operands are read transposed, take longer. Joining parts is a launch and their traffic.
+float product_time(const Product& p, int tile, int64_t total, int splits) {
+    struct Cost {
+        int wgs;
+        float step[4], start;
+    };
+    static constexpr Cost c256{1, {1.55f}, 6.f}, c128{2, {0.7f, 1.0f}, 4.f}, c64{4, {0.5f, 0.57f, 0.68f, 0.8f}, 3.f};
+    const Cost& c = tile == 256 ? c256 : tile == 128 ? c128 : c64;
+    const int64_t wgs = ceil_div(p.M, tile) * ceil_div(p.N, tile) * splits;
+    const int64_t on_cu = std::min<int64_t>(c.wgs, ceil_div(wgs, CUS));
+    const float side = p.a_col ? 1.17f : p.b_col ? 1.1f : 1.f;
+    const float main = (float)ceil_div(wgs, CUS * on_cu) * ((float)ceil_div(total, splits) * c.step[on_cu - 1] * side + c.start);
+    return splits == 1 ? main : main + 5.f + (float)splits * (float)(p.M * p.N) * (8.f / 6.5e6f);
+}
+
 Plan plan_of(int dt, const Product& p) {
     Plan q{};
     q.skinny = p.M <= SKINNY_ROWS && !p.a_col && !p.b_col;
-    if (q.skinny) {
-        // parts of K until two work-groups share a CU, each wave with 8 steps at least
-        const int64_t n = ceil_div(p.N, 32), kp = dt == DT_F32 ? 16 : 32;
-        q.splits = (int)std::max<int64_t>(1, std::min(ceil_div(CUS, n), p.K / (kp * 64)));
-    } else {
-        q.a = p.a_col ? operand_of(dt, p.A, p.lda, false, p.K, p.M) : operand_of(dt, p.A, p.lda, false, p.M, p.K);
-        const bool packed = p.bp.q != nullptr;
-        q.b = p.b_col ? operand_of(dt, p.B, p.ldb, packed, p.K, p.N) : operand_of(dt, p.B, p.ldb, packed, p.N, p.K);
-        q.ksteps = (int)ceil_div(p.K, BK);
-        q.nseg = q.a.planes ? (q.b.planes ? 6 : 3) : 1;
-        const int64_t total = (int64_t)q.ksteps * q.nseg;
-        const int64_t t256 = ceil_div(p.M, 256) * ceil_div(p.N, 256);
-        q.tile = t256 >= 160 ? 256 : 128;
-        q.tiles_m = ceil_div(p.M, q.tile);
-        q.tiles_n = ceil_div(p.N, q.tile);
-        q.splits = 1;
-        if (q.tile == 128)
-            q.splits = (int)std::max<int64_t>(1, std::min<int64_t>(2 * CUS / (q.tiles_m * q.tiles_n), total / 4));
-    }
-    q.splits = std::min(q.splits, 64);
+    q.splits = 1;
+    if (q.skinny) return q;
+    q.a = p.a_col ? operand_of(dt, p.A, p.lda, false, p.K, p.M) : operand_of(dt, p.A, p.lda, false, p.M, p.K);
+    const bool packed = p.bp.q != nullptr;
+    q.b = p.b_col ? operand_of(dt, p.B, p.ldb, packed, p.K, p.N) : operand_of(dt, p.B, p.ldb, packed, p.N, p.K);
+    q.ksteps = (int)ceil_div(p.K, BK);
+    q.nseg = q.a.planes ? (q.b.planes ? 6 : 3) : 1;
+    const int64_t total = (int64_t)q.ksteps * q.nseg;
+    float best = 0.f;
+    for (int tile : {256, 128, 64})
+        for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+            if (splits > total || (splits > 1 && p.M * p.N * splits > (int64_t(1) << 26))) break;
+            const float t = product_time(p, tile, total, splits);
+            if (q.tile && t >= best) continue;
+            best = t;
+            q.tile = tile;
+            q.splits = splits;
+        }
+    q.tiles_m = ceil_div(p.M, q.tile);
+    q.tiles_n = ceil_div(p.N, q.tile);
     if (q.splits > 1) q.part_bytes = (size_t)round_up(p.M * p.N * q.splits * 4, 256);
     return q;
 }
@@ -680,7 +704,8 @@ template <typename T, bool ACOL, bool BCOL>
 hipError_t run_product(const Product& p, const Plan& q, const GemmArgs& g, hipStream_t st) {
     const dim3 grid((unsigned)(q.tiles_m * q.tiles_n), (unsigned)q.splits);
     const int64_t bytes = (p.M * p.K + p.N * p.K) * 2 * (q.nseg > 1 ? 3 : 1) + p.M * p.N * dtype_bytes(g.e.out_dt);
-    if (q.tile == 128) k_product<T, ACOL, BCOL, 128, 128, 2, 2, false><<<grid, 256, 0, st>>>(g);
+    if (q.tile == 64) k_product<T, ACOL, BCOL, 64, 64, 2, 2, false><<<grid, 256, 0, st>>>(g);
+    else if (q.tile == 128) k_product<T, ACOL, BCOL, 128, 128, 2, 2, false><<<grid, 256, 0, st>>>(g);
     else if (bytes <= LAST_LEVEL_CACHE) k_product<T, ACOL, BCOL, 256, 256, 2, 4, false><<<grid, 512, 0, st>>>(g);
     else k_product<T, ACOL, BCOL, 256, 256, 2, 4, true><<<grid, 512, 0, st>>>(g);
     return hipGetLastError();
@@ -702,6 +727,13 @@ hipError_t run_finish(const Product& p, const float* part, int splits, const Epi
 
 }  // namespace
 
+template <typename F>
+void by_operand(int dt, F f) {
+    if (dt == DT_F32) f((float*)nullptr);
+    else if (dt == DT_BF16) f((bf16*)nullptr);
+    else f((f16*)nullptr);
+}
+
 size_t product_workspace_bytes(int dt, const Product& p) {
     const Plan q = plan_of(dt, p);
     return q.a.bytes + q.b.bytes + q.part_bytes;
@@ -712,11 +744,15 @@ hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws,
     char* w = (char*)ws;
     hipError_t err;
     if (q.skinny) {
-        SkinnyArgs g{p.A, p.B, p.lda, p.ldb, p.M, p.N, p.K, q.splits, (float*)w, e};
-        const dim3 grid((unsigned)ceil_div(p.N, 32), (unsigned)q.splits);
-        if (dt == DT_F32) k_skinny<float><<<grid, 512, 0, st>>>(g);
-        else if (dt == DT_BF16) k_skinny<bf16><<<grid, 512, 0, st>>>(g);
-        else k_skinny<f16><<<grid, 512, 0, st>>>(g);
+        SkinnyArgs g{p.A, p.B, p.lda, p.ldb, p.M, p.N, p.K, e};
+        // 16 rows of W a work-group as long as there are no more than CUs; an 8-bit copy of z
+        // needs the 32 columns of a group in one
+        const bool wide = e.p.q || p.N > 16 * CUS;
+        by_operand(dt, [&](auto* t) {
+            using T = std::remove_reference_t<decltype(*t)>;
+            if (wide) k_skinny<T, 2><<<(unsigned)ceil_div(p.N, 32), NW * 64, 0, st>>>(g);
+            else k_skinny<T, 1><<<(unsigned)ceil_div(p.N, 16), NW * 64, 0, st>>>(g);
+        });
         err = hipGetLastError();
     } else {
         GemmArgs g{};

@@ -226,7 +226,7 @@ template <typename T, typename TW, int NT, int NCH, bool PACKED>
 __global__ __launch_bounds__(norm_block(NT)) void k_norm_bwd(NormBwdArgs<T, TW> g) {
     constexpr int RPB = norm_block(NT) / NT;
     __shared__ float red[4 * (NT / 64)];
-    __shared__ float cols_of[RPB > 1 ? RPB * NT * 8 : 1];
+    __shared__ float cols_of[RPB > 1 ? 2 * NCH : 1][RPB > 1 ? RPB * NT * 8 : 1];
     int turn = 0;
     const int t = threadIdx.x % NT;
     // 1024 threads have 128 registers each: no room for the next row, nor for w
@@ -288,23 +288,26 @@ __global__ __launch_bounds__(norm_block(NT)) void k_norm_bwd(NormBwdArgs<T, TW> 
         }
     }
     if (!g.part) return;
-    // the column sums of this work-group's rows, joined over its waves where each has rows of its own
+    // the column sums of this work-group's rows, joined over its waves where each has rows of
+    // its own: a wave to each of the 2 NCH arrays
     float* out = g.part + (int64_t)blockIdx.x * 2 * g.cols;
+    if constexpr (RPB > 1) {
 #pragma unroll
-    for (int v = 0; v < 2; ++v) {
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+            for (int j = 0; j < NCH; ++j) *reinterpret_cast<f8*>(&cols_of[v * NCH + j][threadIdx.x * 8]) = v ? sb[j] : sw[j];
+        __syncthreads();
+        const int a = threadIdx.x / NT;
+        if (a >= 2 * NCH) return;
+        f8 s = *reinterpret_cast<const f8*>(&cols_of[a][t * 8]);
+#pragma unroll
+        for (int r = 1; r < RPB; ++r) s += *reinterpret_cast<const f8*>(&cols_of[a][(r * NT + t) * 8]);
+        store8(out + a / NCH * g.cols, (int64_t)(a % NCH * NT + t) * 8, g.cols, s);
+    } else {
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
-            const int64_t c = (int64_t)(j * NT + t) * 8;
-            f8 s = v ? sb[j] : sw[j];
-            if constexpr (RPB > 1) {
-                __syncthreads();
-                *reinterpret_cast<f8*>(&cols_of[threadIdx.x * 8]) = s;
-                __syncthreads();
-                if (threadIdx.x >= NT) continue;
-#pragma unroll
-                for (int r = 1; r < RPB; ++r) s += *reinterpret_cast<const f8*>(&cols_of[(r * NT + t) * 8]);
-            }
-            store8(out + v * g.cols, c, g.cols, s);
+            store8(out, (int64_t)(j * NT + t) * 8, g.cols, sw[j]);
+            store8(out + g.cols, (int64_t)(j * NT + t) * 8, g.cols, sb[j]);
         }
     }
 }
