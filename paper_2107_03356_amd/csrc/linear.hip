@@ -380,10 +380,13 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int wm = wave / WN, wn = wave % WN;
 
-    // tile of this work-group: neighbours share an XCD, and go over bands of 8 tile rows
-    const int ntile = g.tiles_m * g.tiles_n;
-    int p = blockIdx.x;
-    if (ntile % 8 == 0) p = (p % 8) * (ntile / 8) + p / 8;
+    // Tile and part of K of this work-group. Work-groups go round-robin over the 8 XCDs, each
+    // with its own L2: an XCD takes neighbours of a list that has the tiles of one part
+    // of K together, in bands of 8 tile rows.
+    const int ntile = g.tiles_m * g.tiles_n, total_wgs = ntile * g.splits;
+    const int xcd = blockIdx.x % 8, each = total_wgs / 8, more = total_wgs % 8;
+    const int at = xcd * each + min(xcd, more) + blockIdx.x / 8;
+    const int k_part = at / ntile, p = at - k_part * ntile;
     constexpr int BAND = 8;
     const int band = p / (BAND * g.tiles_n), in_band = p % (BAND * g.tiles_n);
     const int height = min(BAND, g.tiles_m - band * BAND);
@@ -396,8 +399,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
     const int64_t a0 = ACOL ? (int64_t)m0 * 2 : m0 * g.lda, b0 = BCOL ? (int64_t)n0 * 2 : n0 * g.ldb;
 
     const int total = g.ksteps * g.nseg;
-    const int s_begin = (int)((int64_t)total * blockIdx.y / g.splits);
-    const int s_end = (int)((int64_t)total * (blockIdx.y + 1) / g.splits);
+    const int s_begin = (int)((int64_t)total * k_part / g.splits);
+    const int s_end = (int)((int64_t)total * (k_part + 1) / g.splits);
     int seg = s_begin / g.ksteps, ks = s_begin % g.ksteps;
     auto issue = [&](int stage) {
         const char* a = g.A + (g.pa >> (4 * seg) & 15) * g.apl + a0 + ks * ca.step;
@@ -468,7 +471,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
         multiply(1);
     }
 
-    float* part = g.splits > 1 ? g.part + (int64_t)blockIdx.y * g.M * g.N : nullptr;
+    float* part = g.splits > 1 ? g.part + (int64_t)k_part * g.M * g.N : nullptr;
     const int m = m0 + wm * (TM / WM) + (lane & 15), n = n0 + wn * (TN / WN) + 4 * (lane >> 4);
     if (n0 + TN <= g.N) epilogue<T, KIND, false, STREAM>(g, part, lane, m, n, acc);
     else epilogue<T, KIND, true, STREAM>(g, part, lane, m, n, acc);
@@ -545,19 +548,33 @@ __global__ __launch_bounds__(NW * 64) void k_skinny(SkinnyArgs g) {
         c[h] = v4{0.f, 0.f, 0.f, 0.f};
     }
     const int64_t kl = (lane >> 4) * Piece<T>::K;
-    for (int64_t s = s0; s < s1; s += U) {
-        typename Piece<T>::type xv[U], a[U][NH];
+    typedef typename Piece<T>::type V;
+    typedef typename VecOf<T, Piece<T>::K>::type Unaligned;
+    // U steps at a time while they lie within K, then one by one with a check (code that is
+    // not run still has to be fetched past: checks on every load cost 2 us a launch)
+    int64_t s = s0;
+    for (const int64_t whole = min(s1, g.K / KP); s + U <= whole; s += U) {
+        V xv[U], a[U][NH];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t k = s + u < s1 ? (s + u) * KP + kl : g.K;   // past K: zeros
+            const int64_t k = (s + u) * KP + kl;
 #pragma unroll
-            for (int h = 0; h < NH; ++h) a[u][h] = load_piece(w[h], k, g.K);
-            xv[u] = load_piece(x, k, g.K);
+            for (int h = 0; h < NH; ++h) a[u][h] = *reinterpret_cast<const Unaligned*>(w[h] + k);
+            xv[u] = *reinterpret_cast<const Unaligned*>(x + k);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int h = 0; h < NH; ++h) c[h] = mma_piece(a[u][h], xv[u], c[h]);
+    }
+#pragma unroll 1
+    for (; s < s1; ++s) {
+        V a[NH];
+#pragma unroll
+        for (int h = 0; h < NH; ++h) a[h] = load_piece(w[h], s * KP + kl, g.K);
+        const V xv = load_piece(x, s * KP + kl, g.K);
+#pragma unroll
+        for (int h = 0; h < NH; ++h) c[h] = mma_piece(a[h], xv, c[h]);
     }
 #pragma unroll
     for (int h = 0; h < NH; ++h)
@@ -702,7 +719,7 @@ hipError_t lay_out(int dt, const Operand& o, const void* src, int64_t ld, Packed
 
 template <typename T, bool ACOL, bool BCOL>
 hipError_t run_product(const Product& p, const Plan& q, const GemmArgs& g, hipStream_t st) {
-    const dim3 grid((unsigned)(q.tiles_m * q.tiles_n), (unsigned)q.splits);
+    const unsigned grid = (unsigned)(q.tiles_m * q.tiles_n * q.splits);
     const int64_t bytes = (p.M * p.K + p.N * p.K) * 2 * (q.nseg > 1 ? 3 : 1) + p.M * p.N * dtype_bytes(g.e.out_dt);
     if (q.tile == 64) k_product<T, ACOL, BCOL, 64, 64, 2, 2, false><<<grid, 256, 0, st>>>(g);
     else if (q.tile == 128) k_product<T, ACOL, BCOL, 128, 128, 2, 2, false><<<grid, 256, 0, st>>>(g);

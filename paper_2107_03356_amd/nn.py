@@ -50,8 +50,12 @@ class Packed8:
     @staticmethod
     def empty(rows, cols, device):
         """Room for a copy; rows of q lie a multiple of 32 bytes apart."""
-        q = torch.empty((rows, -(-cols // GROUP) * GROUP), dtype=torch.int8, device=device)
-        return Packed8(q[:, :cols], torch.empty((rows, -(-cols // GROUP)), dtype=torch.uint8, device=device))
+        groups = -(-cols // GROUP)
+        q = torch.empty((rows, groups * GROUP), dtype=torch.int8, device=device)
+        p = Packed8.__new__(Packed8)   # nothing to check
+        p.q = q if cols == groups * GROUP else q[:, :cols]
+        p.s = torch.empty((rows, groups), dtype=torch.uint8, device=device)
+        return p
 
     @property
     def shape(self):
@@ -113,14 +117,15 @@ def _ptr(t):
 
 
 def _same(what, t, like, shape):
-    if t.dtype != like.dtype or t.device != like.device or t.shape != shape:
+    if t.dtype is not like.dtype or t.shape != shape or t.device != like.device:
         raise ValueError(f"{what}: {tuple(shape)} {like.dtype} on {like.device}, not {tuple(t.shape)} {t.dtype} on "
                          f"{t.device}")
 
 
 def _param(what, p, data, n):
     """A parameter vector of n values in float32 or the data's type."""
-    if p.dtype not in (torch.float32, data.dtype) or p.device != data.device or p.shape != (n,):
+    d = p.dtype
+    if (d is not torch.float32 and d is not data.dtype) or p.shape != (n,) or p.device != data.device:
         raise ValueError(f"{what}: {n} values in float32 or {data.dtype} on {data.device}, not {tuple(p.shape)} "
                          f"{p.dtype} on {p.device}")
     return p.contiguous()
@@ -133,13 +138,26 @@ def _act(name):
         raise ValueError(f"act: one of {', '.join(ACTIVATIONS)}, not {name!r}") from None
 
 
+# torch.cuda.current_device and current_stream without the objects they build (2 us a call)
+_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+_functions = {}
+
+
+def _function(name):
+    fn = _functions.get(name)
+    if fn is None:
+        fn = _functions[name] = getattr(load(), name)
+    return fn
+
+
 def _call(name, device, *args):
     """The C call of this name on the current stream of `device`."""
-    if device.index == torch._C._cuda_getDevice():
-        status = getattr(load(), name)(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    index = device.index
+    if index == _device():
+        status = _function(name)(*args, _raw_stream(index))
     else:
         with torch.cuda.device(device):
-            status = getattr(load(), name)(*args, torch.cuda.current_stream(device).cuda_stream)
+            status = _function(name)(*args, torch.cuda.current_stream(device).cuda_stream)
     if status != B.MFAC_OK:
         raise MfacError(name, status)
 
@@ -153,7 +171,7 @@ def _workspace(nbytes, device):
     """(pointer, bytes, the tensor that holds them)"""
     if nbytes == 0:
         return None, 0, None
-    w = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    w = torch.empty((nbytes,), dtype=torch.uint8, device=device)
     return w.data_ptr(), nbytes, w
 
 
@@ -183,7 +201,7 @@ def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, pack=False):
     rows, cols = x2.shape
     w, b, wt = _norm_params(weight, bias, x2)
     y = _like(x)
-    rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+    rstd = torch.empty((rows,), dtype=torch.float32, device=x.device)
     mean = None if pack else torch.empty_like(rstd)
     p = Packed8.empty(rows, cols, x.device) if pack else None
     _call("mfac_layer_norm", x.device, _type(x2, "layer_norm: x"), wt, rows, cols, *_mat(x2), _ptr(w), _ptr(b),
@@ -231,7 +249,7 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, add=None, params=True):
     if params:
         grads = torch.empty((2, cols), dtype=torch.float32 if w is None else w.dtype, device=dy.device)
         dw, db = grads.unbind(0)
-        ws = _workspace(load().mfac_layer_norm_bwd_workspace_bytes(rows, cols), dy.device)
+        ws = _workspace(_function("mfac_layer_norm_bwd_workspace_bytes")(rows, cols), dy.device)
     _call("mfac_layer_norm_bwd", dy.device, _type(dy2, "layer_norm: dy"), wt, rows, cols, *_mat(dy2), *xm, _ptr(mean),
           rstd.data_ptr(), *packed, _ptr(w), *_mat(add), dx.data_ptr(), cols, _ptr(dw), _ptr(db), ws[0], ws[1])
     return dx, dw, db
@@ -254,12 +272,12 @@ def linear_forward(x, weight, bias=None, act="none", residual=None, keep=None):
     if residual is not None:
         residual = _rows(residual, "linear: residual")
         _same("linear: residual", residual, x2, (rows, cout))
-    y = torch.empty(shape, dtype=x.dtype, device=x.device)
-    z = torch.empty(shape, dtype=x.dtype, device=x.device) if keep == "z" else None
+    y = x.new_empty(shape)
+    z = x.new_empty(shape) if keep == "z" else None
     p = Packed8.empty(rows, cout, x.device) if keep == "pack8" else None
     t = _type(x2, "linear: x")
     xm, wm = _mat(x2), _mat(w)
-    ws = _workspace(load().mfac_linear_workspace_bytes(t, rows, cin, cout, *xm, *wm), x.device)
+    ws = _workspace(_function("mfac_linear_workspace_bytes")(t, rows, cin, cout, *xm, *wm), x.device)
     _call("mfac_linear", x.device, t, t if b is None else _TYPES[b.dtype], a, rows, cin, cout, *xm, *wm, _ptr(b),
           *_mat(residual), y.data_ptr(), cout, _ptr(z), cout, *(_NO_COPY if p is None else p._args()), ws[0], ws[1])
     return y if keep is None else (y, z if keep == "z" else p)
@@ -288,7 +306,7 @@ def act_backward(dy, z=None, act="none", want_a=False, want_db=True):
     db = torch.empty(cols, dtype=torch.float32, device=dy.device) if want_db else None
     if z is None and not want_db:
         return dz, None, None
-    ws = _workspace(load().mfac_act_bwd_workspace_bytes(rows, cols) if want_db else 0, dy.device)
+    ws = _workspace(_function("mfac_act_bwd_workspace_bytes")(rows, cols) if want_db else 0, dy.device)
     _call("mfac_act_bwd", dy.device, _type(dy2, "act: dy"), code, rows, cols, *_mat(dy2), *zm, *packed,
           None if z is None else dz.data_ptr(), cols, _ptr(a), cols, _ptr(db), ws[0], ws[1])
     return dz, a, db
@@ -304,10 +322,10 @@ def linear_backward_input(dz, weight, add=None):
     if add is not None:
         add = _rows(add, "linear: add")
         _same("linear: add", add, dz2, (rows, cin))
-    dx = torch.empty(dz.shape[:-1] + (cin,), dtype=dz.dtype, device=dz.device)
+    dx = dz.new_empty(dz.shape[:-1] + (cin,))
     t = _type(dz2, "linear: dz")
     zm, wm = _mat(dz2), _mat(w)
-    ws = _workspace(load().mfac_linear_bwd_input_workspace_bytes(t, rows, cin, cout, *zm, *wm), dz.device)
+    ws = _workspace(_function("mfac_linear_bwd_input_workspace_bytes")(t, rows, cin, cout, *zm, *wm), dz.device)
     _call("mfac_linear_bwd_input", dz.device, t, rows, cin, cout, *zm, *wm, *_mat(add), dx.data_ptr(), cin, ws[0],
           ws[1])
     return dx
@@ -340,7 +358,7 @@ def linear_backward_weight(dz, x, affine=None, db=None, grad_dtype=None):
     dw = torch.empty((cout, cin), dtype=grad_dtype, device=dz.device)
     t = _type(dz2, "linear: dz")
     zm = _mat(dz2)
-    ws = _workspace(load().mfac_linear_bwd_weight_workspace_bytes(t, rows, cin, cout, *zm, *xm), dz.device)
+    ws = _workspace(_function("mfac_linear_bwd_weight_workspace_bytes")(t, rows, cin, cout, *zm, *xm), dz.device)
     _call("mfac_linear_bwd_weight", dz.device, t, _TYPES[grad_dtype], rows, cin, cout, *zm, *xm, *packed, _ptr(gamma),
           _ptr(beta), _ptr(db) if affine is not None else None, dw.data_ptr(), cin, ws[0], ws[1])
     return dw
