@@ -494,12 +494,14 @@ __global__ __launch_bounds__(256) void k_finish(const float* __restrict__ part, 
 }
 
 // ---------------------------------------------------------------- few rows
-// C (M <= 16 rows) = x W^T. A work-group takes 16 NH rows of W and all of K, which its NW waves
-// share out in pieces of 16 bytes a row; lane l holds row l % 16 of x and of W, and the k
-// of piece l / 16. The waves' sums are joined through LDS. 16-bit types on
-// v_mfma_f32_16x16x32, fp32 on v_mfma_f32_16x16x4. Bound by reading W. All of K in one
-// work-group, because joining parts of it would be a launch more: 5 us, where a CU reads
-// W's share of a 4 MB layer in 2.
+// C (M <= 16 rows) = x W^T. A work-group takes 16 NH rows of W (or 8) and all of K, which its NW
+// waves share out in pieces of 16 bytes a row; lane l holds row l % 16 of x and of W, and
+// the k of piece l / 16. The waves' sums are joined through LDS. 16-bit types on
+// v_mfma_f32_16x16x32, fp32 on v_mfma_f32_16x16x4. Bound by reading W, 33.5 MB in 9.4 us. A CU
+// takes in about 20 bytes a ns from beyond its L2, so all of them are wanted: narrow
+// layers take 8 rows a work-group, the other half of the lanes reading the eighth again.
+// Sharing K out over work-groups would be a launch more, which costs the host 3 us and the
+// device 4.
 template <typename T>
 struct Piece {
     static constexpr int K = 16 / sizeof(T);   // values in 16 bytes
@@ -526,6 +528,7 @@ __device__ __forceinline__ typename Piece<T>::type load_piece(const T* __restric
 struct SkinnyArgs {
     const void *x, *w;
     int64_t ldx, ldw, M, N, K;
+    int rows;   // of W a work-group: 16 NH, or 8
     Epilogue e;
 };
 
@@ -536,7 +539,7 @@ __global__ __launch_bounds__(NW * 64) void k_skinny(SkinnyArgs g) {
     constexpr int U = 8 / NH;             // steps in flight
     __shared__ float red[NW][16 * NH][17];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t n0 = (int64_t)blockIdx.x * 16 * NH;
+    const int64_t n0 = (int64_t)blockIdx.x * g.rows;
     const int64_t nsteps = (g.K + KP - 1) / KP;
     const int64_t s0 = nsteps * wave / NW, s1 = nsteps * (wave + 1) / NW;
     const T* x = (const T*)g.x + min((int64_t)(lane & 15), g.M - 1) * g.ldx;
@@ -544,7 +547,7 @@ __global__ __launch_bounds__(NW * 64) void k_skinny(SkinnyArgs g) {
     v4 c[NH];
 #pragma unroll
     for (int h = 0; h < NH; ++h) {
-        w[h] = (const T*)g.w + min(n0 + 16 * h + (lane & 15), g.N - 1) * g.ldw;
+        w[h] = (const T*)g.w + min(n0 + min(16 * h + (lane & 15), g.rows - 1), g.N - 1) * g.ldw;
         c[h] = v4{0.f, 0.f, 0.f, 0.f};
     }
     const int64_t kl = (lane >> 4) * Piece<T>::K;
@@ -589,8 +592,9 @@ __global__ __launch_bounds__(NW * 64) void k_skinny(SkinnyArgs g) {
         red[0][n][m] = s;
     }
     __syncthreads();
-    if (threadIdx.x >= 32 * NH) return;
-    const int m = lane / (2 * NH), n = lane % (2 * NH) * 8;
+    const int across = g.rows / 8;   // lanes to a row of C, eight columns each
+    if ((int)threadIdx.x >= 16 * across) return;
+    const int m = lane / across, n = lane % across * 8;
     f8 v;
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = red[0][n + i][m];
@@ -761,14 +765,17 @@ hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws,
     char* w = (char*)ws;
     hipError_t err;
     if (q.skinny) {
-        SkinnyArgs g{p.A, p.B, p.lda, p.ldb, p.M, p.N, p.K, e};
-        // 16 rows of W a work-group as long as there are no more than CUs; an 8-bit copy of z
-        // needs the 32 columns of a group in one
-        const bool wide = e.p.q || p.N > 16 * CUS;
+        SkinnyArgs g{p.A, p.B, p.lda, p.ldb, p.M, p.N, p.K, 16, e};
+        // Rows of W a work-group: the 32 columns of a group in one for an 8-bit copy of z; else so
+        // that the work-groups are about as many as CUs. 1024 x 4096, 12 rows: fp32 14.6 us with 16,
+        // 13.4 with 8 (a quarter of it the fp32 MFMAs); bf16 9.4 and 8.2.
+        if (e.p.q || p.N > 16 * CUS) g.rows = 32;
+        else if (p.N <= 8 * CUS) g.rows = 8;
+        const unsigned grid = (unsigned)ceil_div(p.N, g.rows);
         by_operand(dt, [&](auto* t) {
             using T = std::remove_reference_t<decltype(*t)>;
-            if (wide) k_skinny<T, 2><<<(unsigned)ceil_div(p.N, 32), NW * 64, 0, st>>>(g);
-            else k_skinny<T, 1><<<(unsigned)ceil_div(p.N, 16), NW * 64, 0, st>>>(g);
+            if (g.rows == 32) k_skinny<T, 2><<<grid, NW * 64, 0, st>>>(g);
+            else k_skinny<T, 1><<<grid, NW * 64, 0, st>>>(g);
         });
         err = hipGetLastError();
     } else {
