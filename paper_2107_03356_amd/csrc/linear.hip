@@ -264,15 +264,23 @@ struct Copier {
             }
         }
     }
-    // base: the tile's first element at this step; left: K's elements from there on
-    __device__ __forceinline__ void issue(const char* base, int left, char* lds, int wave) const {
-        const __amdgpu_buffer_rsrc_t r =
-            __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)OUT_OF_RANGE, 0x00020000);
+    // base: the tile's first element at this step; left: K's elements from there on. In
+    // assembly because the compiler waits for the builtin's copies before the next transposing
+    // read of LDS, whichever buffer that reads (dx and dW of 8192^3: 899 and 921 us with it);
+    // the kernel's own waits are all that is needed. Nothing is loaded into registers.
+    __device__ __forceinline__ void issue(const char* base, int left, unsigned lds, int wave) const {
+        typedef int i4 __attribute__((ext_vector_type(4)));
+        const uint64_t b = (uint64_t)base;
+        // base, stride 0, size OUT_OF_RANGE, raw 32-bit data
+        const i4 r = {__builtin_amdgcn_readfirstlane((int)b), __builtin_amdgcn_readfirstlane((int)(b >> 32)),
+                      (int)OUT_OF_RANGE, 0x00020000};
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             const unsigned o = left >= BK || k[COL ? i : 0] < left ? off[i] : OUT_OF_RANGE;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                r, (__attribute__((address_space(3))) void*)(lds + (i * NT + wave * 64) * 16), 16, (int)o, 0, 0, 0);
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                         :
+                         : "s"(__builtin_amdgcn_readfirstlane(lds + (i * NT + wave * 64) * 16)), "v"(o), "s"(r)
+                         : "memory", "m0");
         }
     }
 };
@@ -402,11 +410,12 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
     const int s_begin = (int)((int64_t)total * k_part / g.splits);
     const int s_end = (int)((int64_t)total * (k_part + 1) / g.splits);
     int seg = s_begin / g.ksteps, ks = s_begin % g.ksteps;
+    const unsigned lds_at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
     auto issue = [&](int stage) {
         const char* a = g.A + (g.pa >> (4 * seg) & 15) * g.apl + a0 + ks * ca.step;
         const char* b = g.B + (g.pb >> (4 * seg) & 15) * g.bpl + b0 + ks * cb.step;
-        ca.issue(a, g.K - ks * BK, lds + stage * STAGE, wave);
-        cb.issue(b, g.K - ks * BK, lds + stage * STAGE + TM * BK * 2, wave);
+        ca.issue(a, g.K - ks * BK, lds_at + stage * STAGE, wave);
+        cb.issue(b, g.K - ks * BK, lds_at + stage * STAGE + TM * BK * 2, wave);
         if (++ks == g.ksteps) {
             ks = 0;
             ++seg;
@@ -448,9 +457,12 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    // this wave's copies have landed and its LDS reads are in registers; then every wave's
+    // This wave's copies have landed and its LDS reads are in registers; then every wave's. The
+    // builtin's wait, unlike one in assembly, is one that the compiler counts: it puts none
+    // of its own before the products.
     auto wait_all = [&]() {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
@@ -462,12 +474,13 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
     for (int s = s_begin; s < s_end; ++s) {
         const int stage = (s - s_begin) & 1;
         __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): the fragments of the first half
         read(stage, 1);
         multiply(0);
         wait_all();
         if (s + 2 < s_end) issue(stage);
         __builtin_amdgcn_sched_barrier(0);
-        if (s + 1 < s_end) read(stage ^ 1, 0);
+        read(stage ^ 1, 0);   // after the last step, of what lies there: not used
         multiply(1);
     }
 
@@ -634,8 +647,9 @@ __global__ __launch_bounds__(256) void k_lay_out_split(const float* __restrict__
 constexpr int64_t SKINNY_ROWS = 16;
 constexpr int64_t CUS = 256;
 // Past the 256 MB of the last-level cache, outputs written through the caches push the operands
-// out: 8192^3, dx and dW 1003 and 1030 us, with nontemporal stores 915 and 943. Below, those
-// are slower: dx of 8192 x 8192 over K = 2048 takes 248 us, with them 271.
+// out: 8192^3, dx and dW took 1003 and 1030 us with plain stores, 915 and 943 with nontemporal
+// ones (both are faster now). Below, those are slower: dx of 8192 x 8192 over K = 2048 took
+// 248 us, with them 271.
 constexpr int64_t LAST_LEVEL_CACHE = int64_t(256) << 20;
 
 // Rows of `cols` elements that the copies into LDS take as they are.
@@ -666,8 +680,8 @@ struct Plan {
 
 // What a product takes in tiles of `tile`, its `total` K steps in `splits` parts: us, fitted to
 // launches of 64 to 16384 rows (within 15% of most). A K step of a CU's work-groups (one of
-// 256 x 256, up to two of 128 x 128, up to four of 64 x 64) takes step[their number]; dx and dW, whose
-// operands are read transposed, take longer. Joining parts is a launch and their traffic.
+// 256 x 256, up to two of 128 x 128, up to four of 64 x 64) takes step[their number]; dW, with both
+// operands read transposed, a little longer. Joining parts is a launch and their traffic.
 float product_time(const Product& p, int tile, int64_t total, int splits) {
     struct Cost {
         int wgs;
@@ -677,7 +691,7 @@ float product_time(const Product& p, int tile, int64_t total, int splits) {
     const Cost& c = tile == 256 ? c256 : tile == 128 ? c128 : c64;
     const int64_t wgs = ceil_div(p.M, tile) * ceil_div(p.N, tile) * splits;
     const int64_t on_cu = std::min<int64_t>(c.wgs, ceil_div(wgs, CUS));
-    const float side = p.a_col ? 1.17f : p.b_col ? 1.1f : 1.f;
+    const float side = p.a_col ? 1.05f : 1.f;
     const float main = (float)ceil_div(wgs, CUS * on_cu) * ((float)ceil_div(total, splits) * c.step[on_cu - 1] * side + c.start);
     return splits == 1 ? main : main + 5.f + (float)splits * (float)(p.M * p.N) * (8.f / 6.5e6f);
 }
