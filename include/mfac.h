@@ -405,7 +405,9 @@ typedef enum {
     MFAC_F32 = 0,
     MFAC_BF16 = 1,
     MFAC_F16 = 2,
-    MFAC_DTYPE_INT32_ = 0x7fffffff /* not a type: widens the enum to int32 */
+    /* not types: they widen the enum to int32, so that any code is a value of it */
+    MFAC_DTYPE_NONE_ = -1,
+    MFAC_DTYPE_INT32_ = 0x7fffffff
 } mfac_dtype;
 
 /* Activations: z, max(z, 0), z Phi(z) (Phi the normal distribution function),
@@ -416,7 +418,8 @@ typedef enum {
     MFAC_ACT_GELU = 2,
     MFAC_ACT_GELU_TANH = 3,
     MFAC_ACT_SILU = 4,
-    MFAC_ACT_INT32_ = 0x7fffffff /* not an activation: widens the enum to int32 */
+    MFAC_ACT_NOT_ONE_ = -1, /* not activations: as above */
+    MFAC_ACT_INT32_ = 0x7fffffff
 } mfac_act;
 
 /* 8-bit copies. Row r of a rows x cols matrix is cut into ceil(cols / 32) groups
@@ -469,9 +472,10 @@ mfac_status mfac_layer_norm_bwd(mfac_dtype type, mfac_dtype wtype, int64_t rows,
  * the backward pass; at most one of the two, both optional. y may be res.
  * Products: fp16 and bf16 values on the matrix cores with fp32 sums; fp32 values
  * as three bf16 parts each, of whose nine products the six largest are taken
- * (what is left out is at most 2^-26 of the product); the parts of a value
- * above 3.39e38 or an infinite one are not finite together, and its products
- * come out NaN. Layers of few rows in fp32 multiply in fp32. */
+ * (what is left out is at most 2^-26 of the product); what of a value lies
+ * below 2^-133 is left out, and the parts of one above 3.39e38, or of an infinite
+ * one, are not finite together: its products come out NaN. Up to 16 rows of
+ * fp32 multiply in fp32. */
 size_t mfac_linear_workspace_bytes(mfac_dtype type, int64_t rows, int64_t cin, int64_t cout, const void* x,
                                    int64_t ldx, const void* w, int64_t ldw);
 mfac_status mfac_linear(mfac_dtype type, mfac_dtype btype, mfac_act act, int64_t rows, int64_t cin, int64_t cout,
