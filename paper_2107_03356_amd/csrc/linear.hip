@@ -380,11 +380,11 @@ __device__ __forceinline__ void epilogue(const GemmArgs& g, float* part, int lan
 // The sums stay in the MFMA's accumulators over all of K: against 64 bits an fp32 dW of
 // random bf16 operands is off by 1.9e-7 (relative, 2-norm) over 8192 rows, 2.8e-7
 // over 16384.
-template <typename T, bool ACOL, bool BCOL, int TM, int TN, int WM, int WN, bool STREAM>
+template <typename T, bool ACOL, bool BCOL, int TM, int TN, int WM, int WN, int STAGES, bool STREAM>
 __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
     constexpr int NT = WM * WN * 64, MT = TM / WM / 16, NTL = TN / WN / 16;
     constexpr int STAGE = (TM + TN) * BK * 2, KIND = ACOL ? WEIGHT : BCOL ? INPUT : FORWARD;
-    __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
+    __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int wm = wave / WN, wn = wave % WN;
 
@@ -430,7 +430,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
 
     // Two halves of a step, 32 k each. While the matrix cores work on one half's fragments,
     // the other's are read from LDS. Between the halves, the next step's copies have
-    // landed, and this step's buffer is free for those of the step after it.
+    // landed, and this step's buffer is free for those of STAGES steps on.
     typename Frag<T>::type fa[2][MT], fb[2][NTL];
     auto read = [&](int stage, int kk) {
         const char* la = lds + stage * STAGE;
@@ -457,31 +457,44 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    // This wave's copies have landed and its LDS reads are in registers; then every wave's. The
-    // builtin's wait, unlike one in assembly, is one that the compiler counts: it puts none
-    // of its own before the products.
-    auto wait_all = [&]() {
+    // This wave's copies of the step that is read next have landed (they land in order, `behind`
+    // of them may be on their way after it) and its LDS reads are in registers; then every
+    // wave's. The builtin's wait, unlike one in assembly, is one that the compiler counts: it
+    // puts none of its own before the products.
+    constexpr int PER_STEP = Copier<TM, NT, ACOL>::NI + Copier<TN, NT, BCOL>::NI;
+    auto wait_all = [&](auto behind) {
+        constexpr int N = decltype(behind)::value;
+        static_assert(N < 16, "the low four bits of the count");
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
+        __builtin_amdgcn_s_waitcnt(0x0070 | N);   // vmcnt(N) lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
+    constexpr std::integral_constant<int, (STAGES - 2) * PER_STEP> rest{};
+    constexpr std::integral_constant<int, 0> none{};
 
-    issue(0);
-    wait_all();
-    if (s_begin + 1 < s_end) issue(1);
+    const int steps = s_end - s_begin;
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (i < steps) issue(i);
+    if (STAGES > 2 && steps >= STAGES - 1) wait_all(rest);
+    else wait_all(none);
+    if (STAGES - 1 < steps) issue(STAGES - 1);
     read(0, 0);
-    for (int s = s_begin; s < s_end; ++s) {
-        const int stage = (s - s_begin) & 1;
+    int stage = 0;
+    for (int s = 0; s < steps; ++s) {
+        const int next = stage + 1 == STAGES ? 0 : stage + 1;
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): the fragments of the first half
         read(stage, 1);
         multiply(0);
-        wait_all();
-        if (s + 2 < s_end) issue(stage);
+        if (STAGES > 2 && s + STAGES <= steps) wait_all(rest);
+        else wait_all(none);
+        if (s + STAGES < steps) issue(stage);
         __builtin_amdgcn_sched_barrier(0);
-        read(stage ^ 1, 0);   // after the last step, of what lies there: not used
+        read(next, 0);   // after the last step, of what lies there: not used
         multiply(1);
+        stage = next;
     }
 
     float* part = g.splits > 1 ? g.part + (int64_t)k_part * g.M * g.N : nullptr;
@@ -687,13 +700,13 @@ float product_time(const Product& p, int tile, int64_t total, int splits) {
         int wgs;
         float step[4], start;
     };
-    static constexpr Cost c256{1, {1.55f}, 6.f}, c128{2, {0.7f, 1.0f}, 4.f}, c64{4, {0.5f, 0.57f, 0.68f, 0.8f}, 3.f};
+    static constexpr Cost c256{1, {1.5f}, 8.f}, c128{2, {0.68f, 1.0f}, 5.f}, c64{4, {0.3f, 0.48f, 0.62f, 0.82f}, 3.f};
     const Cost& c = tile == 256 ? c256 : tile == 128 ? c128 : c64;
     const int64_t wgs = ceil_div(p.M, tile) * ceil_div(p.N, tile) * splits;
     const int64_t on_cu = std::min<int64_t>(c.wgs, ceil_div(wgs, CUS));
     const float side = p.a_col ? 1.05f : 1.f;
     const float main = (float)ceil_div(wgs, CUS * on_cu) * ((float)ceil_div(total, splits) * c.step[on_cu - 1] * side + c.start);
-    return splits == 1 ? main : main + 5.f + (float)splits * (float)(p.M * p.N) * (8.f / 6.5e6f);
+    return splits == 1 ? main : main + 5.f + (float)splits * (float)(p.M * p.N) * (8.f / 8e6f);
 }
 
 Plan plan_of(int dt, const Product& p) {
@@ -739,10 +752,13 @@ template <typename T, bool ACOL, bool BCOL>
 hipError_t run_product(const Product& p, const Plan& q, const GemmArgs& g, hipStream_t st) {
     const unsigned grid = (unsigned)(q.tiles_m * q.tiles_n * q.splits);
     const int64_t bytes = (p.M * p.K + p.N * p.K) * 2 * (q.nseg > 1 ? 3 : 1) + p.M * p.N * dtype_bytes(g.e.out_dt);
-    if (q.tile == 64) k_product<T, ACOL, BCOL, 64, 64, 2, 2, false><<<grid, 256, 0, st>>>(g);
-    else if (q.tile == 128) k_product<T, ACOL, BCOL, 128, 128, 2, 2, false><<<grid, 256, 0, st>>>(g);
-    else if (bytes <= LAST_LEVEL_CACHE) k_product<T, ACOL, BCOL, 256, 256, 2, 4, false><<<grid, 512, 0, st>>>(g);
-    else k_product<T, ACOL, BCOL, 256, 256, 2, 4, true><<<grid, 512, 0, st>>>(g);
+    // 64 x 64 tiles stage three steps: 512 x 1024 over K = 4096, 128 work-groups, takes 22 us with
+    // three or four and 35 with two; 128 x 128 with three leave a CU one work-group, 31 us for
+    // 2048^3 against 27
+    if (q.tile == 64) k_product<T, ACOL, BCOL, 64, 64, 2, 2, 3, false><<<grid, 256, 0, st>>>(g);
+    else if (q.tile == 128) k_product<T, ACOL, BCOL, 128, 128, 2, 2, 2, false><<<grid, 256, 0, st>>>(g);
+    else if (bytes <= LAST_LEVEL_CACHE) k_product<T, ACOL, BCOL, 256, 256, 2, 4, 2, false><<<grid, 512, 0, st>>>(g);
+    else k_product<T, ACOL, BCOL, 256, 256, 2, 4, 2, true><<<grid, 512, 0, st>>>(g);
     return hipGetLastError();
 }
 template <typename T>

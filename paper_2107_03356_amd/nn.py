@@ -23,6 +23,7 @@ stream of the data's device, with workspaces from torch's allocator.
 """
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import _binding as B
 from ._binding import MfacError, load  # noqa: F401
@@ -418,6 +419,7 @@ class _LayerNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         k = _kept(ctx)
         need = ctx.needs_input_grad
@@ -437,6 +439,7 @@ class _Linear(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         k = _kept(ctx)
         need = ctx.needs_input_grad
@@ -462,6 +465,7 @@ class _FeedForward(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         k = _kept(ctx)
         t = ctx.types
