@@ -305,6 +305,41 @@ def test_large_tiles_against_64_bits(dev, dtype):
     holds(dw, want, U[F32] * want.abs() + E32 * growth(rows) * (d.abs().t() @ x.double().abs()), "dw")
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,cin,cout", [(16400, 136, 72), (300, 4104, 520), (2050, 1032, 2056), (40, 2000, 3000), (5000, 24, 8)])
+def test_parts_of_k_and_every_tile(dev, dtype, rows, cin, cout):
+    """Long sums that are shared out over work-groups, and sizes for which each tile is taken, through every
+    epilogue."""
+    from paper_2107_03356_amd import nn
+    say("parts and tiles", dtype, rows, cin, cout)
+    x, w, b, res = linear_inputs(dev, rows, cin, cout, dtype, 0)
+    z64 = x.double() @ w.double().t() + b.double()
+    ze = z_error(x, w, b)
+    y, p = nn.linear_forward(x, w, b, "gelu_tanh", res, keep="pack8")
+    want = act64("gelu_tanh", z64)[0] + res.double()
+    holds(y, want, U[dtype] * want.abs() + 1.2 * ze + act_error(z64) + E32 * want.abs(), "y")
+    step = torch.exp2(p.s.double() - 127).repeat_interleave(32, 1)[:, :cout]
+    holds(nn.unpack8(p), z64, step / 2 + ze, "copy of z")
+    yz, z = nn.linear_forward(x, w, b, "gelu_tanh", res, keep="z")
+    assert torch.equal(yz, y)
+    holds(z, z64, U[dtype] * z64.abs() + ze, "z")
+    dy = rand(dev, 41, rows, cout).to(dtype)
+    gamma, beta = (1 + 0.2 * rand(dev, 33, cin)).to(F32), (0.3 * rand(dev, 34, cin)).to(F32)
+    xp = nn.pack8(x)
+    add = rand(dev, 42, rows, cin).to(dtype)
+    d, dm = dy.double(), dy.double().abs()
+    dx = nn.linear_backward_input(dy, w, add=add)
+    want = d @ w.double() + add.double()
+    holds(dx, want, U[dtype] * want.abs() + E32 * growth(cout) * (dm @ w.double().abs()) + E32 * add.double().abs(), "dx")
+    _, _, db = nn.act_backward(dy)
+    for gtype in {dtype, F32}:
+        xq = unpack64(xp.q, xp.s)
+        want = d.t() @ (xq * gamma.double() + beta.double())
+        dw = nn.linear_backward_weight(dy, xp, (gamma, beta), db, gtype)
+        mag = dm.t() @ (xq.abs() * gamma.double().abs() + beta.double().abs())
+        holds(dw, want, U[gtype] * want.abs() + E32 * 2 * growth(rows) * mag, "dw")
+
+
 def test_skip_connection_joins_the_input_gradient_and_outputs_may_be_their_addend(dev):
     from paper_2107_03356_amd import _binding as B
     from paper_2107_03356_amd import nn
