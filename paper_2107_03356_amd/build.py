@@ -54,7 +54,8 @@ def build(verbose: bool = False) -> str:
         # bounds (k_gram_window, k_gram_blocks, fp64 k_bgemm with a transposed
         # B) are measured wins over fewer waves without them; k_trmm32 (12 and
         # 76 bytes) keeps a few values there that it reloads once per row
-        # tile, outside its k loop
+        # tile, outside its k loop; k_norm_bwd with 1024 threads a row (12 bytes)
+        # has 128 registers and two constants too many
         name = None
         for line in r.stderr.splitlines():
             m = re.search(r"Function Name: (\S+)", line)

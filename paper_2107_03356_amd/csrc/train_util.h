@@ -12,7 +12,6 @@ namespace mfac {
 namespace {
 
 typedef float f8 __attribute__((ext_vector_type(8)));
-typedef float f4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16;
 typedef __bf16 bf16;
 
@@ -22,7 +21,6 @@ template <typename T, int N>
 struct VecOf {
     typedef T plain __attribute__((ext_vector_type(N)));
     typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
-    typedef float wide __attribute__((ext_vector_type(N)));
 };
 
 // Values of other lanes of a row of 16, without a trip through LDS.
