@@ -784,14 +784,14 @@ hipError_t run_finish(const Product& p, const float* part, int splits, const Epi
     return hipGetLastError();
 }
 
-}  // namespace
-
 template <typename F>
 void by_operand(int dt, F f) {
     if (dt == DT_F32) f((float*)nullptr);
     else if (dt == DT_BF16) f((bf16*)nullptr);
     else f((f16*)nullptr);
 }
+
+}  // namespace
 
 size_t product_workspace_bytes(int dt, const Product& p) {
     const Plan q = plan_of(dt, p);

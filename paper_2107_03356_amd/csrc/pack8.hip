@@ -204,11 +204,13 @@ hipError_t launch_zero_matrix(int dt, int64_t rows, int64_t cols, void* y, int64
     });
 }
 
-// Parts: as many as give about 2048 work-groups, at most one for each row that a work-group has at a time.
+// Parts: as many as give about 2048 work-groups, at most one for each row that a work-group has at a time; one for
+// up to eight rows to each of them, whose sums are then db without a launch that joins parts.
 int64_t act_bwd_parts(int64_t rows, int64_t cols) {
     const Strips s = strips_of(rows, cols);
     const int64_t nsub = 4 * (64 >> s.ll);
-    return std::max<int64_t>(1, std::min(ceil_div(rows, nsub), ceil_div(2048, s.nstrips)));
+    if (rows <= 8 * nsub) return 1;
+    return std::min(ceil_div(rows, nsub), ceil_div(2048, s.nstrips));
 }
 
 hipError_t launch_act_bwd(int dt, int act, int64_t rows, int64_t cols, const void* dy, int64_t lddy, const void* z,
@@ -217,6 +219,7 @@ hipError_t launch_act_bwd(int dt, int act, int64_t rows, int64_t cols, const voi
     const Strips s = strips_of(rows, cols);
     const int64_t ng = ceil_div(cols, 32), nparts = rows > 0 ? act_bwd_parts(rows, cols) : 0;
     if (!db) part = nullptr;
+    else if (nparts == 1) part = db;
     if (rows > 0) {
         const dim3 grid((unsigned)s.nstrips, (unsigned)nparts);
         const hipError_t e = by_type(dt, [&](auto* t) {
@@ -232,7 +235,7 @@ hipError_t launch_act_bwd(int dt, int act, int64_t rows, int64_t cols, const voi
         });
         if (e != hipSuccess) return e;
     }
-    return db ? launch_column_sums(part, nparts, cols, cols, DT_F32, db, nullptr, st) : hipSuccess;
+    return db && nparts != 1 ? launch_column_sums(part, nparts, cols, cols, DT_F32, db, nullptr, st) : hipSuccess;
 }
 
 hipError_t launch_column_sums(const float* part, int64_t nparts, int64_t stride, int64_t cols, int out_dt, void* out_a,
