@@ -9,6 +9,7 @@ import re
 import shutil
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -38,13 +39,15 @@ def build(verbose: bool = False) -> str:
     out_dir = os.path.join(HERE, "_build")
     os.makedirs(out_dir, exist_ok=True)
     cc = hipcc()
-    objs = []
-    for src in SOURCES:
-        obj = os.path.join(out_dir, src.replace(".hip", ".o"))
-        cmd = [cc, *FLAGS, "-Rpass-analysis=kernel-resource-usage", "-c", os.path.join(CSRC, src), "-o", obj]
-        if verbose:
+    objs = [os.path.join(out_dir, src.replace(".hip", ".o")) for src in SOURCES]
+    cmds = [[cc, *FLAGS, "-Rpass-analysis=kernel-resource-usage", "-c", os.path.join(CSRC, src), "-o", obj]
+            for src, obj in zip(SOURCES, objs)]
+    if verbose:
+        for cmd in cmds:
             print(" ".join(cmd), flush=True)
-        r = subprocess.run(cmd, stderr=subprocess.PIPE, text=True)
+    with ThreadPoolExecutor(4) as pool:
+        runs = list(pool.map(lambda cmd: subprocess.run(cmd, stderr=subprocess.PIPE, text=True), cmds))
+    for src, cmd, r in zip(SOURCES, cmds, runs):
         if r.returncode != 0:
             sys.stderr.write(r.stderr)
             raise subprocess.CalledProcessError(r.returncode, cmd)
@@ -64,7 +67,6 @@ def build(verbose: bool = False) -> str:
             m = re.search(r"ScratchSize \[bytes/lane\]: (\d+)", line)
             if m and int(m.group(1)) > 0:
                 print(f"[build] warning: {src}: {name} uses {m.group(1)} bytes/lane of scratch", file=sys.stderr)
-        objs.append(obj)
     tmp = LIB + ".tmp"
     cmd = [cc, *FLAGS, "-shared", *objs, "-o", tmp]
     if verbose:
