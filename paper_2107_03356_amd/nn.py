@@ -354,8 +354,9 @@ def linear_backward_weight(dz, x, affine=None, db=None, grad_dtype=None):
     gamma = beta = None
     if affine is not None:
         gamma, beta = (_param("linear: affine", v.float(), dz2, cin) for v in affine)
-        if db is None or db.dtype != torch.float32 or db.shape != (cout,):
+        if db is None or db.dtype != torch.float32:
             raise ValueError("linear: affine needs db, the column sums of dz in float32")
+        db = _param("linear: db", db, dz2, cout)
     dw = torch.empty((cout, cin), dtype=grad_dtype, device=dz.device)
     t = _type(dz2, "linear: dz")
     zm = _mat(dz2)
