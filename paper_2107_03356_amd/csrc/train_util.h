@@ -201,7 +201,8 @@ __device__ __forceinline__ float erfc_pos(float y, float ex) {
 
 // The forward activations as three formulas, so that a kernel holds three and not five:
 // max(z, lo), lo = -inf or 0; z / (1 + 2^(z (p + q z^2))), for x / (1 + exp(-x)) and
-// (1 + tanh u) / 2 = 1 / (1 + exp(-2u)); z Phi(z).
+// (1 + tanh u) / 2 = 1 / (1 + exp(-2u)), z^2 kept finite so that q = 0 times it is 0 at an
+// infinite z too; z Phi(z).
 struct ActForward {
     int formula;
     float p, q;
@@ -221,7 +222,8 @@ __device__ __forceinline__ void act_apply(const ActForward& f, V (&z)[N]) {
 #pragma unroll
             for (int i = 0; i < W; ++i) {
                 const float x = z[j][i];
-                z[j][i] = x * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * fmaf(f.q * x, x, f.p)));
+                const float x2 = fminf(x * x, __FLT_MAX__);
+                z[j][i] = x * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * fmaf(f.q, x2, f.p)));
             }
     } else if (f.formula == 2) {
 #pragma unroll

@@ -40,3 +40,36 @@ def test_weight_gradient_with_db_of_any_stride(dev):
     for bad in (db.cpu(), db.double(), db[:39], None):
         with pytest.raises(ValueError):
             nn.linear_backward_weight(dz, p, (g, b), bad)
+
+
+# ---------------------------------------------------------------- values
+ENDS = [0.0, 1e-30, -1e-30, 5.0, -5.0, 30.0, -30.0, 300.0, -300.0, 1e4, -1e4, 1e15, -1e15, 1e19, -1e19, 1e20, -1e20, 3e38, -3e38,
+        float("inf")]
+
+
+def end_values(dev, act):
+    """Pre-activations far out, and the infinities that the activation's definition has values for."""
+    z = torch.tensor(ENDS + [float("-inf") if act == "relu" else 0.0] + [1.0] * 11, dtype=F32, device=dev)
+    return z, act64(act, z.double())
+
+
+def end_bound(z, a):
+    z = z.clamp(-1e39, 1e39)   # infinities have no size of their own
+    return act_error(z) * torch.clamp(a.abs() * 1e9, max=1.0) + 1e-30 + E32 * a.abs()
+
+
+# one token, a tile of the products, and a long sum in parts
+@pytest.mark.parametrize("rows,cin", [(3, 64), (40, 64), (40, 8192)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+def test_activations_far_out_and_at_infinity(dev, act, dtype, rows, cin):
+    from paper_2107_03356_amd import nn
+    say("activations far out", act, dtype, rows, cin)
+    z, (a64, _) = end_values(dev, act)
+    x, w = torch.zeros(rows, cin, dtype=dtype, device=dev), rand(dev, 1, z.numel(), cin).to(dtype)
+    y = nn.linear_forward(x, w, z, act)   # 0 + z
+    want = a64.to(dtype).double().expand(rows, -1)
+    bound = end_bound(z.double(), torch.nan_to_num(a64, posinf=0.0)) + U[dtype] * torch.nan_to_num(a64.abs(), posinf=0.0)
+    holds(y, want, bound.expand(rows, -1), "y")
+    same = torch.isinf(want)
+    assert torch.equal(y.double()[same], want[same])
