@@ -73,3 +73,19 @@ def test_activations_far_out_and_at_infinity(dev, act, dtype, rows, cin):
     holds(y, want, bound.expand(rows, -1), "y")
     same = torch.isinf(want)
     assert torch.equal(y.double()[same], want[same])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+def test_slopes_far_out(dev, act, dtype):
+    """Far out a slope is 0 or 1, however large z * z is; act(z) as the forward pass gives it, +inf at +inf."""
+    from paper_2107_03356_amd import nn
+    say("slopes far out", act, dtype)
+    z, _ = end_values(dev, act)
+    z = z.to(dtype)[None]
+    a64, s64 = act64(act, z.double())
+    dz, a, _ = nn.act_backward(torch.ones_like(z), z, act, want_a=True)
+    at = torch.isfinite(z)
+    holds(dz[at], s64[at], act_error(z.double()[at]).clamp(max=1e-6) + U[dtype] * s64[at].abs(), "slope")
+    a64 = a64.to(dtype).double()
+    holds(a, a64, end_bound(z.double(), torch.nan_to_num(a64, posinf=0.0)) + U[dtype] * torch.nan_to_num(a64.abs(), posinf=0.0), "a")
