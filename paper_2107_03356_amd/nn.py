@@ -372,6 +372,8 @@ def linear_backward(dy, x, weight, z=None, act="none", affine=None, grad_dtype=N
     linear_backward_weight; dx is then the gradient of gamma * x + beta. dbias is float32.
     ``need``: which of the three to form; the others are None."""
     need_x, need_w, need_b = need
+    if not (need_x or need_w or need_b):   # z may be absent then
+        return None, None, None
     dz, _, db = act_backward(dy, z, act, want_db=need_b or (need_w and affine is not None))
     dx = linear_backward_input(dz, weight) if need_x else None
     dw = linear_backward_weight(dz, x, affine, db, grad_dtype) if need_w else None

@@ -89,3 +89,16 @@ def test_slopes_far_out(dev, act, dtype):
     holds(dz[at], s64[at], act_error(z.double()[at]).clamp(max=1e-6) + U[dtype] * s64[at].abs(), "slope")
     a64 = a64.to(dtype).double()
     holds(a, a64, end_bound(z.double(), torch.nan_to_num(a64, posinf=0.0)) + U[dtype] * torch.nan_to_num(a64.abs(), posinf=0.0), "a")
+
+
+# ---------------------------------------------------------------- which gradients
+@pytest.mark.parametrize("act", ["none", "gelu"])
+@pytest.mark.parametrize("copy8", [False, True])
+def test_linear_whose_residual_alone_needs_a_gradient(dev, act, copy8):
+    from paper_2107_03356_amd import nn
+    say("residual alone", act, copy8)
+    x, w, b = rand(dev, 1, 20, 64).to(BF16), rand(dev, 2, 48, 64).to(BF16), rand(dev, 3, 48).to(F32)
+    r = rand(dev, 4, 20, 48).to(BF16).requires_grad_()
+    dy = rand(dev, 5, 20, 48).to(BF16)
+    nn.linear(x, w, b, act=act, residual=r, copy8=copy8).backward(dy)
+    assert torch.equal(r.grad, dy)

@@ -43,3 +43,98 @@ def test_weight_gradient_takes_db_of_any_stride(calls):
     for db in (column, torch.full((1,), 2.5).expand(6), column.contiguous()):
         nn.linear_backward_weight(dz, x, affine=(g, g), db=db)
         assert calls.pop()[2] == db.tolist()
+
+
+# ---------------------------------------------------------------- what the layers keep and form
+class Passes:
+    """The passes in elementary operations on the CPU, with a record of what was asked of them."""
+
+    def __init__(self):
+        self.made = []
+
+    def layer_norm_forward(self, x, weight=None, bias=None, eps=1e-5, pack=False):
+        self.made.append("norm+copy" if pack else "norm")
+        mean = x.mean(-1, keepdim=True)
+        rstd = torch.rsqrt((x - mean).square().mean(-1, keepdim=True) + eps)
+        xh = (x - mean) * rstd
+        y = xh if weight is None else xh * weight
+        y = y if bias is None else y + bias
+        flat = x.reshape(-1, x.shape[-1])
+        return (y, self.copy(xh), rstd.flatten()) if pack else (y, mean.flatten(), rstd.flatten()[:flat.shape[0]])
+
+    def copy(self, x):
+        x = x.reshape(-1, x.shape[-1])
+        s = torch.exp2(torch.floor(torch.log2(x.abs().amax().clamp(min=1e-30))) - 5)
+        p = nn.Packed8(torch.round(x / s).to(torch.int8), torch.full((x.shape[0], -(-x.shape[1] // 32)), 127, dtype=torch.uint8))
+        p.q.scale = s
+        return p
+
+    def value(self, p):
+        return p.q.float() if isinstance(p, nn.Packed8) else p
+
+    def pack8(self, x):
+        self.made.append("pack8")
+        return self.copy(x)
+
+    def unpack8(self, p, dtype=torch.float32):
+        self.made.append("unpack8")
+        return p.q.to(dtype)
+
+    def linear_forward(self, x, weight, bias=None, act="none", residual=None, keep=None):
+        self.made.append("linear" if keep is None else "linear+" + keep)
+        z = x @ weight.t() if bias is None else x @ weight.t() + bias
+        y = z if act == "none" else torch.nn.functional.silu(z)
+        y = y if residual is None else y + residual.reshape(y.shape)
+        return y if keep is None else (y, z if keep == "z" else self.copy(z))
+
+    def act_backward(self, dy, z=None, act="none", want_a=False, want_db=True):
+        if (z is None) != (act == "none") or (want_a and z is None):
+            raise ValueError("act: z goes with an activation")
+        self.made.append("act" + "+a" * want_a + "+db" * want_db)
+        if z is None:
+            return dy, None, dy.reshape(-1, dy.shape[-1]).sum(0) if want_db else None
+        v = self.value(z).reshape(dy.shape)
+        p = torch.sigmoid(v)
+        dz = dy * p * (1 + v * (1 - p))
+        return dz, v * p if want_a else None, dz.reshape(-1, dz.shape[-1]).sum(0) if want_db else None
+
+    def linear_backward_input(self, dz, weight, add=None):
+        self.made.append("dx")
+        return dz @ weight
+
+    def linear_backward_weight(self, dz, x, affine=None, db=None, grad_dtype=None):
+        self.made.append("dw")
+        x = self.value(x)
+        if affine is not None:
+            x = x * affine[0] + affine[1]
+        return dz.reshape(-1, dz.shape[-1]).t() @ x.reshape(-1, x.shape[-1])
+
+    def layer_norm_backward(self, dy, x, mean, rstd, weight=None, add=None, params=True):
+        self.made.append("norm_bwd" + "+params" * params)
+        r = rstd.view(*dy.shape[:-1], 1)
+        xh = self.value(x).reshape(dy.shape) if isinstance(x, nn.Packed8) else (x - mean.view(r.shape)) * r
+        h = dy if weight is None else dy * weight
+        dx = r * (h - h.mean(-1, keepdim=True) - xh * (h * xh).mean(-1, keepdim=True))
+        dx = dx if add is None else dx + add
+        n = dy.shape[-1]
+        return (dx, (dy * xh).reshape(-1, n).sum(0), dy.reshape(-1, n).sum(0)) if params else (dx, None, None)
+
+
+@pytest.fixture
+def passes(monkeypatch):
+    p = Passes()
+    for name in ("layer_norm_forward", "pack8", "unpack8", "linear_forward", "act_backward", "linear_backward_input",
+                 "linear_backward_weight", "layer_norm_backward"):
+        monkeypatch.setattr(nn, name, getattr(p, name))
+    return p
+
+
+@pytest.mark.parametrize("act", ["none", "silu"])
+@pytest.mark.parametrize("copy8", [False, True])
+def test_linear_whose_residual_alone_needs_a_gradient(passes, act, copy8):
+    x, w, b, r = torch.randn(5, 8), torch.randn(6, 8), torch.randn(6), torch.randn(5, 6, requires_grad=True)
+    y = nn.linear(x, w, b, act=act, residual=r, copy8=copy8)
+    assert passes.made == ["linear"]
+    dy = torch.randn(5, 6)
+    y.backward(dy)
+    assert torch.equal(r.grad, dy) and passes.made == ["linear"]
