@@ -437,7 +437,8 @@ class _Linear(torch.autograd.Function):
         keep = None if act == "none" or not any(ctx.needs_input_grad[:3]) else "pack8" if copy8 else "z"
         out = linear_forward(x, w, bias, act, residual, keep)
         y, z = (out, None) if keep is None else out
-        ctx.act, ctx.wdtype, ctx.bdtype, ctx.xshape = act, weight.dtype, None if bias is None else bias.dtype, x.shape
+        ctx.act, ctx.wdtype, ctx.bdtype = act, weight.dtype, None if bias is None else bias.dtype
+        ctx.rshape = None if residual is None else residual.shape   # its rows may lie in other dimensions than y's
         _keep(ctx, x=(pack8(x) if copy8 else x) if ctx.needs_input_grad[1] else None, w=w, z=z)
         return y
 
@@ -448,7 +449,7 @@ class _Linear(torch.autograd.Function):
         need = ctx.needs_input_grad
         dx, dw, db = linear_backward(dy, k["x"], k["w"], k["z"], ctx.act, grad_dtype=_grad_dtype(ctx.wdtype, dy),
                                      need=need[:3])
-        return dx, _to(dw, ctx.wdtype), _to(db, ctx.bdtype), None, dy if need[4] else None, None
+        return dx, _to(dw, ctx.wdtype), _to(db, ctx.bdtype), None, dy.reshape(ctx.rshape) if need[4] else None, None
 
 
 class _FeedForward(torch.autograd.Function):

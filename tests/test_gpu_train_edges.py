@@ -102,3 +102,17 @@ def test_linear_whose_residual_alone_needs_a_gradient(dev, act, copy8):
     dy = rand(dev, 5, 20, 48).to(BF16)
     nn.linear(x, w, b, act=act, residual=r, copy8=copy8).backward(dy)
     assert torch.equal(r.grad, dy)
+
+
+def test_gradient_of_a_residual_of_other_dimensions(dev):
+    """A residual whose rows lie in other leading dimensions than y's gets its gradient in its own shape."""
+    from paper_2107_03356_amd import nn
+    say("residual dimensions")
+    x, w = rand(dev, 1, 4, 10, 64).to(BF16), rand(dev, 2, 48, 64).to(BF16)
+    dy = rand(dev, 5, 4, 10, 48).to(BF16)
+    for shape in ((40, 48), (2, 20, 48), (4, 10, 48)):
+        r = rand(dev, 4, *shape).to(BF16).requires_grad_()
+        y = nn.linear(x, w, residual=r)
+        assert y.shape == dy.shape
+        y.backward(dy)
+        assert torch.equal(r.grad, dy.view(shape))

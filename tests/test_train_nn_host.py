@@ -138,3 +138,11 @@ def test_linear_whose_residual_alone_needs_a_gradient(passes, act, copy8):
     dy = torch.randn(5, 6)
     y.backward(dy)
     assert torch.equal(r.grad, dy) and passes.made == ["linear"]
+
+
+@pytest.mark.parametrize("shape", [(20, 6), (2, 10, 6), (4, 5, 6)])
+def test_gradient_of_a_residual_of_other_dimensions(passes, shape):
+    x, w, r = torch.randn(4, 5, 8), torch.randn(6, 8), torch.randn(*shape, requires_grad=True)
+    dy = torch.randn(4, 5, 6)
+    nn.linear(x, w, residual=r).backward(dy)
+    assert torch.equal(r.grad, dy.view(shape))
