@@ -132,6 +132,12 @@ def _param(what, p, data, n):
     return p.contiguous()
 
 
+def _weight(w):
+    if w.dim() != 2:
+        raise ValueError(f"linear: weight is a matrix (cout x cin), not {tuple(w.shape)}")
+    return _rows(w, "linear: weight")
+
+
 def _act(name):
     try:
         return ACTIVATIONS[name]
@@ -263,7 +269,7 @@ def linear_forward(x, weight, bias=None, act="none", residual=None, keep=None):
     a = _act(act)
     x2 = _rows(x, "linear: x")
     rows, cin = x2.shape
-    w = _rows(weight, "linear: weight")
+    w = _weight(weight)
     cout = w.shape[0]
     _same("linear: weight", w, x2, (cout, cin))
     b = None if bias is None else _param("linear: bias", bias, x2, cout)
@@ -317,7 +323,7 @@ def linear_backward_input(dz, weight, add=None):
     """dx = dz weight + add."""
     dz2 = _rows(dz, "linear: dz")
     rows, cout = dz2.shape
-    w = _rows(weight, "linear: weight")
+    w = _weight(weight)
     cin = w.shape[1]
     _same("linear: weight", w, dz2, (cout, cin))
     if add is not None:

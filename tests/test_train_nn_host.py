@@ -146,3 +146,13 @@ def test_gradient_of_a_residual_of_other_dimensions(passes, shape):
     dy = torch.randn(4, 5, 6)
     nn.linear(x, w, residual=r).backward(dy)
     assert torch.equal(r.grad, dy.view(shape))
+
+
+@pytest.mark.parametrize("shape", [(8,), (2, 3, 8), ()])
+def test_a_weight_is_a_matrix(calls, monkeypatch, shape):
+    monkeypatch.setattr(nn, "_rows", lambda t, what: t.reshape(-1, t.shape[-1]) if t.dim() else t.reshape(1, 1))
+    x, w = torch.zeros(4, 8), torch.zeros(shape)
+    for f in (lambda: nn.linear_forward(x, w), lambda: nn.linear(x, w), lambda: nn.linear_backward_input(torch.zeros(4, 6), w)):
+        with pytest.raises(ValueError):
+            f()
+    assert not calls
