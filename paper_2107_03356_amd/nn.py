@@ -416,9 +416,13 @@ def _grad_dtype(param, data):
     return param if param == data.dtype else torch.float32
 
 
+# `grad`, the last argument of each: torch.is_grad_enabled() where it was called. Within forward it is always
+# off, and needs_input_grad says what the inputs ask for whether it is on or not.
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, eps, copy8):
+    def forward(ctx, x, weight, bias, eps, copy8, grad):
+        if not (grad and any(ctx.needs_input_grad)):
+            return layer_norm_forward(x, weight, bias, eps)[0]
         y, kept, rstd = layer_norm_forward(x, weight, bias, eps, pack=copy8)
         ctx.types = tuple(None if p is None else p.dtype for p in (weight, bias))
         if copy8:
@@ -433,19 +437,21 @@ class _LayerNorm(torch.autograd.Function):
         k = _kept(ctx)
         need = ctx.needs_input_grad
         dx, dw, db = layer_norm_backward(dy, k["x"], k["mean"], k["rstd"], k["w"], params=need[1] or need[2])
-        return dx, _to(dw, ctx.types[0]) if need[1] else None, _to(db, ctx.types[1]) if need[2] else None, None, None
+        return (dx, _to(dw, ctx.types[0]) if need[1] else None, _to(db, ctx.types[1]) if need[2] else None, None, None,
+                None)
 
 
 class _Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, act, residual, copy8):
+    def forward(ctx, x, weight, bias, act, residual, copy8, grad):
         w = weight.to(x.dtype)
-        keep = None if act == "none" or not any(ctx.needs_input_grad[:3]) else "pack8" if copy8 else "z"
+        need = [grad and n for n in ctx.needs_input_grad[:3]]
+        keep = None if act == "none" or not any(need) else "pack8" if copy8 else "z"
         out = linear_forward(x, w, bias, act, residual, keep)
         y, z = (out, None) if keep is None else out
         ctx.act, ctx.wdtype, ctx.bdtype = act, weight.dtype, None if bias is None else bias.dtype
         ctx.rshape = None if residual is None else residual.shape   # its rows may lie in other dimensions than y's
-        _keep(ctx, x=(pack8(x) if copy8 else x) if ctx.needs_input_grad[1] else None, w=w, z=z)
+        _keep(ctx, x=(pack8(x) if copy8 else x) if need[1] else None, w=w if need[0] else None, z=z)
         return y
 
     @staticmethod
@@ -455,7 +461,8 @@ class _Linear(torch.autograd.Function):
         need = ctx.needs_input_grad
         dx, dw, db = linear_backward(dy, k["x"], k["w"], k["z"], ctx.act, grad_dtype=_grad_dtype(ctx.wdtype, dy),
                                      need=need[:3])
-        return dx, _to(dw, ctx.wdtype), _to(db, ctx.bdtype), None, dy.reshape(ctx.rshape) if need[4] else None, None
+        dres = dy.reshape(ctx.rshape) if need[4] else None
+        return dx, _to(dw, ctx.wdtype), _to(db, ctx.bdtype), None, dres, None, None
 
 
 class _FeedForward(torch.autograd.Function):
@@ -464,9 +471,12 @@ class _FeedForward(torch.autograd.Function):
     the pre-activation, from which act(z) is formed again for W2's gradient."""
 
     @staticmethod
-    def forward(ctx, x, lw, lb, w1, b1, w2, b2, act, eps, copy8):
-        h, kept, rstd = layer_norm_forward(x, lw, lb, eps, pack=copy8)
+    def forward(ctx, x, lw, lb, w1, b1, w2, b2, act, eps, copy8, grad):
         c1, c2 = w1.to(x.dtype), w2.to(x.dtype)
+        if not (grad and any(ctx.needs_input_grad)):
+            a = linear_forward(layer_norm_forward(x, lw, lb, eps)[0], c1, b1, act)
+            return linear_forward(a, c2, b2, residual=x)
+        h, kept, rstd = layer_norm_forward(x, lw, lb, eps, pack=copy8)
         a, z = linear_forward(h, c1, b1, act, keep="pack8" if copy8 else "z")
         y = linear_forward(a, c2, b2, residual=x)
         ctx.act, ctx.copy8, ctx.types = act, copy8, tuple(p.dtype for p in (lw, lb, w1, b1, w2, b2))
@@ -491,20 +501,20 @@ class _FeedForward(torch.autograd.Function):
         dh = linear_backward_input(dz, k["c1"])
         dx, dlw, dlb = layer_norm_backward(dh, k["x"], k["mean"], k["rstd"], k["lw"], add=dy)
         return (dx, _to(dlw, t[0]), _to(dlb, t[1]), _to(dw1, t[2]), _to(db1, t[3]), _to(dw2, t[4]), _to(db2, t[5]), None,
-                None, None)
+                None, None, None)
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, copy8=False):
     """Layer norm over the last dimension, differentiable. copy8: keep the normalised x in
     8 bits for the backward pass instead of x."""
-    return _LayerNorm.apply(x, weight, bias, eps, copy8)
+    return _LayerNorm.apply(x, weight, bias, eps, copy8, torch.is_grad_enabled())
 
 
 def linear(x, weight, bias=None, act="none", residual=None, copy8=False):
     """act(x weight^T + bias) + residual, differentiable. copy8: keep x and the
     pre-activation in 8 bits for the backward pass."""
     _act(act)
-    return _Linear.apply(x, weight, bias, act, residual, copy8)
+    return _Linear.apply(x, weight, bias, act, residual, copy8, torch.is_grad_enabled())
 
 
 def feed_forward(x, ln_weight, ln_bias, w1, b1, w2, b2, act="gelu", eps=1e-5, copy8=False):
@@ -512,7 +522,7 @@ def feed_forward(x, ln_weight, ln_bias, w1, b1, w2, b2, act="gelu", eps=1e-5, co
     pass needs is kept in 8 bits."""
     if _act(act) == B.MFAC_ACT_NONE:
         raise ValueError("feed_forward: needs an activation")
-    return _FeedForward.apply(x, ln_weight, ln_bias, w1, b1, w2, b2, act, eps, copy8)
+    return _FeedForward.apply(x, ln_weight, ln_bias, w1, b1, w2, b2, act, eps, copy8, torch.is_grad_enabled())
 
 
 # ---------------------------------------------------------------- modules

@@ -116,3 +116,27 @@ def test_gradient_of_a_residual_of_other_dimensions(dev):
         assert y.shape == dy.shape
         y.backward(dy)
         assert torch.equal(r.grad, dy.view(shape))
+
+
+@pytest.mark.parametrize("copy8", [False, True])
+def test_inference_gives_the_same_and_keeps_nothing(dev, copy8):
+    from paper_2107_03356_amd import nn
+    say("inference", copy8)
+    torch.manual_seed(2)
+    rows, dim, hid = 2048, 128, 4096
+    block, lin = nn.FeedForward(dim, hid, copy8=copy8, device=dev), nn.Linear(dim, hid, act="silu", copy8=copy8, device=dev)
+    norm = nn.LayerNorm(dim, copy8=copy8, device=dev)
+    x = rand(dev, 1, rows, dim).to(BF16)
+    trained = [m(x).detach() for m in (block, lin, norm)]
+    kept = []
+    with torch.no_grad(), torch.autograd.graph.saved_tensors_hooks(lambda t: kept.append(t) or t, lambda t: t):
+        assert all(torch.equal(m(x), t) for m, t in zip((block, lin, norm), trained))
+    assert not kept
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    with torch.no_grad():
+        block(x)
+    # the hidden activation, the weights in 16 bits and the rows of dim; z, in 16 bits or 8, is half as much again at least
+    most = 2 * rows * hid + 2 * 2 * dim * hid + 4 * 2 * rows * dim
+    assert torch.cuda.max_memory_allocated() - before < most + (1 << 21)

@@ -156,3 +156,43 @@ def test_a_weight_is_a_matrix(calls, monkeypatch, shape):
         with pytest.raises(ValueError):
             f()
     assert not calls
+
+
+def modules(copy8):
+    torch.manual_seed(1)
+    return nn.LayerNorm(64, copy8=copy8), nn.Linear(64, 64, act="silu", copy8=copy8), nn.FeedForward(64, 32, act="silu", copy8=copy8)
+
+
+@pytest.mark.parametrize("copy8", [False, True])
+@pytest.mark.parametrize("mode", [torch.no_grad, torch.inference_mode])
+def test_inference_keeps_nothing(passes, mode, copy8):
+    norm, lin, block = modules(copy8)
+    x = torch.randn(3, 4, 64)
+    trained = [m(x).detach() for m in (norm, lin, block)]
+    del passes.made[:]
+    with mode():
+        assert torch.equal(norm(x), trained[0]) and passes.made == ["norm"]
+        assert torch.equal(lin(x), trained[1]) and passes.made[1:] == ["linear"]
+        assert torch.equal(block(x), trained[2]) and passes.made[2:] == ["norm", "linear", "linear"]
+
+
+@pytest.mark.parametrize("copy8", [False, True])
+def test_layers_without_gradients_keep_nothing(passes, copy8):
+    norm, lin, block = (m.requires_grad_(False) for m in modules(copy8))
+    x = torch.randn(3, 64)
+    norm(x), lin(x), block(x)
+    assert passes.made == ["norm", "linear", "norm", "linear", "linear"]
+    saved = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: saved.append(t) or t, lambda t: t):
+        lin(x, residual=torch.randn(3, 64, requires_grad=True))
+    assert not saved
+
+
+def test_training_keeps_what_it_did(passes):
+    x = torch.randn(3, 64, requires_grad=True)
+    for copy8, want in ((False, ["norm", "linear+z", "norm", "linear+z", "linear"]),
+                        (True, ["norm+copy", "linear+pack8", "pack8", "norm+copy", "linear+pack8", "linear"])):
+        del passes.made[:]
+        for m in modules(copy8):
+            m(x)
+        assert passes.made == want
