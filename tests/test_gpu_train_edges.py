@@ -132,11 +132,18 @@ def test_inference_gives_the_same_and_keeps_nothing(dev, copy8):
     with torch.no_grad(), torch.autograd.graph.saved_tensors_hooks(lambda t: kept.append(t) or t, lambda t: t):
         assert all(torch.equal(m(x), t) for m, t in zip((block, lin, norm), trained))
     assert not kept
-    torch.cuda.synchronize()
-    torch.cuda.reset_peak_memory_stats()
-    before = torch.cuda.memory_allocated()
-    with torch.no_grad():
-        block(x)
-    # the hidden activation, the weights in 16 bits and the rows of dim; z, in 16 bits or 8, is half as much again at least
-    most = 2 * rows * hid + 2 * 2 * dim * hid + 4 * 2 * rows * dim
-    assert torch.cuda.max_memory_allocated() - before < most + (1 << 21)
+
+    def by_hand(x):
+        c1, c2 = block.up.weight.to(BF16), block.down.weight.to(BF16)
+        a = nn.linear_forward(nn.layer_norm_forward(x, block.norm.weight, block.norm.bias)[0], c1, block.up.bias, "gelu")
+        return nn.linear_forward(a, c2, block.down.bias, residual=x)
+
+    peaks = []
+    for f in (by_hand, block):   # z or its copy, rows x hid, would come on top
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        with torch.no_grad():
+            f(x)
+        peaks.append(torch.cuda.max_memory_allocated() - before)
+    assert peaks[1] <= peaks[0], peaks
