@@ -476,32 +476,47 @@ class _FeedForward(torch.autograd.Function):
         if not (grad and any(ctx.needs_input_grad)):
             a = linear_forward(layer_norm_forward(x, lw, lb, eps)[0], c1, b1, act)
             return linear_forward(a, c2, b2, residual=x)
-        h, kept, rstd = layer_norm_forward(x, lw, lb, eps, pack=copy8)
-        a, z = linear_forward(h, c1, b1, act, keep="pack8" if copy8 else "z")
+        need = ctx.needs_input_grad
+        norm, hidden = any(need[:3]), any(need[:5])   # whether a gradient passes through the norm, or through act
+        pack = copy8 and (norm or need[3])
+        h, kept, rstd = layer_norm_forward(x, lw, lb, eps, pack=pack)
+        keep = None if not (hidden or need[5]) else "pack8" if copy8 else "z"
+        out = linear_forward(h, c1, b1, act, keep=keep)
+        a, z = (out, None) if keep is None else out
         y = linear_forward(a, c2, b2, residual=x)
         ctx.act, ctx.copy8, ctx.types = act, copy8, tuple(p.dtype for p in (lw, lb, w1, b1, w2, b2))
-        _keep(ctx, x=kept if copy8 else x, mean=None if copy8 else kept, rstd=rstd, h=None if copy8 else h, z=z, lw=lw,
-              lb=lb, c1=c1, c2=c2)
+        _keep(ctx, x=kept if pack else x if norm else None, mean=kept if norm and not pack else None,
+              rstd=rstd if norm else None, h=h if need[3] and not copy8 else None, z=z, lw=lw if norm or pack else None,
+              lb=lb if pack else None, c1=c1 if norm else None, c2=c2 if hidden else None)
         return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
         k = _kept(ctx)
-        t = ctx.types
-        _, _, db2 = act_backward(dy)
-        da = linear_backward_input(dy, k["c2"])
-        dz, a, db1 = act_backward(da, k["z"], ctx.act, want_a=True)
-        dw2 = linear_backward_weight(dy, a, grad_dtype=_grad_dtype(t[4], dy))
-        del a, da
-        if ctx.copy8:
-            dw1 = linear_backward_weight(dz, k["x"], (k["lw"], k["lb"]), db1, _grad_dtype(t[2], dy))
-        else:
-            dw1 = linear_backward_weight(dz, k["h"], grad_dtype=_grad_dtype(t[2], dy))
-        dh = linear_backward_input(dz, k["c1"])
-        dx, dlw, dlb = layer_norm_backward(dh, k["x"], k["mean"], k["rstd"], k["lw"], add=dy)
-        return (dx, _to(dlw, t[0]), _to(dlb, t[1]), _to(dw1, t[2]), _to(db1, t[3]), _to(dw2, t[4]), _to(db2, t[5]), None,
-                None, None, None)
+        t, z = ctx.types, k["z"]
+        nx, nlw, nlb, nw1, nb1, nw2, nb2 = ctx.needs_input_grad[:7]
+        norm, hidden = nx or nlw or nlb, nx or nlw or nlb or nw1 or nb1
+        dx = dlw = dlb = dw1 = db1 = dw2 = db2 = None
+        if nb2:
+            _, _, db2 = act_backward(dy)
+        if hidden or nw2:
+            # where w2 alone asks for act(z), any tensor of its shape will do for the gradient that is not looked at
+            da = linear_backward_input(dy, k["c2"]) if hidden else unpack8(z, dy.dtype) if ctx.copy8 else z
+            dz, a, db1 = act_backward(da, z, ctx.act, want_a=nw2, want_db=nb1 or (nw1 and ctx.copy8))
+            if nw2:
+                dw2 = linear_backward_weight(dy, a, grad_dtype=_grad_dtype(t[4], dy))
+            del a, da
+        if nw1:
+            if ctx.copy8:
+                dw1 = linear_backward_weight(dz, k["x"], (k["lw"], k["lb"]), db1, _grad_dtype(t[2], dy))
+            else:
+                dw1 = linear_backward_weight(dz, k["h"], grad_dtype=_grad_dtype(t[2], dy))
+        if norm:
+            dh = linear_backward_input(dz, k["c1"])
+            dx, dlw, dlb = layer_norm_backward(dh, k["x"], k["mean"], k["rstd"], k["lw"], add=dy, params=nlw or nlb)
+        return (dx, _to(dlw, t[0]), _to(dlb, t[1]), _to(dw1, t[2]), _to(db1, t[3]), _to(dw2, t[4]), _to(db2, t[5]),
+                None, None, None, None)
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, copy8=False):

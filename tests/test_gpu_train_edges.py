@@ -147,3 +147,26 @@ def test_inference_gives_the_same_and_keeps_nothing(dev, copy8):
             f(x)
         peaks.append(torch.cuda.max_memory_allocated() - before)
     assert peaks[1] <= peaks[0], peaks
+
+
+@pytest.mark.parametrize("copy8", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_block_gradients_one_by_one_are_those_of_all(dev, dtype, copy8):
+    from paper_2107_03356_amd import nn
+    say("block gradients one by one", dtype, copy8)
+    dy = rand(dev, 9, 4, 50, 72).to(dtype)
+
+    def gradients(needed):
+        t = [rand(dev, 1, 4, 50, 72).to(dtype), 1 + 0.2 * rand(dev, 2, 72).to(F32), rand(dev, 3, 72).to(F32),
+             rand(dev, 4, 200, 72, scale=0.1).to(F32), rand(dev, 5, 200).to(F32), rand(dev, 6, 72, 200, scale=0.1).to(F32),
+             rand(dev, 7, 72).to(F32)]
+        for i in needed:
+            t[i].requires_grad_()
+        nn.feed_forward(*t, act="gelu_tanh", copy8=copy8).backward(dy)
+        assert [v.grad is not None for v in t] == [i in needed for i in range(7)]
+        return {i: t[i].grad for i in needed}
+
+    every = gradients(range(7))
+    for needed in [[i] for i in range(7)] + [[1, 2], [3, 5], [0, 4, 6]]:
+        for i, g in gradients(needed).items():
+            assert torch.equal(g, every[i]), (needed, i)

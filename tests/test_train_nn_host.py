@@ -64,13 +64,11 @@ class Passes:
 
     def copy(self, x):
         x = x.reshape(-1, x.shape[-1])
-        s = torch.exp2(torch.floor(torch.log2(x.abs().amax().clamp(min=1e-30))) - 5)
-        p = nn.Packed8(torch.round(x / s).to(torch.int8), torch.full((x.shape[0], -(-x.shape[1] // 32)), 127, dtype=torch.uint8))
-        p.q.scale = s
-        return p
+        s = torch.full((x.shape[0], -(-x.shape[1] // 32)), 127 - 5, dtype=torch.uint8)
+        return nn.Packed8(torch.round(x * 32).clamp(-127, 127).to(torch.int8), s)
 
     def value(self, p):
-        return p.q.float() if isinstance(p, nn.Packed8) else p
+        return p.q.float() / 32 if isinstance(p, nn.Packed8) else p
 
     def pack8(self, x):
         self.made.append("pack8")
@@ -78,7 +76,7 @@ class Passes:
 
     def unpack8(self, p, dtype=torch.float32):
         self.made.append("unpack8")
-        return p.q.to(dtype)
+        return self.value(p).to(dtype)
 
     def linear_forward(self, x, weight, bias=None, act="none", residual=None, keep=None):
         self.made.append("linear" if keep is None else "linear+" + keep)
@@ -196,3 +194,37 @@ def test_training_keeps_what_it_did(passes):
         for m in modules(copy8):
             m(x)
         assert passes.made == want
+
+
+NAMES = ["x", "lw", "lb", "w1", "b1", "w2", "b2"]
+
+
+def block_gradients(needed, copy8):
+    torch.manual_seed(4)
+    t = [torch.randn(5, 64), 1 + 0.1 * torch.randn(64), torch.randn(64), torch.randn(32, 64) / 8, torch.randn(32),
+         torch.randn(64, 32) / 6, torch.randn(64)]
+    for name, v in zip(NAMES, t):
+        v.requires_grad_(name in needed)
+    saved = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda v: saved.append(v) or v, lambda v: v):
+        y = nn.feed_forward(*t, act="silu", copy8=copy8)
+    y.backward(torch.linspace(-1, 1, y.numel()).view(y.shape))
+    return {name: v.grad for name, v in zip(NAMES, t) if v.grad is not None}, saved
+
+
+@pytest.mark.parametrize("copy8", [False, True])
+@pytest.mark.parametrize("needed,products", [
+    (["x"], ["dx", "dx"]), (["b2"], []), (["w2"], ["dw"]), (["w2", "b2"], ["dw"]), (["b1"], ["dx"]), (["w1"], ["dx", "dw"]),
+    (["lw", "lb"], ["dx", "dx"]), (["w1", "w2"], ["dx", "dw", "dw"]), (["x", "b1", "b2"], ["dx", "dx"]),
+    (NAMES[1:], ["dx", "dx", "dw", "dw"]), (NAMES, ["dx", "dx", "dw", "dw"])])
+def test_block_forms_the_gradients_that_are_needed(passes, needed, products, copy8):
+    every, _ = block_gradients(NAMES, copy8)
+    del passes.made[:]
+    some, saved = block_gradients(needed, copy8)
+    assert sorted(some) == sorted(needed)
+    for name in needed:
+        torch.testing.assert_close(some[name], every[name])
+    assert sorted(m for m in passes.made if m in ("dx", "dw")) == sorted(products)
+    assert any(m.startswith("norm_bwd") for m in passes.made) == any(n in needed for n in NAMES[:3])
+    if needed == ["b2"]:
+        assert not saved and passes.made == ["norm", "linear", "linear", "act+db"]
