@@ -537,6 +537,8 @@ def feed_forward(x, ln_weight, ln_bias, w1, b1, w2, b2, act="gelu", eps=1e-5, co
     pass needs is kept in 8 bits."""
     if _act(act) == B.MFAC_ACT_NONE:
         raise ValueError("feed_forward: needs an activation")
+    if any(p is None for p in (ln_weight, ln_bias, w1, b1, w2, b2)):
+        raise ValueError("feed_forward: needs its six parameters")
     return _FeedForward.apply(x, ln_weight, ln_bias, w1, b1, w2, b2, act, eps, copy8, torch.is_grad_enabled())
 
 

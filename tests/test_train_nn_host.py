@@ -228,3 +228,13 @@ def test_block_forms_the_gradients_that_are_needed(passes, needed, products, cop
     assert any(m.startswith("norm_bwd") for m in passes.made) == any(n in needed for n in NAMES[:3])
     if needed == ["b2"]:
         assert not saved and passes.made == ["norm", "linear", "linear", "act+db"]
+
+
+def test_block_refuses_a_missing_parameter_in_training_and_inference(passes):
+    t = [torch.randn(5, 64), torch.ones(64), torch.zeros(64), torch.randn(32, 64), torch.zeros(32), torch.randn(64, 32),
+         torch.zeros(64)]
+    for grad in (True, False):
+        for i in range(1, 7):
+            with torch.set_grad_enabled(grad), pytest.raises(ValueError):
+                nn.feed_forward(*[v if j != i else None for j, v in enumerate(t)])
+    assert not passes.made
