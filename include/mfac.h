@@ -473,9 +473,8 @@ mfac_status mfac_layer_norm_bwd(mfac_dtype type, mfac_dtype wtype, int64_t rows,
  * Products: fp16 and bf16 values on the matrix cores with fp32 sums; fp32 values
  * as three bf16 parts each, of whose nine products the six largest are taken
  * (what is left out is at most 2^-26 of the product); what of a value lies
- * below 2^-133 is left out, and the parts of one above 3.39e38, or of an infinite
- * one, are not finite together: its products come out NaN. Up to 16 rows of
- * fp32 multiply in fp32. */
+ * below 2^-133 is left out, and an infinite one has no such parts: its products come
+ * out NaN. Up to 16 rows of a forward pass in fp32 multiply in fp32. */
 size_t mfac_linear_workspace_bytes(mfac_dtype type, int64_t rows, int64_t cin, int64_t cout, const void* x,
                                    int64_t ldx, const void* w, int64_t ldw);
 mfac_status mfac_linear(mfac_dtype type, mfac_dtype btype, mfac_act act, int64_t rows, int64_t cin, int64_t cout,

@@ -657,7 +657,10 @@ __global__ __launch_bounds__(256) void k_lay_out_split(const float* __restrict__
         bf16* d = dst + r * ld + c;
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
-            const b8 h = __builtin_convertvector(x, b8);
+            // the first part cut at bf16's largest value, to which the second adds the rest: rounded, a
+            // value past it would be infinite (infinities and NaN come through in the second part)
+            const f8 v = p ? x : __builtin_elementwise_min(__builtin_elementwise_max(x, f8(-0x1.fep127f)), f8(0x1.fep127f));
+            const b8 h = __builtin_convertvector(v, b8);
             *reinterpret_cast<b8*>(d + p * plane) = h;
             x -= __builtin_convertvector(h, f8);
         }

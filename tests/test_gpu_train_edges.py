@@ -170,3 +170,39 @@ def test_block_gradients_one_by_one_are_those_of_all(dev, dtype, copy8):
     for needed in [[i] for i in range(7)] + [[1, 2], [3, 5], [0, 4, 6]]:
         for i, g in gradients(needed).items():
             assert torch.equal(g, every[i]), (needed, i)
+
+
+def test_fp32_products_of_the_largest_values(dev):
+    """Finite fp32 values near the largest have finite products, whichever kernel forms them."""
+    from paper_2107_03356_amd import nn
+    say("largest fp32 values")
+    big = torch.finfo(F32).max
+    for rows in (5, 40):
+        x, w = rand(dev, 1, rows, 72).to(F32), (rand(dev, 2, 24, 72) * 2.0 ** -30).to(F32)
+        x[2, 7], x[3, 0], x[4, 71] = big, -big, 3.395e38
+        z64 = x.double() @ w.double().t()
+        bound = E32 * (growth(72) + 1) * (x.double().abs() @ w.double().abs().t())
+        holds(nn.linear_forward(x, w), z64, bound, "y")
+        # as the gradient that both products of the backward pass take
+        dx = nn.linear_backward_input(x, w.t().contiguous())
+        holds(dx, z64, bound, "dx")
+        t = rand(dev, 3, rows, 24).to(F32) * 2.0 ** -30
+        dw = nn.linear_backward_weight(x, t)
+        holds(dw, x.double().t() @ t.double(), E32 * (growth(rows) + 1) * (x.double().abs().t() @ t.double().abs()), "dw")
+
+
+def test_fp32_infinities_spoil_their_row_only(dev):
+    """An infinite fp32 value: what the definition gives up to 16 rows; from three bf16 parts its products are not
+    finite. Other rows stay as they are."""
+    from paper_2107_03356_amd import nn
+    say("fp32 infinities")
+    w = rand(dev, 2, 24, 72).to(F32)
+    for rows in (16, 17):
+        x = rand(dev, 1, rows, 72).to(F32)
+        clean = nn.linear_forward(x, w)
+        x[2, 7] = float("inf")
+        y = nn.linear_forward(x, w)
+        assert torch.equal(y[:2], clean[:2]) and torch.equal(y[3:], clean[3:])
+        assert not torch.isfinite(y[2]).any()
+        if rows <= 16:
+            assert torch.equal(y[2].double(), (x.double() @ w.double().t())[2])
