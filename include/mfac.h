@@ -256,7 +256,7 @@ mfac_status mfac_static_precompute(mfac_static* out, int64_t d, int32_t block, i
  * Gram matrices, their Cholesky factors and inverses, and W in fp32 (values
  * and sums; a product of two values, in the large matrix products, as the six
  * largest of the nine products of their three bf16 parts, which leaves out at
- * most 2^-26 of it). A Gram entry is summed over at most 2048 columns,
+ * most 2^-24 (1 + 2^-10) of it). A Gram entry is summed over at most 2048 columns,
  * wider blocks adding their 2048-column splits in fp64, W over the m rows,
  * the squares of W in fp64 for the diagonal. The inverse diagonal then
  * carries the fp32 rounding (on gradient-like data with a well-conditioned
@@ -472,7 +472,7 @@ mfac_status mfac_layer_norm_bwd(mfac_dtype type, mfac_dtype wtype, int64_t rows,
  * the backward pass; at most one of the two, both optional. y may be res.
  * Products: fp16 and bf16 values on the matrix cores with fp32 sums; fp32 values
  * as three bf16 parts each, of whose nine products the six largest are taken
- * (what is left out is at most 2^-26 of the product); what of a value lies
+ * (what is left out is at most 2^-24 (1 + 2^-10) of the product); what of a value lies
  * below 2^-133 is left out, and an infinite one has no such parts: its products come
  * out NaN. Up to 16 rows of a forward pass in fp32 multiply in fp32. */
 size_t mfac_linear_workspace_bytes(mfac_dtype type, int64_t rows, int64_t cin, int64_t cout, const void* x,

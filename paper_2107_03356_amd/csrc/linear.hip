@@ -11,8 +11,9 @@
 //   k_finish   joins the K parts of a product that was split over work-groups.
 // Operands that the copies into LDS cannot take as they are (rows that do not start
 // 16-byte aligned, 8-bit copies, fp32) are laid out first in the workspace: fp32 as
-// three bf16 planes, hi + mid + lo, of whose nine products six are summed (the
-// others are at most 2^-26 of |a b| together).
+// three bf16 planes, hi + mid + lo, of whose nine products six are summed (|mid| is at most
+// 2^-8 and |lo| 2^-17 of the value's power of two, so the others are at most
+// 2^-24 (1 + 2^-10) of |a b| together: one fp32 rounding).
 #include <algorithm>
 #include <utility>
 

@@ -5,8 +5,9 @@
 // 2^-110 up to the largest bf16, 3.39e38. (Below, lo and mid are subnormal and lose
 // what lies under 2^-133; above, hi is infinite and the product NaN, where the
 // value's square is no fp32 value either.) A product a b is then the sum of nine
-// bf16 products, each exact in fp32. Six are formed: the others (mid lo, lo mid, lo
-// lo) are together at most 2^-26 of |a b|, a quarter of one fp32 rounding. Six
+// bf16 products, each exact in fp32. Six are formed: with |mid| at most 2^-8 and |lo| at
+// most 2^-17 of the value's power of two, the others (mid lo, lo mid, lo lo) are
+// together at most 2^-24 (1 + 2^-10) of |a b|, one fp32 rounding. Six
 // v_mfma_f32_32x32x16_bf16 take 6/16 of the time of the fp32 MFMAs for the same
 // product. Their sum over 16 k reaches the accumulator in one fp32 addition. Against
 // 64 bits the entries of G G^T are off by 2.0e-8 to 2.3e-8 (rms, of sqrt(K_ii K_jj), B

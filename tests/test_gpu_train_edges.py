@@ -206,3 +206,14 @@ def test_fp32_infinities_spoil_their_row_only(dev):
         assert not torch.isfinite(y[2]).any()
         if rows <= 16:
             assert torch.equal(y[2].double(), (x.double() @ w.double().t())[2])
+
+
+def test_fp32_products_of_single_values(dev):
+    """One product a sum: off by what the three left out come to, 2^-24 (1 + 2^-10) of it, and by the additions' cuts, a
+    unit of 2^-23 for the last and 2^-8 of one for those before."""
+    from paper_2107_03356_amd import nn
+    say("single products")
+    x = 1 + torch.rand(600, 1, generator=torch.Generator().manual_seed(1)).to(dev)
+    x[0] = 1.0038986
+    want = x.double() @ x.double().t()
+    holds(nn.linear_forward(x, x), want, E32 * (1 + 2.0 ** -10 + 2 * (1 + 5 * 2.0 ** -8)) * want, "y")
