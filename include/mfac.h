@@ -516,6 +516,20 @@ mfac_status mfac_linear_bwd_weight(mfac_dtype type, mfac_dtype gtype, int64_t ro
                                    const float* db, void* dw, int64_t lddw, void* workspace, size_t workspace_bytes,
                                    hipStream_t stream);
 
+/* How a product of these passes is run, for tuning and tests. plan[0]: the side of its square tiles of the result (0:
+ * the kernel for few rows); plan[1]: the parts that its sums are cut into; plan[2]: 1 where results are stored past the
+ * caches. otype is the result's type (gtype for the weight's gradient, `type` otherwise); packed: x is an 8-bit copy
+ * (weight only). rows is at least 1. */
+typedef enum {
+    MFAC_PRODUCT_FORWARD = 0,
+    MFAC_PRODUCT_INPUT = 1,
+    MFAC_PRODUCT_WEIGHT = 2,
+    MFAC_PRODUCT_NONE_ = -1, /* not products: as above */
+    MFAC_PRODUCT_INT32_ = 0x7fffffff
+} mfac_product;
+mfac_status mfac_linear_plan(mfac_dtype type, mfac_dtype otype, mfac_product product, int64_t rows, int64_t cin,
+                             int64_t cout, int32_t packed, int32_t plan[3]);
+
 #ifdef __cplusplus
 }
 #endif

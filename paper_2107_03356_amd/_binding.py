@@ -26,6 +26,7 @@ MFAC_EPRECISION = -6
 MFAC_STATIC_TRACE = 1
 MFAC_STATIC_FP32 = 2
 MFAC_F32, MFAC_BF16, MFAC_F16 = 0, 1, 2
+MFAC_PRODUCT_FORWARD, MFAC_PRODUCT_INPUT, MFAC_PRODUCT_WEIGHT = range(3)
 MFAC_ACT_NONE, MFAC_ACT_RELU, MFAC_ACT_GELU, MFAC_ACT_GELU_TANH, MFAC_ACT_SILU = range(5)
 
 _c = ctypes
@@ -89,6 +90,7 @@ SIGNATURES = {
     "mfac_linear_bwd_weight_workspace_bytes": (_SZ, [_I32, _I64, _I64, _I64, _VP, _I64, _VP, _I64]),
     "mfac_linear_bwd_weight": (_c.c_int, [_I32, _I32, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _VP,
                                           _VP, _VP, _I64, _VP, _SZ, _VP]),
+    "mfac_linear_plan": (_c.c_int, [_I32, _I32, _I32, _I64, _I64, _I64, _I32, _VP]),
 }
 
 _lib = None

@@ -17,6 +17,7 @@
 #include <algorithm>
 #include <utility>
 
+#include "../../include/mfac.h"
 #include "internal.h"
 #include "train.h"
 #include "train_util.h"
@@ -760,16 +761,21 @@ hipError_t lay_out(int dt, const Operand& o, const void* src, int64_t ld, Packed
     return hipGetLastError();
 }
 
+// Whether a product's results are stored past the caches: in tiles of 256, where they and the operands exceed them.
+bool streams(const Product& p, const Plan& q, int out_dt) {
+    const int64_t bytes = (p.M * p.K + p.N * p.K) * 2 * (q.nseg > 1 ? 3 : 1) + p.M * p.N * dtype_bytes(out_dt);
+    return q.tile == 256 && bytes > LAST_LEVEL_CACHE;
+}
+
 template <typename T, bool ACOL, bool BCOL>
 hipError_t run_product(const Product& p, const Plan& q, const GemmArgs& g, hipStream_t st) {
     const unsigned grid = (unsigned)(q.tiles_m * q.tiles_n * q.splits);
-    const int64_t bytes = (p.M * p.K + p.N * p.K) * 2 * (q.nseg > 1 ? 3 : 1) + p.M * p.N * dtype_bytes(g.e.out_dt);
     // 64 x 64 tiles stage three steps: 512 x 1024 over K = 4096, 128 work-groups, takes 22 us with
     // three or four and 35 with two; 128 x 128 with three leave a CU one work-group, 31 us for
     // 2048^3 against 27
     if (q.tile == 64) k_product<T, ACOL, BCOL, 64, 64, 2, 2, 3, false><<<grid, 256, 0, st>>>(g);
     else if (q.tile == 128) k_product<T, ACOL, BCOL, 128, 128, 2, 2, 2, false><<<grid, 256, 0, st>>>(g);
-    else if (bytes <= LAST_LEVEL_CACHE) k_product<T, ACOL, BCOL, 256, 256, 2, 4, 2, false><<<grid, 512, 0, st>>>(g);
+    else if (!streams(p, q, g.e.out_dt)) k_product<T, ACOL, BCOL, 256, 256, 2, 4, 2, false><<<grid, 512, 0, st>>>(g);
     else k_product<T, ACOL, BCOL, 256, 256, 2, 4, 2, true><<<grid, 512, 0, st>>>(g);
     return hipGetLastError();
 }
@@ -862,3 +868,28 @@ hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws,
 }
 
 }  // namespace mfac
+
+extern "C" __attribute__((visibility("default"))) mfac_status mfac_linear_plan(mfac_dtype type, mfac_dtype otype,
+                                                                               mfac_product product, int64_t rows,
+                                                                               int64_t cin, int64_t cout,
+                                                                               int32_t packed, int32_t plan[3]) {
+    using namespace mfac;
+    constexpr int64_t most = int64_t(1) << 21;
+    if (type < MFAC_F32 || type > MFAC_F16 || (otype != MFAC_F32 && otype != type) || product < MFAC_PRODUCT_FORWARD ||
+        product > MFAC_PRODUCT_WEIGHT || rows < 1 || rows > (int64_t(1) << 30) || cin < 1 || cin > most || cout < 1 ||
+        cout > most || (packed && product != MFAC_PRODUCT_WEIGHT) || !plan)
+        return MFAC_EINVAL;
+    Product p{};   // the plan is one of sizes and types; addresses only decide what is laid out first
+    p.M = product == MFAC_PRODUCT_WEIGHT ? cout : rows;
+    p.N = product == MFAC_PRODUCT_FORWARD ? cout : cin;
+    p.K = product == MFAC_PRODUCT_FORWARD ? cin : product == MFAC_PRODUCT_INPUT ? cout : rows;
+    p.a_col = product == MFAC_PRODUCT_WEIGHT;
+    p.b_col = product != MFAC_PRODUCT_FORWARD;
+    int8_t some;
+    if (packed) p.bp.q = &some;
+    const Plan q = plan_of(type, p);
+    plan[0] = q.tile;
+    plan[1] = q.splits;
+    plan[2] = q.splits == 1 && streams(p, q, otype);   // parts are joined by plain stores
+    return MFAC_OK;
+}

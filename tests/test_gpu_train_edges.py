@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from gpu_common import require_gpu, say
+from train_cases import PRODUCTS, layer, runs
 from train_ref import E32, TINY, U, act64, act_error, growth, off, pack64, unpack64  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -217,3 +218,91 @@ def test_fp32_products_of_single_values(dev):
     x[0] = 1.0038986
     want = x.double() @ x.double().t()
     holds(nn.linear_forward(x, x), want, E32 * (1 + 2.0 ** -10 + 2 * (1 + 5 * 2.0 ** -8)) * want, "y")
+
+
+# ---------------------------------------------------------------- every kernel of the large products, with every epilogue
+TYPE = {"f32": F32, "bf16": BF16, "f16": F16}
+KERNELS = [(t, size, want) for size, want, types in PRODUCTS for t in types]
+
+
+def matrix(dev, seed, dtype, *shape, scale=1.0):
+    g = torch.Generator(device=dev).manual_seed(seed)
+    return (torch.randn(*shape, generator=g, device=dev) * scale).to(dtype)
+
+
+@pytest.mark.parametrize("t,size,want", KERNELS)
+def test_forward_product_of_each_kernel(dev, t, size, want):
+    from paper_2107_03356_amd import _binding as B
+    from paper_2107_03356_amd import nn
+    say("forward product", t, size, want)
+    dtype = TYPE[t]
+    rows, cin, cout = layer(B.MFAC_PRODUCT_FORWARD, *size)
+    assert runs(t, t, B.MFAC_PRODUCT_FORWARD, size, want)
+    x, w = matrix(dev, 1, dtype, rows, cin), matrix(dev, 2, dtype, cout, cin, scale=cin ** -0.5)
+    b, res = matrix(dev, 3, F32, cout, scale=0.5), matrix(dev, 4, dtype, rows, cout)
+    z64 = x.double() @ w.double().t() + b.double()
+    ze = E32 * (growth(cin) * (x.double().abs() @ w.double().abs().t()) + 2 * b.double().abs())
+    tiny = TINY[dtype]
+    for act in ("none", "relu", "gelu", "gelu_tanh", "silu"):
+        a64, _ = act64(act, z64)
+        err = 1.2 * ze + (act_error(z64) if act != "none" else 0)
+        holds(nn.linear_forward(x, w, b, act), a64, U[dtype] * a64.abs() + err + tiny, act)
+    a64 += res.double()
+    bound = U[dtype] * a64.abs() + err + E32 * a64.abs() + tiny
+    y = nn.linear_forward(x, w, b, act, residual=res)
+    holds(y, a64, bound, "y + res")
+    yz, z = nn.linear_forward(x, w, b, act, residual=res, keep="z")
+    assert torch.equal(yz, y)
+    holds(z, z64, U[dtype] * z64.abs() + ze + tiny, "z")
+    y8, p = nn.linear_forward(x, w, b, act, residual=res, keep="pack8")
+    assert torch.equal(y8, y)
+    step = torch.exp2(p.s.double() - 127)
+    holds(nn.unpack8(p), z64, step.repeat_interleave(32, 1)[:, :cout] / 2 + ze, "copy of z")
+    most = torch.nn.functional.pad(z64.abs() + ze, (0, -cout % 32)).view(rows, -1, 32).amax(2)
+    assert (step <= torch.clamp(2 * most / 127, min=2.0 ** -126)).all()
+    z64 -= b.double()
+    holds(nn.linear_forward(x, w), z64, U[dtype] * z64.abs() + ze + tiny, "no bias")
+
+
+@pytest.mark.parametrize("t,size,want", KERNELS)
+def test_input_product_of_each_kernel(dev, t, size, want):
+    from paper_2107_03356_amd import _binding as B
+    from paper_2107_03356_amd import nn
+    say("input product", t, size, want)
+    dtype = TYPE[t]
+    rows, cin, cout = layer(B.MFAC_PRODUCT_INPUT, *size)
+    assert runs(t, t, B.MFAC_PRODUCT_INPUT, size, want)
+    dz, w = matrix(dev, 5, dtype, rows, cout), matrix(dev, 6, dtype, cout, cin, scale=cout ** -0.5)
+    add = matrix(dev, 7, dtype, rows, cin)
+    want64 = dz.double() @ w.double()
+    err = E32 * growth(cout) * (dz.double().abs() @ w.double().abs()) + TINY[dtype]
+    holds(nn.linear_backward_input(dz, w), want64, U[dtype] * want64.abs() + err, "dx")
+    want64 += add.double()
+    holds(nn.linear_backward_input(dz, w, add=add), want64, (U[dtype] + E32) * want64.abs() + err, "dx + add")
+
+
+@pytest.mark.parametrize("t,size,want", KERNELS)
+def test_weight_product_of_each_kernel(dev, t, size, want):
+    from paper_2107_03356_amd import _binding as B
+    from paper_2107_03356_amd import nn
+    say("weight product", t, size, want)
+    dtype = TYPE[t]
+    rows, cin, cout = layer(B.MFAC_PRODUCT_WEIGHT, *size)
+    dz, x = matrix(dev, 8, dtype, rows, cout), matrix(dev, 9, dtype, rows, cin)
+    gamma, beta = 1 + matrix(dev, 10, F32, cin, scale=0.2), matrix(dev, 11, F32, cin, scale=0.3)
+    d, dm = dz.double(), dz.double().abs()
+    want64 = d.t() @ x.double()
+    err = E32 * growth(rows) * (dm.t() @ x.double().abs())
+    gtypes = [("f32", F32)] + ([(t, dtype)] if t != "f32" else [])
+    for g, gtype in gtypes:
+        assert runs(t, g, B.MFAC_PRODUCT_WEIGHT, size, want)
+        holds(nn.linear_backward_weight(dz, x, grad_dtype=gtype), want64, U[gtype] * want64.abs() + err + TINY[gtype], "dw")
+    p = nn.pack8(x)
+    xq = unpack64(p.q, p.s)
+    _, _, db = nn.act_backward(dz)
+    want64 = d.t() @ (xq * gamma.double() + beta.double())
+    # products, the affine part's three roundings, and db's own sum
+    err = E32 * 2 * growth(rows) * (dm.t() @ (xq.abs() * gamma.double().abs() + beta.double().abs()))
+    for g, gtype in gtypes:
+        got = nn.linear_backward_weight(dz, p, (gamma, beta), db, gtype)
+        holds(got, want64, U[gtype] * want64.abs() + err + TINY[gtype], "dw from the copy")
