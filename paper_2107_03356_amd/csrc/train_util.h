@@ -187,15 +187,20 @@ __device__ __forceinline__ void pack_group(int8_t* __restrict__ qrow, uint8_t* _
 // saturate to 0 and infinity as the formulas want.
 __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 
-// 1 - erf(y) for y >= 0 as poly(t) exp(-y^2), t = 1 / (1 + p y): Abramowitz and
-// Stegun, Handbook of Mathematical Functions, 7.1.26 (absolute error 1.5e-7);
+// 1 - erf(y) for y >= 0 as t poly(t) exp(-y^2), t = 1 / (1 + 0.3 y): poly of degree 8 fitted to the
+// least largest relative error of exp(y^2) (1 - erf(y)) over y <= 10.6, past which exp(-y^2) is 0. 2.0e-8 of the
+// value, 4.4e-7 with the roundings, so the normal distribution function keeps its digits in the negative tail;
 // ex = exp(-y^2) is passed in, since the slope of z Phi(z) needs it too.
 __device__ __forceinline__ float erfc_pos(float y, float ex) {
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, y, 1.f));
-    float p = fmaf(1.061405429f, t, -1.453152027f);
-    p = fmaf(p, t, 1.421413741f);
-    p = fmaf(p, t, -0.284496736f);
-    p = fmaf(p, t, 0.254829592f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3f, y, 1.f));
+    float p = fmaf(-0.129555672f, t, 0.485735327f);
+    p = fmaf(p, t, -0.51266557f);
+    p = fmaf(p, t, 0.5482077f);
+    p = fmaf(p, t, -0.0950254649f);
+    p = fmaf(p, t, 0.215105802f);
+    p = fmaf(p, t, 0.1482867f);
+    p = fmaf(p, t, 0.170723736f);
+    p = fmaf(p, t, 0.169187412f);
     return p * t * ex;
 }
 

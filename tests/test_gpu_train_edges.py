@@ -306,3 +306,22 @@ def test_weight_product_of_each_kernel(dev, t, size, want):
     for g, gtype in gtypes:
         got = nn.linear_backward_weight(dz, p, (gamma, beta), db, gtype)
         holds(got, want64, U[gtype] * want64.abs() + err + TINY[gtype], "dw from the copy")
+
+
+def test_gelu_keeps_its_digits_in_the_tail(dev):
+    """z Phi(z) for negative z is a product of small numbers: its error is relative to itself. By z^2 / 2 of the
+    exponential's argument, which has three roundings (1.5 z^2 units of 2^-24, 2 taken), and about ten roundings of the
+    rest, which the polynomial's terms of both signs and the reciprocal's slope raise to 40."""
+    from paper_2107_03356_amd import nn
+    say("gelu tail")
+    z = torch.linspace(-9, 9, 4001, dtype=F32, device=dev)
+    a64, s64 = act64("gelu", z.double())
+    unit = E32 * (40 + 2 * z.double().square())
+    for rows in (1, 40):
+        y = nn.linear_forward(torch.zeros(rows, 64, device=dev), rand(dev, 1, 4001, 64).to(F32), z, "gelu")
+        holds(y, a64.expand(rows, -1), (unit * a64.abs() + TINY[F32]).expand(rows, -1), "act")
+    dz, a, _ = nn.act_backward(torch.ones(1, 4001, device=dev), z[None], "gelu", want_a=True)
+    holds(a[0], a64, unit * a64.abs() + TINY[F32], "a")
+    zd = z.double()
+    density = zd.abs() * torch.exp(-zd * zd / 2) / (2 * torch.pi) ** 0.5
+    holds(dz[0], s64, unit * (density + (s64 - zd.sign() * density).abs()) + TINY[F32], "slope")
