@@ -6,8 +6,9 @@
 // A lane holds eight neighbouring columns, so four lanes hold a group and find its
 // largest magnitude with two exchanges. Rows narrower than a wave's 512 columns
 // share it: LPR lanes to a row, the power of two from 4 to 64 that covers
-// the row. All of it is elementwise and bound by HBM: bf16 8192 x 8192 into the copy 36 us
-// (5.6 TB/s), back 36, dz and db from an 8-bit z 69 (4.9).
+// the row. All of it is elementwise and bound by HBM: bf16 8192 x 8192 into the copy 36 us launch
+// after launch (5.6 TB/s) and 41 after a pass that leaves its output in the caches (4.9), back 35
+// and 32, dz and db from an 8-bit z 66 with gelu_tanh (5.1) and 78 with gelu, whose arithmetic it waits for.
 #include <algorithm>
 
 #include "internal.h"

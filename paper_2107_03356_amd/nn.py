@@ -18,7 +18,9 @@ Data is float32, bfloat16 or float16 on one CUDA device; leading dimensions are
 rows, the last one needs unit stride (others are copied first). Layer norm's
 parameters and biases are float32 or of the data's type. In the autograd
 functions a float32 weight may come with 16-bit data: it is rounded for the
-products, and its gradient comes back in float32. Calls run on the current
+products at every call, and its gradient comes back in float32 (a weight that is
+used again and again without training is better handed over in 16 bits). Where
+gradients are off, or no input needs one, nothing is kept. Calls run on the current
 stream of the data's device, with workspaces from torch's allocator.
 """
 
@@ -254,6 +256,7 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, add=None, params=True):
     dw = db = None
     ws = (None, 0, None)
     if params:
+        # one allocation for both, whose storage they share
         grads = torch.empty((2, cols), dtype=torch.float32 if w is None else w.dtype, device=dy.device)
         dw, db = grads.unbind(0)
         ws = _workspace(_function("mfac_layer_norm_bwd_workspace_bytes")(rows, cols), dy.device)
