@@ -530,6 +530,104 @@ typedef enum {
 mfac_status mfac_linear_plan(mfac_dtype type, mfac_dtype otype, mfac_product product, int64_t rows, int64_t cin,
                              int64_t cout, int32_t packed, int32_t plan[3]);
 
+/* ----------------------------------------------------------------------
+ * A gated block: gated layers, what lies between two blocks, dropout
+ * ----------------------------------------------------------------------
+ * By the same rules as the calls above. */
+
+/* Gated layer: z = x W^T + b for W of 2 hidden rows (those of the gate, then those
+ * of the other projection; bias likewise), y = act(zg) zu, for x (rows x cin), W
+ * (2 hidden x cin), y (rows x hidden); hidden at most 2^20. Both projections, the
+ * activation and the product are one kernel. bias (2 hidden values of btype) may be NULL. The
+ * pre-activations zg and zu (rows x hidden each) may be kept for the backward
+ * pass, as matrices of `type` with the same ldz (they may be the halves of one), or as
+ * 8-bit copies (qg, sg) and (qu, su) with the same ldq; both or neither of the two. */
+size_t mfac_gated_linear_workspace_bytes(mfac_dtype type, int64_t rows, int64_t cin, int64_t hidden, const void* x,
+                                         int64_t ldx, const void* w, int64_t ldw);
+mfac_status mfac_gated_linear(mfac_dtype type, mfac_dtype btype, mfac_act act, int64_t rows, int64_t cin, int64_t hidden,
+                              const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, void* y,
+                              int64_t ldy, void* zg, void* zu, int64_t ldz, int8_t* qg, uint8_t* sg, int8_t* qu,
+                              uint8_t* su, int64_t ldq, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* The gate's part of its backward pass, from da, the gradient of y, and the
+ * pre-activations (matrices or copies):
+ *   dz = [da zu act'(zg), da act(zg)] (rows x 2 hidden) rounded to type,
+ *   a = act(zg) zu (NULL: not wanted),
+ *   db = the 2 hidden column sums of dz in fp32, before the rounding (NULL: not wanted).
+ * The gradients of x and W are those of a linear layer with cout = 2 hidden. */
+size_t mfac_gated_act_bwd_workspace_bytes(int64_t rows, int64_t hidden);
+mfac_status mfac_gated_act_bwd(mfac_dtype type, mfac_act act, int64_t rows, int64_t hidden, const void* da, int64_t ldda,
+                               const void* zg, const void* zu, int64_t ldz, const int8_t* qg, const uint8_t* sg,
+                               const int8_t* qu, const uint8_t* su, int64_t ldq, void* dz, int64_t lddz, void* a,
+                               int64_t lda, float* db, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* The same behind the layer that follows, a W2^T with W2 (cout x hidden): from dy (rows
+ * x cout), the gradient of that layer's output, da = dy W2 is formed and used in one kernel
+ * and not rounded or stored. */
+size_t mfac_gated_hidden_bwd_workspace_bytes(mfac_dtype type, int64_t rows, int64_t hidden, int64_t cout, const void* dy,
+                                             int64_t lddy, const void* w, int64_t ldw);
+mfac_status mfac_gated_hidden_bwd(mfac_dtype type, mfac_act act, int64_t rows, int64_t hidden, int64_t cout,
+                                  const void* dy, int64_t lddy, const void* w, int64_t ldw, const void* zg,
+                                  const void* zu, int64_t ldz, const int8_t* qg, const uint8_t* sg, const int8_t* qu,
+                                  const uint8_t* su, int64_t ldq, void* dz, int64_t lddz, void* a, int64_t lda,
+                                  void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Dropout. at: two int64 in device memory, seed and offset, 8-byte aligned, read when the kernel runs (so a captured graph
+ * takes what they hold when it is replayed). Element (row, c) of a matrix takes half-word c % 8 of the
+ * Philox 4x32-10 block with counter (c / 8, row, offset mod 2^32, offset / 2^32) and key (seed mod 2^32, seed /
+ * 2^32), both taken as unsigned; half-word i is the lower (i even) or upper half of word i / 2. It is kept
+ * where the half-word is at least T = floor(65536 p + 1/2), and multiplied by 65536 / (65536 - T);
+ * others become 0, infinities and NaN among them. 0 <= p <= 1; with T = 0 every value is kept, with
+ * T = 65536 none. The mask depends on p, at and the place in the matrix alone, not on the type or strides: the
+ * gradient is the same call on dy. y may be x. */
+mfac_status mfac_dropout(mfac_dtype type, int64_t rows, int64_t cols, const void* x, int64_t ldx, double p,
+                         const int64_t* at, void* y, int64_t ldy, hipStream_t stream);
+
+/* What lies between two blocks of a network with a residual stream, row by row:
+ *   n = N_post(y), s = scale res + gate drop(n), h = N_pre(s).
+ * N is rms norm, x rstd w with rstd = 1 / sqrt(mean(x^2) + eps), or with
+ * MFAC_NORM_LAYER layer norm as above, both of one kind; either may be absent (n = y;
+ * no h). post_w, post_b, pre_w, pre_b (cols values of wtype) may be NULL (1 and 0); rms
+ * norm has no b. The gate is one value for each channel (`gate`, cols values of wtype), one for each
+ * element (`gates`, of `type`), or absent (1). drop is dropout with p and at (at may be NULL where T is 0). res and s
+ * may be NULL (no residual; not wanted, where h is). h is formed from s before its rounding. Statistics
+ * (rows fp32 values each) may be NULL; means are layer norm's. q and sq: the 8-bit copy of N_pre's xhat, or both
+ * NULL. cols at most 2^15. eps >= 0 and scale finite. s may be y or res, and h may be y or res, but not s. With
+ * MFAC_NORM_PRE alone and no residual, gate or dropout the call is h = N(y). */
+typedef enum {
+    MFAC_NORM_POST = 1,
+    MFAC_NORM_PRE = 2,
+    MFAC_NORM_LAYER = 4
+} mfac_norms;
+mfac_status mfac_residual_norm(mfac_dtype type, mfac_dtype wtype, int32_t norms, int64_t rows, int64_t cols,
+                               const void* y, int64_t ldy, const void* post_w, const void* post_b, const void* gate,
+                               const void* gates, int64_t ldgates, const void* res, int64_t ldres, double scale, double p,
+                               const int64_t* at, const void* pre_w, const void* pre_b, double eps, void* s, int64_t lds,
+                               void* h, int64_t ldh, float* post_mean, float* post_rstd, float* pre_mean,
+                               float* pre_rstd, int8_t* q, int64_t ldq, uint8_t* sq, hipStream_t stream);
+
+/* Its gradients. ds is the gradient that reaches s from elsewhere (NULL: none; needed without MFAC_NORM_PRE), dh that of
+ * h. With d = ds + the gradient of N_pre at dh,
+ *   dres = scale d, dn = gate drop(d), dgate(s) = d drop(n), dy = the gradient of N_post at dn;
+ * outputs may be NULL (not wanted); those of parameters (wtype) are sums over the rows. s, or the 8-bit copy of N_pre's xhat (then s
+ * and pre_mean are NULL); y may be NULL where neither MFAC_NORM_POST nor a gate's gradient needs it. dy and dres may be
+ * ds or dh, dy may be y. The workspace is needed for parameters' gradients. */
+size_t mfac_residual_norm_bwd_workspace_bytes(int32_t norms, int64_t rows, int64_t cols);
+mfac_status mfac_residual_norm_bwd(mfac_dtype type, mfac_dtype wtype, int32_t norms, int64_t rows, int64_t cols,
+                                   const void* ds, int64_t ldds, const void* dh, int64_t lddh, const void* y,
+                                   int64_t ldy, const float* post_mean, const float* post_rstd, const void* s,
+                                   int64_t lds, const int8_t* q, int64_t ldq, const uint8_t* sq, const float* pre_mean,
+                                   const float* pre_rstd, const void* post_w, const void* post_b, const void* gate,
+                                   const void* gates, int64_t ldgates, double scale, double p, const int64_t* at,
+                                   const void* pre_w, void* dy, int64_t lddy, void* dres, int64_t lddres, void* dgates,
+                                   int64_t lddgates, void* dpost_w, void* dpost_b, void* dgate, void* dpre_w,
+                                   void* dpre_b, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* How the products of a gated layer are run, as mfac_linear_plan: the layer itself, or with `hidden_bwd` != 0 the product of
+ * mfac_gated_hidden_bwd (cin is then its cout). */
+mfac_status mfac_gated_plan(mfac_dtype type, int32_t hidden_bwd, int64_t rows, int64_t cin, int64_t hidden,
+                            int32_t plan[3]);
+
 #ifdef __cplusplus
 }
 #endif

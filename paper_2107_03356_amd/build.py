@@ -17,7 +17,9 @@ LIB = os.path.join(HERE, "libmfac.so")
 ARCH = os.environ.get("MFAC_OFFLOAD_ARCH", "gfx950")
 
 SOURCES = ["pass.hip", "gram.hip", "chol.hip", "factor.hip", "static.hip", "static_query.hip", "capi.hip",
-           "norm.hip", "pack8.hip", "linear.hip", "train_capi.hip"]
+           "norm.hip", "pack8.hip", "linear.hip", "train_capi.hip",
+           "product_hidden.hip", "product_layer.hip", "product_gated.hip", "gated.hip", "dropout.hip", "residual_f32.hip",
+           "residual_bf16.hip", "residual_f16.hip", "residual.hip", "gated_capi.hip"]
 
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

@@ -1,0 +1,177 @@
+// What lies between two blocks of a network with a residual stream, in one pass over its rows:
+//
+//   n = N_post(y)              norm after a block (or n = y)
+//   s = scale r + gate drop(n) the stream; gate: a value for each channel or for each element, or 1
+//   h = N_pre(s)               norm before the next block
+//
+// N is rms norm, x / sqrt(mean(x^2) + eps) w, or layer norm, (x - mean) / sqrt(mean((x - mean)^2) + eps) w + b.
+//
+// A row lives in the registers of NT threads, eight neighbouring values each, so every input is read once and s is not
+// read again for h, which is formed from s before its rounding. A gate for each channel is folded into N_post's weight
+// and bias: gate drop(xhat w + b) = drop(xhat (gate w) + gate b).
+#pragma once
+
+#include "residual.h"
+
+namespace mfac {
+namespace {
+
+// The row's mean (0 for rms norm) and 1 / sqrt(variance + eps) of values v, which become xhat; zeros past the end.
+template <int NT, bool LAYER>
+__device__ __forceinline__ void normalise(f8& v, const Residual& g, int64_t c, float* red, int& turn, float& mean,
+                                          float& rstd) {
+    mean = 0.f;
+    if constexpr (LAYER) {
+        mean = row_sum<NT>(sum8(v), red, turn) / (float)g.cols;   // by division: a row of equal values has that mean
+        v -= mean;
+        zero_past(v, c, g.cols);
+    }
+    rstd = 1.f / sqrtf(row_sum<NT>(sum8(v * v), red, turn) / (float)g.cols + g.eps);
+    v *= rstd;
+}
+
+template <typename T, int NT, int NORMS>
+__global__ __launch_bounds__(norm_block(NT)) void k_residual_fwd(Residual g, int wt) {
+    constexpr int RPB = norm_block(NT) / NT;
+    constexpr bool POST = NORMS & POST_NORM, PRE = NORMS & PRE_NORM, LAYER = NORMS & LAYER_NORM;
+    __shared__ float red[2 * (NT / 64)];
+    int turn = 0;
+    const int t = threadIdx.x % NT;
+    const int64_t c = t * 8;
+    const int64_t step = (int64_t)gridDim.x * RPB, ngroups = (g.cols + 31) / 32;
+    int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / NT;
+    // the next row is on its way while one is worked on
+    Raw8<T> y, r, gate;
+    auto load = [&](int64_t at) {
+        y.load((const T*)g.y + at * g.ldy, c, g.cols);
+        if (g.r) r.load((const T*)g.r + at * g.ldr, c, g.cols);
+        if (g.gates) gate.load((const T*)g.gates + at * g.ldgates, c, g.cols);
+    };
+    if (row < g.rows) load(row);
+    f8 w1 = load_param(POST ? g.w1 : nullptr, wt, c, g.cols, 1.f), b1 = fill8(0.f), w2 = b1, b2 = b1;
+    if constexpr (POST && LAYER) b1 = load_param(g.b1, wt, c, g.cols, 0.f);
+    if (g.gate) {
+        const f8 v = load8_dt(g.gate, wt, 0, c, g.cols);
+        w1 *= v;
+        b1 *= v;
+    }
+    if constexpr (PRE) w2 = load_param(g.w2, wt, c, g.cols, 1.f);
+    if constexpr (PRE && LAYER) b2 = load_param(g.b2, wt, c, g.cols, 0.f);
+    DropKey key{};
+    if (g.drop.threshold) key = drop_key(g.drop);
+    for (; row < g.rows; row += step) {
+        f8 v = y.get(), add = fill8(0.f), by = add;
+        if (g.r) add = g.scale * r.get();
+        if (g.gates) by = gate.get();
+        if (row + step < g.rows) load(row + step);
+        float mean1, rstd1, mean2, rstd2;
+        if constexpr (POST) normalise<NT, LAYER>(v, g, c, red, turn, mean1, rstd1);
+        v *= w1;
+        if constexpr (POST && LAYER) v += b1;
+        if (g.drop.threshold) v = drop8(g.drop, key, (unsigned)row, (unsigned)(c >> 3), v);
+        if (g.gates) v *= by;
+        if (g.r) v += add;
+        if (g.s) store8((T*)g.s + row * g.lds, c, g.cols, v);
+        if constexpr (PRE) {
+            normalise<NT, LAYER>(v, g, c, red, turn, mean2, rstd2);
+            if (g.p.q) pack_group(g.p.q + row * g.p.ldq, g.p.s + row * ngroups, c, g.cols, v);
+            v *= w2;
+            if constexpr (LAYER) v += b2;
+            store8((T*)g.h + row * g.ldh, c, g.cols, v);
+        }
+        if (t == 0) {
+            if (POST && g.mean1) g.mean1[row] = mean1;
+            if (POST && g.rstd1) g.rstd1[row] = rstd1;
+            if (PRE && g.mean2) g.mean2[row] = mean2;
+            if (PRE && g.rstd2) g.rstd2[row] = rstd2;
+        }
+    }
+}
+
+// Wider rows: a work-group of 1024 threads a row, held in LDS in fp32. A thread reads only what it wrote.
+template <typename T, int NORMS>
+__global__ __launch_bounds__(1024) void k_residual_fwd_wide(Residual g, int wt) {
+    constexpr int NT = 1024;
+    constexpr bool POST = NORMS & POST_NORM, PRE = NORMS & PRE_NORM, LAYER = NORMS & LAYER_NORM;
+    extern __shared__ __attribute__((aligned(32))) float held[];
+    __shared__ float red[2 * (NT / 64)];
+    int turn = 0;
+    const int64_t ngroups = (g.cols + 31) / 32, cols = g.cols, end = (cols + 31) & ~int64_t(31);   // whole groups of four lanes
+    DropKey key{};
+    if (g.drop.threshold) key = drop_key(g.drop);
+    auto each = [&](auto f) {
+        for (int64_t c = threadIdx.x * 8; c < end; c += NT * 8) f(c, *reinterpret_cast<f8*>(held + c));
+    };
+    auto statistics = [&](float& mean, float& rstd) {
+        mean = 0.f;
+        float sum = 0.f;
+        if constexpr (LAYER) {
+            each([&](int64_t, f8& v) { sum += sum8(v); });
+            mean = row_sum<NT>(sum, red, turn) / (float)cols;
+            sum = 0.f;
+        }
+        each([&](int64_t c, f8& v) {
+            if constexpr (LAYER) {
+                v -= mean;
+                zero_past(v, c, cols);
+            }
+            sum += sum8(v * v);
+        });
+        rstd = 1.f / sqrtf(row_sum<NT>(sum, red, turn) / (float)cols + g.eps);
+    };
+    for (int64_t row = blockIdx.x; row < g.rows; row += gridDim.x) {
+        float mean1, rstd1 = 1.f, mean2, rstd2;
+        each([&](int64_t c, f8& v) { v = load8((const T*)g.y + row * g.ldy, c, cols); });
+        if constexpr (POST) statistics(mean1, rstd1);
+        each([&](int64_t c, f8& held_v) {
+            f8 v = held_v * rstd1;
+            if constexpr (POST) v *= load_param(g.w1, wt, c, cols, 1.f);
+            if constexpr (POST && LAYER) v += load_param(g.b1, wt, c, cols, 0.f);
+            if (g.gate) v *= load8_dt(g.gate, wt, 0, c, cols);
+            if (g.drop.threshold) v = drop8(g.drop, key, (unsigned)row, (unsigned)(c >> 3), v);
+            if (g.gates) v *= load8((const T*)g.gates + row * g.ldgates, c, cols);
+            if (g.r) v += g.scale * load8((const T*)g.r + row * g.ldr, c, cols);
+            zero_past(v, c, cols);
+            if (g.s) store8((T*)g.s + row * g.lds, c, cols, v);
+            held_v = v;
+        });
+        if constexpr (PRE) {
+            statistics(mean2, rstd2);
+            each([&](int64_t c, f8& held_v) {
+                f8 v = held_v * rstd2;
+                if (g.p.q) pack_group(g.p.q + row * g.p.ldq, g.p.s + row * ngroups, c, cols, v);
+                v *= load_param(g.w2, wt, c, cols, 1.f);
+                if constexpr (LAYER) v += load_param(g.b2, wt, c, cols, 0.f);
+                store8((T*)g.h + row * g.ldh, c, cols, v);
+            });
+        }
+        if (threadIdx.x == 0) {
+            if (POST && g.mean1) g.mean1[row] = mean1;
+            if (POST && g.rstd1) g.rstd1[row] = rstd1;
+            if (PRE && g.mean2) g.mean2[row] = mean2;
+            if (PRE && g.rstd2) g.rstd2[row] = rstd2;
+        }
+    }
+}
+
+}  // namespace
+
+template <typename T>
+hipError_t residual_fwd(int wt, const Residual& g, hipStream_t st) {
+    by_norms(g.norms, [&](auto norms) {
+        constexpr int NORMS = decltype(norms)::value;
+        if (g.cols > HELD_COLS) {
+            const size_t lds = (size_t)round_up(g.cols, 32) * 4;
+            k_residual_fwd_wide<T, NORMS><<<(unsigned)std::min<int64_t>(g.rows, 1024), 1024, lds, st>>>(g, wt);
+            return;
+        }
+        by_threads(g.cols, [&](auto nt) {
+            constexpr int NT = decltype(nt)::value;
+            const unsigned grid = (unsigned)std::min(ceil_div(g.rows, norm_block(NT) / NT), int64_t(2048));
+            k_residual_fwd<T, NT, NORMS><<<grid, norm_block(NT), 0, st>>>(g, wt);
+        });
+    });
+    return hipGetLastError();
+}
+
+}  // namespace mfac

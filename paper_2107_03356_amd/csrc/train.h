@@ -1,5 +1,5 @@
-// Launchers of the training operators (norm.hip, pack8.hip, linear.hip), called
-// by train_capi.hip once the arguments have been checked.
+// Launchers of the training operators (norm.hip, pack8.hip, linear.hip; gated.hip, residual_fwd.hip, residual_bwd.hip,
+// dropout.hip), called by train_capi.hip and gated_capi.hip once the arguments have been checked.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -58,6 +58,18 @@ struct Epilogue {
     Packed p;            // the same as an 8-bit copy
     const float *gamma, *beta;  // over n: c gamma + db[m] beta
     const float* db;
+    // a gated layer (Product::gate): z and p are the gate's pre-activation, these the other one's, of the same strides
+    void* z2;
+    Packed p2;
+    void* a;             // act(z) z2, where HIDDEN forms it (null: not wanted)
+    int64_t lda;
+};
+
+// What a product's N columns are.
+enum : int {
+    GATE_NONE = 0,
+    GATE_FORWARD = 1,  // of a forward product: 2 hidden rows of W, the gate's and the other projection's; out is rows x hidden
+    GATE_HIDDEN = 2    // of an input product: hidden columns of da, whose epilogue writes dz (out, rows x 2 hidden)
 };
 
 // C (M x N) = A B^T summed over K; A is [m][k] (a_col false) or [k][m], B likewise over n.
@@ -70,8 +82,66 @@ struct Product {
     int64_t ldb;
     bool b_col;
     Packed bp;  // B as an 8-bit copy (B null)
+    int gate;   // GATE_*; N counts what the product has, 2 hidden or hidden
 };
 size_t product_workspace_bytes(int dt, const Product& p);
 hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws, hipStream_t st);
+
+// The gate's part of a backward pass. part: gated_bwd_parts(rows, hidden) * 2 * hidden floats (unused if db is null)
+int64_t gated_bwd_parts(int64_t rows, int64_t hidden);
+hipError_t launch_gated_act_bwd(int dt, int act, int64_t rows, int64_t hidden, const void* da, int64_t ldda,
+                                const void* zg, const void* zu, int64_t ldz, Packed pg, Packed pu, void* dz, int64_t lddz,
+                                void* a, int64_t lda, float* db, float* part, hipStream_t st);
+
+// Dropout's mask; threshold 0: none.
+struct Drop {
+    unsigned threshold;
+    float scale;
+    const int64_t* at;   // seed, offset
+};
+hipError_t launch_dropout(int dt, int64_t rows, int64_t cols, const void* x, int64_t ldx, Drop d, void* y, int64_t ldy,
+                          hipStream_t st);
+
+// n = N_post(y), s = scale r + gate drop(n), h = N_pre(s); see residual_fwd.hip. Pointers of what is absent or not
+// wanted are null.
+struct Residual {
+    int norms;           // MFAC_NORM_*
+    int64_t rows, cols;
+    const void* y;
+    int64_t ldy;
+    const void *w1, *b1, *w2, *b2, *gate;   // of the post norm, the pre norm; cols values each, of type wt
+    const void* gates;   // rows x cols, like y
+    int64_t ldgates;
+    const void* r;
+    int64_t ldr;
+    float scale, eps;
+    Drop drop;
+    void* s;
+    int64_t lds;
+    void* h;
+    int64_t ldh;
+    float *mean1, *rstd1, *mean2, *rstd2;
+    Packed p;            // the 8-bit copy of the pre norm's xhat
+};
+hipError_t launch_residual(int dt, int wt, const Residual& g, hipStream_t st);
+
+// Its gradients: of Residual the inputs (s an input too, or p), and
+struct ResidualBwd {
+    const void* ds;
+    int64_t ldds;
+    const void* dh;
+    int64_t lddh;
+    void* dy;
+    int64_t lddy;
+    void* dr;
+    int64_t lddr;
+    void* dgates;
+    int64_t lddgates;
+    void *dw1, *db1, *dw2, *db2, *dgate;   // of type wt
+    float* part;         // residual_bwd_parts(rows, cols) * residual_sums(norms) * cols (unused if these are null)
+};
+int64_t residual_bwd_parts(int64_t rows, int64_t cols);
+int residual_sums(int norms);
+hipError_t launch_residual_bwd(int dt, int wt, const Residual& g, const ResidualBwd& b, hipStream_t st);
 
 }  // namespace mfac

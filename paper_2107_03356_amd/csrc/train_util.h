@@ -8,6 +8,8 @@
 
 #include <type_traits>
 
+#include "train.h"
+
 namespace mfac {
 namespace {
 
@@ -71,6 +73,18 @@ __device__ __forceinline__ void store8(T* __restrict__ row, int64_t c, int64_t c
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (c + i < cols) row[c + i] = w[i];
+}
+
+// The same of a type that is known at run time (DT_*).
+__device__ __forceinline__ f8 load8_dt(const void* p, int dt, int64_t off, int64_t c, int64_t cols) {
+    if (dt == DT_F32) return load8((const float*)p + off, c, cols);
+    if (dt == DT_BF16) return load8((const bf16*)p + off, c, cols);
+    return load8((const f16*)p + off, c, cols);
+}
+__device__ __forceinline__ void store8_dt(void* p, int dt, int64_t off, int64_t c, int64_t cols, f8 v) {
+    if (dt == DT_F32) store8((float*)p + off, c, cols, v);
+    else if (dt == DT_BF16) store8((bf16*)p + off, c, cols, v);
+    else store8((f16*)p + off, c, cols, v);
 }
 
 // ---------------------------------------------------------------- 8-bit copies
@@ -290,6 +304,45 @@ __device__ __forceinline__ void with_act(int act, F f) {
         case 3: f(std::integral_constant<int, 3>()); break;
         case 4: f(std::integral_constant<int, 4>()); break;
         default: f(std::integral_constant<int, 0>()); break;
+    }
+}
+
+// The gate of a gated layer, backward: of N values g, u and da, dg = da u act'(g), du = da act(g), a = act(g) u, in the
+// places of da, u and g. As three formulas, as forward (the products' epilogue holds this code for each sixteen rows): of
+// act_slope's, relu and none as one, and gelu_tanh and silu as z / (1 + e), e = 2^(z (p + q z^2)), whose slope is
+// P + P (1 - P) z (r + s z^2), P = 1 / (1 + e).
+template <typename V, int N>
+__device__ __forceinline__ void gate_slopes(int act, V (&g)[N], V (&u)[N], V (&da)[N]) {
+    constexpr int W = sizeof(V) / 4;
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                float a;
+                const float slope = f(g[j][i], a), x = u[j][i], d = da[j][i];
+                da[j][i] = d * x * slope;
+                u[j][i] = d * a;
+                g[j][i] = a * x;
+            }
+    };
+    const ActForward f = act_forward(act);
+    if (f.formula == 1) {
+        const float r = act == 4 ? 1.f : 1.59576912160573072f, s = act == 4 ? 0.f : 0.21406444881780073f;
+        each([&](float z, float& a) {
+            const float z2 = fminf(z * z, 1e30f);
+            const float e = __builtin_amdgcn_exp2f(z * fmaf(f.q, z2, f.p));
+            const float p = __builtin_amdgcn_rcpf(1.f + e);
+            a = z * p;
+            return fmaf(p * (fminf(e, __FLT_MAX__) * p) * z, fmaf(s, z2, r), p);
+        });
+    } else if (f.formula == 2) {
+        each([&](float z, float& a) { return act_slope<2>(z, &a); });
+    } else {
+        each([&](float z, float& a) {
+            a = z < f.p ? f.p : z;   // a NaN stays one
+            return act == 0 || z > 0.f ? 1.f : z != z ? z : 0.f;
+        });
     }
 }
 

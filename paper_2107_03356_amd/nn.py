@@ -1,4 +1,4 @@
-"""Layer norm, linear layers and 8-bit activation copies for PyTorch on MI355X.
+"""Norms, linear and gated layers, dropout and 8-bit activation copies for PyTorch on MI355X.
 
 The forward and backward passes of a transformer's feed-forward block on the
 library's kernels (the training operators of include/mfac.h), for models trained
@@ -9,10 +9,20 @@ as 8-bit copies, about half of the bytes of 16-bit activations.
 Three levels:
 
 * ``layer_norm_forward``, ``layer_norm_backward``, ``linear_forward``,
-  ``linear_backward``, ``act_backward``, ``pack8``, ``unpack8``: the passes
-  themselves, on tensors and ``Packed8`` copies;
-* ``layer_norm``, ``linear``, ``feed_forward``: the same with autograd;
-* ``LayerNorm``, ``Linear``, ``FeedForward``: modules.
+  ``linear_backward``, ``act_backward``, ``pack8``, ``unpack8``,
+  ``gated_linear_forward``, ``gated_act_backward``, ``gated_hidden_backward``,
+  ``gated_feed_forward_backward``, ``residual_norm_forward``,
+  ``residual_norm_backward``, ``dropout_forward``: the passes themselves, on
+  tensors and ``Packed8`` copies;
+* ``layer_norm``, ``rms_norm``, ``residual_norm``, ``linear``, ``gated_linear``,
+  ``feed_forward``, ``gated_feed_forward``, ``dropout``: the same with autograd;
+* ``LayerNorm``, ``RMSNorm``, ``Linear``, ``GatedLinear``, ``FeedForward``,
+  ``GatedFeedForward``, ``GatedStack``, ``Dropout``: modules.
+
+Dropout's masks come from a counter-based generator (include/mfac.h) and are never
+stored. Where they start, ``at``, is a tensor of two int64 on the device: by default
+drawn with torch's generator of the device, so that torch's seed, activation
+checkpointing and captured graphs work as with torch's own dropout.
 
 Data is float32, bfloat16 or float16 on one CUDA device; leading dimensions are
 rows, the last one needs unit stride (others are copied first). Layer norm's
@@ -23,6 +33,8 @@ used again and again without training is better handed over in 16 bits). Where
 gradients are off, or no input needs one, nothing is kept. Calls run on the current
 stream of the data's device, with workspaces from torch's allocator.
 """
+
+from typing import NamedTuple, Optional
 
 import torch
 from torch.autograd.function import once_differentiable
@@ -389,6 +401,325 @@ def linear_backward(dy, x, weight, z=None, act="none", affine=None, grad_dtype=N
     return dx, dw, db if need_b else None
 
 
+# ---------------------------------------------------------------- gated layers
+def _gate_weight(weight, bias, x2):
+    w = _weight(weight)
+    n, cin = w.shape[0] // 2, x2.shape[1]
+    if w.shape[0] % 2 or n == 0:
+        raise ValueError(f"gated_linear: weight has the gate's rows and as many of the other projection, not {tuple(w.shape)}")
+    _same("gated_linear: weight", w, x2, (2 * n, cin))
+    return w, n, None if bias is None else _param("gated_linear: bias", bias, x2, 2 * n)
+
+
+def gated_linear_forward(x, weight, bias=None, act="silu", keep=None):
+    """y = act(x Wg^T + bg) * (x Wu^T + bu) for weight = [Wg; Wu], one matrix of 2 hidden rows, and
+    bias = [bg, bu]. ``keep``: also return the pair of pre-activations (gate, other) for the
+    backward pass, "z" as tensors (the halves of one) or "pack8" as their 8-bit copies."""
+    a = _act(act)
+    x2 = _rows(x, "gated_linear: x")
+    w, n, b = _gate_weight(weight, bias, x2)
+    rows, cin = x2.shape
+    if keep not in (None, "z", "pack8"):
+        raise ValueError(f"gated_linear: keep is None, 'z' or 'pack8', not {keep!r}")
+    y = x.new_empty(x.shape[:-1] + (n,))
+    zg = zu = None
+    zm, packed = (None, None, 0), (None, None, None, None, 0)
+    if keep == "z":
+        z = x.new_empty(x.shape[:-1] + (2 * n,))
+        zg, zu = z[..., :n], z[..., n:]
+        zm = z.data_ptr(), z.data_ptr() + n * z.element_size(), 2 * n
+    elif keep == "pack8":
+        zg, zu = (Packed8.empty(rows, n, x.device) for _ in range(2))
+        packed = zg.q.data_ptr(), zg.s.data_ptr(), zu.q.data_ptr(), zu.s.data_ptr(), zg._ld()
+    t = _type(x2, "gated_linear: x")
+    xm, wm = _mat(x2), _mat(w)
+    ws = _workspace(_function("mfac_gated_linear_workspace_bytes")(t, rows, cin, n, *xm, *wm), x.device)
+    _call("mfac_gated_linear", x.device, t, t if b is None else _TYPES[b.dtype], a, rows, cin, n, *xm, *wm, _ptr(b),
+          y.data_ptr(), n, *zm, *packed, ws[0], ws[1])
+    return y if keep is None else (y, (zg, zu))
+
+
+def _gate_pair(z, rows, n, like):
+    """The arguments of the pre-activations z = (gate, other), and what holds them."""
+    try:
+        zg, zu = z
+    except (TypeError, ValueError):
+        raise ValueError("gated: z is the pair (gate, other) of pre-activations") from None
+    if isinstance(zg, Packed8) and isinstance(zu, Packed8):
+        for v in (zg, zu):
+            if v.shape != (rows, n) or v.device != like.device:
+                raise ValueError("gated: 8-bit copies of rows x hidden values")
+        if rows > 1 and zg._ld() != zu._ld():
+            raise ValueError("gated: 8-bit copies whose rows lie equally far apart")
+        return (None, None, 0), (zg.q.data_ptr(), zg.s.data_ptr(), zu.q.data_ptr(), zu.s.data_ptr(), zg._ld()), (zg, zu)
+    if isinstance(zg, Packed8) or isinstance(zu, Packed8):
+        raise ValueError("gated: both pre-activations as tensors, or both as 8-bit copies")
+    zg, zu = (_rows(v, "gated: z") for v in (zg, zu))
+    for v in (zg, zu):
+        _same("gated: z", v, like, (rows, n))
+    if rows > 1 and _ld(zg) != _ld(zu):
+        zg, zu = zg.contiguous(), zu.contiguous()
+    return (zg.data_ptr(), zu.data_ptr(), _ld(zg)), (None, None, None, None, 0), (zg, zu)
+
+
+def gated_act_backward(da, z, act="silu", want_a=False, want_db=True):
+    """(dz, a, db) from da, the gradient of y = act(zg) * zu: dz = [da zu act'(zg), da act(zg)] with 2 hidden columns in
+    da's type, a = y formed again (``want_a``, else None), db the column sums of dz in float32, before its rounding
+    (``want_db``, else None). z is a pair of tensors or of Packed8."""
+    code = _act(act)
+    da2 = _rows(da, "gated: da")
+    rows, n = da2.shape
+    zm, packed, held = _gate_pair(z, rows, n, da2)
+    dz = da.new_empty(da.shape[:-1] + (2 * n,))
+    a = _like(da) if want_a else None
+    db = torch.empty(2 * n, dtype=torch.float32, device=da.device) if want_db else None
+    ws = _workspace(_function("mfac_gated_act_bwd_workspace_bytes")(rows, n) if want_db else 0, da.device)
+    _call("mfac_gated_act_bwd", da.device, _type(da2, "gated: da"), code, rows, n, *_mat(da2), *zm, *packed,
+          dz.data_ptr(), 2 * n, _ptr(a), n, _ptr(db), ws[0], ws[1])
+    return dz, a, db
+
+
+def gated_hidden_backward(dy, weight, z, act="silu", want_a=False):
+    """(dz, a) as of gated_act_backward with da = dy weight, for the layer a weight^T that follows the gate; da is not
+    rounded or stored."""
+    code = _act(act)
+    dy2 = _rows(dy, "gated: dy")
+    rows, cout = dy2.shape
+    w = _weight(weight)
+    n = w.shape[1]
+    _same("gated: weight", w, dy2, (cout, n))
+    zm, packed, held = _gate_pair(z, rows, n, dy2)
+    dz = dy.new_empty(dy.shape[:-1] + (2 * n,))
+    a = dy.new_empty(dy.shape[:-1] + (n,)) if want_a else None
+    t = _type(dy2, "gated: dy")
+    ym, wm = _mat(dy2), _mat(w)
+    ws = _workspace(_function("mfac_gated_hidden_bwd_workspace_bytes")(t, rows, n, cout, *ym, *wm), dy.device)
+    _call("mfac_gated_hidden_bwd", dy.device, t, code, rows, n, cout, *ym, *wm, *zm, *packed, dz.data_ptr(), 2 * n,
+          _ptr(a), n, ws[0], ws[1])
+    return dz, a
+
+
+def gated_feed_forward_backward(dy, x, w1, w2, z, act="silu", affine=None, grad_dtype=None, need=(True,) * 5):
+    """(dx, dw1, db1, dw2, db2) of y = (act(zg) * zu) w2^T + b2, [zg, zu] = x w1^T + b1, from dy, the input x and the
+    pre-activations z (tensors or Packed8; z a pair). ``affine`` = (gamma, beta or None), float32: the input was gamma * x
+    + beta (see linear_backward_weight); dx is then the gradient of that. db1 and db2 are float32. ``need``: which of
+    the five to form; the others are None."""
+    need_x, need_w1, need_b1, need_w2, need_b2 = need
+    dx = dw1 = db1 = dw2 = db2 = dz = a = None
+    if need_b2:
+        _, _, db2 = act_backward(dy)
+    inner = need_x or need_w1 or need_b1
+    beta = affine is not None and affine[1] is not None
+    if need_b1 or (need_w1 and beta):   # column sums of dz, from values that are not rounded
+        dz, a, db1 = gated_act_backward(linear_backward_input(dy, w2), z, act, want_a=need_w2)
+    elif inner or need_w2:
+        dz, a = gated_hidden_backward(dy, w2, z, act, want_a=need_w2)
+    if need_w2:
+        dw2 = linear_backward_weight(dy, a, grad_dtype=grad_dtype)
+    del a
+    if need_x:
+        dx = linear_backward_input(dz, w1)
+    if need_w1:
+        sums = db1
+        if affine is not None and not beta:   # no beta: zeros, and nothing to add to
+            sums = torch.zeros(max(w1.shape), dtype=torch.float32, device=dy.device)
+            affine, sums = (affine[0], sums[:w1.shape[1]]), sums[:w1.shape[0]]
+        dw1 = linear_backward_weight(dz, x, affine, sums, grad_dtype)
+    return dx, dw1, db1 if need_b1 else None, dw2, db2
+
+
+# ---------------------------------------------------------------- between two blocks
+KINDS = {"rms": 0, "layer": B.MFAC_NORM_LAYER}
+
+
+class ResidualNorm(NamedTuple):
+    """s, h, and what the backward pass takes: the norms' (mean, rstd), one float32 for each row (mean None for rms norm),
+    and the 8-bit copy of N_pre's xhat. None for what there is not."""
+    s: Optional[torch.Tensor]
+    h: Optional[torch.Tensor]
+    post: Optional[tuple]
+    pre: Optional[tuple]
+    copy: Optional[Packed8]
+
+
+class ResidualNormGrads(NamedTuple):
+    """Gradients; dpost and dpre are (dweight, dbias)."""
+    dy: Optional[torch.Tensor]
+    dresidual: Optional[torch.Tensor]
+    dgate: Optional[torch.Tensor]
+    dpost: tuple
+    dpre: tuple
+
+
+def dropout_at(device):
+    """Where a mask starts: seed and offset, drawn with torch's generator of the device."""
+    return torch.empty(2, dtype=torch.int64, device=device).random_()
+
+
+def _drop(p, at, data):
+    p = float(p)
+    if not 0 <= p <= 1:
+        raise ValueError(f"dropout: p between 0 and 1, not {p}")
+    if at is not None and (at.dtype != torch.int64 or at.shape != (2,) or at.device != data.device or not at.is_contiguous()):
+        raise ValueError(f"dropout: at is two int64 on {data.device}")
+    if p > 0 and at is None:
+        raise ValueError("dropout: needs at, where the mask starts")
+    return p, _ptr(at) if p > 0 else None
+
+
+def dropout_forward(x, p, at):
+    """x where the mask of (p, at) keeps a value, times 65536 / (65536 - T), T = floor(65536 p + 0.5); 0 elsewhere. The
+    mask depends on the row (leading dimensions are rows) and the column; the gradient of x is the same of dy."""
+    x2 = _rows(x, "dropout: x")
+    p, ptr = _drop(p, at, x2)
+    y = _like(x)
+    if p == 0:
+        return y.copy_(x)
+    _call("mfac_dropout", x.device, _type(x2, "dropout: x"), *x2.shape, *_mat(x2), p, ptr, y.data_ptr(), x2.shape[1])
+    return y
+
+
+def _between(y, post, pre, gate, kind):
+    """(norms, type code of the parameters, post w, post b, pre w, pre b, gate, gates) for rows like y."""
+    if kind not in KINDS:
+        raise ValueError(f"residual_norm: kind is one of {', '.join(KINDS)}, not {kind!r}")
+    norms = (B.MFAC_NORM_POST if post is not None else 0) | (B.MFAC_NORM_PRE if pre is not None else 0)
+    found, like = [], None
+    for what, norm in (("post", post), ("pre", pre)):
+        try:
+            w, b = (None, None) if norm is None else norm
+        except (TypeError, ValueError):
+            raise ValueError(f"residual_norm: {what} is None or a pair (weight, bias)") from None
+        if b is not None and kind == "rms":
+            raise ValueError("residual_norm: rms norm has no bias")
+        found += [w, b]
+    vector = gate is not None and gate.dim() == 1
+    found.append(gate if vector else None)
+    for i, v in enumerate(found):
+        if v is not None:
+            found[i] = v = _param("residual_norm: parameters", v, y, y.shape[1])
+            like = v if like is None else like
+            if v.dtype is not like.dtype:
+                raise ValueError("residual_norm: parameters of one type")
+    gates = None
+    if gate is not None and not vector:
+        gates = _rows(gate, "residual_norm: gate")
+        _same("residual_norm: gate", gates, y, y.shape)
+    return (norms | KINDS[kind] if norms else 0, _TYPES[torch.float32 if like is None else like.dtype], *found, gates)
+
+
+def residual_norm_forward(y, residual=None, post=None, pre=None, gate=None, scale=1.0, p=0.0, at=None, kind="rms", eps=1e-6,
+                          pack=False, stats=True):
+    """What lies between two blocks of a network with a residual stream, as a ResidualNorm:
+
+        n = N_post(y), s = scale * residual + gate * dropout(n), h = N_pre(s)
+
+    over the last dimension. ``post`` and ``pre`` are None (no norm; n = y, no h) or (weight, bias), either None; ``kind``
+    "rms" (no biases) or "layer" for both. ``gate``: one value for each channel, or a tensor like y. ``p`` and ``at``: see
+    dropout_forward. ``pack``: also the 8-bit copy of N_pre's xhat. ``stats=False``: no statistics. With pre alone h is y's
+    norm, and s is y itself."""
+    y2 = _rows(y, "residual_norm: y")
+    rows, cols = y2.shape
+    norms, wt, w1, b1, w2, b2, gv, gm = _between(y2, post, pre, gate, kind)
+    p, ptr = _drop(p, at, y2)
+    if residual is not None:
+        residual = _rows(residual, "residual_norm: residual")
+        _same("residual_norm: residual", residual, y2, y2.shape)
+    if pack and pre is None:
+        raise ValueError("residual_norm: the 8-bit copy is of pre's xhat")
+    plain = residual is None and post is None and gate is None and p == 0
+    if plain and pre is None:
+        return ResidualNorm(y, None, None, None, None)
+    s = None if plain else _like(y)
+    h = None if pre is None else _like(y)
+    layer = kind == "layer"
+
+    def row_values(on):
+        return torch.empty((rows,), dtype=torch.float32, device=y.device) if on and stats else None
+
+    m1, r1 = row_values(post is not None and layer), row_values(post is not None)
+    m2, r2 = row_values(pre is not None and layer), row_values(pre is not None)
+    copy = Packed8.empty(rows, cols, y.device) if pack else None
+    q = _NO_COPY if copy is None else copy._args()
+    _call("mfac_residual_norm", y.device, _type(y2, "residual_norm: y"), wt, norms, rows, cols, *_mat(y2), _ptr(w1),
+          _ptr(b1), _ptr(gv), *_mat(gm), *_mat(residual), float(scale), p, ptr, _ptr(w2), _ptr(b2), float(eps), _ptr(s),
+          cols, _ptr(h), cols, _ptr(m1), _ptr(r1), _ptr(m2), _ptr(r2), *q)
+    return ResidualNorm(y if plain else s, h, None if r1 is None else (m1, r1), None if r2 is None else (m2, r2), copy)
+
+
+def residual_norm_backward(ds, dh, y, s, post_stats=None, pre_stats=None, post=None, pre=None, gate=None, scale=1.0, p=0.0,
+                           at=None, kind="rms", need=(True, True, True, True)):
+    """The gradients of residual_norm_forward as ResidualNormGrads, from ds, the gradient that reaches s by its other uses
+    (None: none), dh, that of h, and what the forward pass took and returned: y (None where neither post nor the gate's
+    gradient needs it), s or the 8-bit copy of N_pre's xhat (a Packed8 as s), the statistics. ``need``: which of dy,
+    dresidual, dgate and the parameters' gradients to form; the others are None. dresidual is dy itself where they are equal."""
+    if (dh is None) != (pre is None) or (ds is None and dh is None):
+        raise ValueError("residual_norm: dh goes with pre, and without it ds is needed")
+    like = ds if ds is not None else dh
+    d2 = _rows(like, "residual_norm: ds, dh")
+    rows, cols = d2.shape
+    norms, wt, w1, b1, w2, b2, gv, gm = _between(d2, post, pre, gate, kind)
+    p, ptr = _drop(p, at, d2)
+    layer = kind == "layer"
+    need_y, need_r, need_gate, need_params = need
+    need_gate = need_gate and gate is not None
+
+    def rows_of(t, what):
+        t = _rows(t, "residual_norm: " + what)
+        _same("residual_norm: " + what, t, d2, d2.shape)
+        return t
+
+    def stats_of(stats, on, what, mean_needed):
+        mean, rstd = (None, None) if not on else stats if stats is not None else (None, None)
+        for t in (mean, rstd):
+            if t is not None and (t.dtype != torch.float32 or t.numel() != rows or not t.is_contiguous()
+                                  or t.device != d2.device):
+                raise ValueError(f"residual_norm: {what} statistics are contiguous float32 tensors, one value for each row")
+        if on and (rstd is None or (mean_needed and mean is None)):
+            raise ValueError(f"residual_norm: needs {what} statistics")
+        return mean if mean_needed else None, rstd
+
+    if dh is not None:
+        dh = rows_of(dh, "dh")
+    if ds is not None:
+        ds = rows_of(ds, "ds")
+    needs_y = post is not None or need_gate
+    if needs_y and y is None:
+        raise ValueError("residual_norm: post and the gate's gradient need y")
+    y = rows_of(y, "y") if needs_y else None
+    sm, packed = (None, 0), _NO_COPY
+    if pre is not None:
+        if isinstance(s, Packed8):
+            if s.shape != d2.shape or s.device != d2.device:
+                raise ValueError("residual_norm: an 8-bit copy of dh's shape")
+            packed = s._args()
+        elif s is None:
+            raise ValueError("residual_norm: pre needs s or the 8-bit copy")
+        else:
+            s = rows_of(s, "s")
+            sm = _mat(s)
+    m1, r1 = stats_of(post_stats, post is not None, "post", layer and post is not None)
+    m2, r2 = stats_of(pre_stats, pre is not None, "pre", layer and pre is not None and not isinstance(s, Packed8))
+
+    same = post is None and gate is None and p == 0 and float(scale) == 1
+    dy = _like(like) if need_y or (same and need_r) else None
+    dr = dy if same else _like(like) if need_r else None
+    wanted = [v is not None and need_params for v in (w1, b1, w2, b2)] + [gv is not None and need_gate]
+    grads, ws = [None] * 5, (None, 0, None)
+    if any(wanted):
+        dtype = next(v.dtype for v in (w1, b1, w2, b2, gv) if v is not None)
+        parts = iter(torch.empty((sum(wanted), cols), dtype=dtype, device=like.device).unbind(0))
+        grads = [next(parts) if on else None for on in wanted]
+        ws = _workspace(_function("mfac_residual_norm_bwd_workspace_bytes")(norms, rows, cols), like.device)
+    dg = _like(gate) if gm is not None and need_gate else None
+    _call("mfac_residual_norm_bwd", like.device, _type(d2, "residual_norm: ds, dh"), wt, norms, rows, cols, *_mat(ds),
+          *_mat(dh), *_mat(y), _ptr(m1), _ptr(r1), *sm, *packed, _ptr(m2), _ptr(r2), _ptr(w1), _ptr(b1), _ptr(gv),
+          *_mat(gm), float(scale), p, ptr, _ptr(w2), _ptr(dy), cols, None if same else _ptr(dr), cols, _ptr(dg), cols,
+          _ptr(grads[0]), _ptr(grads[1]), _ptr(grads[4]), _ptr(grads[2]), _ptr(grads[3]), ws[0], ws[1])
+    return ResidualNormGrads(dy if need_y else None, dr if need_r else None, grads[4] if gm is None else dg,
+                             (grads[0], grads[1]), (grads[2], grads[3]))
+
+
 # ---------------------------------------------------------------- autograd
 def _keep(ctx, **values):
     """Saves tensors and copies for the backward pass, None among them."""
@@ -522,6 +853,111 @@ class _FeedForward(torch.autograd.Function):
                 None, None, None, None)
 
 
+class _GatedLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, act, copy8, grad):
+        w = weight.to(x.dtype)
+        need = [grad and n for n in ctx.needs_input_grad[:3]]
+        if not any(need):
+            return gated_linear_forward(x, w, bias, act)
+        y, (zg, zu) = gated_linear_forward(x, w, bias, act, "pack8" if copy8 else "z")
+        ctx.act, ctx.wdtype, ctx.bdtype = act, weight.dtype, None if bias is None else bias.dtype
+        _keep(ctx, x=(pack8(x) if copy8 else x) if need[1] else None, w=w if need[0] else None, zg=zg, zu=zu)
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        k = _kept(ctx)
+        need_x, need_w, need_b = ctx.needs_input_grad[:3]
+        dz, _, db = gated_act_backward(dy, (k["zg"], k["zu"]), ctx.act, want_db=need_b)
+        dx = linear_backward_input(dz, k["w"]) if need_x else None
+        dw = linear_backward_weight(dz, k["x"], grad_dtype=_grad_dtype(ctx.wdtype, dy)) if need_w else None
+        return dx, _to(dw, ctx.wdtype), _to(db, ctx.bdtype), None, None, None
+
+
+class _GatedFeedForward(torch.autograd.Function):
+    """y = (act(zg) * zu) W2^T + b2, [zg, zu] = x W1^T + b1. act(zg) * zu is formed again in the backward pass."""
+
+    @staticmethod
+    def forward(ctx, x, w1, b1, w2, b2, act, copy8, grad):
+        c1, c2 = w1.to(x.dtype), w2.to(x.dtype)
+        need = [grad and n for n in ctx.needs_input_grad[:5]]
+        inner = any(need[:3])   # whether a gradient passes through the gate
+        if not (inner or need[3]):
+            ctx.types = tuple(None if p is None else p.dtype for p in (w1, b1, w2, b2))
+            _keep(ctx, x=None, zg=None, zu=None, c1=None, c2=None)
+            return linear_forward(gated_linear_forward(x, c1, b1, act), c2, b2)
+        a, (zg, zu) = gated_linear_forward(x, c1, b1, act, "pack8" if copy8 else "z")
+        y = linear_forward(a, c2, b2)
+        ctx.act, ctx.types = act, tuple(None if p is None else p.dtype for p in (w1, b1, w2, b2))
+        _keep(ctx, x=(pack8(x) if copy8 else x) if need[1] else None, zg=zg, zu=zu, c1=c1 if need[0] else None, c2=c2)
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        k = _kept(ctx)
+        t = ctx.types
+        need = ctx.needs_input_grad[:5]
+        if not any(need[:4]):
+            return None, None, None, None, _to(act_backward(dy)[2], t[3]), None, None, None
+        # in float32 where either weight has neither its own type nor the data's
+        grad = dy.dtype if t[0] == t[2] == dy.dtype else torch.float32
+        dx, dw1, db1, dw2, db2 = gated_feed_forward_backward(dy, k["x"], k["c1"], k["c2"], (k["zg"], k["zu"]), ctx.act,
+                                                             grad_dtype=grad, need=need)
+        return dx, _to(dw1, t[0]), _to(db1, t[1]), _to(dw2, t[2]), _to(db2, t[3]), None, None, None
+
+
+class _Residual(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, y, residual, w1, b1, w2, b2, gate, post, pre, scale, p, at, kind, eps, copy8, grad):
+        ctx.set_materialize_grads(False)
+        need = [grad and n for n in ctx.needs_input_grad[:7]]
+        train = any(need)
+        o = residual_norm_forward(y, residual, (w1, b1) if post else None, (w2, b2) if pre else None, gate, scale, p, at, kind,
+                                  eps, pack=copy8 and pre and train, stats=train)
+        plain = o.s is y
+        if train:
+            ctx.options = post, pre, scale, p, kind
+            ctx.rshape = None if residual is None else residual.shape   # its rows may lie in other dimensions than y's
+            m1, r1 = o.post if post else (None, None)
+            m2, r2 = o.pre if pre else (None, None)
+            _keep(ctx, y=y if post or need[6] else None, s=o.copy if o.copy is not None else o.s if pre else None, m1=m1, r1=r1,
+                  m2=m2, r2=r2, w1=w1, b1=b1, w2=w2, b2=b2, gate=gate, at=at if p > 0 else None)
+        return o.h if plain else (o.s, o.h)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, *grads):
+        post, pre, scale, p, kind = ctx.options
+        ds, dh = grads if len(grads) == 2 else (None, grads[0])
+        if ds is None and dh is None:
+            return (None,) * 16
+        k = _kept(ctx)
+        need = ctx.needs_input_grad[:7]
+        used = dh is not None   # s alone may have been used
+        g = residual_norm_backward(ds, dh, k["y"], k["s"], (k["m1"], k["r1"]), (k["m2"], k["r2"]),
+                                   (k["w1"], k["b1"]) if post else None, (k["w2"], k["b2"]) if used else None, k["gate"],
+                                   scale, p, k["at"], kind, need=(need[0], need[1], need[6], any(need[2:6])))
+        dr = None if g.dresidual is None else g.dresidual.reshape(ctx.rshape)
+        params = [v if n else None for v, n in zip((*g.dpost, *g.dpre), need[2:6])]
+        return (g.dy, dr, *params, g.dgate if need[6] else None) + (None,) * 9
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, p, at):
+        ctx.p = p
+        ctx.save_for_backward(at)
+        return dropout_forward(x, p, at)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        return dropout_forward(dy, ctx.p, *ctx.saved_tensors), None, None
+
+
 def layer_norm(x, weight=None, bias=None, eps=1e-5, copy8=False):
     """Layer norm over the last dimension, differentiable. copy8: keep the normalised x in
     8 bits for the backward pass instead of x."""
@@ -543,6 +979,47 @@ def feed_forward(x, ln_weight, ln_bias, w1, b1, w2, b2, act="gelu", eps=1e-5, co
     if any(p is None for p in (ln_weight, ln_bias, w1, b1, w2, b2)):
         raise ValueError("feed_forward: needs its six parameters")
     return _FeedForward.apply(x, ln_weight, ln_bias, w1, b1, w2, b2, act, eps, copy8, torch.is_grad_enabled())
+
+
+def gated_linear(x, weight, bias=None, act="silu", copy8=False):
+    """act(x Wg^T + bg) * (x Wu^T + bu), differentiable, for weight = [Wg; Wu] (2 hidden x cin) and bias = [bg, bu].
+    copy8: keep x and the pre-activations in 8 bits for the backward pass."""
+    _act(act)
+    return _GatedLinear.apply(x, weight, bias, act, copy8, torch.is_grad_enabled())
+
+
+def gated_feed_forward(x, w1, w2, b1=None, b2=None, act="silu", copy8=False):
+    """gated_linear(x, w1, b1, act) w2^T + b2, differentiable. copy8: what the backward pass needs is kept in 8 bits."""
+    _act(act)
+    return _GatedFeedForward.apply(x, w1, b1, w2, b2, act, copy8, torch.is_grad_enabled())
+
+
+def residual_norm(y, residual=None, post=None, pre=None, gate=None, scale=1.0, p=0.0, at=None, kind="rms", eps=1e-6,
+                  copy8=False):
+    """(s, h) of residual_norm_forward, differentiable; h is None without pre, and s is y where nothing lies between.
+    ``at`` is drawn where p > 0 and none is given. copy8: keep N_pre's xhat in 8 bits for the backward pass instead of s."""
+    if post is None and pre is None and gate is None and residual is None and p == 0:
+        return y, None
+    _between(_rows(y, "residual_norm: y"), post, pre, gate, kind)
+    if p > 0 and at is None:
+        at = dropout_at(y.device)
+    out = _Residual.apply(y, residual, *(post or (None, None)), *(pre or (None, None)), gate, post is not None,
+                          pre is not None, scale, p, at, kind, eps, copy8, torch.is_grad_enabled())
+    return out if isinstance(out, tuple) else (y, out)
+
+
+def rms_norm(x, weight=None, eps=1e-6, copy8=False):
+    """x / sqrt(mean(x^2) + eps) * weight over the last dimension, differentiable. copy8: keep the normalised x in 8 bits
+    for the backward pass instead of x."""
+    return residual_norm(x, pre=(weight, None), eps=eps, copy8=copy8)[1]
+
+
+def dropout(x, p=0.5, training=True, at=None):
+    """Dropout, differentiable: see dropout_forward. ``at`` is drawn where none is given."""
+    if not training or p == 0:
+        return x
+    at = dropout_at(x.device) if at is None else at
+    return _Dropout.apply(x, p, at)
 
 
 # ---------------------------------------------------------------- modules
@@ -588,3 +1065,103 @@ class FeedForward(torch.nn.Module):
     def forward(self, x):
         return feed_forward(x, self.norm.weight, self.norm.bias, self.up.weight, self.up.bias, self.down.weight,
                             self.down.bias, self.up.act, self.norm.eps, self.copy8)
+
+
+class RMSNorm(torch.nn.Module):
+    """RMS norm over the last dimension, of size `dim`."""
+
+    def __init__(self, dim, eps=1e-6, copy8=False, device=None):
+        super().__init__()
+        self.eps, self.copy8 = eps, copy8
+        self.weight = torch.nn.Parameter(torch.ones(dim, device=device))
+
+    def forward(self, x):
+        return rms_norm(x, self.weight, self.eps, self.copy8)
+
+
+class GatedLinear(torch.nn.Module):
+    """act(x Wg^T + bg) * (x Wu^T + bu); weight = [Wg; Wu], uniform within 1 / sqrt(cin)."""
+
+    def __init__(self, cin, hidden, bias=False, act="silu", copy8=False, device=None):
+        super().__init__()
+        _act(act)
+        self.act, self.copy8 = act, copy8
+        r = cin ** -0.5
+        self.weight = torch.nn.Parameter(torch.empty(2 * hidden, cin, device=device).uniform_(-r, r))
+        self.bias = torch.nn.Parameter(torch.empty(2 * hidden, device=device).uniform_(-r, r)) if bias else None
+
+    def forward(self, x):
+        return gated_linear(x, self.weight, self.bias, self.act, self.copy8)
+
+
+class Dropout(torch.nn.Module):
+    """Dropout whose mask is not stored, in training mode."""
+
+    def __init__(self, p=0.5):
+        super().__init__()
+        if not 0 <= p <= 1:
+            raise ValueError(f"dropout: p between 0 and 1, not {p}")
+        self.p = p
+
+    def forward(self, x, at=None):
+        return dropout(x, self.p, self.training, at)
+
+
+class GatedFeedForward(torch.nn.Module):
+    """A gated feed-forward block with its norms and skip connection:
+    scale * x + gate * dropout(N_post(FF(N_pre(x)))), FF(h) = (act(h Wg^T) * (h Wu^T)) W2^T.
+
+    kind: "rms" or "layer"; post_norm: whether there is a norm after the block; gate: the first value of a learned gate for
+    each channel, or None for none; p: dropout's, in training mode."""
+
+    def __init__(self, dim, hidden, act="silu", kind="rms", eps=1e-6, post_norm=False, gate=None, scale=1.0, p=0.0, bias=False,
+                 copy8=False, device=None):
+        super().__init__()
+        if kind not in KINDS or not 0 <= p <= 1:
+            raise ValueError(f"GatedFeedForward: kind is one of {', '.join(KINDS)}, and p between 0 and 1")
+        self.kind, self.eps, self.scale, self.p, self.copy8 = kind, eps, scale, p, copy8
+
+        def norm():
+            return RMSNorm(dim, eps, device=device) if kind == "rms" else LayerNorm(dim, eps, device=device)
+
+        self.norm, self.post = norm(), norm() if post_norm else None
+        self.up = GatedLinear(dim, hidden, bias, act, device=device)
+        self.down = Linear(hidden, dim, bias, device=device)
+        self.gate = None if gate is None else torch.nn.Parameter(torch.full((dim,), float(gate), device=device))
+
+    def inner(self, h):
+        """The block without its norms and skip connection."""
+        return gated_feed_forward(h, self.up.weight, self.down.weight, self.up.bias, self.down.bias, self.up.act, self.copy8)
+
+    def join(self, y, x, pre=None):
+        """(s, h): the stream after the block, and its norm `pre` (the next block's; None: no h)."""
+        return residual_norm(y, x, _norm_of(self.post), _norm_of(pre), self.gate, self.scale, self.p if self.training else 0.0,
+                             kind=self.kind, eps=self.eps, copy8=self.copy8)
+
+    def forward(self, x):
+        h = residual_norm(x, pre=_norm_of(self.norm), kind=self.kind, eps=self.eps, copy8=self.copy8)[1]
+        return self.join(self.inner(h), x)[0]
+
+
+def _norm_of(module):
+    return None if module is None else (module.weight, getattr(module, "bias", None))
+
+
+class GatedStack(torch.nn.Module):
+    """`depth` GatedFeedForward blocks and a last norm. The norms after a block and before the next, with what lies between
+    them, are one pass over the rows."""
+
+    def __init__(self, dim, hidden, depth, kind="rms", eps=1e-6, device=None, **block):
+        super().__init__()
+        if depth < 1:
+            raise ValueError("GatedStack: at least one block")
+        self.blocks = torch.nn.ModuleList([GatedFeedForward(dim, hidden, kind=kind, eps=eps, device=device, **block)
+                                           for _ in range(depth)])
+        self.norm = RMSNorm(dim, eps, device=device) if kind == "rms" else LayerNorm(dim, eps, device=device)
+
+    def forward(self, x):
+        first = self.blocks[0]
+        h = residual_norm(x, pre=_norm_of(first.norm), kind=first.kind, eps=first.eps, copy8=first.copy8)[1]
+        for block, norm in zip(self.blocks, [b.norm for b in self.blocks[1:]] + [self.norm]):
+            x, h = block.join(block.inner(h), x, norm)
+        return h
