@@ -553,24 +553,40 @@ mfac_status mfac_gated_linear(mfac_dtype type, mfac_dtype btype, mfac_act act, i
  * pre-activations (matrices or copies):
  *   dz = [da zu act'(zg), da act(zg)] (rows x 2 hidden) rounded to type,
  *   a = act(zg) zu (NULL: not wanted),
- *   db = the 2 hidden column sums of dz in fp32, before the rounding (NULL: not wanted).
+ *   db = the 2 hidden column sums of dz in fp32, before the rounding (NULL: not wanted),
+ *   dz_lo, a_lo (of dz's and a's strides, 16-bit types only, NULL: not wanted) = what the rounding of dz and
+ *   a to type leaves, rounded to type, for gradients of weights that are wanted in
+ *   fp32 (mfac_linear_bwd_weight_parts).
  * The gradients of x and W are those of a linear layer with cout = 2 hidden. */
 size_t mfac_gated_act_bwd_workspace_bytes(int64_t rows, int64_t hidden);
 mfac_status mfac_gated_act_bwd(mfac_dtype type, mfac_act act, int64_t rows, int64_t hidden, const void* da, int64_t ldda,
                                const void* zg, const void* zu, int64_t ldz, const int8_t* qg, const uint8_t* sg,
-                               const int8_t* qu, const uint8_t* su, int64_t ldq, void* dz, int64_t lddz, void* a,
-                               int64_t lda, float* db, void* workspace, size_t workspace_bytes, hipStream_t stream);
+                               const int8_t* qu, const uint8_t* su, int64_t ldq, void* dz, void* dz_lo, int64_t lddz,
+                               void* a, void* a_lo, int64_t lda, float* db, void* workspace, size_t workspace_bytes,
+                               hipStream_t stream);
 
 /* The same behind the layer that follows, a W2^T with W2 (cout x hidden): from dy (rows
- * x cout), the gradient of that layer's output, da = dy W2 is formed and used in one kernel
- * and not rounded or stored. */
+ * x cout), the gradient of that layer's output, da = dy W2 is formed and not rounded; without db and where hidden
+ * is a multiple of 64 it is not stored either. */
 size_t mfac_gated_hidden_bwd_workspace_bytes(mfac_dtype type, int64_t rows, int64_t hidden, int64_t cout, const void* dy,
-                                             int64_t lddy, const void* w, int64_t ldw);
+                                             int64_t lddy, const void* w, int64_t ldw, int32_t want_db);
 mfac_status mfac_gated_hidden_bwd(mfac_dtype type, mfac_act act, int64_t rows, int64_t hidden, int64_t cout,
                                   const void* dy, int64_t lddy, const void* w, int64_t ldw, const void* zg,
                                   const void* zu, int64_t ldz, const int8_t* qg, const uint8_t* sg, const int8_t* qu,
-                                  const uint8_t* su, int64_t ldq, void* dz, int64_t lddz, void* a, int64_t lda,
-                                  void* workspace, size_t workspace_bytes, hipStream_t stream);
+                                  const uint8_t* su, int64_t ldq, void* dz, void* dz_lo, int64_t lddz, void* a,
+                                  void* a_lo, int64_t lda, float* db, void* workspace, size_t workspace_bytes,
+                                  hipStream_t stream);
+
+/* mfac_linear_bwd_weight for 16-bit data of which dz (dz + dz_lo) or x (x + x_lo) comes in two parts, one of the two; the
+ * second part has the first's strides. */
+size_t mfac_linear_bwd_weight_parts_workspace_bytes(mfac_dtype type, int64_t rows, int64_t cin, int64_t cout,
+                                                    const void* dz, const void* dz_lo, int64_t lddz, const void* x,
+                                                    const void* x_lo, int64_t ldx);
+mfac_status mfac_linear_bwd_weight_parts(mfac_dtype type, mfac_dtype gtype, int64_t rows, int64_t cin, int64_t cout,
+                                         const void* dz, const void* dz_lo, int64_t lddz, const void* x,
+                                         const void* x_lo, int64_t ldx, const int8_t* q, int64_t ldq, const uint8_t* s,
+                                         const float* gamma, const float* beta, const float* db, void* dw, int64_t lddw,
+                                         void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* Dropout. at: two int64 in device memory, seed and offset, 8-byte aligned, read when the kernel runs (so a captured graph
  * takes what they hold when it is replayed). Element (row, c) of a matrix takes half-word c % 8 of the

@@ -97,10 +97,13 @@ SIGNATURES = {
                                      _I64, _VP, _VP, _VP, _VP, _I64, _VP, _SZ, _VP]),
     "mfac_gated_act_bwd_workspace_bytes": (_SZ, [_I64, _I64]),
     "mfac_gated_act_bwd": (_c.c_int, [_I32, _I32, _I64, _I64, _VP, _I64, _VP, _VP, _I64, _VP, _VP, _VP, _VP, _I64, _VP,
-                                      _I64, _VP, _I64, _VP, _VP, _SZ, _VP]),
-    "mfac_gated_hidden_bwd_workspace_bytes": (_SZ, [_I32, _I64, _I64, _I64, _VP, _I64, _VP, _I64]),
+                                      _VP, _I64, _VP, _VP, _I64, _VP, _VP, _SZ, _VP]),
+    "mfac_gated_hidden_bwd_workspace_bytes": (_SZ, [_I32, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _I32]),
     "mfac_gated_hidden_bwd": (_c.c_int, [_I32, _I32, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _I64, _VP, _VP,
-                                         _VP, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _SZ, _VP]),
+                                         _VP, _VP, _I64, _VP, _VP, _I64, _VP, _VP, _I64, _VP, _VP, _SZ, _VP]),
+    "mfac_linear_bwd_weight_parts_workspace_bytes": (_SZ, [_I32, _I64, _I64, _I64, _VP, _VP, _I64, _VP, _VP, _I64]),
+    "mfac_linear_bwd_weight_parts": (_c.c_int, [_I32, _I32, _I64, _I64, _I64, _VP, _VP, _I64, _VP, _VP, _I64, _VP, _I64,
+                                                _VP, _VP, _VP, _VP, _VP, _I64, _VP, _SZ, _VP]),
     "mfac_dropout": (_c.c_int, [_I32, _I64, _I64, _VP, _I64, _F64, _VP, _VP, _I64, _VP]),
     "mfac_residual_norm": (_c.c_int, [_I32, _I32, _I32, _I64, _I64, _VP, _I64, _VP, _VP, _VP, _VP, _I64, _VP, _I64,
                                       _F64, _F64, _VP, _VP, _VP, _F64, _VP, _I64, _VP, _I64, _VP, _VP, _VP, _VP, _VP,

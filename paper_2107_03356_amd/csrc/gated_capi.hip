@@ -23,6 +23,9 @@ bool act_ok(int a) { return a >= MFAC_ACT_NONE && a <= MFAC_ACT_SILU; }
 bool gated_ok(int64_t rows, int64_t cin, int64_t hidden) {
     return rows >= 0 && rows <= MOST && cin >= 1 && cin <= MOST_WIDTH && hidden >= 1 && hidden <= MOST_WIDTH / 2;
 }
+bool layer_ok(int64_t rows, int64_t cin, int64_t cout) {
+    return rows >= 0 && rows <= MOST && cin >= 1 && cin <= MOST_WIDTH && cout >= 1 && cout <= MOST_WIDTH;
+}
 bool aligned(const void* p, int type) { return (uintptr_t)p % (type == MFAC_F32 ? 4 : 2) == 0; }
 bool matrix_ok(const void* p, int type, int64_t ld, int64_t cols) {
     return p && ld >= cols && ld <= (int64_t(1) << 33) && aligned(p, type);
@@ -48,6 +51,14 @@ Product hidden_product(int64_t rows, int64_t hidden, int64_t cout, const void* d
     return Product{rows, hidden, cout, dy, lddy, false, w, ldw, true, Packed{}, GATE_HIDDEN};
 }
 
+Product da_product(int64_t rows, int64_t hidden, int64_t cout, const void* dy, int64_t lddy, const void* w, int64_t ldw) {
+    return Product{rows, hidden, cout, dy, lddy, false, w, ldw, true, Packed{}};
+}
+Product weight_product(int64_t rows, int64_t cin, int64_t cout, const void* dz, const void* dz_lo, int64_t lddz,
+                       const void* x, const void* x_lo, int64_t ldx, Packed p) {
+    return Product{cout, cin, rows, dz, lddz, true, x, ldx, true, p, GATE_NONE, dz_lo, x_lo};
+}
+
 // Both pre-activations as tensors, or both as copies; `absent_ok`: or neither.
 bool pair_ok(int type, int64_t hidden, const void* zg, const void* zu, int64_t ldz, const void* qg, const void* sg,
              const void* qu, const void* su, int64_t ldq, bool absent_ok) {
@@ -59,6 +70,47 @@ bool pair_ok(int type, int64_t hidden, const void* zg, const void* zu, int64_t l
 }
 Packed packed(const int8_t* q, int64_t ldq, const uint8_t* s) {
     return Packed{const_cast<int8_t*>(q), ldq, const_cast<uint8_t*>(s)};
+}
+
+// What forms dz and a from da.
+Epilogue gate_epilogue(int type, int act, const void* zg, const void* zu, int64_t ldz, Packed pg, Packed pu, void* dz,
+                       void* dz_lo, int64_t lddz, void* a, void* a_lo, int64_t lda) {
+    Epilogue e{};
+    e.out_dt = e.io_dt = type;
+    e.act = act;
+    e.out = dz;
+    e.out_lo = dz_lo;
+    e.ldo = lddz;
+    e.z = const_cast<void*>(zg);
+    e.z2 = const_cast<void*>(zu);
+    e.ldz = ldz;
+    e.p = pg;
+    e.p2 = pu;
+    e.a = a;
+    e.a_lo = a_lo;
+    e.lda = lda;
+    return e;
+}
+
+// The workspace of mfac_gated_hidden_bwd. Where db is wanted, or hidden is not a multiple of what a wave of the fused
+// product holds, da is formed in fp32 and read again: in the product's epilogue the column sums of dz would have to be joined
+// over the tiles, and the checks for each column would double a code that is run through once a tile. bf16, 8192
+// rows, hidden 8192, cout 2048: TIME_FUSED us fused, TIME_UNFUSED so.
+struct HiddenWorkspace {
+    bool fused;
+    size_t product, da, total;
+};
+HiddenWorkspace hidden_workspace(int type, int64_t rows, int64_t hidden, int64_t cout, const void* dy, int64_t lddy,
+                                 const void* w, int64_t ldw, bool want_db) {
+    HiddenWorkspace n{!want_db && hidden % 64 == 0, 0, 0, 0};
+    const Product p = n.fused ? hidden_product(rows, hidden, cout, dy, lddy, w, ldw)
+                              : da_product(rows, hidden, cout, dy, lddy, w, ldw);
+    if (rows > 0) n.product = product_workspace_bytes(type, p);
+    n.total = n.product;
+    if (n.fused) return n;
+    n.da = (size_t)round_up(rows * hidden * 4, 256);
+    n.total += n.da + (want_db ? mfac_gated_act_bwd_workspace_bytes(rows, hidden) : 0);
+    return n;
 }
 
 // p: the probability of a value to be dropped, in units of 2^-16.
@@ -119,11 +171,14 @@ MFAC_API size_t mfac_gated_act_bwd_workspace_bytes(int64_t rows, int64_t hidden)
 MFAC_API mfac_status mfac_gated_act_bwd(mfac_dtype type, mfac_act act, int64_t rows, int64_t hidden, const void* da,
                                         int64_t ldda, const void* zg, const void* zu, int64_t ldz, const int8_t* qg,
                                         const uint8_t* sg, const int8_t* qu, const uint8_t* su, int64_t ldq, void* dz,
-                                        int64_t lddz, void* a, int64_t lda, float* db, void* workspace,
-                                        size_t workspace_bytes, hipStream_t stream) {
-    if (!type_ok(type) || !act_ok(act) || !gated_ok(rows, 1, hidden) || !vector_ok(db, MFAC_F32)) return MFAC_EINVAL;
+                                        void* dz_lo, int64_t lddz, void* a, void* a_lo, int64_t lda, float* db,
+                                        void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    if (!type_ok(type) || !act_ok(act) || !gated_ok(rows, 1, hidden) || !vector_ok(db, MFAC_F32) ||
+        (type == MFAC_F32 && (dz_lo || a_lo)) || (a_lo && !a))
+        return MFAC_EINVAL;
     if (rows > 0 && (!matrix_ok(da, type, ldda, hidden) || !matrix_ok(dz, type, lddz, 2 * hidden) ||
-                     !matrix_or_none(a, type, lda, hidden) ||
+                     !matrix_or_none(dz_lo, type, lddz, 2 * hidden) || !matrix_or_none(a, type, lda, hidden) ||
+                     !matrix_or_none(a_lo, type, lda, hidden) ||
                      !pair_ok(type, hidden, zg, zu, ldz, qg, sg, qu, su, ldq, false)))
         return MFAC_EINVAL;
     if (db) {
@@ -131,42 +186,94 @@ MFAC_API mfac_status mfac_gated_act_bwd(mfac_dtype type, mfac_act act, int64_t r
             check_workspace(mfac_gated_act_bwd_workspace_bytes(rows, hidden), workspace, workspace_bytes);
         if (e != MFAC_OK) return e;
     }
-    return done(launch_gated_act_bwd(type, act, rows, hidden, da, ldda, zg, zu, ldz, packed(qg, ldq, sg),
-                                     packed(qu, ldq, su), dz, lddz, a, lda, db, (float*)workspace, stream));
+    const Epilogue e = gate_epilogue(type, act, zg, zu, ldz, packed(qg, ldq, sg), packed(qu, ldq, su), dz, dz_lo, lddz, a,
+                                     a_lo, lda);
+    return done(launch_gated_act_bwd(type, type, rows, hidden, da, ldda, e, db, (float*)workspace, stream));
 }
 
 MFAC_API size_t mfac_gated_hidden_bwd_workspace_bytes(mfac_dtype type, int64_t rows, int64_t hidden, int64_t cout,
-                                                      const void* dy, int64_t lddy, const void* w, int64_t ldw) {
-    if (!type_ok(type) || !gated_ok(rows, cout, hidden) || rows == 0) return 0;
-    return product_workspace_bytes(type, hidden_product(rows, hidden, cout, dy, lddy, w, ldw));
+                                                      const void* dy, int64_t lddy, const void* w, int64_t ldw,
+                                                      int32_t want_db) {
+    if (!type_ok(type) || !gated_ok(rows, cout, hidden)) return 0;
+    return hidden_workspace(type, rows, hidden, cout, dy, lddy, w, ldw, want_db != 0).total;
 }
 
 MFAC_API mfac_status mfac_gated_hidden_bwd(mfac_dtype type, mfac_act act, int64_t rows, int64_t hidden, int64_t cout,
                                            const void* dy, int64_t lddy, const void* w, int64_t ldw, const void* zg,
                                            const void* zu, int64_t ldz, const int8_t* qg, const uint8_t* sg,
-                                           const int8_t* qu, const uint8_t* su, int64_t ldq, void* dz, int64_t lddz,
-                                           void* a, int64_t lda, void* workspace, size_t workspace_bytes,
-                                           hipStream_t stream) {
-    if (!type_ok(type) || !act_ok(act) || !gated_ok(rows, cout, hidden)) return MFAC_EINVAL;
-    if (rows == 0) return MFAC_OK;
-    if (!matrix_ok(dy, type, lddy, cout) || !matrix_ok(w, type, ldw, hidden) || !matrix_ok(dz, type, lddz, 2 * hidden) ||
-        !matrix_or_none(a, type, lda, hidden) || !pair_ok(type, hidden, zg, zu, ldz, qg, sg, qu, su, ldq, false))
+                                           const int8_t* qu, const uint8_t* su, int64_t ldq, void* dz, void* dz_lo,
+                                           int64_t lddz, void* a, void* a_lo, int64_t lda, float* db, void* workspace,
+                                           size_t workspace_bytes, hipStream_t stream) {
+    if (!type_ok(type) || !act_ok(act) || !gated_ok(rows, cout, hidden) || !vector_ok(db, MFAC_F32) ||
+        (type == MFAC_F32 && (dz_lo || a_lo)) || (a_lo && !a))
         return MFAC_EINVAL;
-    const Product p = hidden_product(rows, hidden, cout, dy, lddy, w, ldw);
+    if (rows > 0 && (!matrix_ok(dy, type, lddy, cout) || !matrix_ok(w, type, ldw, hidden) ||
+                     !matrix_ok(dz, type, lddz, 2 * hidden) || !matrix_or_none(dz_lo, type, lddz, 2 * hidden) ||
+                     !matrix_or_none(a, type, lda, hidden) || !matrix_or_none(a_lo, type, lda, hidden) ||
+                     !pair_ok(type, hidden, zg, zu, ldz, qg, sg, qu, su, ldq, false)))
+        return MFAC_EINVAL;
+    if (rows == 0 && !db) return MFAC_OK;
+    const HiddenWorkspace need = hidden_workspace(type, rows, hidden, cout, dy, lddy, w, ldw, db != nullptr);
+    const mfac_status st = check_workspace(need.total, workspace, workspace_bytes);
+    if (st != MFAC_OK) return st;
+    const Epilogue e = gate_epilogue(type, act, zg, zu, ldz, packed(qg, ldq, sg), packed(qu, ldq, su), dz, dz_lo, lddz, a,
+                                     a_lo, lda);
+    char* ws = (char*)workspace;
+    if (need.fused) return done(launch_product(type, hidden_product(rows, hidden, cout, dy, lddy, w, ldw), e, ws, stream));
+    // da in fp32, then the gate's pass over it
+    float* da = (float*)(ws + need.product);
+    if (rows > 0) {
+        Epilogue plain{};
+        plain.out_dt = MFAC_F32;
+        plain.io_dt = type;
+        plain.out = da;
+        plain.ldo = hidden;
+        const hipError_t err = launch_product(type, da_product(rows, hidden, cout, dy, lddy, w, ldw), plain, ws, stream);
+        if (err != hipSuccess) return done(err);
+    }
+    return done(launch_gated_act_bwd(type, MFAC_F32, rows, hidden, da, hidden, e, db, (float*)(ws + need.product + need.da),
+                                     stream));
+}
+
+// ---------------------------------------------------------------- weight gradients from two parts
+MFAC_API size_t mfac_linear_bwd_weight_parts_workspace_bytes(mfac_dtype type, int64_t rows, int64_t cin, int64_t cout,
+                                                             const void* dz, const void* dz_lo, int64_t lddz, const void* x,
+                                                             const void* x_lo, int64_t ldx) {
+    if ((type != MFAC_BF16 && type != MFAC_F16) || !layer_ok(rows, cin, cout) || rows == 0) return 0;
+    int8_t some;   // an 8-bit copy, by its presence alone
+    return product_workspace_bytes(type, weight_product(rows, cin, cout, dz, dz_lo, lddz, x, x_lo, ldx,
+                                                        x ? Packed{} : Packed{&some, cin, nullptr}));
+}
+
+MFAC_API mfac_status mfac_linear_bwd_weight_parts(mfac_dtype type, mfac_dtype gtype, int64_t rows, int64_t cin, int64_t cout,
+                                                  const void* dz, const void* dz_lo, int64_t lddz, const void* x,
+                                                  const void* x_lo, int64_t ldx, const int8_t* q, int64_t ldq,
+                                                  const uint8_t* s, const float* gamma, const float* beta, const float* db,
+                                                  void* dw, int64_t lddw, void* workspace, size_t workspace_bytes,
+                                                  hipStream_t stream) {
+    if ((type != MFAC_BF16 && type != MFAC_F16) || !param_type_ok(gtype, type) || !layer_ok(rows, cin, cout) ||
+        !matrix_ok(dw, gtype, lddw, cin))
+        return MFAC_EINVAL;
+    if (rows == 0) return done(launch_zero_matrix(gtype, cout, cin, dw, lddw, stream));
+    const bool copy = q || s;
+    if (!matrix_ok(dz, type, lddz, cout) || !matrix_or_none(dz_lo, type, lddz, cout) || copy == (x != nullptr) ||
+        (copy ? !copy_ok(q, ldq, s, cin) : !matrix_ok(x, type, ldx, cin)) || !matrix_or_none(x_lo, type, ldx, cin) ||
+        (dz_lo != nullptr) == (x_lo != nullptr) || (x_lo && !x))
+        return MFAC_EINVAL;
+    if ((gamma != nullptr) != (beta != nullptr) || (gamma && !db) || !vector_ok(gamma, MFAC_F32) ||
+        !vector_ok(beta, MFAC_F32) || !vector_ok(db, MFAC_F32))
+        return MFAC_EINVAL;
+    const Product p = weight_product(rows, cin, cout, dz, dz_lo, lddz, x, x_lo, ldx, packed(q, ldq, s));
     const mfac_status st = check_workspace(product_workspace_bytes(type, p), workspace, workspace_bytes);
     if (st != MFAC_OK) return st;
     Epilogue e{};
-    e.out_dt = e.io_dt = type;
-    e.act = act;
-    e.out = dz;
-    e.ldo = lddz;
-    e.z = const_cast<void*>(zg);
-    e.z2 = const_cast<void*>(zu);
-    e.ldz = ldz;
-    e.p = packed(qg, ldq, sg);
-    e.p2 = packed(qu, ldq, su);
-    e.a = a;
-    e.lda = lda;
+    e.out_dt = gtype;
+    e.io_dt = type;
+    e.out = dw;
+    e.ldo = lddw;
+    e.gamma = gamma;
+    e.beta = beta;
+    e.db = db;
     return done(launch_product(type, p, e, workspace, stream));
 }
 

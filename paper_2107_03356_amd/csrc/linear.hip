@@ -225,11 +225,11 @@ bool plain16(const void* p, int64_t ld, int64_t cols) {
     return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && cols % 8 == 0 && ld <= (int64_t(1) << 21);
 }
 
-Operand operand_of(int dt, const void* p, int64_t ld, bool packed, int64_t rows, int64_t cols) {
-    Operand o{dt == DT_F32 && !packed, true, rows, cols, round_up(cols, 8), 0};
-    o.lay_out = o.planes || packed || !plain16(p, ld, cols);
+Operand operand_of(int dt, const void* p, const void* lo, int64_t ld, bool packed, int64_t rows, int64_t cols) {
+    Operand o{packed ? 1 : dt == DT_F32 ? 3 : lo ? 2 : 1, true, rows, cols, round_up(cols, 8), 0};
+    o.lay_out = o.planes == 3 || packed || !plain16(p, ld, cols) || (lo && !plain16(lo, ld, cols));
     if (!o.lay_out) o.ld = ld;
-    else o.bytes = (size_t)round_up(rows * o.ld * 2 * (o.planes ? 3 : 1), 256);
+    else o.bytes = (size_t)round_up(rows * o.ld * 2 * o.planes, 256);
     return o;
 }
 
@@ -256,11 +256,11 @@ Plan plan_of(int dt, const Product& p) {
     q.skinny = p.M <= SKINNY_ROWS && !p.a_col && !p.b_col;
     q.splits = 1;
     if (q.skinny) return q;
-    q.a = p.a_col ? operand_of(dt, p.A, p.lda, false, p.K, p.M) : operand_of(dt, p.A, p.lda, false, p.M, p.K);
-    const bool packed = p.bp.q != nullptr;
-    q.b = p.b_col ? operand_of(dt, p.B, p.ldb, packed, p.K, p.N) : operand_of(dt, p.B, p.ldb, packed, p.N, p.K);
+    const int64_t ar = p.a_col ? p.K : p.M, ac = p.a_col ? p.M : p.K, br = p.b_col ? p.K : p.N, bc = p.b_col ? p.N : p.K;
+    q.a = operand_of(dt, p.A, p.A_lo, p.lda, false, ar, ac);
+    q.b = operand_of(dt, p.B, p.B_lo, p.ldb, p.bp.q != nullptr, br, bc);
     q.ksteps = (int)ceil_div(p.K, BK);
-    q.nseg = q.a.planes ? (q.b.planes ? 6 : 3) : 1;
+    q.nseg = q.a.planes * q.b.planes == 9 ? 6 : q.a.planes * q.b.planes;   // not both of two parts
     const int64_t total = (int64_t)q.ksteps * q.nseg;
     float best = 0.f;
     for (int tile : {256, 128, 64})
@@ -278,16 +278,21 @@ Plan plan_of(int dt, const Product& p) {
     return q;
 }
 
-hipError_t lay_out(int dt, const Operand& o, const void* src, int64_t ld, Packed p, void* dst, hipStream_t st) {
+hipError_t lay_out(int dt, const Operand& o, const void* src, const void* lo, int64_t ld, Packed p, void* dst,
+                   hipStream_t st) {
     if (p.q) return launch_unpack8(dt == DT_F16 ? DT_F16 : DT_BF16, o.rows, o.cols, p, dst, o.ld, st);
     const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(o.rows * (o.ld / 8), 256), 4096);
-    if (o.planes)
+    if (o.planes == 3)
         k_lay_out_split<<<grid, 256, 0, st>>>((const float*)src, ld, o.rows, o.cols, (bf16*)dst, o.ld, o.rows * o.ld);
     else if (dt == DT_BF16)
         k_lay_out<bf16><<<grid, 256, 0, st>>>((const bf16*)src, ld, o.rows, o.cols, (bf16*)dst, o.ld);
     else
         k_lay_out<f16><<<grid, 256, 0, st>>>((const f16*)src, ld, o.rows, o.cols, (f16*)dst, o.ld);
-    return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || o.planes != 2) return e;
+    Operand second = o;
+    second.planes = 1;
+    return lay_out(dt, second, lo, nullptr, ld, p, (char*)dst + o.rows * o.ld * 2, st);
 }
 
 template <typename T>
@@ -349,19 +354,19 @@ hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws,
         g.A = (const char*)p.A;
         g.B = (const char*)p.B;
         if (q.a.lay_out) {
-            if ((err = lay_out(dt, q.a, p.A, p.lda, Packed{}, w, st)) != hipSuccess) return err;
+            if ((err = lay_out(dt, q.a, p.A, p.A_lo, p.lda, Packed{}, w, st)) != hipSuccess) return err;
             g.A = w;
             w += q.a.bytes;
         }
         if (q.b.lay_out) {
-            if ((err = lay_out(dt, q.b, p.B, p.ldb, p.bp, w, st)) != hipSuccess) return err;
+            if ((err = lay_out(dt, q.b, p.B, p.B_lo, p.ldb, p.bp, w, st)) != hipSuccess) return err;
             g.B = w;
             w += q.b.bytes;
         }
         g.lda = q.a.ld * 2;
         g.ldb = q.b.ld * 2;
-        g.apl = q.a.rows * q.a.ld * 2;
-        g.bpl = q.b.rows * q.b.ld * 2;
+        g.apl = q.a.lay_out || !p.A_lo ? q.a.rows * q.a.ld * 2 : (const char*)p.A_lo - g.A;
+        g.bpl = q.b.lay_out || !p.B_lo ? q.b.rows * q.b.ld * 2 : (const char*)p.B_lo - g.B;
         g.M = (int)p.M;
         g.N = (int)(p.gate == GATE_FORWARD ? p.N / 2 : p.N);
         g.up = g.N * g.ldb;
@@ -374,6 +379,8 @@ hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws,
             g.pb = 0u | 2u << 4 | 1u << 8 | 0u << 12 | 1u << 16 | 0u << 20;
         } else if (q.nseg == 3) {
             g.pa = 2u | 1u << 4 | 0u << 8;
+        } else if (q.nseg == 2) {
+            (q.a.planes == 2 ? g.pa : g.pb) = 1u | 0u << 4;
         }
         g.tiles_m = (int)q.tiles_m;
         g.tiles_n = (int)q.tiles_n;

@@ -25,7 +25,8 @@ struct GemmArgs {
 };
 
 struct Operand {
-    bool planes, lay_out;
+    int planes;               // 16-bit parts: 3 of fp32, 2 of a value and what its rounding left
+    bool lay_out;
     int64_t rows, cols, ld;   // as laid out in memory
     size_t bytes;             // in the workspace
 };
@@ -67,6 +68,7 @@ __device__ __forceinline__ void for_each_index(std::integer_sequence<int, I...>,
 enum : int { FORWARD = 0, INPUT = 1, WEIGHT = 2, GATED = 3, HIDDEN = 4 };
 constexpr bool a_is_col(int kind) { return kind == WEIGHT; }
 constexpr bool b_is_col(int kind) { return kind == INPUT || kind == WEIGHT || kind == HIDDEN; }
+constexpr int HIDDEN_COLS = 64;   // HIDDEN's N is a multiple of a wave's columns in every tile
 
 // What an epilogue reads for columns n .. n + 7, whichever the row.
 struct OfColumn {
@@ -168,6 +170,12 @@ __device__ __forceinline__ void finish_hidden8(const Epilogue& e, int64_t N, boo
     store8_dt(e.out, e.out_dt, m * e.ldo, n, N, d[0]);
     store8_dt(e.out, e.out_dt, m * e.ldo + N, n, N, u[0]);
     if (e.a) store8_dt(e.a, e.out_dt, m * e.lda, n, N, g[0]);
+    auto rest = [&](f8 v) { return e.out_dt == DT_BF16 ? rest_of<bf16>(v) : rest_of<f16>(v); };
+    if (e.out_lo) {
+        store8_dt(e.out_lo, e.out_dt, m * e.ldo, n, N, rest(d[0]));
+        store8_dt(e.out_lo, e.out_dt, m * e.ldo + N, n, N, rest(u[0]));
+    }
+    if (e.a_lo) store8_dt(e.a_lo, e.out_dt, m * e.lda, n, N, rest(g[0]));
 }
 
 // Four sums at a time, as the matrix cores leave them: lane l has columns n .. n + 3, n = 4 (l / 16)
@@ -491,35 +499,23 @@ __device__ __forceinline__ void epilogue_gated(const GemmArgs& g, float* part, i
 }
 
 // Four neighbouring pre-activations as loaded: fp32, T, or of an 8-bit copy.
-template <bool EDGE, typename T>
+template <typename T>
 struct RawQuad {
     typedef unsigned u4 __attribute__((ext_vector_type(4)));
     typedef unsigned u2 __attribute__((ext_vector_type(2)));
     u4 w;
-    __device__ __forceinline__ void load(const void* z, int dt, int64_t ldz, const Packed& p, int64_t m, int64_t n, int64_t N) {
+    __device__ __forceinline__ void load(const void* z, int dt, int64_t ldz, const Packed& p, int64_t m, int64_t n,
+                                         int64_t N) {
         if (p.q) {
             struct __attribute__((packed, aligned(1))) Bytes4 {
                 unsigned w;
             };
-            const int8_t* q = p.q + m * p.ldq;
-            w[0] = 0;
-            w[1] = 127;
-            if (EDGE && n >= N) return;
-            w[1] = p.s[m * ((N + 31) / 32) + (n >> 5)];
-            if (!EDGE || n + 4 <= N) w[0] = reinterpret_cast<const Bytes4*>(q + n)->w;
-            else
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (n + i < N) w[0] |= (unsigned)(uint8_t)q[n + i] << (8 * i);
+            w[0] = reinterpret_cast<const Bytes4*>(p.q + m * p.ldq + n)->w;
+            w[1] = p.s[m * (N / 32) + (n >> 5)];
         } else if (dt == DT_F32) {
-            w = __builtin_bit_cast(u4, load4<EDGE>((const float*)z + m * ldz, n, N));
+            w = __builtin_bit_cast(u4, load4<false>((const float*)z + m * ldz, n, N));
         } else {
-            typename VecOf<T, 4>::plain v;
-            const T* row = (const T*)z + m * ldz;
-            if (!EDGE || n + 4 <= N) v = *reinterpret_cast<const typename VecOf<T, 4>::type*>(row + n);
-            else
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = n + i < N ? row[n + i] : (T)0.f;
+            const typename VecOf<T, 4>::plain v = *reinterpret_cast<const typename VecOf<T, 4>::type*>((const T*)z + m * ldz + n);
             const u2 b = __builtin_bit_cast(u2, v);
             w[0] = b[0];
             w[1] = b[1];
@@ -540,14 +536,15 @@ struct RawQuad {
 };
 
 // The gradient da of a gated layer's output becomes dz and a; the pre-activations of the next sixteen rows are on their
-// way while these are worked on.
-template <typename T, bool EDGE, bool STREAM, int MT, int NTL>
+// way while these are worked on. N is a multiple of the columns that a wave has (HIDDEN_COLS), so a wave has them all or
+// none: with checks for each column this code would be twice as long, and a wave runs all of it once a tile.
+template <typename T, bool STREAM, int MT, int NTL>
 __device__ __forceinline__ void epilogue_hidden(const GemmArgs& g, float* part, int lane, int64_t m0, int64_t n,
                                                 v4 (&acc)[MT][NTL]) {
     const Epilogue& e = g.e;
     const int64_t N = g.N;
     const bool packed = e.p.q;
-    RawQuad<EDGE, T> zg[NTL], zu[NTL];
+    RawQuad<T> zg[NTL], zu[NTL];
     auto load = [&](int64_t m) {
         m = min(m, (int64_t)g.M - 1);
 #pragma unroll
@@ -563,7 +560,7 @@ __device__ __forceinline__ void epilogue_hidden(const GemmArgs& g, float* part, 
         if (part) {
             if (m >= g.M) return;
 #pragma unroll
-            for (int j = 0; j < NTL; ++j) store4<EDGE, false>(part + m * N, n + j * 16, N, acc[i][j]);
+            for (int j = 0; j < NTL; ++j) store4<false, false>(part + m * N, n + j * 16, N, acc[i][j]);
             return;
         }
         v4 a[NTL], u[NTL];
@@ -575,9 +572,23 @@ __device__ __forceinline__ void epilogue_hidden(const GemmArgs& g, float* part, 
         if (i + 1 < MT) load(m + 16);
         if (m >= g.M) return;   // the four lanes of a row leave together
         gate_slopes(e.act, a, u, acc[i]);
-        store_quads<EDGE, STREAM, T>(e.out, e.out_dt, m * e.ldo, n, N, lane, acc[i]);
-        store_quads<EDGE, STREAM, T>(e.out, e.out_dt, m * e.ldo + N, n, N, lane, u);
-        if (e.a) store_quads<EDGE, STREAM, T>(e.a, e.out_dt, m * e.lda, n, N, lane, a);
+        store_quads<false, STREAM, T>(e.out, e.out_dt, m * e.ldo, n, N, lane, acc[i]);
+        store_quads<false, STREAM, T>(e.out, e.out_dt, m * e.ldo + N, n, N, lane, u);
+        if (e.a) store_quads<false, STREAM, T>(e.a, e.out_dt, m * e.lda, n, N, lane, a);
+        auto rest = [&](v4 (&v)[NTL]) {
+#pragma unroll
+            for (int j = 0; j < NTL; ++j) v[j] = rest_of<T>(v[j]);
+        };
+        if (e.out_lo) {
+            rest(acc[i]);
+            rest(u);
+            store_quads<false, STREAM, T>(e.out_lo, e.out_dt, m * e.ldo, n, N, lane, acc[i]);
+            store_quads<false, STREAM, T>(e.out_lo, e.out_dt, m * e.ldo + N, n, N, lane, u);
+        }
+        if (e.a_lo) {
+            rest(a);
+            store_quads<false, STREAM, T>(e.a_lo, e.out_dt, m * e.lda, n, N, lane, a);
+        }
     });
 }
 
@@ -716,14 +727,16 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
 
     float* part = g.splits > 1 ? g.part + (int64_t)k_part * g.M * g.N * (KIND == GATED ? 2 : 1) : nullptr;
     const int m = m0 + wm * (TM / WM) + (lane & 15), n = n0 + wn * (COLS / WN) + 4 * (lane >> 4);
+    if constexpr (KIND == HIDDEN) {
+        if (n < g.N) epilogue_hidden<T, STREAM>(g, part, lane, m, n, acc);
+        return;
+    }
     auto finish = [&](auto edge) {
         constexpr bool EDGE = decltype(edge)::value;
         if constexpr (KIND == GATED) epilogue_gated<T, EDGE, STREAM>(g, part, lane, m, n, acc);
-        else if constexpr (KIND == HIDDEN) epilogue_hidden<T, EDGE, STREAM>(g, part, lane, m, n, acc);
-        else epilogue<T, KIND, EDGE, STREAM>(g, part, lane, m, n, acc);
+        else if constexpr (KIND != HIDDEN) epilogue<T, KIND, EDGE, STREAM>(g, part, lane, m, n, acc);
     };
-    // HIDDEN's is the longest epilogue: its smaller tiles have the one with the checks only
-    if ((KIND != HIDDEN || TM == 256) && n0 + COLS <= g.N) finish(std::false_type());
+    if (n0 + COLS <= g.N) finish(std::false_type());
     else finish(std::true_type());
 }
 

@@ -63,6 +63,7 @@ struct Epilogue {
     Packed p2;
     void* a;             // act(z) z2, where HIDDEN forms it (null: not wanted)
     int64_t lda;
+    void *out_lo, *a_lo; // what out's and a's rounding to 16 bits leaves (null: not wanted), rows ldo and lda apart
 };
 
 // What a product's N columns are.
@@ -83,15 +84,16 @@ struct Product {
     bool b_col;
     Packed bp;  // B as an 8-bit copy (B null)
     int gate;   // GATE_*; N counts what the product has, 2 hidden or hidden
+    const void *A_lo, *B_lo;   // of 16-bit operands, a second part that is added to the first (null: none), at the same strides
 };
 size_t product_workspace_bytes(int dt, const Product& p);
 hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws, hipStream_t st);
 
-// The gate's part of a backward pass. part: gated_bwd_parts(rows, hidden) * 2 * hidden floats (unused if db is null)
+// The gate's part of a backward pass; da is of type da_dt, dt or fp32. Of the epilogue out (dz), z, p, z2, p2, a, out_lo
+// and a_lo are used, and act. part: gated_bwd_parts(rows, hidden) * 2 * hidden floats (unused if db is null)
 int64_t gated_bwd_parts(int64_t rows, int64_t hidden);
-hipError_t launch_gated_act_bwd(int dt, int act, int64_t rows, int64_t hidden, const void* da, int64_t ldda,
-                                const void* zg, const void* zu, int64_t ldz, Packed pg, Packed pu, void* dz, int64_t lddz,
-                                void* a, int64_t lda, float* db, float* part, hipStream_t st);
+hipError_t launch_gated_act_bwd(int dt, int da_dt, int64_t rows, int64_t hidden, const void* da, int64_t ldda,
+                                const Epilogue& e, float* db, float* part, hipStream_t st);
 
 // Dropout's mask; threshold 0: none.
 struct Drop {

@@ -346,6 +346,13 @@ __device__ __forceinline__ void gate_slopes(int act, V (&g)[N], V (&u)[N], V (&d
     }
 }
 
+// What the rounding of v to T leaves.
+template <typename T, typename V>
+__device__ __forceinline__ V rest_of(V v) {
+    typedef typename VecOf<T, sizeof(V) / 4>::plain R;
+    return v - __builtin_convertvector(__builtin_convertvector(v, R), V);
+}
+
 // ---------------------------------------------------------------- sums over a wave
 __device__ __forceinline__ float wave_sum(float v) {
     v += __uint_as_float(dpp<DPP_XOR1>(__float_as_uint(v)));

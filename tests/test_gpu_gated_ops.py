@@ -166,11 +166,22 @@ def test_gated_act_backward(dev, act, dtype, rows, hid):
         holds(db, v.sum(0), E32 * (rows / 4 + 60) * v.abs().sum(0) + e.sum(0) + 1e-30, "db")
         dz2, none, _ = nn.gated_act_backward(da, z, act, want_db=False)
         assert torch.equal(dz2, dz) and none is None
+        if dtype != F32:
+            (d, d_lo), (b, b_lo), _ = nn.gated_act_backward(da, z, act, want_a=True, parts=True)
+            two_parts(d, d_lo, v, e, tiny, "dz"), two_parts(b, b_lo, *a64, tiny, "a")
+            assert torch.equal(d, dz) and torch.equal(b, a)
+
+
+def two_parts(first, second, value, error, tiny, what):
+    """A value in two parts: the second is what the first's rounding leaves, rounded."""
+    u = U[first.dtype]
+    holds(first, value, u * value.abs() + 1.01 * error + tiny, what)
+    holds(first.double() + second.double(), value, (u * u + E32) * value.abs() * 1.02 + 1.01 * error + tiny, what + " in two parts")
 
 
 # (rows, hidden, cout)
-HIDDEN = [(1, 33, 40), (20, 100, 64), (300, 261, 520), (1003, 523, 264), (301, 261, 4104), (1101, 1029, 4104), (2051, 1027, 200),
-          (3001, 3077, 264)]
+HIDDEN = [(1, 33, 40), (20, 128, 64), (20, 100, 64), (300, 256, 520), (1003, 523, 264), (1003, 576, 264), (301, 320, 4104),
+          (301, 261, 4104), (1101, 1088, 4104), (2051, 1024, 200), (3001, 3008, 264), (3001, 3077, 264)]
 
 
 def test_hidden_sizes_run_every_kernel(dev):
@@ -196,19 +207,31 @@ def test_gated_hidden_backward(dev, dtype, rows, hid, cout):
             for pair in (z, packs) if act in ("silu", "gelu") else (z,):
                 g64, u64 = (unpack64(v.q, v.s) for v in pair) if pair is packs else (v.double() for v in pair)
                 dg, du, a64 = gate_slopes64(act, g64, u64, da, ed)
-                dz, a = nn.gated_hidden_backward(dy, w, pair, act, want_a=True)
+                dz, a, _ = nn.gated_hidden_backward(dy, w, pair, act, want_a=True)
                 holds(dz[:, :hid], dg[0], rounded(*dg, dtype, tiny), (act, "dz of the gate"))
                 holds(dz[:, hid:], du[0], rounded(*du, dtype, tiny), (act, "dz of the other"))
                 holds(a, a64[0], rounded(*a64, dtype, tiny), (act, "a"))
-        assert torch.equal(nn.gated_hidden_backward(dy, w, pair, act)[0], dz)
+        # with db, which is formed from a stored da
+        dz2, none, db = nn.gated_hidden_backward(dy, w, pair, act, want_db=True)
+        v, e = torch.cat([dg[0], du[0]], 1), torch.cat([dg[1], du[1]], 1)
+        holds(db, v.sum(0), E32 * (rows / 4 + 60) * v.abs().sum(0) + e.sum(0) + 1e-30, "db")
+        holds(dz2, v, rounded(v, e, dtype, tiny), "dz beside db")
+        assert none is None
+        if dtype != F32:
+            for db in (False, True):
+                (d, d_lo), (b, b_lo), _ = nn.gated_hidden_backward(dy, w, pair, act, want_a=True, want_db=db, parts=True)
+                two_parts(d, d_lo, v, e, tiny, "dz"), two_parts(b, b_lo, *a64, tiny, "a")
+                assert torch.equal(d, dz2 if db else dz)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("rows,dim,hid", [(1, 64, 96), (130, 72, 200), (700, 264, 515)])
 def test_gated_feed_forward_backward(dev, dtype, rows, dim, hid):
-    """Against the formulas, with dz and a as the call rounds them counted."""
+    """Against the formulas, with dz and a counted as the call rounds them: to the data's type for dx and for gradients
+    of that type, in two parts for gradients in float32."""
     from paper_2107_03356_amd import nn
     say("gated feed forward backward", dtype, rows, dim, hid)
+    tiny = TINY[dtype]
     dy, x = rand(dev, 1, rows, dim, dtype=dtype), rand(dev, 2, rows, dim, dtype=dtype)
     w1 = rand(dev, 3, 2 * hid, dim, dtype=dtype, scale=dim ** -0.5)
     w2 = rand(dev, 4, dim, hid, dtype=dtype, scale=hid ** -0.5)
@@ -217,29 +240,58 @@ def test_gated_feed_forward_backward(dev, dtype, rows, dim, hid):
     xp, gamma, beta = nn.pack8(x), rand(dev, 6, dim, at=1, scale=0.2), rand(dev, 7, dim)
     da = dy.double() @ w2.double()
     ed = E32 * growth(dim) * (dy.double().abs() @ w2.double().abs())
-    unfused = U[dtype] * da.abs()   # where db is formed too, da is stored
+    dm = dy.double().abs()
     for z, kept, affine in (((pair[:, :hid], pair[:, hid:]), x, None), (packs, xp, (gamma, None)), (packs, xp, (gamma, beta))):
         g64, u64 = (unpack64(v.q, v.s) for v in z) if z is packs else (v.double() for v in z)
-        x64 = x.double() if affine is None else unpack64(xp.q, xp.s) * gamma.double() + (0 if affine[1] is None else beta.double())
-        for need in ((True, True, False, True, False), (True,) * 5):
-            rough = unfused if need[2] or (affine is not None and affine[1] is not None) else 0
-            (dg, eg), (du, eu), (a, ea) = gate_slopes64("silu", g64, u64, da, ed + rough)
-            dz, ez = torch.cat([dg, du], 1), torch.cat([eg, eu], 1)
-            ez, ea = ez + U[dtype] * (dz.abs() + ez) + TINY[dtype], ea + U[dtype] * (a.abs() + ea) + TINY[dtype]
-            got = nn.gated_feed_forward_backward(dy, kept, w1, w2, z, affine=affine, grad_dtype=F32, need=need)
-            dx = dz @ w1.double()
-            holds(got[0], dx, rounded(dx, (ez + E32 * growth(2 * hid) * dz.abs()) @ w1.double().abs(), dtype, TINY[dtype]), "dx")
-            dw1 = dz.t() @ x64
-            plus = 0 if affine is None else 4 * E32 * growth(rows)   # the affine part's roundings and db's sum
-            holds(got[1], dw1, (ez + (E32 * growth(rows) + E32 + plus) * dz.abs()).t() @ (x64.abs() + (beta.double().abs() if
-                  affine is not None and affine[1] is not None else 0)) * 1.01 + 1e-30, "dw1")
-            dw2 = dy.double().t() @ a
-            holds(got[3], dw2, dy.double().abs().t() @ (ea + (E32 * growth(rows) + E32) * a.abs()) + 1e-30, "dw2")
-            if need[2]:
-                holds(got[2], dz.sum(0), ez.sum(0) + E32 * (rows / 4 + 60) * dz.abs().sum(0), "db1")
-                holds(got[4], dy.double().sum(0), E32 * (rows / 4 + 60) * dy.double().abs().sum(0) + 1e-30, "db2")
-            else:
-                assert got[2] is None and got[4] is None
+        b64 = beta.double() if affine is not None and affine[1] is not None else torch.zeros_like(gamma).double()
+        x64 = x.double() if affine is None else unpack64(xp.q, xp.s) * gamma.double() + b64
+        x_size = x64.abs() if affine is None else unpack64(xp.q, xp.s).abs() * gamma.double().abs() + b64.abs()
+        (dg, eg), (du, eu), (a, ea) = gate_slopes64("silu", g64, u64, da, ed)
+        dz, e = torch.cat([dg, du], 1), torch.cat([eg, eu], 1)
+        for grad in (F32, dtype):
+            step = U[dtype] if grad == dtype else U[dtype] ** 2 + E32
+            ez, eb = (1.02 * step * v.abs() + 1.01 * err + tiny for v, err in ((dz, e), (a, ea)))
+            for need in ((True, True, False, True, False), (True,) * 5):
+                got = nn.gated_feed_forward_backward(dy, kept, w1, w2, z, affine=affine, grad_dtype=grad, need=need)
+                dx, once = dz @ w1.double(), U[dtype] * dz.abs() + 1.01 * e + tiny
+                holds(got[0], dx, rounded(dx, (once + E32 * growth(2 * hid) * dz.abs()) @ w1.double().abs(), dtype, tiny), "dx")
+                # products over the rows (twice as many of two parts), the affine part's roundings and db's sum
+                units = E32 * (2 * growth(rows) + 1 + (0 if affine is None else growth(rows) + rows / 4 + 60))
+                dw1 = dz.t() @ x64
+                holds(got[1], dw1, rounded(dw1, (ez + units * dz.abs()).t() @ x_size, grad, 1e-30 + TINY[grad]), "dw1")
+                dw2 = dy.double().t() @ a
+                holds(got[3], dw2, rounded(dw2, dm.t() @ (eb + units * a.abs()), grad, 1e-30 + TINY[grad]), "dw2")
+                if need[2]:
+                    holds(got[2], dz.sum(0), e.sum(0) * 1.01 + E32 * (rows / 4 + 60) * dz.abs().sum(0) + 1e-30, "db1")
+                    holds(got[4], dy.double().sum(0), E32 * (rows / 4 + 60) * dm.sum(0) + 1e-30, "db2")
+                else:
+                    assert got[2] is None and got[4] is None
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows,cin,cout", [(1, 64, 96), (300, 264, 520), (301, 77, 35), (4000, 520, 1032)])
+def test_weight_gradient_in_two_parts(dev, dtype, rows, cin, cout):
+    from paper_2107_03356_amd import nn
+    say("two parts", dtype, rows, cin, cout)
+    u = U[dtype]
+    d = [rand(dev, 1, rows, cout, dtype=dtype), rand(dev, 2, rows, cout, dtype=dtype, scale=u)]
+    x = [rand(dev, 3, rows, cin, dtype=dtype), rand(dev, 4, rows, cin, dtype=dtype, scale=u)]
+    p, gamma, beta, db = nn.pack8(x[0]), rand(dev, 5, cin), rand(dev, 6, cin), rand(dev, 7, cout)
+    d64, x64 = (sum(v.double() for v in t) for t in (d, x))
+    for dz, low, xx, x_low, affine, want, size in (
+            (d[0], d[1], x[0], None, None, d64.t() @ x[0].double(), d64.abs().t() @ x[0].double().abs()),
+            (d[0], None, x[0], x[1], None, d[0].double().t() @ x64, d[0].double().abs().t() @ x64.abs()),
+            (d[0], d[1], p, None, (gamma, beta), (d64.t() @ unpack64(p.q, p.s)) * gamma.double() + db[:, None].double() * beta.double(),
+             (d64.abs().t() @ unpack64(p.q, p.s).abs()) * gamma.double().abs() + (db[:, None].double() * beta.double()).abs())):
+        for grad in (F32, dtype):
+            dw = nn.linear_backward_weight(dz, xx, affine, db, grad, dz_low=low, x_low=x_low)
+            holds(dw, want, rounded(want, E32 * (2 * growth(rows) + 4) * size, grad, TINY[grad]), (grad, affine is None))
+    with pytest.raises(ValueError):
+        nn.linear_backward_weight(d[0], x[0], dz_low=d[1], x_low=x[1])
+    with pytest.raises(ValueError):
+        nn.linear_backward_weight(d[0], p, x_low=x[1])
+    with pytest.raises(ValueError):
+        nn.linear_backward_weight(d[0], x[0], dz_low=rand(dev, 1, rows, 2 * cout, dtype=dtype)[:, ::2].float())
 
 
 # ---------------------------------------------------------------- between two blocks
