@@ -628,7 +628,7 @@ mfac_status mfac_residual_norm(mfac_dtype type, mfac_dtype wtype, int32_t norms,
  * outputs may be NULL (not wanted); those of parameters (wtype) are sums over the rows. s, or the 8-bit copy of N_pre's xhat (then s
  * and pre_mean are NULL); y may be NULL where neither MFAC_NORM_POST nor a gate's gradient needs it. dy and dres may be
  * ds or dh, dy may be y. The workspace is needed for parameters' gradients. */
-size_t mfac_residual_norm_bwd_workspace_bytes(int32_t norms, int64_t rows, int64_t cols);
+size_t mfac_residual_norm_bwd_workspace_bytes(mfac_dtype type, int32_t norms, int64_t rows, int64_t cols);
 mfac_status mfac_residual_norm_bwd(mfac_dtype type, mfac_dtype wtype, int32_t norms, int64_t rows, int64_t cols,
                                    const void* ds, int64_t ldds, const void* dh, int64_t lddh, const void* y,
                                    int64_t ldy, const float* post_mean, const float* post_rstd, const void* s,

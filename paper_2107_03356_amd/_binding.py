@@ -108,7 +108,7 @@ SIGNATURES = {
     "mfac_residual_norm": (_c.c_int, [_I32, _I32, _I32, _I64, _I64, _VP, _I64, _VP, _VP, _VP, _VP, _I64, _VP, _I64,
                                       _F64, _F64, _VP, _VP, _VP, _F64, _VP, _I64, _VP, _I64, _VP, _VP, _VP, _VP, _VP,
                                       _I64, _VP, _VP]),
-    "mfac_residual_norm_bwd_workspace_bytes": (_SZ, [_I32, _I64, _I64]),
+    "mfac_residual_norm_bwd_workspace_bytes": (_SZ, [_I32, _I32, _I64, _I64]),
     "mfac_residual_norm_bwd": (_c.c_int, [_I32, _I32, _I32, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _VP,
                                           _I64, _VP, _I64, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _I64, _F64, _F64, _VP,
                                           _VP, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _VP, _VP, _VP, _VP, _SZ,

@@ -330,9 +330,10 @@ MFAC_API mfac_status mfac_residual_norm(mfac_dtype type, mfac_dtype wtype, int32
     return done(launch_residual(type, wtype, g, stream));
 }
 
-MFAC_API size_t mfac_residual_norm_bwd_workspace_bytes(int32_t norms, int64_t rows, int64_t cols) {
-    if (!norms_ok(norms) || rows < 0 || rows > MOST || cols < 1 || cols > MOST_HELD) return 0;
-    return (size_t)round_up(residual_bwd_parts(std::max<int64_t>(rows, 1), cols) * residual_sums(norms) * cols * 4, 256);
+MFAC_API size_t mfac_residual_norm_bwd_workspace_bytes(mfac_dtype type, int32_t norms, int64_t rows,
+                                                       int64_t cols) {
+    if (!type_ok(type) || !norms_ok(norms) || rows < 0 || rows > MOST || cols < 1 || cols > MOST_HELD) return 0;
+    return (size_t)round_up(residual_bwd_parts(type, std::max<int64_t>(rows, 1), cols) * residual_sums(norms) * cols * 4, 256);
 }
 
 MFAC_API mfac_status mfac_residual_norm_bwd(mfac_dtype type, mfac_dtype wtype, int32_t norms, int64_t rows, int64_t cols,
@@ -377,7 +378,7 @@ MFAC_API mfac_status mfac_residual_norm_bwd(mfac_dtype type, mfac_dtype wtype, i
     }
     if (dpost_w || dpost_b || dgate || dpre_w || dpre_b) {
         const mfac_status e =
-            check_workspace(mfac_residual_norm_bwd_workspace_bytes(norms, rows, cols), workspace, workspace_bytes);
+            check_workspace(mfac_residual_norm_bwd_workspace_bytes(type, norms, rows, cols), workspace, workspace_bytes);
         if (e != MFAC_OK) return e;
     }
     g.norms = norms;

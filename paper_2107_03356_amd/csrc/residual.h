@@ -1,5 +1,5 @@
-// Shared by the kernels of what lies between two blocks (residual_fwd.h, residual_bwd.h): which norms there are,
-// parameters, the ends of rows, the threads that a row takes.
+// Shared by the kernels of what lies between two blocks (residual_fwd.h, residual_bwd.h): which norms there are, the
+// threads that a row takes, rows of any length eight values at a time, parameters.
 #pragma once
 
 #include <algorithm>
@@ -37,16 +37,28 @@ void by_norms(int norms, F f) {
     }
 }
 
-// f(constant of the threads that hold a row, eight values each). Two chunks of eight a thread take twice the registers, and
-// 16384 columns by 1024 threads would spill up to 900 bytes a lane: wider rows than these have kernels of their own.
-constexpr int64_t HELD_COLS = 8192;
-template <typename F>
+// f(constant of the threads that hold a row, constant of the chunks of eight values that each has). Wider rows, whose chunks
+// would be past the registers, have kernels of their own, which rows of fewer than eight values run through as well.
+inline bool in_registers(int64_t cols) { return cols >= 8 && cols <= 8192; }
+template <typename T, typename F>
 void by_threads(int64_t cols, F f) {
-    if (cols <= 512) f(constant<64>());
-    else if (cols <= 1024) f(constant<128>());
-    else if (cols <= 2048) f(constant<256>());
-    else if (cols <= 4096) f(constant<512>());
-    else f(constant<1024>());
+    constexpr int C = sizeof(T) == 2 ? 2 : 1;
+    if (cols <= 512) f(constant<64>(), constant<1>());
+    else if (cols <= 1024) f(constant<128 / C>(), constant<C>());
+    else if (cols <= 2048) f(constant<256 / C>(), constant<C>());
+    else if (cols <= 4096) f(constant<512 / C>(), constant<C>());
+    else f(constant<1024 / C>(), constant<C>());
+}
+// Rows that a work-group has at a time.
+inline int64_t rows_at_a_time(int dt, int64_t cols) {
+    return !in_registers(cols) ? 1 : cols <= (dt == DT_F32 ? 512 : 1024) ? 4 : 1;
+}
+// The first row of this thread's wave, as a scalar: addresses of rows are then scalars too.
+template <int NT>
+__device__ __forceinline__ int64_t first_row() {
+    constexpr int RPB = norm_block(NT) / NT;
+    if constexpr (RPB == 1) return blockIdx.x;
+    return (int64_t)blockIdx.x * RPB + __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
 }
 
 __device__ __forceinline__ f8 fill8(float v) { return f8{v, v, v, v, v, v, v, v}; }
@@ -56,7 +68,77 @@ __device__ __forceinline__ void zero_past(f8& v, int64_t c, int64_t cols) {
         for (int i = 0; i < 8; ++i)
             if (c + i >= cols) v[i] = 0.f;
 }
-// Columns c .. c + 7 of a parameter, or `absent` where there is none.
+
+// Eight neighbouring values of a row as loaded, where a row has at least eight: the thread at the row's end loads the last eight
+// and moves what is its own to the front, zeros behind it, which takes no branch and no address of its own for each value.
+struct Place {
+    unsigned at;  // of the load
+    int shift;    // values in it that are another thread's, 8: all
+    bool ragged;  // some thread of the wave has one
+};
+__device__ __forceinline__ Place place_of(int c, int64_t cols) {
+    const int at = min(c, (int)cols - 8), shift = min(c - at, 8);
+    return {(unsigned)at, shift, __any(shift != 0) != 0};
+}
+template <int N>
+struct Words {
+    typedef unsigned type __attribute__((ext_vector_type(N)));
+};
+// N words, `by` words (0 to N) towards the front.
+template <int N>
+__device__ __forceinline__ typename Words<N>::type move_words(typename Words<N>::type w, int by) {
+#pragma unroll
+    for (int step = N; step > 0; step /= 2)
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = by & step ? (i + step < N ? w[i + step] : 0u) : w[i];
+    return w;
+}
+template <typename T>
+struct Row8 {
+    static constexpr int N = 2 * sizeof(T);
+    typename Words<N>::type w;
+    __device__ __forceinline__ void load(const T* __restrict__ row, const Place& p) {
+        const typename VecOf<T, 8>::plain v = *reinterpret_cast<const typename VecOf<T, 8>::type*>(row + p.at);
+        w = __builtin_bit_cast(typename Words<N>::type, v);
+        if (!p.ragged) return;
+        if constexpr (sizeof(T) == 4) {
+            w = move_words<N>(w, p.shift);
+        } else {
+            w = move_words<N>(w, p.shift / 2);
+            if (p.shift & 1)
+#pragma unroll
+                for (int i = 0; i < N; ++i) w[i] = __builtin_amdgcn_alignbit(i + 1 < N ? w[i + 1] : 0u, w[i], 16);
+        }
+    }
+    // of an 8-bit copy: q, and the group's byte in the third word
+    __device__ __forceinline__ void load_copy(const int8_t* __restrict__ q, const uint8_t* __restrict__ s, int c,
+                                              const Place& p) {
+        const Bytes8 b = *reinterpret_cast<const Bytes8*>(q + p.at);
+        uint64_t v = (uint64_t)b.hi << 32 | b.lo;
+        if (p.ragged) v = p.shift < 8 ? v >> (8 * p.shift) : 0;
+        w[0] = (unsigned)v;
+        w[1] = (unsigned)(v >> 32);
+        w[2] = s[min((unsigned)c, p.at + 7) >> 5];   // a thread past the end reads the last
+    }
+    __device__ __forceinline__ f8 get() const {
+        return __builtin_convertvector(__builtin_bit_cast(typename VecOf<T, 8>::plain, w), f8);
+    }
+    __device__ __forceinline__ f8 get_copy() const { return RawPacked8{{w[0], w[1]}, w[2]}.get(); }
+};
+
+// Columns c .. c + 7 of a parameter of type wt, T or fp32, or `absent` where there is none.
+template <typename T>
+__device__ __forceinline__ f8 load_param(const void* p, int wt, const Place& at, float absent) {
+    if (!p) return fill8(absent);
+    if (wt == DT_F32) {
+        Row8<float> v;
+        v.load((const float*)p, at);
+        return v.get();
+    }
+    Row8<T> v;
+    v.load((const T*)p, at);
+    return v.get();
+}
 __device__ __forceinline__ f8 load_param(const void* p, int wt, int64_t c, int64_t cols, float absent) {
     return p ? load8_dt(p, wt, 0, c, cols) : fill8(absent);
 }

@@ -13,30 +13,31 @@ extern template hipError_t residual_bwd<f16>(int, const Residual&, const Residua
 
 namespace {
 
-// Joins the work-groups' column sums in order, a work-group to 64 columns, its 16 waves every 16th part each. blockIdx.y 0:
-// the pre norm's gradients; 1: those behind the post norm, from P and Q.
+// Joins the work-groups' column sums in order. A work-group has 16 columns, its 64 groups of 16 threads every 64th part each:
+// with 64 columns to one, as where only one sum a column is joined, 1000 columns of 1024 parts took 23 us, what
+// 32 CUs can read. blockIdx.y 0: the pre norm's gradients; 1: those behind the post norm, from P and Q.
 template <typename TW>
 __global__ __launch_bounds__(1024) void k_residual_params(const float* __restrict__ part, int64_t nparts, int sums,
                                                           int64_t cols, bool post, const TW* w1, const TW* b1,
                                                           const TW* gate, TW* dw1, TW* db1, TW* dgate, TW* dw2, TW* db2) {
-    __shared__ float of[2][16][64];
-    const int which = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    __shared__ float of[2][64][17];
+    const int which = blockIdx.y, lane = threadIdx.x & 15, group = threadIdx.x >> 4;
+    const int64_t c = (int64_t)blockIdx.x * 16 + lane;
     float p = 0.f, q = 0.f;
     if (c < cols) {
         const float* at = part + which * cols + c;
 #pragma unroll 8
-        for (int64_t i = wave; i < nparts; i += 16) {
+        for (int64_t i = group; i < nparts; i += 64) {
             p += at[i * sums * cols];
             if (sums > 2) q += at[(i * sums + 2) * cols];
         }
     }
-    of[0][wave][lane] = p;
-    of[1][wave][lane] = q;
+    of[0][group][lane] = p;
+    of[1][group][lane] = q;
     __syncthreads();
-    if (wave != 0 || c >= cols) return;
+    if (threadIdx.x >= 16 || c >= cols) return;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) {
+    for (int i = 1; i < 64; ++i) {
         p += of[0][i][lane];
         q += of[1][i][lane];
     }
@@ -56,21 +57,22 @@ __global__ __launch_bounds__(1024) void k_residual_params(const float* __restric
 }
 
 template <typename TW>
-void params(const Residual& g, const ResidualBwd& b, hipStream_t st) {
+void params(int dt, const Residual& g, const ResidualBwd& b, hipStream_t st) {
     const bool post = g.norms & POST_NORM;
-    k_residual_params<TW><<<dim3((unsigned)ceil_div(g.cols, 64), 2), 1024, 0, st>>>(
-        b.part, g.rows > 0 ? residual_bwd_parts(g.rows, g.cols) : 0, residual_sums(g.norms), g.cols, post,
+    k_residual_params<TW><<<dim3((unsigned)ceil_div(g.cols, 16), 2), 1024, 0, st>>>(
+        b.part, g.rows > 0 ? residual_bwd_parts(dt, g.rows, g.cols) : 0, residual_sums(g.norms), g.cols, post,
         (const TW*)(post ? g.w1 : nullptr), (const TW*)(post ? g.b1 : nullptr), (const TW*)g.gate, (TW*)b.dw1, (TW*)b.db1,
         (TW*)b.dgate, (TW*)b.dw2, (TW*)b.db2);
 }
 
 }  // namespace
 
-// Work-groups of the backward pass, each with its column sums: two waves to a SIMD; four for narrow rows, whose sums are small.
-int64_t residual_bwd_parts(int64_t rows, int64_t cols) {
-    const int64_t per = cols <= 512 ? 4 : 1;
-    const int64_t grid = cols > 4096 ? 256 : cols > 2048 ? 512 : 1024;
-    return std::min(ceil_div(rows, per), grid);
+// Work-groups of the backward pass, each with its column sums: as many as are on the card at once (eight waves to a CU), and no
+// more than one to four of the rows that it has at a time, since their sums are written and read again.
+int64_t residual_bwd_parts(int dt, int64_t rows, int64_t cols) {
+    const int64_t turns = ceil_div(rows, rows_at_a_time(dt, cols));
+    const int64_t waves = !in_registers(cols) ? 16 : cols <= 1024 ? 4 : ceil_div(cols, dt == DT_F32 ? 2048 : 4096) * 4;
+    return std::max(int64_t(1), std::min(ceil_div(turns, 4), 256 * std::max(int64_t(1), 8 / waves)));
 }
 // dw_pre and P; for layer norms db_pre and Q too.
 int residual_sums(int norms) { return norms & LAYER_NORM ? 4 : 2; }
@@ -90,9 +92,9 @@ hipError_t launch_residual_bwd(int dt, int wt, const Residual& g, const Residual
         if (e != hipSuccess) return e;
     }
     if (!(b.dw1 || b.db1 || b.dw2 || b.db2 || b.dgate)) return hipSuccess;
-    if (wt == DT_F32) params<float>(g, k, st);
-    else if (wt == DT_BF16) params<bf16>(g, k, st);
-    else params<f16>(g, k, st);
+    if (wt == DT_F32) params<float>(dt, g, k, st);
+    else if (wt == DT_BF16) params<bf16>(dt, g, k, st);
+    else params<f16>(dt, g, k, st);
     return hipGetLastError();
 }
 

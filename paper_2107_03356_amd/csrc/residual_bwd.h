@@ -16,17 +16,6 @@
 namespace mfac {
 namespace {
 
-// s or the 8-bit copy of its xhat, as loaded.
-template <typename T>
-struct RawStream {
-    Raw8<T> s;
-    RawPacked8 q;
-    __device__ __forceinline__ void load(const Residual& g, int64_t row, int64_t c, int64_t ngroups) {
-        if (g.p.q) q.load(g.p.q + row * g.p.ldq, g.p.s + row * ngroups, c, g.cols);
-        else s.load((const T*)g.s + row * g.lds, c, g.cols);
-    }
-};
-
 __device__ __forceinline__ f8 xhat_of(f8 x, float mean, float rstd, int64_t c, int64_t cols) {
     x = (x - mean) * rstd;
     zero_past(x, c, cols);
@@ -46,103 +35,151 @@ __device__ __forceinline__ void row_means(float& a, float& b, float inv_cols, fl
     b *= inv_cols;
 }
 
-template <typename T, int NT, int NORMS>
-__global__ __launch_bounds__(norm_block(NT)) void k_residual_bwd(Residual g, ResidualBwd b, int wt) {
+template <typename T, int NT, int NCH, int NORMS>
+__global__ __launch_bounds__(norm_block(NT), 2) void k_residual_bwd(Residual g, ResidualBwd b, int wt) {
     constexpr int RPB = norm_block(NT) / NT;
     constexpr bool POST = NORMS & POST_NORM, PRE = NORMS & PRE_NORM, LAYER = NORMS & LAYER_NORM;
     constexpr int SUMS = LAYER ? 4 : 2;
     __shared__ float red[4 * (NT / 64)];
-    __shared__ __attribute__((aligned(32))) float cols_of[RPB > 1 ? SUMS : 1][RPB > 1 ? RPB * NT * 8 : 1];
+    __shared__ __attribute__((aligned(32))) float cols_of[RPB > 1 ? SUMS : 1][RPB > 1 ? RPB * NT * NCH * 8 : 1];
     int turn = 0;
     const int t = threadIdx.x % NT;
-    const int64_t c = t * 8, cols = g.cols, ngroups = (cols + 31) / 32;
+    const int64_t cols = g.cols, ngroups = (cols + 31) / 32;
     const int64_t step = (int64_t)gridDim.x * RPB;
     const float inv_cols = 1.f / (float)cols;
-    int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / NT;
-    Raw8<T> dh, ds, y, gate;
-    RawStream<T> s;
+    int64_t row = first_row<NT>();
+    Place at[NCH];
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) at[j] = place_of((j * NT + t) * 8, cols);
+    // the next row is on its way while one is worked on
+    Row8<T> dh[NCH], ds[NCH], y[NCH], gate[NCH], s[NCH];   // s, or the 8-bit copy of its xhat
     float mean1 = 0.f, rstd1 = 0.f, mean2 = 0.f, rstd2 = 0.f;
-    auto load = [&](int64_t at) {
+    auto load = [&](int64_t row) {
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            if constexpr (PRE) {
+                dh[j].load((const T*)b.dh + row * b.lddh, at[j]);
+                if (g.p.q) s[j].load_copy(g.p.q + row * g.p.ldq, g.p.s + row * ngroups, (j * NT + t) * 8, at[j]);
+                else s[j].load((const T*)g.s + row * g.lds, at[j]);
+            }
+            if (b.ds) ds[j].load((const T*)b.ds + row * b.ldds, at[j]);
+            if (g.y) y[j].load((const T*)g.y + row * g.ldy, at[j]);
+            if (g.gates) gate[j].load((const T*)g.gates + row * g.ldgates, at[j]);
+        }
         if constexpr (PRE) {
-            dh.load((const T*)b.dh + at * b.lddh, c, cols);
-            s.load(g, at, c, ngroups);
-            rstd2 = g.rstd2[at];
-            if (LAYER && !g.p.q) mean2 = g.mean2[at];
+            rstd2 = g.rstd2[row];
+            if (LAYER && !g.p.q) mean2 = g.mean2[row];
         }
-        if (b.ds) ds.load((const T*)b.ds + at * b.ldds, c, cols);
-        if (g.y) y.load((const T*)g.y + at * g.ldy, c, cols);
         if constexpr (POST) {
-            rstd1 = g.rstd1[at];
-            if (LAYER) mean1 = g.mean1[at];
+            rstd1 = g.rstd1[row];
+            if (LAYER) mean1 = g.mean1[row];
         }
-        if (g.gates) gate.load((const T*)g.gates + at * g.ldgates, c, cols);
     };
     if (row < g.rows) load(row);
-    f8 w2 = fill8(0.f), w1 = load_param(POST ? g.w1 : nullptr, wt, c, cols, 1.f);
-    if constexpr (PRE) w2 = load_param(g.w2, wt, c, cols, 1.f);
-    if (g.gate) w1 *= load8_dt(g.gate, wt, 0, c, cols);
+    f8 w1[NCH], w2[PRE ? NCH : 1], sum[SUMS][NCH];   // dw_pre, P, db_pre, Q
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+        w1[j] = load_param<T>(g.gate, wt, at[j], 1.f) * load_param<T>(POST ? g.w1 : nullptr, wt, at[j], 1.f);
+        if constexpr (PRE) w2[j] = load_param<T>(g.w2, wt, at[j], 1.f);
+#pragma unroll
+        for (int i = 0; i < SUMS; ++i) sum[i][j] = fill8(0.f);
+    }
     DropKey key{};
     if (g.drop.threshold) key = drop_key(g.drop);
-    f8 sum[SUMS];   // dw_pre, P, db_pre, Q
-#pragma unroll
-    for (int i = 0; i < SUMS; ++i) sum[i] = fill8(0.f);
     for (; row < g.rows; row += step) {
-        f8 d = fill8(0.f), h = d, xh2 = d, xh1 = d, by = d;
-        if (b.ds) d = ds.get();
-        if constexpr (PRE) {
-            h = dh.get();
-            xh2 = g.p.q ? s.q.get() : xhat_of(s.s.get(), mean2, rstd2, c, cols);
+        Row8<T> dh_now[NCH], ds_now[NCH], y_now[NCH], gate_now[NCH], s_now[NCH];   // made fp32 where they are used
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            dh_now[j] = dh[j];
+            ds_now[j] = ds[j];
+            y_now[j] = y[j];
+            gate_now[j] = gate[j];
+            s_now[j] = s[j];
         }
-        if (g.y) xh1 = y.get();
-        if constexpr (POST) xh1 = xhat_of(xh1, mean1, rstd1, c, cols);
-        if (g.gates) by = gate.get();
-        const float r1 = rstd1, r2 = rstd2;
+        const float r1 = rstd1, r2 = rstd2, mu1 = mean1, mu2 = mean2;
         if (row + step < g.rows) load(row + step);
+        f8 d[NCH], xh[NCH];
         if constexpr (PRE) {
-            sum[0] += h * xh2;
-            if constexpr (LAYER) sum[2] += h;
-            h *= w2;
-            float m1 = sum8(h), m2 = sum8(h * xh2);
-            row_means<NT, LAYER>(m1, m2, inv_cols, red, turn);
-            d += (h - m1 - xh2 * m2) * r2;
-            if constexpr (LAYER) zero_past(d, c, cols);   // m1 is everywhere
-        }
-        if (b.dr) store8((T*)b.dr + row * b.lddr, c, cols, g.scale * d);
-        if (g.drop.threshold) d = drop8(g.drop, key, (unsigned)row, (unsigned)(c >> 3), d);
-        if (g.gates) {   // there is no gate for each channel: w1 is N_post's
-            if (b.dgates) {
-                f8 n = xh1;
-                if constexpr (POST) n *= w1;
-                if constexpr (POST && LAYER) n += load_param(g.b1, wt, c, cols, 0.f);
-                store8((T*)b.dgates + row * b.lddgates, c, cols, d * n);
+            float m1 = 0.f, m2 = 0.f;
+#pragma unroll
+            for (int j = 0; j < NCH; ++j) {
+                const int c = (j * NT + t) * 8;
+                f8 h = dh_now[j].get();
+                xh[j] = g.p.q ? s_now[j].get_copy() : xhat_of(s_now[j].get(), mu2, r2, c, cols);
+                sum[0][j] += h * xh[j];
+                if constexpr (LAYER) sum[2][j] += h;
+                h *= w2[j];
+                m1 += sum8(h);
+                m2 += sum8(h * xh[j]);
+                d[j] = h;
+                __builtin_amdgcn_sched_barrier(0);
             }
-            d *= by;
-        }
-        sum[1] += d * xh1;
-        if constexpr (LAYER) sum[3] += d;
-        d *= w1;
-        if constexpr (POST) {
-            float m1 = sum8(d), m2 = sum8(d * xh1);
             row_means<NT, LAYER>(m1, m2, inv_cols, red, turn);
-            d = (d - m1 - xh1 * m2) * r1;
+#pragma unroll
+            for (int j = 0; j < NCH; ++j) {
+                d[j] = (d[j] - m1 - xh[j] * m2) * r2;
+                if constexpr (LAYER) zero_past(d[j], (j * NT + t) * 8, cols);   // m1 is everywhere
+                if (b.ds) d[j] += ds_now[j].get();
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NCH; ++j) d[j] = ds_now[j].get();   // there is one without N_pre
         }
-        if (b.dy) store8((T*)b.dy + row * b.lddy, c, cols, d);
+        float n1 = 0.f, n2 = 0.f;
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            const int c = (j * NT + t) * 8;
+            if (b.dr) store8((T*)b.dr + row * b.lddr, c, cols, g.scale * d[j]);
+            if (g.drop.threshold) d[j] = drop8(g.drop, key, (unsigned)row, (unsigned)(c >> 3), d[j]);
+            xh[j] = fill8(0.f);
+            if (g.y) xh[j] = y_now[j].get();
+            if constexpr (POST) xh[j] = xhat_of(xh[j], mu1, r1, c, cols);
+            if (g.gates) {   // there is no gate for each channel: w1 is N_post's
+                if (b.dgates) {
+                    f8 n = xh[j];
+                    if constexpr (POST) n *= w1[j];
+                    if constexpr (POST && LAYER) n += load_param<T>(g.b1, wt, at[j], 0.f);
+                    store8((T*)b.dgates + row * b.lddgates, c, cols, d[j] * n);
+                }
+                d[j] *= gate_now[j].get();
+            }
+            sum[1][j] += d[j] * xh[j];
+            if constexpr (LAYER) sum[3][j] += d[j];
+            d[j] *= w1[j];
+            n1 += sum8(d[j]);
+            n2 += sum8(d[j] * xh[j]);
+            __builtin_amdgcn_sched_barrier(0);   // one chunk's mask after the other's: together they take 20 registers more
+        }
+        if constexpr (POST) row_means<NT, LAYER>(n1, n2, inv_cols, red, turn);
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            if constexpr (POST) d[j] = (d[j] - n1 - xh[j] * n2) * r1;
+            if (b.dy) store8((T*)b.dy + row * b.lddy, (j * NT + t) * 8, cols, d[j]);
+        }
     }
     if (!b.part) return;
     float* out = b.part + (int64_t)blockIdx.x * SUMS * cols;
     if constexpr (RPB > 1) {   // joined over the waves, each of which has rows of its own
 #pragma unroll
-        for (int i = 0; i < SUMS; ++i) *reinterpret_cast<f8*>(&cols_of[i][threadIdx.x * 8]) = sum[i];
+        for (int i = 0; i < SUMS; ++i)
+#pragma unroll
+            for (int j = 0; j < NCH; ++j)
+                *reinterpret_cast<f8*>(&cols_of[i][((threadIdx.x / NT * NCH + j) * NT + t) * 8]) = sum[i][j];
         __syncthreads();
         const int i = threadIdx.x / NT;   // a wave to each sum
         if (i >= SUMS) return;
-        f8 v = *reinterpret_cast<const f8*>(&cols_of[i][t * 8]);
 #pragma unroll
-        for (int r = 1; r < RPB; ++r) v += *reinterpret_cast<const f8*>(&cols_of[i][(r * NT + t) * 8]);
-        store8(out + i * cols, c, cols, v);
+        for (int j = 0; j < NCH; ++j) {
+            f8 v = *reinterpret_cast<const f8*>(&cols_of[i][(j * NT + t) * 8]);
+#pragma unroll
+            for (int r = 1; r < RPB; ++r) v += *reinterpret_cast<const f8*>(&cols_of[i][((r * NCH + j) * NT + t) * 8]);
+            store8(out + i * cols, (j * NT + t) * 8, cols, v);
+        }
     } else {
 #pragma unroll
-        for (int i = 0; i < SUMS; ++i) store8(out + i * cols, c, cols, sum[i]);
+        for (int i = 0; i < SUMS; ++i)
+#pragma unroll
+            for (int j = 0; j < NCH; ++j) store8(out + i * cols, (j * NT + t) * 8, cols, sum[i][j]);
     }
 }
 
@@ -250,16 +287,17 @@ __global__ __launch_bounds__(1024) void k_residual_bwd_wide(Residual g, Residual
 
 template <typename T>
 hipError_t residual_bwd(int wt, const Residual& g, const ResidualBwd& b, hipStream_t st) {
-    const unsigned grid = (unsigned)residual_bwd_parts(g.rows, g.cols);
+    constexpr int DT = sizeof(T) == 4 ? DT_F32 : DT_BF16;
+    const unsigned grid = (unsigned)residual_bwd_parts(DT, g.rows, g.cols);
     by_norms(g.norms, [&](auto norms) {
         constexpr int NORMS = decltype(norms)::value;
-        if (g.cols > HELD_COLS) {
+        if (!in_registers(g.cols)) {
             k_residual_bwd_wide<T, NORMS><<<grid, 1024, (size_t)round_up(g.cols, 8) * 4, st>>>(g, b, wt);
             return;
         }
-        by_threads(g.cols, [&](auto nt) {
+        by_threads<T>(g.cols, [&](auto nt, auto nch) {
             constexpr int NT = decltype(nt)::value;
-            k_residual_bwd<T, NT, NORMS><<<grid, norm_block(NT), 0, st>>>(g, b, wt);
+            k_residual_bwd<T, NT, decltype(nch)::value, NORMS><<<grid, norm_block(NT), 0, st>>>(g, b, wt);
         });
     });
     return hipGetLastError();

@@ -6,8 +6,8 @@
 //
 // N is rms norm, x / sqrt(mean(x^2) + eps) w, or layer norm, (x - mean) / sqrt(mean((x - mean)^2) + eps) w + b.
 //
-// A row lives in the registers of NT threads, eight neighbouring values each, so every input is read once and s is not
-// read again for h, which is formed from s before its rounding. A gate for each channel is folded into N_post's weight
+// A row lives in the registers of NT threads (NCH chunks of eight neighbouring values each), so every input is read once and s
+// is not read again for h, which is formed from s before its rounding. A gate for each channel is folded into N_post's weight
 // and bias: gate drop(xhat w + b) = drop(xhat (gate w) + gate b).
 #pragma once
 
@@ -17,67 +17,95 @@ namespace mfac {
 namespace {
 
 // The row's mean (0 for rms norm) and 1 / sqrt(variance + eps) of values v, which become xhat; zeros past the end.
-template <int NT, bool LAYER>
-__device__ __forceinline__ void normalise(f8& v, const Residual& g, int64_t c, float* red, int& turn, float& mean,
+template <int NT, int NCH, bool LAYER>
+__device__ __forceinline__ void normalise(f8 (&v)[NCH], const Residual& g, int t, float* red, int& turn, float& mean,
                                           float& rstd) {
     mean = 0.f;
+    float sum = 0.f;
     if constexpr (LAYER) {
-        mean = row_sum<NT>(sum8(v), red, turn) / (float)g.cols;   // by division: a row of equal values has that mean
-        v -= mean;
-        zero_past(v, c, g.cols);
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) sum += sum8(v[j]);
+        mean = row_sum<NT>(sum, red, turn) / (float)g.cols;   // by division: a row of equal values has that mean
+        sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            v[j] -= mean;
+            zero_past(v[j], (j * NT + t) * 8, g.cols);
+        }
     }
-    rstd = 1.f / sqrtf(row_sum<NT>(sum8(v * v), red, turn) / (float)g.cols + g.eps);
-    v *= rstd;
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) sum += sum8(v[j] * v[j]);
+    rstd = 1.f / sqrtf(row_sum<NT>(sum, red, turn) / (float)g.cols + g.eps);
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) v[j] *= rstd;
 }
 
-template <typename T, int NT, int NORMS>
+template <typename T, int NT, int NCH, int NORMS>
 __global__ __launch_bounds__(norm_block(NT)) void k_residual_fwd(Residual g, int wt) {
     constexpr int RPB = norm_block(NT) / NT;
     constexpr bool POST = NORMS & POST_NORM, PRE = NORMS & PRE_NORM, LAYER = NORMS & LAYER_NORM;
     __shared__ float red[2 * (NT / 64)];
     int turn = 0;
     const int t = threadIdx.x % NT;
-    const int64_t c = t * 8;
     const int64_t step = (int64_t)gridDim.x * RPB, ngroups = (g.cols + 31) / 32;
-    int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / NT;
+    int64_t row = first_row<NT>();
+    Place at[NCH];
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) at[j] = place_of((j * NT + t) * 8, g.cols);
     // the next row is on its way while one is worked on
-    Raw8<T> y, r, gate;
-    auto load = [&](int64_t at) {
-        y.load((const T*)g.y + at * g.ldy, c, g.cols);
-        if (g.r) r.load((const T*)g.r + at * g.ldr, c, g.cols);
-        if (g.gates) gate.load((const T*)g.gates + at * g.ldgates, c, g.cols);
+    Row8<T> y[NCH], r[NCH], gate[NCH];
+    auto load = [&](int64_t row) {
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            y[j].load((const T*)g.y + row * g.ldy, at[j]);
+            if (g.r) r[j].load((const T*)g.r + row * g.ldr, at[j]);
+            if (g.gates) gate[j].load((const T*)g.gates + row * g.ldgates, at[j]);
+        }
     };
     if (row < g.rows) load(row);
-    f8 w1 = load_param(POST ? g.w1 : nullptr, wt, c, g.cols, 1.f), b1 = fill8(0.f), w2 = b1, b2 = b1;
-    if constexpr (POST && LAYER) b1 = load_param(g.b1, wt, c, g.cols, 0.f);
-    if (g.gate) {
-        const f8 v = load8_dt(g.gate, wt, 0, c, g.cols);
-        w1 *= v;
-        b1 *= v;
+    f8 w1[NCH], b1[POST && LAYER ? NCH : 1], w2[PRE ? NCH : 1], b2[PRE && LAYER ? NCH : 1];
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+        const f8 by = load_param<T>(g.gate, wt, at[j], 1.f);
+        w1[j] = by * load_param<T>(POST ? g.w1 : nullptr, wt, at[j], 1.f);
+        if constexpr (POST && LAYER) b1[j] = by * load_param<T>(g.b1, wt, at[j], 0.f);
+        if constexpr (PRE) w2[j] = load_param<T>(g.w2, wt, at[j], 1.f);
+        if constexpr (PRE && LAYER) b2[j] = load_param<T>(g.b2, wt, at[j], 0.f);
     }
-    if constexpr (PRE) w2 = load_param(g.w2, wt, c, g.cols, 1.f);
-    if constexpr (PRE && LAYER) b2 = load_param(g.b2, wt, c, g.cols, 0.f);
     DropKey key{};
     if (g.drop.threshold) key = drop_key(g.drop);
     for (; row < g.rows; row += step) {
-        f8 v = y.get(), add = fill8(0.f), by = add;
-        if (g.r) add = g.scale * r.get();
-        if (g.gates) by = gate.get();
+        f8 v[NCH];
+        Row8<T> r_now[NCH], gate_now[NCH];   // made fp32 where they are used
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            v[j] = y[j].get();
+            r_now[j] = r[j];
+            gate_now[j] = gate[j];
+        }
         if (row + step < g.rows) load(row + step);
         float mean1, rstd1, mean2, rstd2;
-        if constexpr (POST) normalise<NT, LAYER>(v, g, c, red, turn, mean1, rstd1);
-        v *= w1;
-        if constexpr (POST && LAYER) v += b1;
-        if (g.drop.threshold) v = drop8(g.drop, key, (unsigned)row, (unsigned)(c >> 3), v);
-        if (g.gates) v *= by;
-        if (g.r) v += add;
-        if (g.s) store8((T*)g.s + row * g.lds, c, g.cols, v);
+        if constexpr (POST) normalise<NT, NCH, LAYER>(v, g, t, red, turn, mean1, rstd1);
+#pragma unroll
+        for (int j = 0; j < NCH; ++j) {
+            const int c = (j * NT + t) * 8;
+            v[j] *= w1[j];
+            if constexpr (POST && LAYER) v[j] += b1[j];
+            if (g.drop.threshold) v[j] = drop8(g.drop, key, (unsigned)row, (unsigned)(c >> 3), v[j]);
+            if (g.gates) v[j] *= gate_now[j].get();
+            if (g.r) v[j] += g.scale * r_now[j].get();
+            if (g.s) store8((T*)g.s + row * g.lds, c, g.cols, v[j]);
+        }
         if constexpr (PRE) {
-            normalise<NT, LAYER>(v, g, c, red, turn, mean2, rstd2);
-            if (g.p.q) pack_group(g.p.q + row * g.p.ldq, g.p.s + row * ngroups, c, g.cols, v);
-            v *= w2;
-            if constexpr (LAYER) v += b2;
-            store8((T*)g.h + row * g.ldh, c, g.cols, v);
+            normalise<NT, NCH, LAYER>(v, g, t, red, turn, mean2, rstd2);
+#pragma unroll
+            for (int j = 0; j < NCH; ++j) {
+                const int c = (j * NT + t) * 8;
+                if (g.p.q) pack_group(g.p.q + row * g.p.ldq, g.p.s + row * ngroups, c, g.cols, v[j]);
+                v[j] *= w2[j];
+                if constexpr (LAYER) v[j] += b2[j];
+                store8((T*)g.h + row * g.ldh, c, g.cols, v[j]);
+            }
         }
         if (t == 0) {
             if (POST && g.mean1) g.mean1[row] = mean1;
@@ -160,15 +188,15 @@ template <typename T>
 hipError_t residual_fwd(int wt, const Residual& g, hipStream_t st) {
     by_norms(g.norms, [&](auto norms) {
         constexpr int NORMS = decltype(norms)::value;
-        if (g.cols > HELD_COLS) {
+        if (!in_registers(g.cols)) {
             const size_t lds = (size_t)round_up(g.cols, 32) * 4;
             k_residual_fwd_wide<T, NORMS><<<(unsigned)std::min<int64_t>(g.rows, 1024), 1024, lds, st>>>(g, wt);
             return;
         }
-        by_threads(g.cols, [&](auto nt) {
+        by_threads<T>(g.cols, [&](auto nt, auto nch) {
             constexpr int NT = decltype(nt)::value;
             const unsigned grid = (unsigned)std::min(ceil_div(g.rows, norm_block(NT) / NT), int64_t(2048));
-            k_residual_fwd<T, NT, NORMS><<<grid, norm_block(NT), 0, st>>>(g, wt);
+            k_residual_fwd<T, NT, decltype(nch)::value, NORMS><<<grid, norm_block(NT), 0, st>>>(g, wt);
         });
     });
     return hipGetLastError();

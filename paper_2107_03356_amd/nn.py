@@ -734,14 +734,15 @@ def residual_norm_backward(ds, dh, y, s, post_stats=None, pre_stats=None, post=N
     dy = _like(like) if need_y or (same and need_r) else None
     dr = dy if same else _like(like) if need_r else None
     wanted = [v is not None and need_params for v in (w1, b1, w2, b2)] + [gv is not None and need_gate]
+    t = _type(d2, "residual_norm: ds, dh")
     grads, ws = [None] * 5, (None, 0, None)
     if any(wanted):
         dtype = next(v.dtype for v in (w1, b1, w2, b2, gv) if v is not None)
         parts = iter(torch.empty((sum(wanted), cols), dtype=dtype, device=like.device).unbind(0))
         grads = [next(parts) if on else None for on in wanted]
-        ws = _workspace(_function("mfac_residual_norm_bwd_workspace_bytes")(norms, rows, cols), like.device)
+        ws = _workspace(_function("mfac_residual_norm_bwd_workspace_bytes")(t, norms, rows, cols), like.device)
     dg = _like(gate) if gm is not None and need_gate else None
-    _call("mfac_residual_norm_bwd", like.device, _type(d2, "residual_norm: ds, dh"), wt, norms, rows, cols, *_mat(ds),
+    _call("mfac_residual_norm_bwd", like.device, t, wt, norms, rows, cols, *_mat(ds),
           *_mat(dh), *_mat(y), _ptr(m1), _ptr(r1), *sm, *packed, _ptr(m2), _ptr(r2), _ptr(w1), _ptr(b1), _ptr(gv),
           *_mat(gm), float(scale), p, ptr, _ptr(w2), _ptr(dy), cols, None if same else _ptr(dr), cols, _ptr(dg), cols,
           _ptr(grads[0]), _ptr(grads[1]), _ptr(grads[4]), _ptr(grads[2]), _ptr(grads[3]), ws[0], ws[1])
