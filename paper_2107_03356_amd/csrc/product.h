@@ -498,96 +498,104 @@ __device__ __forceinline__ void epilogue_gated(const GemmArgs& g, float* part, i
     });
 }
 
-// Four neighbouring pre-activations as loaded: fp32, T, or of an 8-bit copy.
+// Eight neighbouring pre-activations as loaded: fp32, T, or of an 8-bit copy.
 template <typename T>
-struct RawQuad {
+struct RawEight {
+    typedef unsigned u8 __attribute__((ext_vector_type(8)));
     typedef unsigned u4 __attribute__((ext_vector_type(4)));
-    typedef unsigned u2 __attribute__((ext_vector_type(2)));
-    u4 w;
+    u8 w;
     __device__ __forceinline__ void load(const void* z, int dt, int64_t ldz, const Packed& p, int64_t m, int64_t n,
                                          int64_t N) {
         if (p.q) {
-            struct __attribute__((packed, aligned(1))) Bytes4 {
-                unsigned w;
-            };
-            w[0] = reinterpret_cast<const Bytes4*>(p.q + m * p.ldq + n)->w;
-            w[1] = p.s[m * (N / 32) + (n >> 5)];
+            const Bytes8 b = *reinterpret_cast<const Bytes8*>(p.q + m * p.ldq + n);
+            w[0] = b.lo;
+            w[1] = b.hi;
+            w[2] = p.s[m * (N / 32) + (n >> 5)];
         } else if (dt == DT_F32) {
-            w = __builtin_bit_cast(u4, load4<false>((const float*)z + m * ldz, n, N));
+            const VecOf<float, 8>::plain v = *reinterpret_cast<const VecOf<float, 8>::type*>((const float*)z + m * ldz + n);
+            w = __builtin_bit_cast(u8, v);
         } else {
-            const typename VecOf<T, 4>::plain v = *reinterpret_cast<const typename VecOf<T, 4>::type*>((const T*)z + m * ldz + n);
-            const u2 b = __builtin_bit_cast(u2, v);
-            w[0] = b[0];
-            w[1] = b[1];
+            const typename VecOf<T, 8>::plain v = *reinterpret_cast<const typename VecOf<T, 8>::type*>((const T*)z + m * ldz + n);
+            const u4 b = __builtin_bit_cast(u4, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = b[i];
         }
     }
-    __device__ __forceinline__ v4 get(bool packed, int dt) const {
-        if (packed) {
-            const float s = unpack_scale(w[1]);
-            v4 r;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] = (float)(int8_t)(w[0] >> (8 * i)) * s;
-            return r;
-        }
-        if (dt == DT_F32) return __builtin_bit_cast(v4, w);
-        const u2 b = {w[0], w[1]};
-        return __builtin_convertvector(__builtin_bit_cast(typename VecOf<T, 4>::plain, b), v4);
+    __device__ __forceinline__ f8 get(bool packed, int dt) const {
+        if (packed) return RawPacked8{{w[0], w[1]}, w[2]}.get();
+        if (dt == DT_F32) return __builtin_bit_cast(f8, w);
+        const u4 b = {w[0], w[1], w[2], w[3]};
+        return __builtin_convertvector(__builtin_bit_cast(typename VecOf<T, 8>::plain, b), f8);
     }
 };
+template <bool STREAM, typename T>
+__device__ __forceinline__ void store_eight(void* p, int dt, int64_t off, f8 v) {
+    if (dt == DT_F32) put<STREAM>(v, reinterpret_cast<VecOf<float, 8>::type*>((float*)p + off));
+    else put<STREAM>(__builtin_convertvector(v, typename VecOf<T, 8>::plain), reinterpret_cast<typename VecOf<T, 8>::type*>((T*)p + off));
+}
 
-// The gradient da of a gated layer's output becomes dz and a; the pre-activations of the next sixteen rows are on their
-// way while these are worked on. N is a multiple of the columns that a wave has (HIDDEN_COLS), so a wave has them all or
+// The gradient da of a gated layer's output becomes dz and a. The sums of two tiles of 16 columns are exchanged first, so that
+// a lane has eight neighbours and takes 16 bytes of z at a time; the pre-activations of the next sixteen rows are on
+// their way while these are worked on. N is a multiple of the columns that a wave has (HIDDEN_COLS), so a wave has them all or
 // none: with checks for each column this code would be twice as long, and a wave runs all of it once a tile.
 template <typename T, bool STREAM, int MT, int NTL>
 __device__ __forceinline__ void epilogue_hidden(const GemmArgs& g, float* part, int lane, int64_t m0, int64_t n,
                                                 v4 (&acc)[MT][NTL]) {
+    constexpr int H = NTL / 2;
     const Epilogue& e = g.e;
     const int64_t N = g.N;
     const bool packed = e.p.q;
-    RawQuad<T> zg[NTL], zu[NTL];
-    auto load = [&](int64_t m) {
-        m = min(m, (int64_t)g.M - 1);
-#pragma unroll
-        for (int j = 0; j < NTL; ++j) {
-            zg[j].load(e.z, e.io_dt, e.ldz, e.p, m, n + j * 16, N);
-            zu[j].load(e.z2, e.io_dt, e.ldz, e.p2, m, n + j * 16, N);
-        }
-    };
-    if (!part) load(m0);
-    for_each_index(std::make_integer_sequence<int, MT>(), [&](auto tag) {
-        constexpr int i = decltype(tag)::value;
-        const int64_t m = m0 + i * 16;
-        if (part) {
+    if (part) {
+        for_each_index(std::make_integer_sequence<int, MT>(), [&](auto tag) {
+            constexpr int i = decltype(tag)::value;
+            const int64_t m = m0 + i * 16;
             if (m >= g.M) return;
 #pragma unroll
             for (int j = 0; j < NTL; ++j) store4<false, false>(part + m * N, n + j * 16, N, acc[i][j]);
-            return;
-        }
-        v4 a[NTL], u[NTL];
+        });
+        return;
+    }
+    n += (lane >> 4 & 1) * 12;   // an odd l / 16: 16 further, less 4
+    RawEight<T> zg[H], zu[H];
+    auto load = [&](int64_t m) {
+        m = min(m, (int64_t)g.M - 1);
 #pragma unroll
-        for (int j = 0; j < NTL; ++j) {
+        for (int j = 0; j < H; ++j) {
+            zg[j].load(e.z, e.io_dt, e.ldz, e.p, m, n + j * 32, N);
+            zu[j].load(e.z2, e.io_dt, e.ldz, e.p2, m, n + j * 32, N);
+        }
+    };
+    load(m0);
+    for_each_index(std::make_integer_sequence<int, MT>(), [&](auto tag) {
+        constexpr int i = decltype(tag)::value;
+        const int64_t m = m0 + i * 16;
+        f8 d[H], a[H], u[H];
+#pragma unroll
+        for (int j = 0; j < H; ++j) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                unsigned x = __float_as_uint(acc[i][2 * j][k]), y = __float_as_uint(acc[i][2 * j + 1][k]);
+                swap_rows(x, y);
+                d[j][k] = __uint_as_float(x);
+                d[j][4 + k] = __uint_as_float(y);
+            }
             a[j] = zg[j].get(packed, e.io_dt);
             u[j] = zu[j].get(packed, e.io_dt);
         }
         if (i + 1 < MT) load(m + 16);
-        if (m >= g.M) return;   // the four lanes of a row leave together
-        gate_slopes(e.act, a, u, acc[i]);
-        store_quads<false, STREAM, T>(e.out, e.out_dt, m * e.ldo, n, N, lane, acc[i]);
-        store_quads<false, STREAM, T>(e.out, e.out_dt, m * e.ldo + N, n, N, lane, u);
-        if (e.a) store_quads<false, STREAM, T>(e.a, e.out_dt, m * e.lda, n, N, lane, a);
-        auto rest = [&](v4 (&v)[NTL]) {
+        if (m >= g.M) return;
+        gate_slopes(e.act, a, u, d);
 #pragma unroll
-            for (int j = 0; j < NTL; ++j) v[j] = rest_of<T>(v[j]);
-        };
-        if (e.out_lo) {
-            rest(acc[i]);
-            rest(u);
-            store_quads<false, STREAM, T>(e.out_lo, e.out_dt, m * e.ldo, n, N, lane, acc[i]);
-            store_quads<false, STREAM, T>(e.out_lo, e.out_dt, m * e.ldo + N, n, N, lane, u);
-        }
-        if (e.a_lo) {
-            rest(a);
-            store_quads<false, STREAM, T>(e.a_lo, e.out_dt, m * e.lda, n, N, lane, a);
+        for (int j = 0; j < H; ++j) {
+            const int64_t at = m * e.ldo + n + j * 32, at_a = m * e.lda + n + j * 32;
+            store_eight<STREAM, T>(e.out, e.out_dt, at, d[j]);
+            store_eight<STREAM, T>(e.out, e.out_dt, at + N, u[j]);
+            if (e.a) store_eight<STREAM, T>(e.a, e.out_dt, at_a, a[j]);
+            if (e.out_lo) {
+                store_eight<STREAM, T>(e.out_lo, e.out_dt, at, rest_of<T>(d[j]));
+                store_eight<STREAM, T>(e.out_lo, e.out_dt, at + N, rest_of<T>(u[j]));
+            }
+            if (e.a_lo) store_eight<STREAM, T>(e.a_lo, e.out_dt, at_a, rest_of<T>(a[j]));
         }
     });
 }
@@ -752,6 +760,7 @@ hipError_t run_product(const Product& p, const Plan& q, const GemmArgs& g, hipSt
     constexpr int WM = KIND == GATED ? 4 : 2;
     if (q.tile == 64) k_product<T, KIND, 64, 64, WM, 4 / WM, 3, false><<<grid, 256, 0, st>>>(g);
     else if (q.tile == 128) k_product<T, KIND, 128, 128, 2, 2, 2, false><<<grid, 256, 0, st>>>(g);
+    else if constexpr (KIND == HIDDEN) k_product<T, KIND, 256, 256, 2, 4, 2, false><<<grid, 512, 0, st>>>(g);
     else if (!streams(p, q, g.e.out_dt)) k_product<T, KIND, 256, 256, 2, 4, 2, false><<<grid, 512, 0, st>>>(g);
     else k_product<T, KIND, 256, 256, 2, 4, 2, true><<<grid, 512, 0, st>>>(g);
     return hipGetLastError();
