@@ -549,44 +549,31 @@ mfac_status mfac_gated_linear(mfac_dtype type, mfac_dtype btype, mfac_act act, i
                               int64_t ldy, void* zg, void* zu, int64_t ldz, int8_t* qg, uint8_t* sg, int8_t* qu,
                               uint8_t* su, int64_t ldq, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
-/* The gate's part of its backward pass, from da, the gradient of y, and the
- * pre-activations (matrices or copies):
- *   dz = [da zu act'(zg), da act(zg)] (rows x 2 hidden) rounded to type,
- *   a = act(zg) zu (NULL: not wanted),
- *   db = the 2 hidden column sums of dz in fp32, before the rounding (NULL: not wanted),
- *   dz_lo, a_lo (of dz's and a's strides, 16-bit types only, NULL: not wanted) = what the rounding of dz and
- *   a to type leaves, rounded to type, for gradients of weights that are wanted in
- *   fp32 (mfac_linear_bwd_weight_parts).
- * The gradients of x and W are those of a linear layer with cout = 2 hidden. */
-size_t mfac_gated_act_bwd_workspace_bytes(int64_t rows, int64_t hidden);
-mfac_status mfac_gated_act_bwd(mfac_dtype type, mfac_act act, int64_t rows, int64_t hidden, const void* da, int64_t ldda,
-                               const void* zg, const void* zu, int64_t ldz, const int8_t* qg, const uint8_t* sg,
-                               const int8_t* qu, const uint8_t* su, int64_t ldq, void* dz, void* dz_lo, int64_t lddz,
-                               void* a, void* a_lo, int64_t lda, float* db, void* workspace, size_t workspace_bytes,
-                               hipStream_t stream);
-
-/* The same behind the layer that follows, a W2^T with W2 (cout x hidden): from dy (rows
- * x cout), the gradient of that layer's output, da = dy W2 is formed and not rounded; without db and where hidden
- * is a multiple of 64 it is not stored either. */
-size_t mfac_gated_hidden_bwd_workspace_bytes(mfac_dtype type, int64_t rows, int64_t hidden, int64_t cout, const void* dy,
-                                             int64_t lddy, const void* w, int64_t ldw, int32_t want_db);
-mfac_status mfac_gated_hidden_bwd(mfac_dtype type, mfac_act act, int64_t rows, int64_t hidden, int64_t cout,
-                                  const void* dy, int64_t lddy, const void* w, int64_t ldw, const void* zg,
-                                  const void* zu, int64_t ldz, const int8_t* qg, const uint8_t* sg, const int8_t* qu,
-                                  const uint8_t* su, int64_t ldq, void* dz, void* dz_lo, int64_t lddz, void* a,
-                                  void* a_lo, int64_t lda, float* db, void* workspace, size_t workspace_bytes,
-                                  hipStream_t stream);
-
-/* mfac_linear_bwd_weight for 16-bit data of which dz (dz + dz_lo) or x (x + x_lo) comes in two parts, one of the two; the
- * second part has the first's strides. */
-size_t mfac_linear_bwd_weight_parts_workspace_bytes(mfac_dtype type, int64_t rows, int64_t cin, int64_t cout,
-                                                    const void* dz, const void* dz_lo, int64_t lddz, const void* x,
-                                                    const void* x_lo, int64_t ldx);
-mfac_status mfac_linear_bwd_weight_parts(mfac_dtype type, mfac_dtype gtype, int64_t rows, int64_t cin, int64_t cout,
-                                         const void* dz, const void* dz_lo, int64_t lddz, const void* x,
-                                         const void* x_lo, int64_t ldx, const int8_t* q, int64_t ldq, const uint8_t* s,
-                                         const float* gamma, const float* beta, const float* db, void* dw, int64_t lddw,
-                                         void* workspace, size_t workspace_bytes, hipStream_t stream);
+/* Its backward pass, by itself (cout 0: dy is the gradient of y, rows x hidden) or with that of the layer y W2^T that follows
+ * (dy is rows x cout, W2 cout x hidden; that layer's bias has the column sums of dy). From the pre-activations (matrices or
+ * copies), with da = dy W2, or dy,
+ *   dz = [da zu act'(zg), da act(zg)], a = act(zg) zu,
+ *   dx = dz W, dw1 = dz^T x (gtype), db1 = column sums of dz in fp32, dw2 = dy^T a (gtype);
+ * those that are NULL are not formed, nor what they alone need. da is not rounded. dz and a are rounded to `type` for the products;
+ * for dw1 and dw2 of 16-bit data in fp32 (gtype) they are taken in two parts, the second what the first's
+ * rounding leaves. x, or its 8-bit copy (q, s; x NULL), and W1 (w1) are needed for dw1 and dx. gamma and beta (cin fp32
+ * values each; beta may be NULL) say that x stands for gamma x + beta in dw1. The workspace query takes, besides
+ * addresses that are not read (x NULL: a copy), what is wanted as bits. */
+#define MFAC_GATED_DX 1u
+#define MFAC_GATED_DW1 2u
+#define MFAC_GATED_DB1 4u
+#define MFAC_GATED_DW2 8u
+#define MFAC_GATED_BETA 16u /* beta is given */
+size_t mfac_gated_bwd_workspace_bytes(mfac_dtype type, mfac_dtype gtype, int64_t rows, int64_t cin, int64_t hidden,
+                                      int64_t cout, const void* dy, int64_t lddy, const void* w2, int64_t ldw2,
+                                      const void* x, int64_t ldx, const void* w1, int64_t ldw1, uint32_t wanted);
+mfac_status mfac_gated_bwd(mfac_dtype type, mfac_dtype gtype, mfac_act act, int64_t rows, int64_t cin, int64_t hidden,
+                           int64_t cout, const void* dy, int64_t lddy, const void* w2, int64_t ldw2, const void* x,
+                           int64_t ldx, const int8_t* q, int64_t ldq, const uint8_t* s, const float* gamma,
+                           const float* beta, const void* w1, int64_t ldw1, const void* zg, const void* zu, int64_t ldz,
+                           const int8_t* qg, const uint8_t* sg, const int8_t* qu, const uint8_t* su, int64_t ldqz,
+                           void* dx, int64_t lddx, void* dw1, int64_t lddw1, float* db1, void* dw2, int64_t lddw2,
+                           void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* Dropout. at: two int64 in device memory, seed and offset, 8-byte aligned, read when the kernel runs (so a captured graph
  * takes what they hold when it is replayed). Element (row, c) of a matrix takes half-word c % 8 of the
@@ -640,7 +627,7 @@ mfac_status mfac_residual_norm_bwd(mfac_dtype type, mfac_dtype wtype, int32_t no
                                    void* dpre_b, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* How the products of a gated layer are run, as mfac_linear_plan: the layer itself, or with `hidden_bwd` != 0 the product of
- * mfac_gated_hidden_bwd (cin is then its cout). */
+ * mfac_gated_bwd that forms dz (cin is then its cout). */
 mfac_status mfac_gated_plan(mfac_dtype type, int32_t hidden_bwd, int64_t rows, int64_t cin, int64_t hidden,
                             int32_t plan[3]);
 

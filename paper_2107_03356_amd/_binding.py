@@ -27,6 +27,7 @@ MFAC_STATIC_TRACE = 1
 MFAC_STATIC_FP32 = 2
 MFAC_F32, MFAC_BF16, MFAC_F16 = 0, 1, 2
 MFAC_PRODUCT_FORWARD, MFAC_PRODUCT_INPUT, MFAC_PRODUCT_WEIGHT = range(3)
+MFAC_GATED_DX, MFAC_GATED_DW1, MFAC_GATED_DB1, MFAC_GATED_DW2, MFAC_GATED_BETA = 1, 2, 4, 8, 16
 MFAC_NORM_POST, MFAC_NORM_PRE, MFAC_NORM_LAYER = 1, 2, 4
 MFAC_ACT_NONE, MFAC_ACT_RELU, MFAC_ACT_GELU, MFAC_ACT_GELU_TANH, MFAC_ACT_SILU = range(5)
 
@@ -95,15 +96,11 @@ SIGNATURES = {
     "mfac_gated_linear_workspace_bytes": (_SZ, [_I32, _I64, _I64, _I64, _VP, _I64, _VP, _I64]),
     "mfac_gated_linear": (_c.c_int, [_I32, _I32, _I32, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _I64, _VP, _VP,
                                      _I64, _VP, _VP, _VP, _VP, _I64, _VP, _SZ, _VP]),
-    "mfac_gated_act_bwd_workspace_bytes": (_SZ, [_I64, _I64]),
-    "mfac_gated_act_bwd": (_c.c_int, [_I32, _I32, _I64, _I64, _VP, _I64, _VP, _VP, _I64, _VP, _VP, _VP, _VP, _I64, _VP,
-                                      _VP, _I64, _VP, _VP, _I64, _VP, _VP, _SZ, _VP]),
-    "mfac_gated_hidden_bwd_workspace_bytes": (_SZ, [_I32, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _I32]),
-    "mfac_gated_hidden_bwd": (_c.c_int, [_I32, _I32, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _I64, _VP, _VP,
-                                         _VP, _VP, _I64, _VP, _VP, _I64, _VP, _VP, _I64, _VP, _VP, _SZ, _VP]),
-    "mfac_linear_bwd_weight_parts_workspace_bytes": (_SZ, [_I32, _I64, _I64, _I64, _VP, _VP, _I64, _VP, _VP, _I64]),
-    "mfac_linear_bwd_weight_parts": (_c.c_int, [_I32, _I32, _I64, _I64, _I64, _VP, _VP, _I64, _VP, _VP, _I64, _VP, _I64,
-                                                _VP, _VP, _VP, _VP, _VP, _I64, _VP, _SZ, _VP]),
+    "mfac_gated_bwd_workspace_bytes": (_SZ, [_I32, _I32, _I64, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP,
+                                             _I64, _c.c_uint32]),
+    "mfac_gated_bwd": (_c.c_int, [_I32, _I32, _I32, _I64, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64,
+                                  _VP, _VP, _VP, _VP, _I64, _VP, _VP, _I64, _VP, _VP, _VP, _VP, _I64, _VP, _I64, _VP,
+                                  _I64, _VP, _VP, _I64, _VP, _SZ, _VP]),
     "mfac_dropout": (_c.c_int, [_I32, _I64, _I64, _VP, _I64, _F64, _VP, _VP, _I64, _VP]),
     "mfac_residual_norm": (_c.c_int, [_I32, _I32, _I32, _I64, _I64, _VP, _I64, _VP, _VP, _VP, _VP, _I64, _VP, _I64,
                                       _F64, _F64, _VP, _VP, _VP, _F64, _VP, _I64, _VP, _I64, _VP, _VP, _VP, _VP, _VP,

@@ -23,9 +23,6 @@ bool act_ok(int a) { return a >= MFAC_ACT_NONE && a <= MFAC_ACT_SILU; }
 bool gated_ok(int64_t rows, int64_t cin, int64_t hidden) {
     return rows >= 0 && rows <= MOST && cin >= 1 && cin <= MOST_WIDTH && hidden >= 1 && hidden <= MOST_WIDTH / 2;
 }
-bool layer_ok(int64_t rows, int64_t cin, int64_t cout) {
-    return rows >= 0 && rows <= MOST && cin >= 1 && cin <= MOST_WIDTH && cout >= 1 && cout <= MOST_WIDTH;
-}
 bool aligned(const void* p, int type) { return (uintptr_t)p % (type == MFAC_F32 ? 4 : 2) == 0; }
 bool matrix_ok(const void* p, int type, int64_t ld, int64_t cols) {
     return p && ld >= cols && ld <= (int64_t(1) << 33) && aligned(p, type);
@@ -47,18 +44,6 @@ mfac_status check_workspace(size_t need, const void* ws, size_t bytes) {
 Product gated_product(int64_t rows, int64_t cin, int64_t hidden, const void* x, int64_t ldx, const void* w, int64_t ldw) {
     return Product{rows, 2 * hidden, cin, x, ldx, false, w, ldw, false, Packed{}, GATE_FORWARD};
 }
-Product hidden_product(int64_t rows, int64_t hidden, int64_t cout, const void* dy, int64_t lddy, const void* w, int64_t ldw) {
-    return Product{rows, hidden, cout, dy, lddy, false, w, ldw, true, Packed{}, GATE_HIDDEN};
-}
-
-Product da_product(int64_t rows, int64_t hidden, int64_t cout, const void* dy, int64_t lddy, const void* w, int64_t ldw) {
-    return Product{rows, hidden, cout, dy, lddy, false, w, ldw, true, Packed{}};
-}
-Product weight_product(int64_t rows, int64_t cin, int64_t cout, const void* dz, const void* dz_lo, int64_t lddz,
-                       const void* x, const void* x_lo, int64_t ldx, Packed p) {
-    return Product{cout, cin, rows, dz, lddz, true, x, ldx, true, p, GATE_NONE, dz_lo, x_lo};
-}
-
 // Both pre-activations as tensors, or both as copies; `absent_ok`: or neither.
 bool pair_ok(int type, int64_t hidden, const void* zg, const void* zu, int64_t ldz, const void* qg, const void* sg,
              const void* qu, const void* su, int64_t ldq, bool absent_ok) {
@@ -72,46 +57,100 @@ Packed packed(const int8_t* q, int64_t ldq, const uint8_t* s) {
     return Packed{const_cast<int8_t*>(q), ldq, const_cast<uint8_t*>(s)};
 }
 
-// What forms dz and a from da.
-Epilogue gate_epilogue(int type, int act, const void* zg, const void* zu, int64_t ldz, Packed pg, Packed pu, void* dz,
-                       void* dz_lo, int64_t lddz, void* a, void* a_lo, int64_t lda) {
-    Epilogue e{};
-    e.out_dt = e.io_dt = type;
-    e.act = act;
-    e.out = dz;
-    e.out_lo = dz_lo;
-    e.ldo = lddz;
-    e.z = const_cast<void*>(zg);
-    e.z2 = const_cast<void*>(zu);
-    e.ldz = ldz;
-    e.p = pg;
-    e.p2 = pu;
-    e.a = a;
-    e.a_lo = a_lo;
-    e.lda = lda;
-    return e;
-}
-
-// The workspace of mfac_gated_hidden_bwd. Where db is wanted, or hidden is not a multiple of what a wave of the fused
-// product holds, da is formed in fp32 and read again: in the product's epilogue the column sums of dz would have to be joined
-// over the tiles, and the checks for each column would double a code that is run through once a tile. bf16, 8192
-// rows, hidden 8192, cout 2048: TIME_FUSED us fused, TIME_UNFUSED so.
-struct HiddenWorkspace {
+// A gated layer's backward pass: what it takes, what it forms.
+struct GatedBwd {
+    int type, gtype, act;
+    int64_t rows, cin, hidden, cout;   // cout 0: dy is the gradient of the gated layer's own output
+    const void* dy;
+    int64_t lddy;
+    const void* w2;
+    int64_t ldw2;
+    const void* x;
+    int64_t ldx;
+    Packed xp;
+    const float *gamma, *beta;
+    const void* w1;
+    int64_t ldw1;
+    bool dx, dw1, db1, dw2;
+    // places in the workspace: dy as the products take it, da in fp32, dz and a in parts, db and its parts, the products'
     bool fused;
-    size_t product, da, total;
+    int parts;
+    int64_t lddy_in, lddz, lda;
+    size_t dy_in, da, dz, a, db, db_part, product, total;
+
+    bool da_given() const { return cout == 0; }
+    bool sums() const { return db1 || (dw1 && beta); }
+    int64_t dy_part() const { return rows * lddy_in * 2; }
+    int64_t dz_part() const { return rows * lddz * 2; }
+    int64_t a_part() const { return rows * lda * 2; }
+
+    // The products, dy, dz and a being at these addresses.
+    Product da_product(const void* at) const {
+        Product p{rows, hidden, cout, at, dy_laid_out() ? lddy_in : lddy, false, w2, ldw2, true, Packed{},
+                  fused ? GATE_HIDDEN : GATE_NONE};
+        if (dy_laid_out()) p.a_parts = type == MFAC_F32 ? 3 : 1, p.a_part = dy_part();
+        return p;
+    }
+    Product dw2_product(const void* at, const void* a_at) const {
+        Product p{cout, hidden, rows, at, dy_laid_out() ? lddy_in : lddy, true, a_at, lda, true, Packed{}};
+        if (dy_laid_out()) p.a_parts = type == MFAC_F32 ? 3 : 1, p.a_part = dy_part();
+        p.b_parts = parts, p.b_part = a_part();
+        return p;
+    }
+    // dx is of 16-bit data from dz's first part: in two it would be no nearer after its own rounding
+    Product dx_product(const void* dz_at) const {
+        Product p{rows, cin, 2 * hidden, dz_at, lddz, false, w1, ldw1, true, Packed{}};
+        p.a_parts = type == MFAC_F32 ? 3 : 1, p.a_part = dz_part();
+        return p;
+    }
+    Product dw1_product(const void* dz_at) const {
+        Product p{2 * hidden, cin, rows, dz_at, lddz, true, x, ldx, true, xp};
+        p.a_parts = parts, p.a_part = dz_part();
+        return p;
+    }
+    // fp32 is split once for its two products; rows that are not 16-byte aligned are copied once
+    bool dy_laid_out() const {
+        return !da_given() && (type == MFAC_F32 || ((uintptr_t)dy & 15) || lddy % 8 || cout % 8 || lddy > MOST_WIDTH);
+    }
+
+    void place() {
+        fused = parts = 0;
+        lddy_in = round_up(std::max<int64_t>(cout, 1), 8);
+        lddz = round_up(2 * hidden, 8);
+        lda = round_up(hidden, 8);
+        dy_in = da = dz = a = db = db_part = product = total = 0;
+        if (!(dx || dw1 || db1 || dw2)) return;
+        // Gradients of 16-bit weights' data in fp32 are formed from dz and a in two parts: rounded to one, they leave
+        // the gradient 2.3e-3 from 64 bits (relative, 2-norm), in two 3e-6. It doubles these two products.
+        parts = type == MFAC_F32 ? 3 : gtype == MFAC_F32 && (dw1 || dw2) ? 2 : 1;
+        // dz straight from the product that forms da: of 16-bit data, without db, whose sums would have to be joined over the
+        // tiles, and where a wave's columns are all there or none. Otherwise da is stored in fp32 and read again.
+        fused = !da_given() && type != MFAC_F32 && !sums() && hidden % 64 == 0;
+        auto take = [&](size_t bytes) {
+            const size_t at = total;
+            total += (size_t)round_up((int64_t)bytes, 256);
+            return at;
+        };
+        if (dy_laid_out()) dy_in = take((size_t)dy_part() * (type == MFAC_F32 ? 3 : 1));
+        if (!da_given() && !fused) da = take((size_t)rows * hidden * 4);
+        dz = take((size_t)dz_part() * parts);
+        if (dw2) a = take((size_t)a_part() * parts);
+        if (sums()) {
+            db = take((size_t)hidden * 8);
+            db_part = take((size_t)gated_bwd_parts(std::max<int64_t>(rows, 1), hidden) * hidden * 8);
+        }
+        if (rows > 0) {   // one after another in the same place; addresses in the workspace are aligned, and not looked at
+            if (!da_given()) need(da_product(dy_laid_out() ? nullptr : dy));
+            if (dx) need(dx_product(nullptr));
+            if (dw1) need(dw1_product(nullptr));
+            if (dw2) need(dw2_product(dy_laid_out() ? nullptr : dy, nullptr));
+        }
+        const size_t at = total;
+        total += product;
+        product = at;
+    }
+    void need(const Product& p) { product = std::max(product, product_workspace_bytes(type, p)); }
 };
-HiddenWorkspace hidden_workspace(int type, int64_t rows, int64_t hidden, int64_t cout, const void* dy, int64_t lddy,
-                                 const void* w, int64_t ldw, bool want_db) {
-    HiddenWorkspace n{!want_db && hidden % 64 == 0, 0, 0, 0};
-    const Product p = n.fused ? hidden_product(rows, hidden, cout, dy, lddy, w, ldw)
-                              : da_product(rows, hidden, cout, dy, lddy, w, ldw);
-    if (rows > 0) n.product = product_workspace_bytes(type, p);
-    n.total = n.product;
-    if (n.fused) return n;
-    n.da = (size_t)round_up(rows * hidden * 4, 256);
-    n.total += n.da + (want_db ? mfac_gated_act_bwd_workspace_bytes(rows, hidden) : 0);
-    return n;
-}
 
 // p: the probability of a value to be dropped, in units of 2^-16.
 bool drop_of(double p, const int64_t* at, Drop& d) {
@@ -163,118 +202,111 @@ MFAC_API mfac_status mfac_gated_linear(mfac_dtype type, mfac_dtype btype, mfac_a
     return done(launch_product(type, p, e, workspace, stream));
 }
 
-MFAC_API size_t mfac_gated_act_bwd_workspace_bytes(int64_t rows, int64_t hidden) {
-    if (!gated_ok(rows, 1, hidden)) return 0;
-    return (size_t)round_up(gated_bwd_parts(std::max<int64_t>(rows, 1), hidden) * 2 * hidden * 4, 256);
+MFAC_API size_t mfac_gated_bwd_workspace_bytes(mfac_dtype type, mfac_dtype gtype, int64_t rows, int64_t cin, int64_t hidden,
+                                               int64_t cout, const void* dy, int64_t lddy, const void* w2, int64_t ldw2,
+                                               const void* x, int64_t ldx, const void* w1, int64_t ldw1, uint32_t wanted) {
+    if (!type_ok(type) || !param_type_ok(gtype, type) || !gated_ok(rows, cin, hidden) || cout < 0 || cout > MOST_WIDTH ||
+        wanted > 31)
+        return 0;
+    int8_t some;   // an 8-bit copy and a norm's parameters, by their presence alone
+    float one;
+    GatedBwd g{type, gtype, MFAC_ACT_NONE, rows, cin, hidden, cout, dy, lddy, w2, ldw2, x, ldx,
+               x ? Packed{} : Packed{&some, cin, nullptr}, &one, wanted & MFAC_GATED_BETA ? &one : nullptr, w1, ldw1,
+               (wanted & MFAC_GATED_DX) != 0, (wanted & MFAC_GATED_DW1) != 0, (wanted & MFAC_GATED_DB1) != 0,
+               (wanted & MFAC_GATED_DW2) != 0};
+    g.place();
+    return g.total;
 }
 
-MFAC_API mfac_status mfac_gated_act_bwd(mfac_dtype type, mfac_act act, int64_t rows, int64_t hidden, const void* da,
-                                        int64_t ldda, const void* zg, const void* zu, int64_t ldz, const int8_t* qg,
-                                        const uint8_t* sg, const int8_t* qu, const uint8_t* su, int64_t ldq, void* dz,
-                                        void* dz_lo, int64_t lddz, void* a, void* a_lo, int64_t lda, float* db,
-                                        void* workspace, size_t workspace_bytes, hipStream_t stream) {
-    if (!type_ok(type) || !act_ok(act) || !gated_ok(rows, 1, hidden) || !vector_ok(db, MFAC_F32) ||
-        (type == MFAC_F32 && (dz_lo || a_lo)) || (a_lo && !a))
+MFAC_API mfac_status mfac_gated_bwd(mfac_dtype type, mfac_dtype gtype, mfac_act act, int64_t rows, int64_t cin,
+                                    int64_t hidden, int64_t cout, const void* dy, int64_t lddy, const void* w2, int64_t ldw2,
+                                    const void* x, int64_t ldx, const int8_t* q, int64_t ldq, const uint8_t* s,
+                                    const float* gamma, const float* beta, const void* w1, int64_t ldw1, const void* zg,
+                                    const void* zu, int64_t ldz, const int8_t* qg, const uint8_t* sg, const int8_t* qu,
+                                    const uint8_t* su, int64_t ldqz, void* dx, int64_t lddx, void* dw1, int64_t lddw1,
+                                    float* db1, void* dw2, int64_t lddw2, void* workspace, size_t workspace_bytes,
+                                    hipStream_t stream) {
+    if (!type_ok(type) || !param_type_ok(gtype, type) || !act_ok(act) || !gated_ok(rows, cin, hidden) || cout < 0 ||
+        cout > MOST_WIDTH || (cout == 0 && dw2) || !matrix_or_none(dw1, gtype, lddw1, cin) || !vector_ok(db1, MFAC_F32) ||
+        !matrix_or_none(dw2, gtype, lddw2, hidden))
         return MFAC_EINVAL;
-    if (rows > 0 && (!matrix_ok(da, type, ldda, hidden) || !matrix_ok(dz, type, lddz, 2 * hidden) ||
-                     !matrix_or_none(dz_lo, type, lddz, 2 * hidden) || !matrix_or_none(a, type, lda, hidden) ||
-                     !matrix_or_none(a_lo, type, lda, hidden) ||
-                     !pair_ok(type, hidden, zg, zu, ldz, qg, sg, qu, su, ldq, false)))
-        return MFAC_EINVAL;
-    if (db) {
-        const mfac_status e =
-            check_workspace(mfac_gated_act_bwd_workspace_bytes(rows, hidden), workspace, workspace_bytes);
-        if (e != MFAC_OK) return e;
-    }
-    const Epilogue e = gate_epilogue(type, act, zg, zu, ldz, packed(qg, ldq, sg), packed(qu, ldq, su), dz, dz_lo, lddz, a,
-                                     a_lo, lda);
-    return done(launch_gated_act_bwd(type, type, rows, hidden, da, ldda, e, db, (float*)workspace, stream));
-}
-
-MFAC_API size_t mfac_gated_hidden_bwd_workspace_bytes(mfac_dtype type, int64_t rows, int64_t hidden, int64_t cout,
-                                                      const void* dy, int64_t lddy, const void* w, int64_t ldw,
-                                                      int32_t want_db) {
-    if (!type_ok(type) || !gated_ok(rows, cout, hidden)) return 0;
-    return hidden_workspace(type, rows, hidden, cout, dy, lddy, w, ldw, want_db != 0).total;
-}
-
-MFAC_API mfac_status mfac_gated_hidden_bwd(mfac_dtype type, mfac_act act, int64_t rows, int64_t hidden, int64_t cout,
-                                           const void* dy, int64_t lddy, const void* w, int64_t ldw, const void* zg,
-                                           const void* zu, int64_t ldz, const int8_t* qg, const uint8_t* sg,
-                                           const int8_t* qu, const uint8_t* su, int64_t ldq, void* dz, void* dz_lo,
-                                           int64_t lddz, void* a, void* a_lo, int64_t lda, float* db, void* workspace,
-                                           size_t workspace_bytes, hipStream_t stream) {
-    if (!type_ok(type) || !act_ok(act) || !gated_ok(rows, cout, hidden) || !vector_ok(db, MFAC_F32) ||
-        (type == MFAC_F32 && (dz_lo || a_lo)) || (a_lo && !a))
-        return MFAC_EINVAL;
-    if (rows > 0 && (!matrix_ok(dy, type, lddy, cout) || !matrix_ok(w, type, ldw, hidden) ||
-                     !matrix_ok(dz, type, lddz, 2 * hidden) || !matrix_or_none(dz_lo, type, lddz, 2 * hidden) ||
-                     !matrix_or_none(a, type, lda, hidden) || !matrix_or_none(a_lo, type, lda, hidden) ||
-                     !pair_ok(type, hidden, zg, zu, ldz, qg, sg, qu, su, ldq, false)))
-        return MFAC_EINVAL;
-    if (rows == 0 && !db) return MFAC_OK;
-    const HiddenWorkspace need = hidden_workspace(type, rows, hidden, cout, dy, lddy, w, ldw, db != nullptr);
-    const mfac_status st = check_workspace(need.total, workspace, workspace_bytes);
-    if (st != MFAC_OK) return st;
-    const Epilogue e = gate_epilogue(type, act, zg, zu, ldz, packed(qg, ldq, sg), packed(qu, ldq, su), dz, dz_lo, lddz, a,
-                                     a_lo, lda);
-    char* ws = (char*)workspace;
-    if (need.fused) return done(launch_product(type, hidden_product(rows, hidden, cout, dy, lddy, w, ldw), e, ws, stream));
-    // da in fp32, then the gate's pass over it
-    float* da = (float*)(ws + need.product);
+    if (!dx && !dw1 && !db1 && !dw2) return MFAC_OK;
     if (rows > 0) {
+        const bool copy = q || s;
+        if (!matrix_ok(dy, type, lddy, cout ? cout : hidden) || (cout && !matrix_ok(w2, type, ldw2, hidden)) ||
+            !pair_ok(type, hidden, zg, zu, ldz, qg, sg, qu, su, ldqz, false) ||
+            (dx && (!matrix_ok(w1, type, ldw1, cin) || !matrix_ok(dx, type, lddx, cin))))
+            return MFAC_EINVAL;
+        if (dw1 && (copy == (x != nullptr) || (copy ? !copy_ok(q, ldq, s, cin) : !matrix_ok(x, type, ldx, cin)) ||
+                    (beta && !gamma) || !vector_ok(gamma, MFAC_F32) || !vector_ok(beta, MFAC_F32)))
+            return MFAC_EINVAL;
+    }
+    GatedBwd g{type, gtype, act, rows, cin, hidden, cout, dy, lddy, w2, ldw2, x, ldx, packed(q, ldq, s), gamma, beta, w1, ldw1,
+               dx != nullptr, dw1 != nullptr, db1 != nullptr, dw2 != nullptr};
+    g.place();
+    const mfac_status st = check_workspace(g.total, workspace, workspace_bytes);
+    if (st != MFAC_OK) return st;
+    char* ws = (char*)workspace;
+    hipError_t err = hipSuccess;
+    if (rows == 0) {
+        if (dw1) err = launch_zero_matrix(gtype, 2 * hidden, cin, dw1, lddw1, stream);
+        if (err == hipSuccess && dw2) err = launch_zero_matrix(gtype, cout, hidden, dw2, lddw2, stream);
+        if (err == hipSuccess && db1) err = launch_zero_matrix(MFAC_F32, 1, 2 * hidden, db1, 2 * hidden, stream);
+        return done(err);
+    }
+    const void* dy_at = g.dy;
+    if (g.dy_laid_out()) {
+        dy_at = ws + g.dy_in;
+        err = launch_lay_out(type, rows, cout, dy, lddy, ws + g.dy_in, g.lddy_in, stream);
+        if (err != hipSuccess) return done(err);
+    }
+    Epilogue e{};   // what forms dz and a from da
+    e.out_dt = e.io_dt = type;
+    e.act = act;
+    e.z = const_cast<void*>(zg);
+    e.z2 = const_cast<void*>(zu);
+    e.ldz = ldz;
+    e.p = packed(qg, ldqz, sg);
+    e.p2 = packed(qu, ldqz, su);
+    e.out = ws + g.dz;
+    e.ldo = g.lddz;
+    e.a = dw2 ? ws + g.a : nullptr;
+    e.lda = g.lda;
+    e.parts = g.parts;
+    e.out_part = g.dz_part();
+    e.a_part = g.a_part();
+    float* db = db1 ? db1 : g.sums() ? (float*)(ws + g.db) : nullptr;
+    if (g.fused) {
+        err = launch_product(type, g.da_product(dy_at), e, ws + g.product, stream);
+    } else if (g.da_given()) {
+        err = launch_gated_act_bwd(type, type, rows, hidden, dy, lddy, e, db, (float*)(ws + g.db_part), stream);
+    } else {
         Epilogue plain{};
         plain.out_dt = MFAC_F32;
         plain.io_dt = type;
-        plain.out = da;
+        plain.out = ws + g.da;
         plain.ldo = hidden;
-        const hipError_t err = launch_product(type, da_product(rows, hidden, cout, dy, lddy, w, ldw), plain, ws, stream);
-        if (err != hipSuccess) return done(err);
+        err = launch_product(type, g.da_product(dy_at), plain, ws + g.product, stream);
+        if (err == hipSuccess)
+            err = launch_gated_act_bwd(type, MFAC_F32, rows, hidden, ws + g.da, hidden, e, db, (float*)(ws + g.db_part), stream);
     }
-    return done(launch_gated_act_bwd(type, MFAC_F32, rows, hidden, da, hidden, e, db, (float*)(ws + need.product + need.da),
-                                     stream));
-}
-
-// ---------------------------------------------------------------- weight gradients from two parts
-MFAC_API size_t mfac_linear_bwd_weight_parts_workspace_bytes(mfac_dtype type, int64_t rows, int64_t cin, int64_t cout,
-                                                             const void* dz, const void* dz_lo, int64_t lddz, const void* x,
-                                                             const void* x_lo, int64_t ldx) {
-    if ((type != MFAC_BF16 && type != MFAC_F16) || !layer_ok(rows, cin, cout) || rows == 0) return 0;
-    int8_t some;   // an 8-bit copy, by its presence alone
-    return product_workspace_bytes(type, weight_product(rows, cin, cout, dz, dz_lo, lddz, x, x_lo, ldx,
-                                                        x ? Packed{} : Packed{&some, cin, nullptr}));
-}
-
-MFAC_API mfac_status mfac_linear_bwd_weight_parts(mfac_dtype type, mfac_dtype gtype, int64_t rows, int64_t cin, int64_t cout,
-                                                  const void* dz, const void* dz_lo, int64_t lddz, const void* x,
-                                                  const void* x_lo, int64_t ldx, const int8_t* q, int64_t ldq,
-                                                  const uint8_t* s, const float* gamma, const float* beta, const float* db,
-                                                  void* dw, int64_t lddw, void* workspace, size_t workspace_bytes,
-                                                  hipStream_t stream) {
-    if ((type != MFAC_BF16 && type != MFAC_F16) || !param_type_ok(gtype, type) || !layer_ok(rows, cin, cout) ||
-        !matrix_ok(dw, gtype, lddw, cin))
-        return MFAC_EINVAL;
-    if (rows == 0) return done(launch_zero_matrix(gtype, cout, cin, dw, lddw, stream));
-    const bool copy = q || s;
-    if (!matrix_ok(dz, type, lddz, cout) || !matrix_or_none(dz_lo, type, lddz, cout) || copy == (x != nullptr) ||
-        (copy ? !copy_ok(q, ldq, s, cin) : !matrix_ok(x, type, ldx, cin)) || !matrix_or_none(x_lo, type, ldx, cin) ||
-        (dz_lo != nullptr) == (x_lo != nullptr) || (x_lo && !x))
-        return MFAC_EINVAL;
-    if ((gamma != nullptr) != (beta != nullptr) || (gamma && !db) || !vector_ok(gamma, MFAC_F32) ||
-        !vector_ok(beta, MFAC_F32) || !vector_ok(db, MFAC_F32))
-        return MFAC_EINVAL;
-    const Product p = weight_product(rows, cin, cout, dz, dz_lo, lddz, x, x_lo, ldx, packed(q, ldq, s));
-    const mfac_status st = check_workspace(product_workspace_bytes(type, p), workspace, workspace_bytes);
-    if (st != MFAC_OK) return st;
-    Epilogue e{};
-    e.out_dt = gtype;
-    e.io_dt = type;
-    e.out = dw;
-    e.ldo = lddw;
-    e.gamma = gamma;
-    e.beta = beta;
-    e.db = db;
-    return done(launch_product(type, p, e, workspace, stream));
+    auto product = [&](const Product& p, int out_dt, void* out, int64_t ldo, bool affine) {
+        Epilogue o{};
+        o.out_dt = out_dt;
+        o.io_dt = type;
+        o.out = out;
+        o.ldo = ldo;
+        if (affine) {
+            o.gamma = gamma;
+            o.beta = beta;
+            o.db = db;
+        }
+        if (err == hipSuccess) err = launch_product(type, p, o, ws + g.product, stream);
+    };
+    if (dw2) product(g.dw2_product(dy_at, ws + g.a), gtype, dw2, lddw2, false);
+    if (dx) product(g.dx_product(ws + g.dz), type, dx, lddx, false);
+    if (dw1) product(g.dw1_product(ws + g.dz), gtype, dw1, lddw1, true);
+    return done(err);
 }
 
 // ---------------------------------------------------------------- between two blocks

@@ -225,9 +225,9 @@ bool plain16(const void* p, int64_t ld, int64_t cols) {
     return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && cols % 8 == 0 && ld <= (int64_t(1) << 21);
 }
 
-Operand operand_of(int dt, const void* p, const void* lo, int64_t ld, bool packed, int64_t rows, int64_t cols) {
-    Operand o{packed ? 1 : dt == DT_F32 ? 3 : lo ? 2 : 1, true, rows, cols, round_up(cols, 8), 0};
-    o.lay_out = o.planes == 3 || packed || !plain16(p, ld, cols) || (lo && !plain16(lo, ld, cols));
+Operand operand_of(int dt, const void* p, int laid_out, int64_t ld, bool packed, int64_t rows, int64_t cols) {
+    Operand o{laid_out ? laid_out : dt == DT_F32 && !packed ? 3 : 1, true, rows, cols, round_up(cols, 8), 0};
+    o.lay_out = !laid_out && (o.planes == 3 || packed || !plain16(p, ld, cols));
     if (!o.lay_out) o.ld = ld;
     else o.bytes = (size_t)round_up(rows * o.ld * 2 * o.planes, 256);
     return o;
@@ -257,8 +257,8 @@ Plan plan_of(int dt, const Product& p) {
     q.splits = 1;
     if (q.skinny) return q;
     const int64_t ar = p.a_col ? p.K : p.M, ac = p.a_col ? p.M : p.K, br = p.b_col ? p.K : p.N, bc = p.b_col ? p.N : p.K;
-    q.a = operand_of(dt, p.A, p.A_lo, p.lda, false, ar, ac);
-    q.b = operand_of(dt, p.B, p.B_lo, p.ldb, p.bp.q != nullptr, br, bc);
+    q.a = operand_of(dt, p.A, p.a_parts, p.lda, false, ar, ac);
+    q.b = operand_of(dt, p.B, p.b_parts, p.ldb, p.bp.q != nullptr, br, bc);
     q.ksteps = (int)ceil_div(p.K, BK);
     q.nseg = q.a.planes * q.b.planes == 9 ? 6 : q.a.planes * q.b.planes;   // not both of two parts
     const int64_t total = (int64_t)q.ksteps * q.nseg;
@@ -278,8 +278,7 @@ Plan plan_of(int dt, const Product& p) {
     return q;
 }
 
-hipError_t lay_out(int dt, const Operand& o, const void* src, const void* lo, int64_t ld, Packed p, void* dst,
-                   hipStream_t st) {
+hipError_t lay_out(int dt, const Operand& o, const void* src, int64_t ld, Packed p, void* dst, hipStream_t st) {
     if (p.q) return launch_unpack8(dt == DT_F16 ? DT_F16 : DT_BF16, o.rows, o.cols, p, dst, o.ld, st);
     const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(o.rows * (o.ld / 8), 256), 4096);
     if (o.planes == 3)
@@ -288,11 +287,7 @@ hipError_t lay_out(int dt, const Operand& o, const void* src, const void* lo, in
         k_lay_out<bf16><<<grid, 256, 0, st>>>((const bf16*)src, ld, o.rows, o.cols, (bf16*)dst, o.ld);
     else
         k_lay_out<f16><<<grid, 256, 0, st>>>((const f16*)src, ld, o.rows, o.cols, (f16*)dst, o.ld);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || o.planes != 2) return e;
-    Operand second = o;
-    second.planes = 1;
-    return lay_out(dt, second, lo, nullptr, ld, p, (char*)dst + o.rows * o.ld * 2, st);
+    return hipGetLastError();
 }
 
 template <typename T>
@@ -323,6 +318,11 @@ void by_operand(int dt, F f) {
 
 }  // namespace
 
+hipError_t launch_lay_out(int dt, int64_t rows, int64_t cols, const void* src, int64_t lds, void* dst, int64_t ld,
+                          hipStream_t st) {
+    return lay_out(dt, Operand{dt == DT_F32 ? 3 : 1, true, rows, cols, ld, 0}, src, lds, Packed{}, dst, st);
+}
+
 size_t product_workspace_bytes(int dt, const Product& p) {
     const Plan q = plan_of(dt, p);
     return q.a.bytes + q.b.bytes + q.part_bytes;
@@ -337,8 +337,9 @@ hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws,
         SkinnyArgs g{p.A, p.B, p.lda, p.ldb, p.M, gated ? p.N / 2 : p.N, p.K, 16, e};
         // Rows of W a work-group: the 32 columns of a group in one for an 8-bit copy of z; else so
         // that the work-groups are about as many as CUs. 1024 x 4096, 12 rows: fp32 14.6 us with 16,
-        // 13.4 with 8 (a quarter of it the fp32 MFMAs); bf16 9.4 and 8.2.
-        if (e.p.q || g.N > 16 * CUS) g.rows = 32;
+        // 13.4 with 8 (a quarter of it the fp32 MFMAs); bf16 9.4 and 8.2. A gated layer has twice the rows of W to
+        // one: 8192 columns, bf16 over 2048, 13.7 us with 16, 14.7 with 32, 17.8 with 8.
+        if (e.p.q || (!gated && g.N > 16 * CUS)) g.rows = 32;
         else if (g.N <= 8 * CUS) g.rows = 8;
         const unsigned grid = (unsigned)ceil_div(g.N, g.rows);
         by_operand(dt, [&](auto* t) {
@@ -354,19 +355,19 @@ hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws,
         g.A = (const char*)p.A;
         g.B = (const char*)p.B;
         if (q.a.lay_out) {
-            if ((err = lay_out(dt, q.a, p.A, p.A_lo, p.lda, Packed{}, w, st)) != hipSuccess) return err;
+            if ((err = lay_out(dt, q.a, p.A, p.lda, Packed{}, w, st)) != hipSuccess) return err;
             g.A = w;
             w += q.a.bytes;
         }
         if (q.b.lay_out) {
-            if ((err = lay_out(dt, q.b, p.B, p.B_lo, p.ldb, p.bp, w, st)) != hipSuccess) return err;
+            if ((err = lay_out(dt, q.b, p.B, p.ldb, p.bp, w, st)) != hipSuccess) return err;
             g.B = w;
             w += q.b.bytes;
         }
         g.lda = q.a.ld * 2;
         g.ldb = q.b.ld * 2;
-        g.apl = q.a.lay_out || !p.A_lo ? q.a.rows * q.a.ld * 2 : (const char*)p.A_lo - g.A;
-        g.bpl = q.b.lay_out || !p.B_lo ? q.b.rows * q.b.ld * 2 : (const char*)p.B_lo - g.B;
+        g.apl = p.a_parts ? p.a_part : q.a.rows * q.a.ld * 2;
+        g.bpl = p.b_parts ? p.b_part : q.b.rows * q.b.ld * 2;
         g.M = (int)p.M;
         g.N = (int)(p.gate == GATE_FORWARD ? p.N / 2 : p.N);
         g.up = g.N * g.ldb;
@@ -378,7 +379,7 @@ hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws,
             g.pa = 2u | 0u << 4 | 1u << 8 | 1u << 12 | 0u << 16 | 0u << 20;
             g.pb = 0u | 2u << 4 | 1u << 8 | 0u << 12 | 1u << 16 | 0u << 20;
         } else if (q.nseg == 3) {
-            g.pa = 2u | 1u << 4 | 0u << 8;
+            (q.a.planes == 3 ? g.pa : g.pb) = 2u | 1u << 4 | 0u << 8;
         } else if (q.nseg == 2) {
             (q.a.planes == 2 ? g.pa : g.pb) = 1u | 0u << 4;
         }

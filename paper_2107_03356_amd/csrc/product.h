@@ -44,9 +44,11 @@ struct Plan {
 // 248 us, with them 271.
 constexpr int64_t LAST_LEVEL_CACHE = int64_t(256) << 20;
 // Whether a product's results are stored past the caches: in tiles of 256, where they and the operands exceed them.
-inline bool streams(const Product& p, const Plan& q, int out_dt) {
-    const int64_t out = p.gate == GATE_FORWARD ? p.M * p.N / 2 : p.gate == GATE_HIDDEN ? 3 * p.M * p.N : p.M * p.N;
-    const int64_t bytes = (p.M * p.K + p.N * p.K) * 2 * (q.nseg > 1 ? 3 : 1) + out * dtype_bytes(out_dt);
+// `kept`: bytes of a gated layer's pre-activations (bf16 8192 x 8192 over 2048 with 8-bit copies: 499 us so, 514 through the
+// caches).
+inline bool streams(const Product& p, const Plan& q, int out_dt, int64_t kept = 0) {
+    const int64_t out = p.gate == GATE_FORWARD ? p.M * p.N / 2 : p.M * p.N;
+    const int64_t bytes = (p.M * p.K + p.N * p.K) * 2 * (q.nseg > 1 ? 3 : 1) + out * dtype_bytes(out_dt) + kept;
     return q.tile == 256 && bytes > LAST_LEVEL_CACHE;
 }
 
@@ -80,7 +82,7 @@ __device__ __forceinline__ OfColumn of_column(const Epilogue& e, int64_t N, int6
     if (KIND == FORWARD && e.bias) o.bias = load8_dt(e.bias, e.bias_dt, 0, n, N);
     if (KIND == WEIGHT && e.gamma) {
         o.bias = load8(e.gamma, n, N);
-        o.beta = load8(e.beta, n, N);
+        if (e.beta) o.beta = load8(e.beta, n, N);
     }
     return o;
 }
@@ -93,7 +95,7 @@ template <int KIND>
 __device__ __forceinline__ OfPlace of_place(const Epilogue& e, int64_t N, bool in, int64_t m, int64_t n) {
     OfPlace o{};
     if (KIND != WEIGHT && e.add && in) o.add = load8_dt(e.add, e.io_dt, m * e.ldadd, n, N);
-    if (KIND == WEIGHT && e.gamma && in) o.db = e.db[m];
+    if (KIND == WEIGHT && e.beta && in) o.db = e.db[m];
     return o;
 }
 
@@ -154,7 +156,7 @@ __device__ __forceinline__ void finish_gated8(const Epilogue& e, int64_t N, bool
     act_apply(act_forward(e.act), one);
     store8_dt(e.out, e.out_dt, m * e.ldo, n, N, one[0] * u);
 }
-// And of the gradient of its output, c: dz and a.
+// And of the gradient of its output, c: dz and a, of 16-bit data.
 __device__ __forceinline__ void finish_hidden8(const Epilogue& e, int64_t N, bool in, int64_t m, int64_t n, f8 c) {
     if (!in || n >= N) return;
     f8 d[1] = {c}, g[1], u[1];
@@ -167,15 +169,14 @@ __device__ __forceinline__ void finish_hidden8(const Epilogue& e, int64_t N, boo
         u[0] = load8_dt(e.z2, e.io_dt, m * e.ldz, n, N);
     }
     gate_slopes(e.act, g, u, d);
-    store8_dt(e.out, e.out_dt, m * e.ldo, n, N, d[0]);
-    store8_dt(e.out, e.out_dt, m * e.ldo + N, n, N, u[0]);
-    if (e.a) store8_dt(e.a, e.out_dt, m * e.lda, n, N, g[0]);
-    auto rest = [&](f8 v) { return e.out_dt == DT_BF16 ? rest_of<bf16>(v) : rest_of<f16>(v); };
-    if (e.out_lo) {
-        store8_dt(e.out_lo, e.out_dt, m * e.ldo, n, N, rest(d[0]));
-        store8_dt(e.out_lo, e.out_dt, m * e.ldo + N, n, N, rest(u[0]));
-    }
-    if (e.a_lo) store8_dt(e.a_lo, e.out_dt, m * e.lda, n, N, rest(g[0]));
+    auto store = [&](void* base, int64_t apart, int64_t off, f8 v) {
+        store8_dt(base, e.out_dt, off, n, N, v);
+        if (e.parts == 1) return;
+        store8_dt((char*)base + apart, e.out_dt, off, n, N, e.out_dt == DT_BF16 ? rest_of<bf16>(v) : rest_of<f16>(v));
+    };
+    store(e.out, e.out_part, m * e.ldo, d[0]);
+    store(e.out, e.out_part, m * e.ldo + N, u[0]);
+    if (e.a) store(e.a, e.a_part, m * e.lda, g[0]);
 }
 
 // Four sums at a time, as the matrix cores leave them: lane l has columns n .. n + 3, n = 4 (l / 16)
@@ -404,7 +405,8 @@ __device__ __forceinline__ void epilogue(const GemmArgs& g, float* part, int lan
         if constexpr (WGT)
             if (e.gamma) {
                 bias[j] = load4<EDGE>(e.gamma, n + j * 16, N);
-                beta[j] = load4<EDGE>(e.beta, n + j * 16, N);
+                beta[j] = v4{0.f, 0.f, 0.f, 0.f};
+                if (e.beta) beta[j] = load4<EDGE>(e.beta, n + j * 16, N);
             }
     }
     // by templates: the body is past what the compiler unrolls, and acc must stay in registers
@@ -430,7 +432,7 @@ __device__ __forceinline__ void epilogue(const GemmArgs& g, float* part, int lan
         }
         if constexpr (WGT)
             if (e.gamma) {
-                const float db = e.db[m];
+                const float db = e.beta ? e.db[m] : 0.f;
 #pragma unroll
                 for (int j = 0; j < NTL; ++j) acc[i][j] = acc[i][j] * bias[j] + db * beta[j];
             }
@@ -498,50 +500,38 @@ __device__ __forceinline__ void epilogue_gated(const GemmArgs& g, float* part, i
     });
 }
 
-// Eight neighbouring pre-activations as loaded: fp32, T, or of an 8-bit copy.
+// Eight neighbouring pre-activations as loaded, or of an 8-bit copy.
 template <typename T>
 struct RawEight {
-    typedef unsigned u8 __attribute__((ext_vector_type(8)));
     typedef unsigned u4 __attribute__((ext_vector_type(4)));
-    u8 w;
-    __device__ __forceinline__ void load(const void* z, int dt, int64_t ldz, const Packed& p, int64_t m, int64_t n,
-                                         int64_t N) {
+    u4 w;
+    __device__ __forceinline__ void load(const void* z, int64_t ldz, const Packed& p, int64_t m, int64_t n, int64_t N) {
         if (p.q) {
             const Bytes8 b = *reinterpret_cast<const Bytes8*>(p.q + m * p.ldq + n);
             w[0] = b.lo;
             w[1] = b.hi;
             w[2] = p.s[m * (N / 32) + (n >> 5)];
-        } else if (dt == DT_F32) {
-            const VecOf<float, 8>::plain v = *reinterpret_cast<const VecOf<float, 8>::type*>((const float*)z + m * ldz + n);
-            w = __builtin_bit_cast(u8, v);
         } else {
             const typename VecOf<T, 8>::plain v = *reinterpret_cast<const typename VecOf<T, 8>::type*>((const T*)z + m * ldz + n);
-            const u4 b = __builtin_bit_cast(u4, v);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = b[i];
+            w = __builtin_bit_cast(u4, v);
         }
     }
-    __device__ __forceinline__ f8 get(bool packed, int dt) const {
+    __device__ __forceinline__ f8 get(bool packed) const {
         if (packed) return RawPacked8{{w[0], w[1]}, w[2]}.get();
-        if (dt == DT_F32) return __builtin_bit_cast(f8, w);
-        const u4 b = {w[0], w[1], w[2], w[3]};
-        return __builtin_convertvector(__builtin_bit_cast(typename VecOf<T, 8>::plain, b), f8);
+        return __builtin_convertvector(__builtin_bit_cast(typename VecOf<T, 8>::plain, w), f8);
     }
 };
-template <bool STREAM, typename T>
-__device__ __forceinline__ void store_eight(void* p, int dt, int64_t off, f8 v) {
-    if (dt == DT_F32) put<STREAM>(v, reinterpret_cast<VecOf<float, 8>::type*>((float*)p + off));
-    else put<STREAM>(__builtin_convertvector(v, typename VecOf<T, 8>::plain), reinterpret_cast<typename VecOf<T, 8>::type*>((T*)p + off));
-}
 
-// The gradient da of a gated layer's output becomes dz and a. The sums of two tiles of 16 columns are exchanged first, so that
-// a lane has eight neighbours and takes 16 bytes of z at a time; the pre-activations of the next sixteen rows are on
-// their way while these are worked on. N is a multiple of the columns that a wave has (HIDDEN_COLS), so a wave has them all or
-// none: with checks for each column this code would be twice as long, and a wave runs all of it once a tile.
-template <typename T, bool STREAM, int MT, int NTL>
+// The gradient da of a gated layer's output becomes dz and a, of 16-bit data, in one part or two. The sums of two tiles of
+// 16 columns are exchanged first, so that a lane has eight neighbours and takes 16 bytes of z at a time; the pre-activations
+// of the next sixteen rows are on their way while these are worked on. N is a multiple of the columns that a wave has
+// (HIDDEN_COLS), so a wave has them all or none: with checks for each column this code would be twice as long, and a wave runs
+// all of it once a tile.
+template <typename T, int MT, int NTL>
 __device__ __forceinline__ void epilogue_hidden(const GemmArgs& g, float* part, int lane, int64_t m0, int64_t n,
                                                 v4 (&acc)[MT][NTL]) {
     constexpr int H = NTL / 2;
+    typedef typename VecOf<T, 8>::plain V;
     const Epilogue& e = g.e;
     const int64_t N = g.N;
     const bool packed = e.p.q;
@@ -561,9 +551,17 @@ __device__ __forceinline__ void epilogue_hidden(const GemmArgs& g, float* part, 
         m = min(m, (int64_t)g.M - 1);
 #pragma unroll
         for (int j = 0; j < H; ++j) {
-            zg[j].load(e.z, e.io_dt, e.ldz, e.p, m, n + j * 32, N);
-            zu[j].load(e.z2, e.io_dt, e.ldz, e.p2, m, n + j * 32, N);
+            zg[j].load(e.z, e.ldz, e.p, m, n + j * 32, N);
+            zu[j].load(e.z2, e.ldz, e.p2, m, n + j * 32, N);
         }
+    };
+    auto store = [&](void* base, int64_t apart, int64_t off, f8 v) {
+        T* at = (T*)base + off;
+        const V first = __builtin_convertvector(v, V);
+        *reinterpret_cast<typename VecOf<T, 8>::type*>(at) = first;
+        if (e.parts == 1) return;
+        at = (T*)((char*)at + apart);
+        *reinterpret_cast<typename VecOf<T, 8>::type*>(at) = __builtin_convertvector(v - __builtin_convertvector(first, f8), V);
     };
     load(m0);
     for_each_index(std::make_integer_sequence<int, MT>(), [&](auto tag) {
@@ -579,23 +577,17 @@ __device__ __forceinline__ void epilogue_hidden(const GemmArgs& g, float* part, 
                 d[j][k] = __uint_as_float(x);
                 d[j][4 + k] = __uint_as_float(y);
             }
-            a[j] = zg[j].get(packed, e.io_dt);
-            u[j] = zu[j].get(packed, e.io_dt);
+            a[j] = zg[j].get(packed);
+            u[j] = zu[j].get(packed);
         }
         if (i + 1 < MT) load(m + 16);
         if (m >= g.M) return;
         gate_slopes(e.act, a, u, d);
 #pragma unroll
         for (int j = 0; j < H; ++j) {
-            const int64_t at = m * e.ldo + n + j * 32, at_a = m * e.lda + n + j * 32;
-            store_eight<STREAM, T>(e.out, e.out_dt, at, d[j]);
-            store_eight<STREAM, T>(e.out, e.out_dt, at + N, u[j]);
-            if (e.a) store_eight<STREAM, T>(e.a, e.out_dt, at_a, a[j]);
-            if (e.out_lo) {
-                store_eight<STREAM, T>(e.out_lo, e.out_dt, at, rest_of<T>(d[j]));
-                store_eight<STREAM, T>(e.out_lo, e.out_dt, at + N, rest_of<T>(u[j]));
-            }
-            if (e.a_lo) store_eight<STREAM, T>(e.a_lo, e.out_dt, at_a, rest_of<T>(a[j]));
+            store(e.out, e.out_part, m * e.ldo + n + j * 32, d[j]);
+            store(e.out, e.out_part, m * e.ldo + N + n + j * 32, u[j]);
+            if (e.a) store(e.a, e.a_part, m * e.lda + n + j * 32, a[j]);
         }
     });
 }
@@ -736,7 +728,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
     float* part = g.splits > 1 ? g.part + (int64_t)k_part * g.M * g.N * (KIND == GATED ? 2 : 1) : nullptr;
     const int m = m0 + wm * (TM / WM) + (lane & 15), n = n0 + wn * (COLS / WN) + 4 * (lane >> 4);
     if constexpr (KIND == HIDDEN) {
-        if (n < g.N) epilogue_hidden<T, STREAM>(g, part, lane, m, n, acc);
+        if (n < g.N) epilogue_hidden<T>(g, part, lane, m, n, acc);
         return;
     }
     auto finish = [&](auto edge) {
@@ -758,11 +750,13 @@ hipError_t run_product(const Product& p, const Plan& q, const GemmArgs& g, hipSt
     // 2048^3 against 27
     // (a gated layer's waves have 32 columns of the result, one group of an 8-bit copy: four waves of 16 rows then)
     constexpr int WM = KIND == GATED ? 4 : 2;
+    const int64_t kept = KIND != GATED ? 0 : g.e.z ? p.M * p.N * dtype_bytes(g.e.io_dt) : g.e.p.q ? p.M * p.N : 0;
+    // HIDDEN writes three to six times what it reads, past what the caches hold in any case: 2.09 ms for a backward pass of bf16
+    // 8192 rows, 2048 to 8192, with plain stores, 2.11 with nontemporal ones
     if (q.tile == 64) k_product<T, KIND, 64, 64, WM, 4 / WM, 3, false><<<grid, 256, 0, st>>>(g);
     else if (q.tile == 128) k_product<T, KIND, 128, 128, 2, 2, 2, false><<<grid, 256, 0, st>>>(g);
-    else if constexpr (KIND == HIDDEN) k_product<T, KIND, 256, 256, 2, 4, 2, false><<<grid, 512, 0, st>>>(g);
-    else if (!streams(p, q, g.e.out_dt)) k_product<T, KIND, 256, 256, 2, 4, 2, false><<<grid, 512, 0, st>>>(g);
-    else k_product<T, KIND, 256, 256, 2, 4, 2, true><<<grid, 512, 0, st>>>(g);
+    else if (KIND == HIDDEN || !streams(p, q, g.e.out_dt, kept)) k_product<T, KIND, 256, 256, 2, 4, 2, false><<<grid, 512, 0, st>>>(g);
+    else if constexpr (KIND != HIDDEN) k_product<T, KIND, 256, 256, 2, 4, 2, true><<<grid, 512, 0, st>>>(g);
     return hipGetLastError();
 }
 

@@ -63,7 +63,9 @@ struct Epilogue {
     Packed p2;
     void* a;             // act(z) z2, where HIDDEN forms it (null: not wanted)
     int64_t lda;
-    void *out_lo, *a_lo; // what out's and a's rounding to 16 bits leaves (null: not wanted), rows ldo and lda apart
+    // out and a in this many 16-bit parts (1, 2; of fp32 3), each what the rounding of those before it leaves, bytes apart
+    int parts;
+    int64_t out_part, a_part;
 };
 
 // What a product's N columns are.
@@ -84,13 +86,22 @@ struct Product {
     bool b_col;
     Packed bp;  // B as an 8-bit copy (B null)
     int gate;   // GATE_*; N counts what the product has, 2 hidden or hidden
-    const void *A_lo, *B_lo;   // of 16-bit operands, a second part that is added to the first (null: none), at the same strides
+    // operands that are laid out already: in so many 16-bit parts (0: not), bytes apart, rows 16-byte aligned and zeros
+    // up to the next multiple of 8 columns
+    int a_parts;
+    int64_t a_part;
+    int b_parts;
+    int64_t b_part;
 };
 size_t product_workspace_bytes(int dt, const Product& p);
+// A matrix as the products take it: parts of `ld` elements a row (a multiple of 8), three of fp32.
+hipError_t launch_lay_out(int dt, int64_t rows, int64_t cols, const void* src, int64_t lds, void* dst, int64_t ld,
+                          hipStream_t st);
 hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws, hipStream_t st);
 
-// The gate's part of a backward pass; da is of type da_dt, dt or fp32. Of the epilogue out (dz), z, p, z2, p2, a, out_lo
-// and a_lo are used, and act. part: gated_bwd_parts(rows, hidden) * 2 * hidden floats (unused if db is null)
+// The gate's part of a backward pass; da is of type da_dt, dt or fp32. Of the epilogue act, z, p, z2, p2, out (dz), a and
+// their parts are used; out and a are 16-bit (bf16 for fp32 data), ldo and lda multiples of 8, zeros past their columns.
+// part: gated_bwd_parts(rows, hidden) * 2 * hidden floats (unused if db is null)
 int64_t gated_bwd_parts(int64_t rows, int64_t hidden);
 hipError_t launch_gated_act_bwd(int dt, int da_dt, int64_t rows, int64_t hidden, const void* da, int64_t ldda,
                                 const Epilogue& e, float* db, float* part, hipStream_t st);

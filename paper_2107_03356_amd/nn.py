@@ -10,7 +10,7 @@ Three levels:
 
 * ``layer_norm_forward``, ``layer_norm_backward``, ``linear_forward``,
   ``linear_backward``, ``act_backward``, ``pack8``, ``unpack8``,
-  ``gated_linear_forward``, ``gated_act_backward``, ``gated_hidden_backward``,
+  ``gated_linear_forward``, ``gated_linear_backward``,
   ``gated_feed_forward_backward``, ``residual_norm_forward``,
   ``residual_norm_backward``, ``dropout_forward``: the passes themselves, on
   tensors and ``Packed8`` copies;
@@ -353,11 +353,10 @@ def linear_backward_input(dz, weight, add=None):
     return dx
 
 
-def linear_backward_weight(dz, x, affine=None, db=None, grad_dtype=None, dz_low=None, x_low=None):
+def linear_backward_weight(dz, x, affine=None, db=None, grad_dtype=None):
     """dW = dz^T x (cout x cin) in ``grad_dtype`` (float32 or dz's type, the default). x is a
     tensor or a Packed8. ``affine`` = (gamma, beta), float32: the layer's input was
-    gamma * x + beta; db, the column sums of dz in float32, is then needed. ``dz_low`` or
-    ``x_low`` (16-bit data, one of the two): a second part, added to dz or to x."""
+    gamma * x + beta; db, the column sums of dz in float32, is then needed."""
     dz2 = _rows(dz, "linear: dz")
     rows, cout = dz2.shape
     xm, packed = (None, 0), _NO_COPY
@@ -382,22 +381,6 @@ def linear_backward_weight(dz, x, affine=None, db=None, grad_dtype=None, dz_low=
     dw = torch.empty((cout, cin), dtype=grad_dtype, device=dz.device)
     t = _type(dz2, "linear: dz")
     zm = _mat(dz2)
-    if dz_low is not None or x_low is not None:
-        if t == B.MFAC_F32 or (dz_low is not None and x_low is not None) or (x_low is not None and isinstance(x, Packed8)):
-            raise ValueError("linear: a second part of dz or of x, of 16-bit data")
-        low = []   # with the first part's strides
-        for first, second in ((dz2, dz_low), (x, x_low)):
-            if second is not None:
-                second = _rows(second, "linear: second part")
-                _same("linear: second part", second, first, first.shape)
-                if rows > 1 and _ld(second) != _ld(first):
-                    raise ValueError("linear: parts whose rows lie equally far apart")
-            low.append(second)
-        args = _ptr(low[0]), zm[1], xm[0], _ptr(low[1]), xm[1]
-        ws = _workspace(_function("mfac_linear_bwd_weight_parts_workspace_bytes")(t, rows, cin, cout, zm[0], *args), dz.device)
-        _call("mfac_linear_bwd_weight_parts", dz.device, t, _TYPES[grad_dtype], rows, cin, cout, zm[0], *args, *packed,
-              _ptr(gamma), _ptr(beta), _ptr(db) if affine is not None else None, dw.data_ptr(), cin, ws[0], ws[1])
-        return dw
     ws = _workspace(_function("mfac_linear_bwd_weight_workspace_bytes")(t, rows, cin, cout, *zm, *xm), dz.device)
     _call("mfac_linear_bwd_weight", dz.device, t, _TYPES[grad_dtype], rows, cin, cout, *zm, *xm, *packed, _ptr(gamma),
           _ptr(beta), _ptr(db) if affine is not None else None, dw.data_ptr(), cin, ws[0], ws[1])
@@ -479,82 +462,77 @@ def _gate_pair(z, rows, n, like):
     return (zg.data_ptr(), zu.data_ptr(), _ld(zg)), (None, None, None, None, 0), (zg, zu)
 
 
-def _gate_room(lead, n, like, want_a, want_db, parts):
-    """Room for dz, dz's second part, a, a's, db."""
-    def room(cols, on):
-        return like.new_empty(lead + (cols,)) if on else None
-
-    if parts and like.dtype == torch.float32:
-        raise ValueError("gated: parts are of 16-bit data")
-    return (room(2 * n, True), room(2 * n, parts), room(n, want_a), room(n, want_a and parts),
-            torch.empty(2 * n, dtype=torch.float32, device=like.device) if want_db else None)
-
-
-def gated_act_backward(da, z, act="silu", want_a=False, want_db=True, parts=False):
-    """(dz, a, db) from da, the gradient of y = act(zg) * zu: dz = [da zu act'(zg), da act(zg)] with 2 hidden columns in
-    da's type, a = y formed again (``want_a``, else None), db the column sums of dz in float32, before its rounding
-    (``want_db``, else None). z is a pair of tensors or of Packed8. ``parts`` (16-bit data): dz and a are pairs, each with
-    what its rounding to the data's type leaves, for gradients of weights in float32 (see linear_backward_weight)."""
-    code = _act(act)
-    da2 = _rows(da, "gated: da")
-    rows, n = da2.shape
-    zm, packed, held = _gate_pair(z, rows, n, da2)
-    dz, dz_lo, a, a_lo, db = _gate_room(da.shape[:-1], n, da, want_a, want_db, parts)
-    ws = _workspace(_function("mfac_gated_act_bwd_workspace_bytes")(rows, n) if want_db else 0, da.device)
-    _call("mfac_gated_act_bwd", da.device, _type(da2, "gated: da"), code, rows, n, *_mat(da2), *zm, *packed,
-          dz.data_ptr(), _ptr(dz_lo), 2 * n, _ptr(a), _ptr(a_lo), n, _ptr(db), ws[0], ws[1])
-    return (dz, dz_lo) if parts else dz, (a, a_lo) if parts and want_a else a, db
-
-
-def gated_hidden_backward(dy, weight, z, act="silu", want_a=False, want_db=False, parts=False):
-    """(dz, a, db) as of gated_act_backward with da = dy weight, for the layer a weight^T that follows the gate; da is not
-    rounded."""
+def _gated_backward(dy, x, w1, w2, z, act, affine, grad_dtype, need):
+    """(dx, dw1, db1, dw2), of a gated layer (w2 None), or of it and the layer that follows."""
     code = _act(act)
     dy2 = _rows(dy, "gated: dy")
-    rows, cout = dy2.shape
-    w = _weight(weight)
-    n = w.shape[1]
-    _same("gated: weight", w, dy2, (cout, n))
-    zm, packed, held = _gate_pair(z, rows, n, dy2)
-    dz, dz_lo, a, a_lo, db = _gate_room(dy.shape[:-1], n, dy, want_a, want_db, parts)
-    t = _type(dy2, "gated: dy")
-    ym, wm = _mat(dy2), _mat(w)
-    ws = _workspace(_function("mfac_gated_hidden_bwd_workspace_bytes")(t, rows, n, cout, *ym, *wm, int(want_db)), dy.device)
-    _call("mfac_gated_hidden_bwd", dy.device, t, code, rows, n, cout, *ym, *wm, *zm, *packed, dz.data_ptr(), _ptr(dz_lo),
-          2 * n, _ptr(a), _ptr(a_lo), n, _ptr(db), ws[0], ws[1])
-    return (dz, dz_lo) if parts else dz, (a, a_lo) if parts and want_a else a, db
+    rows = dy2.shape[0]
+    need_x, need_w1, need_b1, need_w2 = need
+    if not any(need):
+        return None, None, None, None
+    w2m, cout = (None, 0), 0
+    n = dy2.shape[1]
+    if w2 is not None:
+        w2 = _weight(w2)
+        cout, n = dy2.shape[1], w2.shape[1]
+        _same("gated: w2", w2, dy2, (cout, n))
+        w2m = _mat(w2)
+    zm, packed_z, held = _gate_pair(z, rows, n, dy2)
+    xm, packed, cin, gamma, beta, w1m = (None, 0), _NO_COPY, 1, None, None, (None, 0)
+    if need_x:
+        w1 = _weight(w1)
+        cin = w1.shape[1]
+        _same("gated: w1", w1, dy2, (2 * n, cin))
+        w1m = _mat(w1)
+    if need_w1:
+        if isinstance(x, Packed8):
+            packed = x._args()
+        else:
+            x = _rows(x, "gated: x")
+            _same("gated: x", x, dy2, (rows, x.shape[1]))
+            xm = _mat(x)
+        if x.shape[0] != rows or x.device != dy2.device or (need_x and x.shape[1] != cin):
+            raise ValueError("gated: x has the rows of dy and the columns of w1, on dy's device")
+        cin = x.shape[1]
+        if affine is not None:
+            gamma, beta = (None if v is None else _param("gated: affine", v.float(), dy2, cin) for v in affine)
+            if gamma is None:
+                raise ValueError("gated: affine is (gamma, beta or None)")
+    grad_dtype = dy.dtype if grad_dtype is None else grad_dtype
+    if grad_dtype not in (torch.float32, dy.dtype):
+        raise ValueError(f"gated: grad_dtype is float32 or {dy.dtype}")
+    dx = dy.new_empty(dy.shape[:-1] + (cin,)) if need_x else None
+    dw1 = torch.empty((2 * n, cin), dtype=grad_dtype, device=dy.device) if need_w1 else None
+    db1 = torch.empty(2 * n, dtype=torch.float32, device=dy.device) if need_b1 else None
+    dw2 = torch.empty((cout, n), dtype=grad_dtype, device=dy.device) if need_w2 else None
+    t, gt = _type(dy2, "gated: dy"), _TYPES[grad_dtype]
+    wanted = need_x | need_w1 << 1 | need_b1 << 2 | need_w2 << 3 | (beta is not None) << 4
+    ym = _mat(dy2)
+    ws = _workspace(_function("mfac_gated_bwd_workspace_bytes")(t, gt, rows, cin, n, cout, *ym, *w2m, *xm, *w1m, wanted),
+                    dy.device)
+    _call("mfac_gated_bwd", dy.device, t, gt, code, rows, cin, n, cout, *ym, *w2m, *xm, *packed, _ptr(gamma), _ptr(beta),
+          *w1m, *zm, *packed_z, _ptr(dx), cin, _ptr(dw1), cin, _ptr(db1), _ptr(dw2), n, ws[0], ws[1])
+    return dx, dw1, db1, dw2
+
+
+def gated_linear_backward(dy, x, weight, z, act="silu", affine=None, grad_dtype=None, need=(True, True, True)):
+    """(dx, dweight, dbias) of y = act(zg) * zu, [zg, zu] = x weight^T + bias, from dy, the input x and the pre-activations z
+    (a pair of tensors or of Packed8). ``affine``, ``grad_dtype``: see gated_feed_forward_backward. ``need``: which of the
+    three to form; the others are None."""
+    return _gated_backward(dy, x, weight, None, z, act, affine, grad_dtype, (*map(bool, need), False))[:3]
 
 
 def gated_feed_forward_backward(dy, x, w1, w2, z, act="silu", affine=None, grad_dtype=None, need=(True,) * 5):
     """(dx, dw1, db1, dw2, db2) of y = (act(zg) * zu) w2^T + b2, [zg, zu] = x w1^T + b1, from dy, the input x and the
     pre-activations z (a pair of tensors or of Packed8). ``affine`` = (gamma, beta or None), float32: the input was
-    gamma * x + beta (see linear_backward_weight); dx is then the gradient of that. dw1 and dw2 are of ``grad_dtype``
-    (float32 or dy's type, the default); in float32 of 16-bit data they are those of dz and a in two parts each, which
-    doubles their products: rounded to one, dz and a would leave them off by 2e-3. db1 and db2 are float32. ``need``: which
-    of the five to form; the others are None."""
-    need_x, need_w1, need_b1, need_w2, need_b2 = need
-    dx = dw1 = db1 = dw2 = db2 = None
-    if need_b2:
-        _, _, db2 = act_backward(dy)
-    if not (need_x or need_w1 or need_b1 or need_w2):
-        return dx, dw1, db1, dw2, db2
-    beta = affine is not None and affine[1] is not None
-    parts = grad_dtype == torch.float32 and dy.dtype != torch.float32 and (need_w1 or need_w2)
-    dz, a, db1 = gated_hidden_backward(dy, w2, z, act, want_a=need_w2, want_db=need_b1 or (need_w1 and beta), parts=parts)
-    dz, dz_lo = dz if parts else (dz, None)
-    a, a_lo = a if parts and need_w2 else (a, None)
-    if need_w2:
-        dw2 = linear_backward_weight(dy, a, grad_dtype=grad_dtype, **({"x_low": a_lo} if parts else {}))
-    del a, a_lo
-    if need_x:
-        dx = linear_backward_input(dz, w1)
-    if need_w1:
-        sums = db1
-        if affine is not None and not beta:   # no beta: zeros, and nothing to add to
-            sums = torch.zeros(max(w1.shape), dtype=torch.float32, device=dy.device)
-            affine, sums = (affine[0], sums[:w1.shape[1]]), sums[:w1.shape[0]]
-        dw1 = linear_backward_weight(dz, x, affine, sums, grad_dtype, **({"dz_low": dz_lo} if parts else {}))
-    return dx, dw1, db1 if need_b1 else None, dw2, db2
+    gamma * x + beta; dx is then the gradient of that. dw1 and dw2 are of ``grad_dtype`` (float32 or dy's type, the default);
+    in float32 of 16-bit data they are those of dz and act(zg) * zu in two parts each, which doubles their products: rounded to
+    one, these would leave them off by 2e-3. db1 and db2 are float32. ``need``: which of the five to form; the others are
+    None."""
+    need_x, need_w1, need_b1, need_w2, need_b2 = map(bool, need)
+    db2 = act_backward(dy)[2] if need_b2 else None
+    dx, dw1, db1, dw2 = _gated_backward(dy, x, w1, w2, z, act, affine, grad_dtype, (need_x, need_w1, need_b1, need_w2))
+    return dx, dw1, db1, dw2, db2
 
 
 # ---------------------------------------------------------------- between two blocks
@@ -899,13 +877,8 @@ class _GatedLinear(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy):
         k = _kept(ctx)
-        need_x, need_w, need_b = ctx.needs_input_grad[:3]
-        grad = _grad_dtype(ctx.wdtype, dy)
-        parts = need_w and grad != dy.dtype   # in float32 of 16-bit data
-        dz, _, db = gated_act_backward(dy, (k["zg"], k["zu"]), ctx.act, want_db=need_b, parts=parts)
-        dz, low = dz if parts else (dz, None)
-        dx = linear_backward_input(dz, k["w"]) if need_x else None
-        dw = linear_backward_weight(dz, k["x"], grad_dtype=grad, dz_low=low) if need_w else None
+        dx, dw, db = gated_linear_backward(dy, k["x"], k["w"], (k["zg"], k["zu"]), ctx.act,
+                                           grad_dtype=_grad_dtype(ctx.wdtype, dy), need=ctx.needs_input_grad[:3])
         return dx, _to(dw, ctx.wdtype), _to(db, ctx.bdtype), None, None, None
 
 

@@ -143,12 +143,18 @@ def test_gated_forward(dev, dtype, rows, cin, hid):
         holds(nn.gated_linear_forward(x, w, b.to(dtype), act), y64, rounded(y64, ye, dtype, tiny), "bias of the data's type")
 
 
-@pytest.mark.parametrize("rows,hid", [(1, 1), (3, 40), (70, 515), (2000, 33), (9, 5000), (3000, 1030)])
+def halves(dev, n, dtype):
+    """Weights [I; 0] and [0; I], by which dx is the gate's half of dz, or the other one."""
+    eye = torch.eye(n, device=dev, dtype=dtype)
+    return torch.cat([eye, 0 * eye]), torch.cat([0 * eye, eye])
+
+
+@pytest.mark.parametrize("rows,hid", [(1, 1), (3, 40), (70, 515), (2000, 33), (9, 2050), (3000, 1030)])
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 @pytest.mark.parametrize("act", ACTS)
-def test_gated_act_backward(dev, act, dtype, rows, hid):
+def test_gated_linear_backward_through_the_gate(dev, act, dtype, rows, hid):
     from paper_2107_03356_amd import nn
-    say("gated act backward", act, dtype, rows, hid)
+    say("gated backward through the gate", act, dtype, rows, hid)
     tiny = TINY[dtype]
     da = rand(dev, 1, rows, hid, dtype=dtype, pad=1)
     pair = rand(dev, 2, rows, 2 * hid, dtype=dtype, scale=2.0)
@@ -156,27 +162,16 @@ def test_gated_act_backward(dev, act, dtype, rows, hid):
     packs = nn.pack8(zg), nn.pack8(zu)
     for z in ((zg, zu), packs):
         g64, u64 = ((unpack64(v.q, v.s) for v in z) if z is packs else (zg.double(), zu.double()))
-        dg, du, a64 = gate_slopes64(act, g64, u64, da.double(), 0 * g64)
-        dz, a, db = nn.gated_act_backward(da, z, act, want_a=True)
-        assert dz.shape == (rows, 2 * hid)
-        holds(dz[:, :hid], dg[0], rounded(*dg, dtype, tiny), "dz of the gate")
-        holds(dz[:, hid:], du[0], rounded(*du, dtype, tiny), "dz of the other")
-        holds(a, a64[0], rounded(*a64, dtype, tiny), "a")
+        dg, du, _ = gate_slopes64(act, g64, u64, da.double(), 0 * g64)
+        for w, (v, e) in zip(halves(dev, hid, dtype), (dg, du)):
+            dx, none, db = nn.gated_linear_backward(da, None, w, z, act, need=(True, False, True))
+            # one product with 1, others with 0: exact in 16 bits, of three parts in fp32 to two roundings
+            holds(dx, v, rounded(v, e + 2 * E32 * v.abs() * (dtype == F32), dtype, tiny), "dz")
+            assert none is None
         v, e = torch.cat([dg[0], du[0]], 1), torch.cat([dg[1], du[1]], 1)
         holds(db, v.sum(0), E32 * (rows / 4 + 60) * v.abs().sum(0) + e.sum(0) + 1e-30, "db")
-        dz2, none, _ = nn.gated_act_backward(da, z, act, want_db=False)
-        assert torch.equal(dz2, dz) and none is None
-        if dtype != F32:
-            (d, d_lo), (b, b_lo), _ = nn.gated_act_backward(da, z, act, want_a=True, parts=True)
-            two_parts(d, d_lo, v, e, tiny, "dz"), two_parts(b, b_lo, *a64, tiny, "a")
-            assert torch.equal(d, dz) and torch.equal(b, a)
-
-
-def two_parts(first, second, value, error, tiny, what):
-    """A value in two parts: the second is what the first's rounding leaves, rounded."""
-    u = U[first.dtype]
-    holds(first, value, u * value.abs() + 1.01 * error + tiny, what)
-    holds(first.double() + second.double(), value, (u * u + E32) * value.abs() * 1.02 + 1.01 * error + tiny, what + " in two parts")
+        again = nn.gated_linear_backward(da, None, w, z, act, need=(True, False, False))
+        assert torch.equal(again[0], dx) and again[2] is None
 
 
 # (rows, hidden, cout)
@@ -192,10 +187,12 @@ def test_hidden_sizes_run_every_kernel(dev):
 
 @pytest.mark.parametrize("rows,hid,cout", HIDDEN)
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
-def test_gated_hidden_backward(dev, dtype, rows, hid, cout):
+def test_gated_backward_behind_the_next_layer(dev, dtype, rows, hid, cout):
+    """dz where da = dy w2, formed in that product (16-bit data, hidden a multiple of 64, no db) or from a stored da."""
     from paper_2107_03356_amd import nn
-    say("gated hidden backward", dtype, rows, hid, cout)
+    say("gated backward behind the next layer", dtype, rows, hid, cout)
     tiny = TINY[dtype]
+    weights = halves(dev, hid, dtype)
     for pad in (0, 3):
         dy = rand(dev, 1, rows, cout, dtype=dtype, pad=pad)
         w = rand(dev, 2, cout, hid, dtype=dtype, scale=cout ** -0.5, pad=pad)
@@ -206,22 +203,32 @@ def test_gated_hidden_backward(dev, dtype, rows, hid, cout):
         for act in ACTS if rows < 400 else ACTS[2:]:
             for pair in (z, packs) if act in ("silu", "gelu") else (z,):
                 g64, u64 = (unpack64(v.q, v.s) for v in pair) if pair is packs else (v.double() for v in pair)
-                dg, du, a64 = gate_slopes64(act, g64, u64, da, ed)
-                dz, a, _ = nn.gated_hidden_backward(dy, w, pair, act, want_a=True)
-                holds(dz[:, :hid], dg[0], rounded(*dg, dtype, tiny), (act, "dz of the gate"))
-                holds(dz[:, hid:], du[0], rounded(*du, dtype, tiny), (act, "dz of the other"))
-                holds(a, a64[0], rounded(*a64, dtype, tiny), (act, "a"))
-        # with db, which is formed from a stored da
-        dz2, none, db = nn.gated_hidden_backward(dy, w, pair, act, want_db=True)
+                dg, du, _ = gate_slopes64(act, g64, u64, da, ed)
+                for w1, (v, e) in zip(weights, (dg, du)):
+                    bound = rounded(v, e + 2 * E32 * v.abs() * (dtype == F32), dtype, tiny)
+                    dx = nn.gated_feed_forward_backward(dy, None, w1, w, pair, act, need=(True, False, False, False, False))[0]
+                    holds(dx, v, bound, (act, "dz"))
+        dx, _, db, _, _ = nn.gated_feed_forward_backward(dy, None, w1, w, pair, act, need=(True, False, True, False, False))
+        holds(dx, v, bound, "dz beside db")
         v, e = torch.cat([dg[0], du[0]], 1), torch.cat([dg[1], du[1]], 1)
         holds(db, v.sum(0), E32 * (rows / 4 + 60) * v.abs().sum(0) + e.sum(0) + 1e-30, "db")
-        holds(dz2, v, rounded(v, e, dtype, tiny), "dz beside db")
-        assert none is None
-        if dtype != F32:
-            for db in (False, True):
-                (d, d_lo), (b, b_lo), _ = nn.gated_hidden_backward(dy, w, pair, act, want_a=True, want_db=db, parts=True)
-                two_parts(d, d_lo, v, e, tiny, "dz"), two_parts(b, b_lo, *a64, tiny, "a")
-                assert torch.equal(d, dz2 if db else dz)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("rows,hid", [(1, 64), (40, 64), (70, 100), (130, 1028)])
+def test_gated_activation_formed_again(dev, dtype, rows, hid):
+    """With dy the identity, dw2 is act(zg) zu itself: rounded to the data's type, or in two parts for a gradient in fp32."""
+    from paper_2107_03356_amd import nn
+    say("gated activation formed again", dtype, rows, hid)
+    dy, w2 = torch.eye(rows, dtype=dtype, device=dev), rand(dev, 1, rows, hid, dtype=dtype)
+    z = rand(dev, 2, rows, hid, dtype=dtype, scale=2.0), rand(dev, 3, rows, hid, dtype=dtype)
+    for act in ACTS:
+        _, _, (a, e) = gate_slopes64(act, z[0].double(), z[1].double(), w2.double(), 0 * w2.double())
+        for grad in (F32, dtype):
+            got = nn.gated_feed_forward_backward(dy, None, None, w2, z, act, grad_dtype=grad, need=(False, False, False, True, False))
+            step = U[dtype] if grad == dtype else U[dtype] ** 2 + 2 * E32
+            holds(got[3], a, 1.02 * step * a.abs() + 1.01 * e + 2 * E32 * a.abs() + TINY[dtype], (act, grad))
+            assert got[0] is got[1] is got[2] is got[4] is None
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -266,32 +273,6 @@ def test_gated_feed_forward_backward(dev, dtype, rows, dim, hid):
                     holds(got[4], dy.double().sum(0), E32 * (rows / 4 + 60) * dm.sum(0) + 1e-30, "db2")
                 else:
                     assert got[2] is None and got[4] is None
-
-
-@pytest.mark.parametrize("dtype", [BF16, F16])
-@pytest.mark.parametrize("rows,cin,cout", [(1, 64, 96), (300, 264, 520), (301, 77, 35), (4000, 520, 1032)])
-def test_weight_gradient_in_two_parts(dev, dtype, rows, cin, cout):
-    from paper_2107_03356_amd import nn
-    say("two parts", dtype, rows, cin, cout)
-    u = U[dtype]
-    d = [rand(dev, 1, rows, cout, dtype=dtype), rand(dev, 2, rows, cout, dtype=dtype, scale=u)]
-    x = [rand(dev, 3, rows, cin, dtype=dtype), rand(dev, 4, rows, cin, dtype=dtype, scale=u)]
-    p, gamma, beta, db = nn.pack8(x[0]), rand(dev, 5, cin), rand(dev, 6, cin), rand(dev, 7, cout)
-    d64, x64 = (sum(v.double() for v in t) for t in (d, x))
-    for dz, low, xx, x_low, affine, want, size in (
-            (d[0], d[1], x[0], None, None, d64.t() @ x[0].double(), d64.abs().t() @ x[0].double().abs()),
-            (d[0], None, x[0], x[1], None, d[0].double().t() @ x64, d[0].double().abs().t() @ x64.abs()),
-            (d[0], d[1], p, None, (gamma, beta), (d64.t() @ unpack64(p.q, p.s)) * gamma.double() + db[:, None].double() * beta.double(),
-             (d64.abs().t() @ unpack64(p.q, p.s).abs()) * gamma.double().abs() + (db[:, None].double() * beta.double()).abs())):
-        for grad in (F32, dtype):
-            dw = nn.linear_backward_weight(dz, xx, affine, db, grad, dz_low=low, x_low=x_low)
-            holds(dw, want, rounded(want, E32 * (2 * growth(rows) + 4) * size, grad, TINY[grad]), (grad, affine is None))
-    with pytest.raises(ValueError):
-        nn.linear_backward_weight(d[0], x[0], dz_low=d[1], x_low=x[1])
-    with pytest.raises(ValueError):
-        nn.linear_backward_weight(d[0], p, x_low=x[1])
-    with pytest.raises(ValueError):
-        nn.linear_backward_weight(d[0], x[0], dz_low=rand(dev, 1, rows, 2 * cout, dtype=dtype)[:, ::2].float())
 
 
 # ---------------------------------------------------------------- between two blocks
