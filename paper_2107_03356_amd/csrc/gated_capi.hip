@@ -75,8 +75,8 @@ struct GatedBwd {
     // places in the workspace: dy as the products take it, da in fp32, dz and a in parts, db and its parts, the products'
     bool fused;
     int parts;
-    int64_t lddy_in, lddz, lda;
-    size_t dy_in, da, dz, a, db, db_part, product, total;
+    int64_t lddy_in, ldw2_in, ldx_in, ldw1_in, lddz, lda;
+    size_t dy_in, w2_in, x_in, w1_in, da, dz, a, db, db_part, product, total;
 
     bool da_given() const { return cout == 0; }
     bool sums() const { return db1 || (dw1 && beta); }
@@ -84,11 +84,12 @@ struct GatedBwd {
     int64_t dz_part() const { return rows * lddz * 2; }
     int64_t a_part() const { return rows * lda * 2; }
 
-    // The products, dy, dz and a being at these addresses.
-    Product da_product(const void* at) const {
+    // The products, dy, dz and a being at these addresses; ws: the workspace (or null, where only sizes are looked at).
+    Product da_product(const void* at, const char* ws) const {
         Product p{rows, hidden, cout, at, dy_laid_out() ? lddy_in : lddy, false, w2, ldw2, true, Packed{},
                   fused ? GATE_HIDDEN : GATE_NONE};
         if (dy_laid_out()) p.a_parts = type == MFAC_F32 ? 3 : 1, p.a_part = dy_part();
+        if (type == MFAC_F32) p.B = ws + w2_in, p.ldb = ldw2_in, p.b_parts = 3, p.b_part = cout * ldw2_in * 2;
         return p;
     }
     Product dw2_product(const void* at, const void* a_at) const {
@@ -98,17 +99,28 @@ struct GatedBwd {
         return p;
     }
     // dx is of 16-bit data from dz's first part: in two it would be no nearer after its own rounding
-    Product dx_product(const void* dz_at) const {
+    Product dx_product(const void* dz_at, const char* ws) const {
         Product p{rows, cin, 2 * hidden, dz_at, lddz, false, w1, ldw1, true, Packed{}};
         p.a_parts = type == MFAC_F32 ? 3 : 1, p.a_part = dz_part();
+        if (type == MFAC_F32) p.B = ws + w1_in, p.ldb = ldw1_in, p.b_parts = 3, p.b_part = 2 * hidden * ldw1_in * 2;
         return p;
     }
-    Product dw1_product(const void* dz_at) const {
+    Product dw1_product(const void* dz_at, const char* ws) const {
         Product p{2 * hidden, cin, rows, dz_at, lddz, true, x, ldx, true, xp};
         p.a_parts = parts, p.a_part = dz_part();
+        if (type == MFAC_F32 && x) p.B = ws + x_in, p.ldb = ldx_in, p.b_parts = 3, p.b_part = rows * ldx_in * 2;
         return p;
     }
-    // fp32 is split once for its two products; rows that are not 16-byte aligned are copied once
+    // What is laid out before the products, in one launch: fp32, split once, and dy where its rows are not 16-byte aligned.
+    int lay_outs(char* ws, LayOut (&jobs)[4]) const {
+        int n = 0;
+        if (dy_laid_out()) jobs[n++] = LayOut{dy, lddy, rows, cout, ws + dy_in, lddy_in};
+        if (type != MFAC_F32) return n;
+        if (!da_given()) jobs[n++] = LayOut{w2, ldw2, cout, hidden, ws + w2_in, ldw2_in};
+        if (dw1 && x) jobs[n++] = LayOut{x, ldx, rows, cin, ws + x_in, ldx_in};
+        if (dx) jobs[n++] = LayOut{w1, ldw1, 2 * hidden, cin, ws + w1_in, ldw1_in};
+        return n;
+    }
     bool dy_laid_out() const {
         return !da_given() && (type == MFAC_F32 || ((uintptr_t)dy & 15) || lddy % 8 || cout % 8 || lddy > MOST_WIDTH);
     }
@@ -117,8 +129,9 @@ struct GatedBwd {
         fused = parts = 0;
         lddy_in = round_up(std::max<int64_t>(cout, 1), 8);
         lddz = round_up(2 * hidden, 8);
-        lda = round_up(hidden, 8);
-        dy_in = da = dz = a = db = db_part = product = total = 0;
+        lda = ldw2_in = round_up(hidden, 8);
+        ldx_in = ldw1_in = round_up(cin, 8);
+        dy_in = w2_in = x_in = w1_in = da = dz = a = db = db_part = product = total = 0;
         if (!(dx || dw1 || db1 || dw2)) return;
         // Gradients of 16-bit weights' data in fp32 are formed from dz and a in two parts: rounded to one, they leave
         // the gradient 2.3e-3 from 64 bits (relative, 2-norm), in two 3e-6. It doubles these two products.
@@ -132,6 +145,11 @@ struct GatedBwd {
             return at;
         };
         if (dy_laid_out()) dy_in = take((size_t)dy_part() * (type == MFAC_F32 ? 3 : 1));
+        if (type == MFAC_F32) {
+            if (!da_given()) w2_in = take((size_t)cout * ldw2_in * 6);
+            if (dw1 && x) x_in = take((size_t)rows * ldx_in * 6);
+            if (dx) w1_in = take((size_t)hidden * ldw1_in * 12);
+        }
         if (!da_given() && !fused) da = take((size_t)rows * hidden * 4);
         dz = take((size_t)dz_part() * parts);
         if (dw2) a = take((size_t)a_part() * parts);
@@ -140,9 +158,9 @@ struct GatedBwd {
             db_part = take((size_t)gated_bwd_parts(std::max<int64_t>(rows, 1), hidden) * hidden * 8);
         }
         if (rows > 0) {   // one after another in the same place; addresses in the workspace are aligned, and not looked at
-            if (!da_given()) need(da_product(dy_laid_out() ? nullptr : dy));
-            if (dx) need(dx_product(nullptr));
-            if (dw1) need(dw1_product(nullptr));
+            if (!da_given()) need(da_product(dy_laid_out() ? nullptr : dy, nullptr));
+            if (dx) need(dx_product(nullptr, nullptr));
+            if (dw1) need(dw1_product(nullptr, nullptr));
             if (dw2) need(dw2_product(dy_laid_out() ? nullptr : dy, nullptr));
         }
         const size_t at = total;
@@ -254,12 +272,10 @@ MFAC_API mfac_status mfac_gated_bwd(mfac_dtype type, mfac_dtype gtype, mfac_act 
         if (err == hipSuccess && db1) err = launch_zero_matrix(MFAC_F32, 1, 2 * hidden, db1, 2 * hidden, stream);
         return done(err);
     }
-    const void* dy_at = g.dy;
-    if (g.dy_laid_out()) {
-        dy_at = ws + g.dy_in;
-        err = launch_lay_out(type, rows, cout, dy, lddy, ws + g.dy_in, g.lddy_in, stream);
-        if (err != hipSuccess) return done(err);
-    }
+    LayOut jobs[4];
+    const int njobs = g.lay_outs(ws, jobs);
+    const void* dy_at = g.dy_laid_out() ? ws + g.dy_in : g.dy;
+    if ((err = launch_lay_out(type, njobs, jobs, stream)) != hipSuccess) return done(err);
     Epilogue e{};   // what forms dz and a from da
     e.out_dt = e.io_dt = type;
     e.act = act;
@@ -277,7 +293,7 @@ MFAC_API mfac_status mfac_gated_bwd(mfac_dtype type, mfac_dtype gtype, mfac_act 
     e.a_part = g.a_part();
     float* db = db1 ? db1 : g.sums() ? (float*)(ws + g.db) : nullptr;
     if (g.fused) {
-        err = launch_product(type, g.da_product(dy_at), e, ws + g.product, stream);
+        err = launch_product(type, g.da_product(dy_at, ws), e, ws + g.product, stream);
     } else if (g.da_given()) {
         err = launch_gated_act_bwd(type, type, rows, hidden, dy, lddy, e, db, (float*)(ws + g.db_part), stream);
     } else {
@@ -286,7 +302,7 @@ MFAC_API mfac_status mfac_gated_bwd(mfac_dtype type, mfac_dtype gtype, mfac_act 
         plain.io_dt = type;
         plain.out = ws + g.da;
         plain.ldo = hidden;
-        err = launch_product(type, g.da_product(dy_at), plain, ws + g.product, stream);
+        err = launch_product(type, g.da_product(dy_at, ws), plain, ws + g.product, stream);
         if (err == hipSuccess)
             err = launch_gated_act_bwd(type, MFAC_F32, rows, hidden, ws + g.da, hidden, e, db, (float*)(ws + g.db_part), stream);
     }
@@ -304,8 +320,8 @@ MFAC_API mfac_status mfac_gated_bwd(mfac_dtype type, mfac_dtype gtype, mfac_act 
         if (err == hipSuccess) err = launch_product(type, p, o, ws + g.product, stream);
     };
     if (dw2) product(g.dw2_product(dy_at, ws + g.a), gtype, dw2, lddw2, false);
-    if (dx) product(g.dx_product(ws + g.dz), type, dx, lddx, false);
-    if (dw1) product(g.dw1_product(ws + g.dz), gtype, dw1, lddw1, true);
+    if (dx) product(g.dx_product(ws + g.dz, ws), type, dx, lddx, false);
+    if (dw1) product(g.dw1_product(ws + g.dz, ws), gtype, dw1, lddw1, true);
     return done(err);
 }
 

@@ -43,7 +43,8 @@ extern template hipError_t run_product<f16, HIDDEN>(const Product&, const Plan&,
 
 namespace {
 
-// Joins the K parts in order and finishes.
+// Joins the K parts in order and finishes. Eight parts are on their way at a time: one by one, many parts of few sums wait
+// for each.
 template <int KIND>
 __global__ __launch_bounds__(256) void k_finish(const float* __restrict__ part, int splits, int64_t M, int64_t N,
                                                 Epilogue e) {
@@ -52,17 +53,62 @@ __global__ __launch_bounds__(256) void k_finish(const float* __restrict__ part, 
     for (int64_t u0 = (int64_t)blockIdx.x * 256; u0 < total; u0 += (int64_t)gridDim.x * 256) {
         const int64_t u = u0 + threadIdx.x, m = u / pieces, n = (u - m * pieces) * 8;
         const bool in = m < M;
-        constexpr int ROWS = KIND == GATED ? 2 : 1;   // of N sums for one of the result
-        f8 v = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, other = v;
-        if (in)
-            for (int z = 0; z < splits; ++z) {
-                const float* row = part + (z * M + m) * N * ROWS;
-                v += load8(row, n, N);
-                if constexpr (KIND == GATED) other += load8(row + N, n, N);
-            }
-        if constexpr (KIND == GATED) finish_gated8(e, N, in, m, n, v, other);
-        else if constexpr (KIND == HIDDEN) finish_hidden8(e, N, in, m, n, v);
-        else finish8<KIND>(e, N, in, m, n, v);
+        f8 v = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        constexpr int AHEAD = 8;
+        for (int z = 0; in && z < splits; z += AHEAD) {
+            f8 a[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) a[i] = load8(part + (min(z + i, splits - 1) * M + m) * N, n, N);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (z + i < splits) v += a[i];
+        }
+        finish8<KIND>(e, N, in, m, n, v);
+    }
+}
+// The same of a gated layer (KIND GATED or HIDDEN): a work-group has 256 / GROUPS pieces of eight columns, of which its GROUPS
+// groups of threads sum every GROUPS-th part, joined in order. Where there are many parts there are few sums, and a CU takes
+// in about 20 bytes a ns: 64 parts of 181 x 276 sums took 46 us in 15 work-groups.
+template <int KIND, int GROUPS>
+__global__ __launch_bounds__(256) void k_finish_gated(const float* __restrict__ part, int splits, int64_t M, int64_t N,
+                                                      Epilogue e) {
+    constexpr int EACH = 256 / GROUPS, SIDES = KIND == GATED ? 2 : 1;   // sides: N sums each for N of the result
+    __shared__ __attribute__((aligned(32))) float of[GROUPS > 1 ? SIDES : 1][GROUPS > 1 ? 256 * 8 : 1];
+    const int64_t pieces = (N + 31) / 32 * 4, total = M * pieces;
+    const int group = threadIdx.x / EACH;
+    for (int64_t u0 = (int64_t)blockIdx.x * EACH; u0 < total; u0 += (int64_t)gridDim.x * EACH) {
+        const int64_t u = u0 + threadIdx.x % EACH, m = u / pieces, n = (u - m * pieces) * 8;
+        const bool in = m < M;
+        f8 v[SIDES];
+#pragma unroll
+        for (int k = 0; k < SIDES; ++k) v[k] = f8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int z = group; in && z < splits; z += GROUPS * 4) {
+            f8 a[4][SIDES];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int k = 0; k < SIDES; ++k)
+                    a[i][k] = load8(part + ((min(z + i * GROUPS, splits - 1) * M + m) * SIDES + k) * N, n, N);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (z + i * GROUPS < splits)
+#pragma unroll
+                    for (int k = 0; k < SIDES; ++k) v[k] += a[i][k];
+        }
+        if constexpr (GROUPS > 1) {
+            __syncthreads();   // what the turn before this one left has been read
+#pragma unroll
+            for (int k = 0; k < SIDES; ++k) *reinterpret_cast<f8*>(&of[k][threadIdx.x * 8]) = v[k];
+            __syncthreads();
+            if (group == 0)
+#pragma unroll
+                for (int k = 0; k < SIDES; ++k)
+                    for (int q = 1; q < GROUPS; ++q) v[k] += *reinterpret_cast<const f8*>(&of[k][(q * EACH + threadIdx.x) * 8]);
+        }
+        if (group == 0) {   // whole groups of four lanes (the exchanges of an 8-bit copy)
+            if constexpr (KIND == GATED) finish_gated8(e, N, in, m, n, v[0], v[1]);
+            else finish_hidden8(e, N, in, m, n, v[0]);
+        }
     }
 }
 
@@ -186,25 +232,31 @@ __global__ __launch_bounds__(NW * 64) void k_skinny(SkinnyArgs g) {
 }
 
 // ---------------------------------------------------------------- operands into the workspace
+// Up to four matrices in one launch (blockIdx.y), since a launch takes longer than a small matrix:
 // dst (rows of ld elements, ld a multiple of 8) <- src, zeros past cols.
+struct LayOuts {
+    LayOut of[4];
+};
 template <typename T>
-__global__ __launch_bounds__(256) void k_lay_out(const T* __restrict__ src, int64_t lds, int64_t rows, int64_t cols,
-                                                 T* __restrict__ dst, int64_t ld) {
-    const int64_t pieces = ld / 8, total = rows * pieces;
+__global__ __launch_bounds__(256) void k_lay_out(LayOuts jobs) {
+    const LayOut& j = jobs.of[blockIdx.y];
+    const T* src = (const T*)j.src;
+    T* dst = (T*)j.dst;
+    const int64_t pieces = j.ld / 8, total = j.rows * pieces;
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
         const int64_t r = u / pieces, c = (u - r * pieces) * 8;
-        store8(dst + r * ld, c, ld, load8(src + r * lds, c, cols));
+        store8(dst + r * j.ld, c, j.ld, load8(src + r * j.lds, c, j.cols));
     }
 }
-// The same from fp32 into three bf16 planes, `plane` elements apart.
-__global__ __launch_bounds__(256) void k_lay_out_split(const float* __restrict__ src, int64_t lds, int64_t rows,
-                                                       int64_t cols, bf16* __restrict__ dst, int64_t ld, int64_t plane) {
+// The same from fp32 into three bf16 planes, one after another.
+__global__ __launch_bounds__(256) void k_lay_out_split(LayOuts jobs) {
     typedef VecOf<bf16, 8>::plain b8;
-    const int64_t pieces = ld / 8, total = rows * pieces;
+    const LayOut& j = jobs.of[blockIdx.y];
+    const int64_t pieces = j.ld / 8, total = j.rows * pieces, plane = j.rows * j.ld;
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
         const int64_t r = u / pieces, c = (u - r * pieces) * 8;
-        f8 x = load8(src + r * lds, c, cols);
-        bf16* d = dst + r * ld + c;
+        f8 x = load8((const float*)j.src + r * j.lds, c, j.cols);
+        bf16* d = (bf16*)j.dst + r * j.ld + c;
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
             // the first part cut at bf16's largest value, to which the second adds the rest: rounded, a
@@ -278,18 +330,6 @@ Plan plan_of(int dt, const Product& p) {
     return q;
 }
 
-hipError_t lay_out(int dt, const Operand& o, const void* src, int64_t ld, Packed p, void* dst, hipStream_t st) {
-    if (p.q) return launch_unpack8(dt == DT_F16 ? DT_F16 : DT_BF16, o.rows, o.cols, p, dst, o.ld, st);
-    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(o.rows * (o.ld / 8), 256), 4096);
-    if (o.planes == 3)
-        k_lay_out_split<<<grid, 256, 0, st>>>((const float*)src, ld, o.rows, o.cols, (bf16*)dst, o.ld, o.rows * o.ld);
-    else if (dt == DT_BF16)
-        k_lay_out<bf16><<<grid, 256, 0, st>>>((const bf16*)src, ld, o.rows, o.cols, (bf16*)dst, o.ld);
-    else
-        k_lay_out<f16><<<grid, 256, 0, st>>>((const f16*)src, ld, o.rows, o.cols, (f16*)dst, o.ld);
-    return hipGetLastError();
-}
-
 template <typename T>
 hipError_t run_product(const Product& p, const Plan& q, const GemmArgs& g, hipStream_t st) {
     if (p.gate == GATE_FORWARD) return run_product<T, GATED>(p, q, g, st);
@@ -298,11 +338,19 @@ hipError_t run_product(const Product& p, const Plan& q, const GemmArgs& g, hipSt
     return p.b_col ? run_product<T, INPUT>(p, q, g, st) : run_product<T, FORWARD>(p, q, g, st);
 }
 
+template <int KIND>
+void run_finish_gated(const float* part, int splits, int64_t M, int64_t N, const Epilogue& e, hipStream_t st) {
+    const int64_t total = M * (ceil_div(N, 32) * 4);
+    if (splits < 8)
+        k_finish_gated<KIND, 1><<<(unsigned)std::min<int64_t>(ceil_div(total, 256), 8192), 256, 0, st>>>(part, splits, M, N, e);
+    else
+        k_finish_gated<KIND, 16><<<(unsigned)std::min<int64_t>(ceil_div(total, 16), 8192), 256, 0, st>>>(part, splits, M, N, e);
+}
 hipError_t run_finish(const Product& p, const float* part, int splits, const Epilogue& e, hipStream_t st) {
-    const int64_t N = p.gate == GATE_FORWARD ? p.N / 2 : p.N, pieces = ceil_div(N, 32) * 4;
+    const int64_t pieces = ceil_div(p.N, 32) * 4;
     const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(p.M * pieces, 256), 8192);
-    if (p.gate == GATE_FORWARD) k_finish<GATED><<<grid, 256, 0, st>>>(part, splits, p.M, N, e);
-    else if (p.gate == GATE_HIDDEN) k_finish<HIDDEN><<<grid, 256, 0, st>>>(part, splits, p.M, N, e);
+    if (p.gate == GATE_FORWARD) run_finish_gated<GATED>(part, splits, p.M, p.N / 2, e, st);
+    else if (p.gate == GATE_HIDDEN) run_finish_gated<HIDDEN>(part, splits, p.M, p.N, e, st);
     else if (p.a_col) k_finish<WEIGHT><<<grid, 256, 0, st>>>(part, splits, p.M, p.N, e);
     else if (p.b_col) k_finish<INPUT><<<grid, 256, 0, st>>>(part, splits, p.M, p.N, e);
     else k_finish<FORWARD><<<grid, 256, 0, st>>>(part, splits, p.M, p.N, e);
@@ -318,9 +366,19 @@ void by_operand(int dt, F f) {
 
 }  // namespace
 
-hipError_t launch_lay_out(int dt, int64_t rows, int64_t cols, const void* src, int64_t lds, void* dst, int64_t ld,
-                          hipStream_t st) {
-    return lay_out(dt, Operand{dt == DT_F32 ? 3 : 1, true, rows, cols, ld, 0}, src, lds, Packed{}, dst, st);
+hipError_t launch_lay_out(int dt, int n, const LayOut* jobs, hipStream_t st) {
+    if (n == 0) return hipSuccess;
+    LayOuts all{};
+    int64_t most = 1;
+    for (int i = 0; i < n; ++i) {
+        all.of[i] = jobs[i];
+        most = std::max(most, ceil_div(jobs[i].rows * (jobs[i].ld / 8), 256));
+    }
+    const dim3 grid((unsigned)std::min<int64_t>(most, 4096), (unsigned)n);
+    if (dt == DT_F32) k_lay_out_split<<<grid, 256, 0, st>>>(all);
+    else if (dt == DT_BF16) k_lay_out<bf16><<<grid, 256, 0, st>>>(all);
+    else k_lay_out<f16><<<grid, 256, 0, st>>>(all);
+    return hipGetLastError();
 }
 
 size_t product_workspace_bytes(int dt, const Product& p) {
@@ -354,16 +412,20 @@ hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws,
         GemmArgs g{};
         g.A = (const char*)p.A;
         g.B = (const char*)p.B;
+        LayOut jobs[2];
+        int njobs = 0;
         if (q.a.lay_out) {
-            if ((err = lay_out(dt, q.a, p.A, p.lda, Packed{}, w, st)) != hipSuccess) return err;
+            jobs[njobs++] = LayOut{p.A, p.lda, q.a.rows, q.a.cols, w, q.a.ld};
             g.A = w;
             w += q.a.bytes;
         }
         if (q.b.lay_out) {
-            if ((err = lay_out(dt, q.b, p.B, p.ldb, p.bp, w, st)) != hipSuccess) return err;
+            if (!p.bp.q) jobs[njobs++] = LayOut{p.B, p.ldb, q.b.rows, q.b.cols, w, q.b.ld};
+            else if ((err = launch_unpack8(dt == DT_F16 ? DT_F16 : DT_BF16, q.b.rows, q.b.cols, p.bp, w, q.b.ld, st)) != hipSuccess) return err;
             g.B = w;
             w += q.b.bytes;
         }
+        if ((err = launch_lay_out(dt, njobs, jobs, st)) != hipSuccess) return err;
         g.lda = q.a.ld * 2;
         g.ldb = q.b.ld * 2;
         g.apl = p.a_parts ? p.a_part : q.a.rows * q.a.ld * 2;

@@ -94,9 +94,14 @@ struct Product {
     int64_t b_part;
 };
 size_t product_workspace_bytes(int dt, const Product& p);
-// A matrix as the products take it: parts of `ld` elements a row (a multiple of 8), three of fp32.
-hipError_t launch_lay_out(int dt, int64_t rows, int64_t cols, const void* src, int64_t lds, void* dst, int64_t ld,
-                          hipStream_t st);
+// A matrix as the products take it: ld elements a row, a multiple of 8; of fp32 three parts, one after another.
+struct LayOut {
+    const void* src;
+    int64_t lds, rows, cols;
+    void* dst;
+    int64_t ld;
+};
+hipError_t launch_lay_out(int dt, int n, const LayOut* jobs, hipStream_t st);   // n <= 4
 hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws, hipStream_t st);
 
 // The gate's part of a backward pass; da is of type da_dt, dt or fp32. Of the epilogue act, z, p, z2, p2, out (dz), a and
