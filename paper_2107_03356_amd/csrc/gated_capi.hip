@@ -89,7 +89,7 @@ struct GatedBwd {
         Product p{rows, hidden, cout, at, dy_laid_out() ? lddy_in : lddy, false, w2, ldw2, true, Packed{},
                   fused ? GATE_HIDDEN : GATE_NONE};
         if (dy_laid_out()) p.a_parts = type == MFAC_F32 ? 3 : 1, p.a_part = dy_part();
-        if (type == MFAC_F32) p.B = ws + w2_in, p.ldb = ldw2_in, p.b_parts = 3, p.b_part = cout * ldw2_in * 2;
+        if (type == MFAC_F32) p.B = ws ? ws + w2_in : nullptr, p.ldb = ldw2_in, p.b_parts = 3, p.b_part = cout * ldw2_in * 2;
         return p;
     }
     Product dw2_product(const void* at, const void* a_at) const {
@@ -102,13 +102,13 @@ struct GatedBwd {
     Product dx_product(const void* dz_at, const char* ws) const {
         Product p{rows, cin, 2 * hidden, dz_at, lddz, false, w1, ldw1, true, Packed{}};
         p.a_parts = type == MFAC_F32 ? 3 : 1, p.a_part = dz_part();
-        if (type == MFAC_F32) p.B = ws + w1_in, p.ldb = ldw1_in, p.b_parts = 3, p.b_part = 2 * hidden * ldw1_in * 2;
+        if (type == MFAC_F32) p.B = ws ? ws + w1_in : nullptr, p.ldb = ldw1_in, p.b_parts = 3, p.b_part = 2 * hidden * ldw1_in * 2;
         return p;
     }
     Product dw1_product(const void* dz_at, const char* ws) const {
         Product p{2 * hidden, cin, rows, dz_at, lddz, true, x, ldx, true, xp};
         p.a_parts = parts, p.a_part = dz_part();
-        if (type == MFAC_F32 && x) p.B = ws + x_in, p.ldb = ldx_in, p.b_parts = 3, p.b_part = rows * ldx_in * 2;
+        if (type == MFAC_F32 && x) p.B = ws ? ws + x_in : nullptr, p.ldb = ldx_in, p.b_parts = 3, p.b_part = rows * ldx_in * 2;
         return p;
     }
     // What is laid out before the products, in one launch: fp32, split once, and dy where its rows are not 16-byte aligned.

@@ -530,9 +530,8 @@ def gated_feed_forward_backward(dy, x, w1, w2, z, act="silu", affine=None, grad_
     one, these would leave them off by 2e-3. db1 and db2 are float32. ``need``: which of the five to form; the others are
     None."""
     need_x, need_w1, need_b1, need_w2, need_b2 = map(bool, need)
-    db2 = act_backward(dy)[2] if need_b2 else None
     dx, dw1, db1, dw2 = _gated_backward(dy, x, w1, w2, z, act, affine, grad_dtype, (need_x, need_w1, need_b1, need_w2))
-    return dx, dw1, db1, dw2, db2
+    return dx, dw1, db1, dw2, act_backward(dy)[2] if need_b2 else None
 
 
 # ---------------------------------------------------------------- between two blocks
