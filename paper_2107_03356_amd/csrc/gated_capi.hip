@@ -381,7 +381,7 @@ MFAC_API mfac_status mfac_residual_norm(mfac_dtype type, mfac_dtype wtype, int32
 MFAC_API size_t mfac_residual_norm_bwd_workspace_bytes(mfac_dtype type, int32_t norms, int64_t rows,
                                                        int64_t cols) {
     if (!type_ok(type) || !norms_ok(norms) || rows < 0 || rows > MOST || cols < 1 || cols > MOST_HELD) return 0;
-    return (size_t)round_up(residual_bwd_parts(type, std::max<int64_t>(rows, 1), cols) * residual_sums(norms) * cols * 4, 256);
+    return (size_t)round_up(residual_bwd_parts(type, norms, std::max<int64_t>(rows, 1), cols) * residual_sums(norms) * cols * 4, 256);
 }
 
 MFAC_API mfac_status mfac_residual_norm_bwd(mfac_dtype type, mfac_dtype wtype, int32_t norms, int64_t rows, int64_t cols,

@@ -19,6 +19,7 @@ hipError_t residual_bwd(int wt, const Residual& g, const ResidualBwd& b, hipStre
 namespace {
 
 enum : int { POST_NORM = 1, PRE_NORM = 2, LAYER_NORM = 4 };   // as MFAC_NORM_*
+enum : int { NOTHING_BETWEEN = 8 };   // backward, with PRE_NORM alone: no gate, no dropout
 
 template <int N>
 using constant = std::integral_constant<int, N>;
@@ -33,26 +34,17 @@ void by_norms(int norms, F f) {
         case 5: return f(constant<5>());
         case 6: return f(constant<6>());
         case 7: return f(constant<7>());
+        case PRE_NORM | NOTHING_BETWEEN: return f(constant<PRE_NORM | NOTHING_BETWEEN>());
+        case PRE_NORM | LAYER_NORM | NOTHING_BETWEEN: return f(constant<PRE_NORM | LAYER_NORM | NOTHING_BETWEEN>());
         default: return f(constant<0>());
     }
 }
 
-// f(constant of the threads that hold a row, constant of the chunks of eight values that each has). Wider rows, whose chunks
-// would be past the registers, have kernels of their own, which rows of fewer than eight values run through as well.
+// Wider rows, whose values would be past the registers, have kernels of their own, which rows of fewer than eight values run
+// through as well.
 inline bool in_registers(int64_t cols) { return cols >= 8 && cols <= 8192; }
-template <typename T, typename F>
-void by_threads(int64_t cols, F f) {
-    constexpr int C = sizeof(T) == 2 ? 2 : 1;
-    if (cols <= 512) f(constant<64>(), constant<1>());
-    else if (cols <= 1024) f(constant<128 / C>(), constant<C>());
-    else if (cols <= 2048) f(constant<256 / C>(), constant<C>());
-    else if (cols <= 4096) f(constant<512 / C>(), constant<C>());
-    else f(constant<1024 / C>(), constant<C>());
-}
-// Rows that a work-group has at a time.
-inline int64_t rows_at_a_time(int dt, int64_t cols) {
-    return !in_registers(cols) ? 1 : cols <= (dt == DT_F32 ? 512 : 1024) ? 4 : 1;
-}
+// Chunks of eight values that a thread of the backward pass has (see by_threads_bwd).
+constexpr int residual_chunks(bool fp32, bool one) { return fp32 || one ? 1 : 2; }
 // The first row of this thread's wave, as a scalar: addresses of rows are then scalars too.
 template <int NT>
 __device__ __forceinline__ int64_t first_row() {
@@ -74,11 +66,12 @@ __device__ __forceinline__ void zero_past(f8& v, int64_t c, int64_t cols) {
 struct Place {
     unsigned at;  // of the load
     int shift;    // values in it that are another thread's, 8: all
-    bool ragged;  // some thread of the wave has one
+    bool ragged;  // some thread of the wave has one to seven of them
+    bool past;    // some thread has eight
 };
 __device__ __forceinline__ Place place_of(int c, int64_t cols) {
     const int at = min(c, (int)cols - 8), shift = min(c - at, 8);
-    return {(unsigned)at, shift, __any(shift != 0) != 0};
+    return {(unsigned)at, shift, __any(shift % 8 != 0) != 0, __any(shift == 8) != 0};
 }
 template <int N>
 struct Words {
@@ -100,30 +93,38 @@ struct Row8 {
     __device__ __forceinline__ void load(const T* __restrict__ row, const Place& p) {
         const typename VecOf<T, 8>::plain v = *reinterpret_cast<const typename VecOf<T, 8>::type*>(row + p.at);
         w = __builtin_bit_cast(typename Words<N>::type, v);
-        if (!p.ragged) return;
-        if constexpr (sizeof(T) == 4) {
-            w = move_words<N>(w, p.shift);
-        } else {
-            w = move_words<N>(w, p.shift / 2);
-            if (p.shift & 1)
-#pragma unroll
-                for (int i = 0; i < N; ++i) w[i] = __builtin_amdgcn_alignbit(i + 1 < N ? w[i + 1] : 0u, w[i], 16);
-        }
     }
     // of an 8-bit copy: q, and the group's byte in the third word
     __device__ __forceinline__ void load_copy(const int8_t* __restrict__ q, const uint8_t* __restrict__ s, int c,
                                               const Place& p) {
         const Bytes8 b = *reinterpret_cast<const Bytes8*>(q + p.at);
-        uint64_t v = (uint64_t)b.hi << 32 | b.lo;
-        if (p.ragged) v = p.shift < 8 ? v >> (8 * p.shift) : 0;
-        w[0] = (unsigned)v;
-        w[1] = (unsigned)(v >> 32);
+        w[0] = b.lo;
+        w[1] = b.hi;
         w[2] = s[min((unsigned)c, p.at + 7) >> 5];   // a thread past the end reads the last
     }
-    __device__ __forceinline__ f8 get() const {
-        return __builtin_convertvector(__builtin_bit_cast(typename VecOf<T, 8>::plain, w), f8);
+    // The values. Moved here and not where they are loaded, which would wait for them there.
+    __device__ __forceinline__ f8 get(const Place& p) const {
+        typename Words<N>::type m = w;
+        if (p.ragged) {
+            if constexpr (sizeof(T) == 4) {
+                m = move_words<N>(m, p.shift);
+            } else {
+                m = move_words<N>(m, p.shift / 2);
+                if (p.shift & 1)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) m[i] = __builtin_amdgcn_alignbit(i + 1 < N ? m[i + 1] : 0u, m[i], 16);
+            }
+        } else if (p.past) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) m[i] = p.shift ? 0u : m[i];
+        }
+        return __builtin_convertvector(__builtin_bit_cast(typename VecOf<T, 8>::plain, m), f8);
     }
-    __device__ __forceinline__ f8 get_copy() const { return RawPacked8{{w[0], w[1]}, w[2]}.get(); }
+    __device__ __forceinline__ f8 get_copy(const Place& p) const {
+        uint64_t v = (uint64_t)w[1] << 32 | w[0];
+        if (p.ragged || p.past) v = p.shift < 8 ? v >> (8 * p.shift) : 0;
+        return RawPacked8{{(unsigned)v, (unsigned)(v >> 32)}, w[2]}.get();
+    }
 };
 
 // Columns c .. c + 7 of a parameter of type wt, T or fp32, or `absent` where there is none.
@@ -133,11 +134,11 @@ __device__ __forceinline__ f8 load_param(const void* p, int wt, const Place& at,
     if (wt == DT_F32) {
         Row8<float> v;
         v.load((const float*)p, at);
-        return v.get();
+        return v.get(at);
     }
     Row8<T> v;
     v.load((const T*)p, at);
-    return v.get();
+    return v.get(at);
 }
 __device__ __forceinline__ f8 load_param(const void* p, int wt, int64_t c, int64_t cols, float absent) {
     return p ? load8_dt(p, wt, 0, c, cols) : fill8(absent);

@@ -60,19 +60,22 @@ template <typename TW>
 void params(int dt, const Residual& g, const ResidualBwd& b, hipStream_t st) {
     const bool post = g.norms & POST_NORM;
     k_residual_params<TW><<<dim3((unsigned)ceil_div(g.cols, 16), 2), 1024, 0, st>>>(
-        b.part, g.rows > 0 ? residual_bwd_parts(dt, g.rows, g.cols) : 0, residual_sums(g.norms), g.cols, post,
+        b.part, g.rows > 0 ? residual_bwd_parts(dt, g.norms, g.rows, g.cols) : 0, residual_sums(g.norms), g.cols, post,
         (const TW*)(post ? g.w1 : nullptr), (const TW*)(post ? g.b1 : nullptr), (const TW*)g.gate, (TW*)b.dw1, (TW*)b.db1,
         (TW*)b.dgate, (TW*)b.dw2, (TW*)b.db2);
 }
 
 }  // namespace
 
-// Work-groups of the backward pass, each with its column sums: as many as are on the card at once (eight waves to a CU), and no
-// more than one to four of the rows that it has at a time, since their sums are written and read again.
-int64_t residual_bwd_parts(int dt, int64_t rows, int64_t cols) {
-    const int64_t turns = ceil_div(rows, rows_at_a_time(dt, cols));
-    const int64_t waves = !in_registers(cols) ? 16 : cols <= 1024 ? 4 : ceil_div(cols, dt == DT_F32 ? 2048 : 4096) * 4;
-    return std::max(int64_t(1), std::min(ceil_div(turns, 4), 256 * std::max(int64_t(1), 8 / waves)));
+// Work-groups of the backward pass, each with its column sums: as many as are on the card at once, eight waves to a CU (sixteen where
+// a row's inputs are few or the threads' chunks small), and each at least four turns, since its sums are written and read again.
+int64_t residual_bwd_parts(int dt, int norms, int64_t rows, int64_t cols) {
+    const bool fp32 = dt == DT_F32, post = norms & POST_NORM;
+    const int64_t c = residual_chunks(fp32, norms & LAYER_NORM || !post);
+    const int64_t threads = !in_registers(cols) ? 1024 : cols <= 512 ? 64 : cols > 4096 ? 512 : round_up(cols, 512 * c) / 8 / c;
+    const int64_t waves = threads == 64 ? 4 : threads / 64, per = threads == 64 ? 4 : 1;
+    const int64_t most = 256 * std::max(int64_t(1), (!post || (!fp32 && c == 1) ? 16 : 8) / waves);
+    return std::max(int64_t(1), std::min(ceil_div(ceil_div(rows, per), 4), most));
 }
 // dw_pre and P; for layer norms db_pre and Q too.
 int residual_sums(int norms) { return norms & LAYER_NORM ? 4 : 2; }

@@ -35,11 +35,12 @@ __device__ __forceinline__ void row_means(float& a, float& b, float inv_cols, fl
     b *= inv_cols;
 }
 
-template <typename T, int NT, int NCH, int NORMS>
+template <typename T, int NT, int NCH, bool AHEAD, int NORMS>
 __global__ __launch_bounds__(norm_block(NT), 2) void k_residual_bwd(Residual g, ResidualBwd b, int wt) {
     constexpr int RPB = norm_block(NT) / NT;
     constexpr bool POST = NORMS & POST_NORM, PRE = NORMS & PRE_NORM, LAYER = NORMS & LAYER_NORM;
-    constexpr int SUMS = LAYER ? 4 : 2;
+    constexpr bool BETWEEN = !(NORMS & NOTHING_BETWEEN);
+    constexpr int SUMS = LAYER ? 4 : 2;   // without anything between, those behind N_post are not formed
     __shared__ float red[4 * (NT / 64)];
     __shared__ __attribute__((aligned(32))) float cols_of[RPB > 1 ? SUMS : 1][RPB > 1 ? RPB * NT * NCH * 8 : 1];
     int turn = 0;
@@ -51,7 +52,7 @@ __global__ __launch_bounds__(norm_block(NT), 2) void k_residual_bwd(Residual g, 
     Place at[NCH];
 #pragma unroll
     for (int j = 0; j < NCH; ++j) at[j] = place_of((j * NT + t) * 8, cols);
-    // the next row is on its way while one is worked on
+    // AHEAD: the next row is on its way while one is worked on
     Row8<T> dh[NCH], ds[NCH], y[NCH], gate[NCH], s[NCH];   // s, or the 8-bit copy of its xhat
     float mean1 = 0.f, rstd1 = 0.f, mean2 = 0.f, rstd2 = 0.f;
     auto load = [&](int64_t row) {
@@ -63,8 +64,8 @@ __global__ __launch_bounds__(norm_block(NT), 2) void k_residual_bwd(Residual g, 
                 else s[j].load((const T*)g.s + row * g.lds, at[j]);
             }
             if (b.ds) ds[j].load((const T*)b.ds + row * b.ldds, at[j]);
-            if (g.y) y[j].load((const T*)g.y + row * g.ldy, at[j]);
-            if (g.gates) gate[j].load((const T*)g.gates + row * g.ldgates, at[j]);
+            if (BETWEEN && g.y) y[j].load((const T*)g.y + row * g.ldy, at[j]);
+            if (BETWEEN && g.gates) gate[j].load((const T*)g.gates + row * g.ldgates, at[j]);
         }
         if constexpr (PRE) {
             rstd2 = g.rstd2[row];
@@ -75,18 +76,19 @@ __global__ __launch_bounds__(norm_block(NT), 2) void k_residual_bwd(Residual g, 
             if (LAYER) mean1 = g.mean1[row];
         }
     };
-    if (row < g.rows) load(row);
+    if (AHEAD && row < g.rows) load(row);
     f8 w1[NCH], w2[PRE ? NCH : 1], sum[SUMS][NCH];   // dw_pre, P, db_pre, Q
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
-        w1[j] = load_param<T>(g.gate, wt, at[j], 1.f) * load_param<T>(POST ? g.w1 : nullptr, wt, at[j], 1.f);
+        if constexpr (BETWEEN) w1[j] = load_param<T>(g.gate, wt, at[j], 1.f) * load_param<T>(POST ? g.w1 : nullptr, wt, at[j], 1.f);
         if constexpr (PRE) w2[j] = load_param<T>(g.w2, wt, at[j], 1.f);
 #pragma unroll
-        for (int i = 0; i < SUMS; ++i) sum[i][j] = fill8(0.f);
+        for (int i = 0; i < SUMS; ++i) sum[i][j] = fill8(0.f);   // of what is between: stays 0 without it
     }
     DropKey key{};
-    if (g.drop.threshold) key = drop_key(g.drop);
+    if (BETWEEN && g.drop.threshold) key = drop_key(g.drop);
     for (; row < g.rows; row += step) {
+        if (!AHEAD) load(row);
         Row8<T> dh_now[NCH], ds_now[NCH], y_now[NCH], gate_now[NCH], s_now[NCH];   // made fp32 where they are used
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
@@ -97,15 +99,15 @@ __global__ __launch_bounds__(norm_block(NT), 2) void k_residual_bwd(Residual g, 
             s_now[j] = s[j];
         }
         const float r1 = rstd1, r2 = rstd2, mu1 = mean1, mu2 = mean2;
-        if (row + step < g.rows) load(row + step);
+        if (AHEAD && row + step < g.rows) load(row + step);
         f8 d[NCH], xh[NCH];
         if constexpr (PRE) {
             float m1 = 0.f, m2 = 0.f;
 #pragma unroll
             for (int j = 0; j < NCH; ++j) {
                 const int c = (j * NT + t) * 8;
-                f8 h = dh_now[j].get();
-                xh[j] = g.p.q ? s_now[j].get_copy() : xhat_of(s_now[j].get(), mu2, r2, c, cols);
+                f8 h = dh_now[j].get(at[j]);
+                xh[j] = g.p.q ? s_now[j].get_copy(at[j]) : xhat_of(s_now[j].get(at[j]), mu2, r2, c, cols);
                 sum[0][j] += h * xh[j];
                 if constexpr (LAYER) sum[2][j] += h;
                 h *= w2[j];
@@ -119,20 +121,21 @@ __global__ __launch_bounds__(norm_block(NT), 2) void k_residual_bwd(Residual g, 
             for (int j = 0; j < NCH; ++j) {
                 d[j] = (d[j] - m1 - xh[j] * m2) * r2;
                 if constexpr (LAYER) zero_past(d[j], (j * NT + t) * 8, cols);   // m1 is everywhere
-                if (b.ds) d[j] += ds_now[j].get();
+                if (b.ds) d[j] += ds_now[j].get(at[j]);
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < NCH; ++j) d[j] = ds_now[j].get();   // there is one without N_pre
+            for (int j = 0; j < NCH; ++j) d[j] = ds_now[j].get(at[j]);   // there is one without N_pre
         }
         float n1 = 0.f, n2 = 0.f;
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
             const int c = (j * NT + t) * 8;
             if (b.dr) store8((T*)b.dr + row * b.lddr, c, cols, g.scale * d[j]);
+            if constexpr (!BETWEEN) continue;
             if (g.drop.threshold) d[j] = drop8(g.drop, key, (unsigned)row, (unsigned)(c >> 3), d[j]);
             xh[j] = fill8(0.f);
-            if (g.y) xh[j] = y_now[j].get();
+            if (g.y) xh[j] = y_now[j].get(at[j]);
             if constexpr (POST) xh[j] = xhat_of(xh[j], mu1, r1, c, cols);
             if (g.gates) {   // there is no gate for each channel: w1 is N_post's
                 if (b.dgates) {
@@ -141,7 +144,7 @@ __global__ __launch_bounds__(norm_block(NT), 2) void k_residual_bwd(Residual g, 
                     if constexpr (POST && LAYER) n += load_param<T>(g.b1, wt, at[j], 0.f);
                     store8((T*)b.dgates + row * b.lddgates, c, cols, d[j] * n);
                 }
-                d[j] *= gate_now[j].get();
+                d[j] *= gate_now[j].get(at[j]);
             }
             sum[1][j] += d[j] * xh[j];
             if constexpr (LAYER) sum[3][j] += d[j];
@@ -283,21 +286,40 @@ __global__ __launch_bounds__(1024) void k_residual_bwd_wide(Residual g, Residual
     }
 }
 
+// f(threads that hold a row, chunks of eight values that each has, whether a row is loaded ahead), as constants. A row ahead,
+// its column sums and weights are most of the registers: 16-bit rows with rms norms take two chunks a thread (248
+// registers, two waves to a SIMD); with layer norms, whose sums are twice as many, one (16384 x 4096 202 us, 347 with what two
+// would spill), and without anything between too, whose inputs are few, for the sake of more waves (92 us against 108). Above 4096 columns fp32 rows and those of layer norms would need 1024 threads, which have 128
+// registers each: 512 with two chunks and no row ahead.
+template <typename T, bool ONE, typename F>
+void by_threads_bwd(int64_t cols, F f) {
+    constexpr int C = residual_chunks(sizeof(T) == 4, ONE);
+    if (cols <= 512) f(constant<64>(), constant<1>(), std::true_type());
+    else if (cols <= 1024) f(constant<128 / C>(), constant<C>(), std::true_type());
+    else if (cols <= 2048) f(constant<256 / C>(), constant<C>(), std::true_type());
+    else if (cols <= 4096) f(constant<512 / C>(), constant<C>(), std::true_type());
+    else f(constant<512>(), constant<2>(), std::bool_constant<C == 2>());
+}
+
 }  // namespace
 
 template <typename T>
 hipError_t residual_bwd(int wt, const Residual& g, const ResidualBwd& b, hipStream_t st) {
     constexpr int DT = sizeof(T) == 4 ? DT_F32 : DT_BF16;
-    const unsigned grid = (unsigned)residual_bwd_parts(DT, g.rows, g.cols);
-    by_norms(g.norms, [&](auto norms) {
-        constexpr int NORMS = decltype(norms)::value;
-        if (!in_registers(g.cols)) {
-            k_residual_bwd_wide<T, NORMS><<<grid, 1024, (size_t)round_up(g.cols, 8) * 4, st>>>(g, b, wt);
+    const unsigned grid = (unsigned)residual_bwd_parts(DT, g.norms, g.rows, g.cols);
+    const bool between = g.norms & POST_NORM || g.y || g.gate || g.gates || g.drop.threshold;
+    const int norms = between || !in_registers(g.cols) ? g.norms : g.norms | NOTHING_BETWEEN;
+    by_norms(norms, [&](auto tag) {
+        constexpr int NORMS = decltype(tag)::value;
+        // (fp32 with layer norms, 4096 x 8192: 342 us as a wider row, 469 with what 512 threads would spill)
+        if (!in_registers(g.cols) || (sizeof(T) == 4 && g.cols > 4096 && NORMS & LAYER_NORM && !(NORMS & NOTHING_BETWEEN))) {
+            if constexpr (!(NORMS & NOTHING_BETWEEN))
+                k_residual_bwd_wide<T, NORMS><<<grid, 1024, (size_t)round_up(g.cols, 8) * 4, st>>>(g, b, wt);
             return;
         }
-        by_threads<T>(g.cols, [&](auto nt, auto nch) {
+        by_threads_bwd<T, (NORMS & (LAYER_NORM | NOTHING_BETWEEN)) != 0>(g.cols, [&](auto nt, auto nch, auto ahead) {
             constexpr int NT = decltype(nt)::value;
-            k_residual_bwd<T, NT, decltype(nch)::value, NORMS><<<grid, norm_block(NT), 0, st>>>(g, b, wt);
+            k_residual_bwd<T, NT, decltype(nch)::value, decltype(ahead)::value, NORMS><<<grid, norm_block(NT), 0, st>>>(g, b, wt);
         });
     });
     return hipGetLastError();

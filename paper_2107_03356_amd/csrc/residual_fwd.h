@@ -79,7 +79,7 @@ __global__ __launch_bounds__(norm_block(NT)) void k_residual_fwd(Residual g, int
         Row8<T> r_now[NCH], gate_now[NCH];   // made fp32 where they are used
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
-            v[j] = y[j].get();
+            v[j] = y[j].get(at[j]);
             r_now[j] = r[j];
             gate_now[j] = gate[j];
         }
@@ -92,8 +92,8 @@ __global__ __launch_bounds__(norm_block(NT)) void k_residual_fwd(Residual g, int
             v[j] *= w1[j];
             if constexpr (POST && LAYER) v[j] += b1[j];
             if (g.drop.threshold) v[j] = drop8(g.drop, key, (unsigned)row, (unsigned)(c >> 3), v[j]);
-            if (g.gates) v[j] *= gate_now[j].get();
-            if (g.r) v[j] += g.scale * r_now[j].get();
+            if (g.gates) v[j] *= gate_now[j].get(at[j]);
+            if (g.r) v[j] += g.scale * r_now[j].get(at[j]);
             if (g.s) store8((T*)g.s + row * g.lds, c, g.cols, v[j]);
         }
         if constexpr (PRE) {
@@ -180,6 +180,18 @@ __global__ __launch_bounds__(1024) void k_residual_fwd_wide(Residual g, int wt) 
             if (PRE && g.rstd2) g.rstd2[row] = rstd2;
         }
     }
+}
+
+// f(constant of the threads that hold a row, constant of the chunks of eight values that each has): 32 bytes of each input a
+// thread, so that eight waves to a CU keep enough of them on their way.
+template <typename T, typename F>
+void by_threads(int64_t cols, F f) {
+    constexpr int C = sizeof(T) == 2 ? 2 : 1;
+    if (cols <= 512) f(constant<64>(), constant<1>());
+    else if (cols <= 1024) f(constant<128 / C>(), constant<C>());
+    else if (cols <= 2048) f(constant<256 / C>(), constant<C>());
+    else if (cols <= 4096) f(constant<512 / C>(), constant<C>());
+    else f(constant<1024 / C>(), constant<C>());
 }
 
 }  // namespace

@@ -156,9 +156,9 @@ struct ResidualBwd {
     void* dgates;
     int64_t lddgates;
     void *dw1, *db1, *dw2, *db2, *dgate;   // of type wt
-    float* part;         // residual_bwd_parts(dt, rows, cols) * residual_sums(norms) * cols (unused if these are null)
+    float* part;         // residual_bwd_parts(dt, norms, rows, cols) * residual_sums(norms) * cols (unused if these are null)
 };
-int64_t residual_bwd_parts(int dt, int64_t rows, int64_t cols);
+int64_t residual_bwd_parts(int dt, int norms, int64_t rows, int64_t cols);
 int residual_sums(int norms);
 hipError_t launch_residual_bwd(int dt, int wt, const Residual& g, const ResidualBwd& b, hipStream_t st);
 

@@ -85,7 +85,7 @@ hipError_t launch_dropout(int, int64_t, int64_t, const void*, int64_t, Drop d, v
     return launched();
 }
 hipError_t launch_residual(int, int, const Residual&, hipStream_t) { return launched(); }
-int64_t residual_bwd_parts(int, int64_t rows, int64_t) { return rows < 5 ? rows : 5; }
+int64_t residual_bwd_parts(int, int, int64_t rows, int64_t) { return rows < 5 ? rows : 5; }
 int residual_sums(int norms) { return norms & 4 ? 4 : 2; }
 hipError_t launch_residual_bwd(int, int, const Residual&, const ResidualBwd&, hipStream_t) { return launched(); }
 }  // namespace mfac
