@@ -1,6 +1,7 @@
 """Trains a stack of feed-forward blocks with M-FAC, with the activations kept whole or in 8 bits.
 
-    python examples/feed_forward_mfac.py [--copy8] [--bf16] [--steps N] [--dim D] [--blocks B] [--rows R]
+    python examples/feed_forward_mfac.py [--gated [--dropout P]] [--copy8] [--bf16] [--steps N] [--dim D] [--blocks B]
+                                         [--rows R]
 
 The task is regression onto a fixed random network of the same shape. Prints the
 loss, the bytes that the forward pass keeps for the backward pass, and the time
@@ -20,7 +21,10 @@ from paper_2107_03356_amd import nn  # noqa: E402
 from paper_2107_03356_amd.optim import MFAC  # noqa: E402
 
 
-def model(dim, blocks, copy8, device):
+def model(dim, blocks, copy8, device, gated=False, dropout=0.0):
+    if gated:   # rms norms, gated layers, a learned gate for each channel
+        return torch.nn.Sequential(nn.GatedStack(dim, 8 * dim // 3, blocks, gate=1.0, p=dropout, copy8=copy8, device=device),
+                                   nn.Linear(dim, dim, device=device))
     return torch.nn.Sequential(*[nn.FeedForward(dim, 4 * dim, act="gelu_tanh", copy8=copy8, device=device)
                                  for _ in range(blocks)],
                                nn.LayerNorm(dim, copy8=copy8, device=device), nn.Linear(dim, dim, device=device))
@@ -28,6 +32,8 @@ def model(dim, blocks, copy8, device):
 
 def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    ap.add_argument("--gated", action="store_true", help="gated blocks (GatedStack) in place of plain ones")
+    ap.add_argument("--dropout", type=float, default=0.0, help="dropout of the gated blocks")
     ap.add_argument("--copy8", action="store_true", help="keep activations in 8 bits")
     ap.add_argument("--bf16", action="store_true", help="bfloat16 activations (parameters stay float32)")
     ap.add_argument("--steps", type=int, default=60)
@@ -40,9 +46,9 @@ def main():
     dtype = torch.bfloat16 if a.bf16 else torch.float32
     x = torch.randn(a.rows, a.dim, device=dev)
     with torch.no_grad():
-        target = model(a.dim, a.blocks, False, dev)(x)
+        target = model(a.dim, a.blocks, False, dev, a.gated)(x)
     x = x.to(dtype)
-    net = model(a.dim, a.blocks, a.copy8, dev)
+    net = model(a.dim, a.blocks, a.copy8, dev, a.gated, a.dropout)
     opt = MFAC(net.parameters(), lr=0.05, m=32, damp=1e-2)
 
     kept = {}

@@ -587,31 +587,42 @@ def dropout_forward(x, p, at):
 
 def _between(y, post, pre, gate, kind):
     """(norms, type code of the parameters, post w, post b, pre w, pre b, gate, gates) for rows like y."""
-    if kind not in KINDS:
+    layer = KINDS.get(kind)
+    if layer is None:
         raise ValueError(f"residual_norm: kind is one of {', '.join(KINDS)}, not {kind!r}")
-    norms = (B.MFAC_NORM_POST if post is not None else 0) | (B.MFAC_NORM_PRE if pre is not None else 0)
-    found, like = [], None
-    for what, norm in (("post", post), ("pre", pre)):
+    norms, w1, b1, w2, b2, gv, gm = 0, None, None, None, None, None, None
+
+    def vector(v, like):
+        v = _param("residual_norm: parameters", v, y, y.shape[1])
+        if like is not None and v.dtype is not like:
+            raise ValueError("residual_norm: parameters of one type")
+        return v, v.dtype
+
+    found = None
+    for i, norm in ((0, post), (1, pre)):
+        if norm is None:
+            continue
         try:
-            w, b = (None, None) if norm is None else norm
+            w, b = norm
         except (TypeError, ValueError):
-            raise ValueError(f"residual_norm: {what} is None or a pair (weight, bias)") from None
-        if b is not None and kind == "rms":
-            raise ValueError("residual_norm: rms norm has no bias")
-        found += [w, b]
-    vector = gate is not None and gate.dim() == 1
-    found.append(gate if vector else None)
-    for i, v in enumerate(found):
-        if v is not None:
-            found[i] = v = _param("residual_norm: parameters", v, y, y.shape[1])
-            like = v if like is None else like
-            if v.dtype is not like.dtype:
-                raise ValueError("residual_norm: parameters of one type")
-    gates = None
-    if gate is not None and not vector:
-        gates = _rows(gate, "residual_norm: gate")
-        _same("residual_norm: gate", gates, y, y.shape)
-    return (norms | KINDS[kind] if norms else 0, _TYPES[torch.float32 if like is None else like.dtype], *found, gates)
+            raise ValueError("residual_norm: a norm is None or a pair (weight, bias)") from None
+        if w is not None:
+            w, found = vector(w, found)
+        if b is not None:
+            if not layer:
+                raise ValueError("residual_norm: rms norm has no bias")
+            b, found = vector(b, found)
+        if i == 0:
+            w1, b1, norms = w, b, B.MFAC_NORM_POST
+        else:
+            w2, b2, norms = w, b, norms | B.MFAC_NORM_PRE
+    if gate is not None:
+        if gate.dim() == 1:
+            gv, found = vector(gate, found)
+        else:
+            gm = _rows(gate, "residual_norm: gate")
+            _same("residual_norm: gate", gm, y, y.shape)
+    return norms | layer if norms else 0, _TYPES[found or torch.float32], w1, b1, w2, b2, gv, gm
 
 
 def residual_norm_forward(y, residual=None, post=None, pre=None, gate=None, scale=1.0, p=0.0, at=None, kind="rms", eps=1e-6,
@@ -627,7 +638,7 @@ def residual_norm_forward(y, residual=None, post=None, pre=None, gate=None, scal
     y2 = _rows(y, "residual_norm: y")
     rows, cols = y2.shape
     norms, wt, w1, b1, w2, b2, gv, gm = _between(y2, post, pre, gate, kind)
-    p, ptr = _drop(p, at, y2)
+    p, ptr = _drop(p, at, y2) if p != 0 or at is not None else (0.0, None)
     if residual is not None:
         residual = _rows(residual, "residual_norm: residual")
         _same("residual_norm: residual", residual, y2, y2.shape)
@@ -638,13 +649,15 @@ def residual_norm_forward(y, residual=None, post=None, pre=None, gate=None, scal
         return ResidualNorm(y, None, None, None, None)
     s = None if plain else _like(y)
     h = None if pre is None else _like(y)
-    layer = kind == "layer"
-
-    def row_values(on):
-        return torch.empty((rows,), dtype=torch.float32, device=y.device) if on and stats else None
-
-    m1, r1 = row_values(post is not None and layer), row_values(post is not None)
-    m2, r2 = row_values(pre is not None and layer), row_values(pre is not None)
+    m1 = r1 = m2 = r2 = None
+    if stats:
+        layer, device = kind == "layer", y.device
+        if post is not None:
+            r1 = torch.empty(rows, dtype=torch.float32, device=device)
+            m1 = torch.empty_like(r1) if layer else None
+        if pre is not None:
+            r2 = torch.empty(rows, dtype=torch.float32, device=device)
+            m2 = torch.empty_like(r2) if layer else None
     copy = Packed8.empty(rows, cols, y.device) if pack else None
     q = _NO_COPY if copy is None else copy._args()
     _call("mfac_residual_norm", y.device, _type(y2, "residual_norm: y"), wt, norms, rows, cols, *_mat(y2), _ptr(w1),
@@ -670,16 +683,20 @@ def residual_norm_backward(ds, dh, y, s, post_stats=None, pre_stats=None, post=N
     need_y, need_r, need_gate, need_params = need
     need_gate = need_gate and gate is not None
 
+    shape, dtype, device = d2.shape, d2.dtype, d2.device
+
     def rows_of(t, what):
-        t = _rows(t, "residual_norm: " + what)
-        _same("residual_norm: " + what, t, d2, d2.shape)
+        t = _rows(t, what)
+        if t.dtype is not dtype or t.shape != shape or t.device != device:
+            raise ValueError(f"residual_norm: {what}: {tuple(shape)} {dtype} on {device}, not {tuple(t.shape)} {t.dtype} on "
+                             f"{t.device}")
         return t
 
     def stats_of(stats, on, what, mean_needed):
         mean, rstd = (None, None) if not on else stats if stats is not None else (None, None)
         for t in (mean, rstd):
             if t is not None and (t.dtype != torch.float32 or t.numel() != rows or not t.is_contiguous()
-                                  or t.device != d2.device):
+                                  or t.device != device):
                 raise ValueError(f"residual_norm: {what} statistics are contiguous float32 tensors, one value for each row")
         if on and (rstd is None or (mean_needed and mean is None)):
             raise ValueError(f"residual_norm: needs {what} statistics")
@@ -714,8 +731,8 @@ def residual_norm_backward(ds, dh, y, s, post_stats=None, pre_stats=None, post=N
     t = _type(d2, "residual_norm: ds, dh")
     grads, ws = [None] * 5, (None, 0, None)
     if any(wanted):
-        dtype = next(v.dtype for v in (w1, b1, w2, b2, gv) if v is not None)
-        parts = iter(torch.empty((sum(wanted), cols), dtype=dtype, device=like.device).unbind(0))
+        of = next(v.dtype for v in (w1, b1, w2, b2, gv) if v is not None)
+        parts = iter(torch.empty((sum(wanted), cols), dtype=of, device=device).unbind(0))
         grads = [next(parts) if on else None for on in wanted]
         ws = _workspace(_function("mfac_residual_norm_bwd_workspace_bytes")(t, norms, rows, cols), like.device)
     dg = _like(gate) if gm is not None and need_gate else None

@@ -387,3 +387,40 @@ def test_memory_of_dropout_and_copies(dev):
     weights = sum(v.untyped_storage().nbytes() for v in w)
     whole, small = (kept(lambda: nn.gated_feed_forward(x, *w, copy8=c)) - weights for c in (False, True))
     assert whole == 2 * 4096 * (512 + 2048) and small <= 0.52 * whole, (whole, small)
+
+
+@pytest.mark.parametrize("args", [["--gated"], ["--gated", "--dropout", "0.1", "--copy8", "--bf16"]])
+def test_example_runs(dev, args, monkeypatch, capsys):
+    import importlib.util
+    import os
+    import sys
+    say("example", args)
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "feed_forward_mfac.py")
+    spec = importlib.util.spec_from_file_location("feed_forward_mfac", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    monkeypatch.setattr(sys, "argv", [path, "--steps", "3", "--rows", "256", "--dim", "72", "--blocks", "2"] + args)
+    example.main()
+    out = capsys.readouterr().out
+    assert "optimizer status 0" in out and "nan" not in out
+
+
+def test_example_model_gradients(dev):
+    """The example's gated model against the definition in 64 bits."""
+    import importlib.util
+    import os
+    say("example gradients")
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "feed_forward_mfac.py")
+    spec = importlib.util.spec_from_file_location("feed_forward_mfac", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    torch.manual_seed(0)
+    net = example.model(48, 2, False, dev, gated=True)
+    x, dy = rand(dev, 1, 64, 48), rand(dev, 2, 64, 48)
+    net(x).backward(dy)
+    h, p = stack64(net[0], x.double(), [1.0, 1.0])
+    w, b = (v.detach().double().requires_grad_() for v in (net[1].weight, net[1].bias))
+    (h @ w.t() + b).backward(dy.double())
+    for name, v in net[0].named_parameters():
+        assert rel(v.grad, p[name].grad) <= 1e-5, name
+    assert rel(net[1].weight.grad, w.grad) <= 1e-5
