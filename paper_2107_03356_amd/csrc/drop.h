@@ -23,8 +23,9 @@ __device__ __forceinline__ DropKey drop_key(const Drop& d) {
     return {(unsigned)seed, (unsigned)(seed >> 32), (unsigned)offset, (unsigned)(offset >> 32)};
 }
 
-// Columns 8 group .. + 7 of a row: kept values times d.scale, others 0 (an infinity or a NaN too).
-__device__ __forceinline__ f8 drop8(const Drop& d, const DropKey& k, unsigned row, unsigned group, f8 v) {
+// Columns 8 group .. + 7 of a row: kept values times d.scale, others 0 (an infinity or a NaN too). `beside`: values that become
+// 0 with them, unscaled.
+__device__ __forceinline__ f8 drop8(const Drop& d, const DropKey& k, unsigned row, unsigned group, f8 v, f8* beside = nullptr) {
     unsigned c0 = group, c1 = row, c2 = k.c2, c3 = k.c3, k0 = k.k0, k1 = k.k1;
 #pragma unroll
     for (int i = 0; i < 10; ++i) {
@@ -39,9 +40,10 @@ __device__ __forceinline__ f8 drop8(const Drop& d, const DropKey& k, unsigned ro
     const unsigned w[4] = {c0, c1, c2, c3};
     f8 r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        r[2 * i] = (w[i] & 0xffffu) >= d.threshold ? v[2 * i] * d.scale : 0.f;
-        r[2 * i + 1] = (w[i] >> 16) >= d.threshold ? v[2 * i + 1] * d.scale : 0.f;
+    for (int i = 0; i < 8; ++i) {
+        const bool keep = (i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu) >= d.threshold;
+        r[i] = keep ? v[i] * d.scale : 0.f;
+        if (beside) (*beside)[i] = keep ? (*beside)[i] : 0.f;
     }
     return r;
 }

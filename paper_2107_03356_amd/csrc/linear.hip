@@ -43,8 +43,7 @@ extern template hipError_t run_product<f16, HIDDEN>(const Product&, const Plan&,
 
 namespace {
 
-// Joins the K parts in order and finishes. Eight parts are on their way at a time: one by one, many parts of few sums wait
-// for each.
+// Joins the K parts in order and finishes.
 template <int KIND>
 __global__ __launch_bounds__(256) void k_finish(const float* __restrict__ part, int splits, int64_t M, int64_t N,
                                                 Epilogue e) {
@@ -54,15 +53,8 @@ __global__ __launch_bounds__(256) void k_finish(const float* __restrict__ part, 
         const int64_t u = u0 + threadIdx.x, m = u / pieces, n = (u - m * pieces) * 8;
         const bool in = m < M;
         f8 v = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        constexpr int AHEAD = 8;
-        for (int z = 0; in && z < splits; z += AHEAD) {
-            f8 a[AHEAD];
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) a[i] = load8(part + (min(z + i, splits - 1) * M + m) * N, n, N);
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i)
-                if (z + i < splits) v += a[i];
-        }
+        if (in)
+            for (int z = 0; z < splits; ++z) v += load8(part + (z * M + m) * N, n, N);
         finish8<KIND>(e, N, in, m, n, v);
     }
 }
@@ -86,9 +78,9 @@ __global__ __launch_bounds__(256) void k_finish_gated(const float* __restrict__ 
             f8 a[4][SIDES];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
+                if (z + i * GROUPS < splits)
 #pragma unroll
-                for (int k = 0; k < SIDES; ++k)
-                    a[i][k] = load8(part + ((min(z + i * GROUPS, splits - 1) * M + m) * SIDES + k) * N, n, N);
+                    for (int k = 0; k < SIDES; ++k) a[i][k] = load8(part + (((z + i * GROUPS) * M + m) * SIDES + k) * N, n, N);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (z + i * GROUPS < splits)
@@ -232,16 +224,18 @@ __global__ __launch_bounds__(NW * 64) void k_skinny(SkinnyArgs g) {
 }
 
 // ---------------------------------------------------------------- operands into the workspace
-// Up to four matrices in one launch (blockIdx.y), since a launch takes longer than a small matrix:
+// Up to four matrices in one launch (blockIdx.y), since a launch takes longer than a small matrix, or one:
 // dst (rows of ld elements, ld a multiple of 8) <- src, zeros past cols.
 struct LayOuts {
     LayOut of[4];
 };
-template <typename T>
-__global__ __launch_bounds__(256) void k_lay_out(LayOuts jobs) {
-    const LayOut& j = jobs.of[blockIdx.y];
-    const T* src = (const T*)j.src;
-    T* dst = (T*)j.dst;
+__device__ __forceinline__ const LayOut& this_one(const LayOut& j) { return j; }
+__device__ __forceinline__ const LayOut& this_one(const LayOuts& j) { return j.of[blockIdx.y]; }
+template <typename T, typename J>
+__global__ __launch_bounds__(256) void k_lay_out(J jobs) {
+    const LayOut& j = this_one(jobs);
+    const T* __restrict__ src = (const T*)j.src;
+    T* __restrict__ dst = (T*)j.dst;
     const int64_t pieces = j.ld / 8, total = j.rows * pieces;
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
         const int64_t r = u / pieces, c = (u - r * pieces) * 8;
@@ -249,14 +243,17 @@ __global__ __launch_bounds__(256) void k_lay_out(LayOuts jobs) {
     }
 }
 // The same from fp32 into three bf16 planes, one after another.
-__global__ __launch_bounds__(256) void k_lay_out_split(LayOuts jobs) {
+template <typename J>
+__global__ __launch_bounds__(256) void k_lay_out_split(J jobs) {
     typedef VecOf<bf16, 8>::plain b8;
-    const LayOut& j = jobs.of[blockIdx.y];
+    const LayOut& j = this_one(jobs);
+    const float* __restrict__ src = (const float*)j.src;
+    bf16* __restrict__ dst = (bf16*)j.dst;
     const int64_t pieces = j.ld / 8, total = j.rows * pieces, plane = j.rows * j.ld;
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
         const int64_t r = u / pieces, c = (u - r * pieces) * 8;
-        f8 x = load8((const float*)j.src + r * j.lds, c, j.cols);
-        bf16* d = (bf16*)j.dst + r * j.ld + c;
+        f8 x = load8(src + r * j.lds, c, j.cols);
+        bf16* d = dst + r * j.ld + c;
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
             // the first part cut at bf16's largest value, to which the second adds the rest: rounded, a
@@ -375,9 +372,14 @@ hipError_t launch_lay_out(int dt, int n, const LayOut* jobs, hipStream_t st) {
         most = std::max(most, ceil_div(jobs[i].rows * (jobs[i].ld / 8), 256));
     }
     const dim3 grid((unsigned)std::min<int64_t>(most, 4096), (unsigned)n);
-    if (dt == DT_F32) k_lay_out_split<<<grid, 256, 0, st>>>(all);
-    else if (dt == DT_BF16) k_lay_out<bf16><<<grid, 256, 0, st>>>(all);
-    else k_lay_out<f16><<<grid, 256, 0, st>>>(all);
+    auto run = [&](const auto& j) {
+        using J = std::decay_t<decltype(j)>;
+        if (dt == DT_F32) k_lay_out_split<J><<<grid, 256, 0, st>>>(j);
+        else if (dt == DT_BF16) k_lay_out<bf16, J><<<grid, 256, 0, st>>>(j);
+        else k_lay_out<f16, J><<<grid, 256, 0, st>>>(j);
+    };
+    if (n == 1) run(jobs[0]);
+    else run(all);
     return hipGetLastError();
 }
 

@@ -133,10 +133,11 @@ __global__ __launch_bounds__(norm_block(NT), 2) void k_residual_bwd(Residual g, 
             const int c = (j * NT + t) * 8;
             if (b.dr) store8((T*)b.dr + row * b.lddr, c, cols, g.scale * d[j]);
             if constexpr (!BETWEEN) continue;
-            if (g.drop.threshold) d[j] = drop8(g.drop, key, (unsigned)row, (unsigned)(c >> 3), d[j]);
             xh[j] = fill8(0.f);
             if (g.y) xh[j] = y_now[j].get(at[j]);
             if constexpr (POST) xh[j] = xhat_of(xh[j], mu1, r1, c, cols);
+            // y where it was dropped took no part: a NaN there must not come into dgate through 0 times it
+            if (g.drop.threshold) d[j] = drop8(g.drop, key, (unsigned)row, (unsigned)(c >> 3), d[j], POST ? nullptr : &xh[j]);
             if (g.gates) {   // there is no gate for each channel: w1 is N_post's
                 if (b.dgates) {
                     f8 n = xh[j];
@@ -249,9 +250,9 @@ __global__ __launch_bounds__(1024) void k_residual_bwd_wide(Residual g, Residual
                 d += (h - m1 - xhat2(c) * m2) * rstd2;
                 zero_past(d, c, cols);
             }
-            const f8 xh = xhat1(c);
+            f8 xh = xhat1(c);
             if (b.dr) store8((T*)b.dr + row * b.lddr, c, cols, g.scale * d);
-            if (g.drop.threshold) d = drop8(g.drop, key, (unsigned)row, (unsigned)(c >> 3), d);
+            if (g.drop.threshold) d = drop8(g.drop, key, (unsigned)row, (unsigned)(c >> 3), d, POST ? nullptr : &xh);
             if (g.gates) {
                 const f8 by = load8((const T*)g.gates + row * g.ldgates, c, cols);
                 if (b.dgates) {

@@ -590,6 +590,8 @@ def _between(y, post, pre, gate, kind):
     layer = KINDS.get(kind)
     if layer is None:
         raise ValueError(f"residual_norm: kind is one of {', '.join(KINDS)}, not {kind!r}")
+    if y.shape[1] > 1 << 15:
+        raise ValueError(f"residual_norm: at most 32768 columns, not {y.shape[1]}")
     norms, w1, b1, w2, b2, gv, gm = 0, None, None, None, None, None, None
 
     def vector(v, like):

@@ -39,7 +39,7 @@ PAIR = (z(5, 12), z(5, 12))
     lambda: nn.gated_feed_forward_backward(X, X, W1, z(15, 12), PAIR), lambda: nn.gated_feed_forward_backward(X, X, W1, W2, PAIR, "nope"),
     lambda: nn.gated_feed_forward_backward(X, X, W1, W2, PAIR, affine=(z(16, dtype=F32), z(15, dtype=F32))),
     lambda: nn.gated_feed_forward_backward(X, X, W1, W2, PAIR, affine=(None, z(16, dtype=F32))),
-    lambda: nn.residual_norm_forward(X, kind="mean"), lambda: nn.residual_norm_forward(X, z(4, 16)),
+    lambda: nn.residual_norm_forward(z(1, 32769), pre=(None, None)), lambda: nn.residual_norm_forward(X, kind="mean"), lambda: nn.residual_norm_forward(X, z(4, 16)),
     lambda: nn.residual_norm_forward(X, z(5, 16, dtype=F32)), lambda: nn.residual_norm_forward(X, pre=(z(16), z(16))),
     lambda: nn.residual_norm_forward(X, pre=z(15)), lambda: nn.residual_norm_forward(X, pre=(z(15), None)),
     lambda: nn.residual_norm_forward(X, pre=(z(16), None), post=(z(16, dtype=F32), None)), lambda: nn.residual_norm_forward(X, X, pack=True),

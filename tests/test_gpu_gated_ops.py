@@ -404,6 +404,45 @@ def test_rows_that_are_not_finite_stay_alone(dev):
         assert (o.h == 0).all()
 
 
+def test_values_that_are_dropped_take_no_part(dev):
+    """Without a norm after the block, a NaN or an infinity of y that the mask drops comes into nothing, the gate's gradient
+    among it."""
+    from paper_2107_03356_amd import nn
+    say("dropped values")
+    for cols in (200, 9000):
+        at = torch.tensor([3, 4], device=dev)
+        f = drop_factor(40, cols, 0.5, (3, 4)).to(dev)
+        clean, r, ds = rand(dev, 1, 40, cols), rand(dev, 2, 40, cols), rand(dev, 3, 40, cols)
+        clean[f == 0] = 0
+        bad = torch.where((f == 0) & (clean == 0), torch.tensor(float("nan"), device=dev), clean)
+        bad[7] = torch.where(f[7] == 0, torch.tensor(float("inf"), device=dev), clean[7])
+        for gate in (rand(dev, 4, cols), rand(dev, 5, 40, cols)):
+            runs = []
+            for y in (clean, bad):
+                s = nn.residual_norm_forward(y, r, gate=gate, p=0.5, at=at).s
+                g = nn.residual_norm_backward(ds, None, y, s, gate=gate, p=0.5, at=at)
+                runs.append((s, g.dy, g.dresidual, g.dgate))
+            assert all(torch.equal(u, v) and torch.isfinite(u).all() for u, v in zip(*runs))
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_norms_without_parameters(dev, kind):
+    """A norm without weight and bias is that of ones and zeros."""
+    from paper_2107_03356_amd import nn
+    say("no parameters", kind)
+    for cols in (5, 300, 9000):
+        y, r, ds, dh = (rand(dev, s, 20, cols) for s in (1, 2, 3, 4))
+        one, zero = torch.ones(cols, device=dev), torch.zeros(cols, device=dev) if kind == "layer" else None
+        runs = []
+        for norm in ((None, None), (one, zero)):
+            o = nn.residual_norm_forward(y, r, post=norm, pre=norm, kind=kind)
+            g = nn.residual_norm_backward(ds, dh, y, o.s, o.post, o.pre, post=norm, pre=norm, kind=kind)
+            runs.append((o.s, o.h, g.dy, g.dresidual))
+            assert (g.dpost[0] is None) == (g.dpre[0] is None) == (norm[0] is None)
+            assert (g.dpost[1] is None) == (g.dpre[1] is None) == (norm[1] is None)
+        assert all(torch.equal(u, v) for u, v in zip(*runs))
+
+
 def test_no_rows(dev):
     from paper_2107_03356_amd import nn
     say("no rows")
