@@ -12,7 +12,7 @@ namespace mfac {
 namespace {
 
 // v in 16-bit parts of type R, each what the rounding of those before it leaves: one or two of 16-bit data, three of fp32,
-// of which the first is cut at bf16's largest value (see k_lay_out_split in linear.hip).
+// of which the first is cut at bf16's largest value (see k_lay_out_split in linear.hip). fp16's second: see rest_of.
 template <typename T, typename R>
 __device__ __forceinline__ void store_parts_as(void* base, int64_t part, int parts, int64_t off, int64_t c, int64_t cols, f8 v) {
     typedef typename VecOf<R, 8>::plain V;
@@ -22,7 +22,7 @@ __device__ __forceinline__ void store_parts_as(void* base, int64_t part, int par
             x = __builtin_elementwise_min(__builtin_elementwise_max(x, f8(-0x1.fep127f)), f8(0x1.fep127f));
         const f8 r = __builtin_convertvector(__builtin_convertvector(x, V), f8);
         store8((R*)((char*)base + p * part) + off, c, cols, r);
-        v -= r;
+        v = (v - r) * REST_SCALE<R>;
     }
 }
 

@@ -561,7 +561,7 @@ __device__ __forceinline__ void epilogue_hidden(const GemmArgs& g, float* part, 
         *reinterpret_cast<typename VecOf<T, 8>::type*>(at) = first;
         if (e.parts == 1) return;
         at = (T*)((char*)at + apart);
-        *reinterpret_cast<typename VecOf<T, 8>::type*>(at) = __builtin_convertvector(v - __builtin_convertvector(first, f8), V);
+        *reinterpret_cast<typename VecOf<T, 8>::type*>(at) = __builtin_convertvector(rest_of<T>(v), V);
     };
     load(m0);
     for_each_index(std::make_integer_sequence<int, MT>(), [&](auto tag) {
@@ -702,6 +702,9 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
     constexpr std::integral_constant<int, 0> none{};
 
     const int steps = s_end - s_begin;
+    // The second parts of fp16 come first, as stored: after their last step the sums lose their factor.
+    constexpr bool RESTS = KIND == WEIGHT && std::is_same_v<T, f16>;
+    const int rests = RESTS && g.nseg == 2 ? min(g.ksteps - s_begin, steps) : 0;
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i)
         if (i < steps) issue(i);
@@ -723,6 +726,11 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
         read(next, 0);   // after the last step, of what lies there: not used
         multiply(1);
         stage = next;
+        if (RESTS && s + 1 == rests)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NTL; ++j) acc[i][j] *= 1.f / REST_SCALE<T>;
     }
 
     float* part = g.splits > 1 ? g.part + (int64_t)k_part * g.M * g.N * (KIND == GATED ? 2 : 1) : nullptr;

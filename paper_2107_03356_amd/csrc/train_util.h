@@ -346,11 +346,14 @@ __device__ __forceinline__ void gate_slopes(int act, V (&g)[N], V (&u)[N], V (&d
     }
 }
 
-// What the rounding of v to T leaves.
+// What the rounding of v to T leaves, as it is stored beside it: times 2^11 in fp16, whose range would cut it (a gradient of
+// 2^-10 leaves 2^-21, and fp16 has steps of 2^-24). In bf16 it has the range of v. Products take the factor out again.
+template <typename T>
+constexpr float REST_SCALE = std::is_same_v<T, f16> ? 2048.f : 1.f;
 template <typename T, typename V>
 __device__ __forceinline__ V rest_of(V v) {
     typedef typename VecOf<T, sizeof(V) / 4>::plain R;
-    return v - __builtin_convertvector(__builtin_convertvector(v, R), V);
+    return (v - __builtin_convertvector(__builtin_convertvector(v, R), V)) * REST_SCALE<T>;
 }
 
 // ---------------------------------------------------------------- sums over a wave

@@ -275,6 +275,28 @@ def test_gated_feed_forward_backward(dev, dtype, rows, dim, hid):
                     assert got[2] is None and got[4] is None
 
 
+@pytest.mark.parametrize("size", [1.0, 2.0 ** -9, 2.0 ** -16])
+@pytest.mark.parametrize("rows,hid", [(1, 64), (130, 515), (333, 192), (1300, 64)])
+def test_fp16_gradients_as_small_as_they_come(dev, rows, hid, size):
+    """With x the identity, dw1 is dz transposed, from two fp16 parts: the second is stored times 2^11, where a step of
+    fp16 is at least 2^-24, so the two are within 2^-36 of a value, however small."""
+    from paper_2107_03356_amd import nn
+    say("fp16 gradients as small as they come", rows, hid, size)
+    dim, x = 40, torch.eye(rows, dtype=F16, device=dev)
+    z = rand(dev, 2, rows, hid, dtype=F16), rand(dev, 3, rows, hid, dtype=F16)
+    dy, w2 = (rand(dev, 4, rows, dim) * size).to(F16), rand(dev, 5, dim, hid, dtype=F16, scale=dim ** -0.5)
+    w1, mine = rand(dev, 6, 2 * hid, rows, dtype=F16), (rand(dev, 7, rows, hid) * size).to(F16)
+    zero = torch.zeros(rows, hid, dtype=torch.float64, device=dev)
+    da, ed = dy.double() @ w2.double(), E32 * growth(dim) * (dy.double().abs() @ w2.double().abs())
+    for d, err, got in (
+            (da, ed, nn.gated_feed_forward_backward(dy, x, w1, w2, z, grad_dtype=F32, need=(False, True, False, True, False))[1]),
+            (mine.double(), zero, nn.gated_linear_backward(mine, x, w1, z, grad_dtype=F32, need=(False, True, False))[1])):
+        (dg, eg), (du, eu), _ = gate_slopes64("silu", z[0].double(), z[1].double(), d, err)
+        dz, e = torch.cat([dg, du], 1), torch.cat([eg, eu], 1)
+        # a product with 1 and sums with 0 are exact; the two parts' sum is rounded once, joined parts of K once more
+        holds(got, dz.t(), (1.02 * U[F16] ** 2 * dz.abs() + 1.01 * e + 2.0 ** -36 + 2 * E32 * dz.abs()).t(), (rows, hid, size))
+
+
 # ---------------------------------------------------------------- between two blocks
 SIZES = [(1, 1), (3, 7), (5, 64), (77, 512), (33, 513), (9, 1000), (6, 1025), (7, 2048), (4, 4093), (5, 8192), (3, 8193), (4, 9000),
          (2, 32768), (1500, 40)]
