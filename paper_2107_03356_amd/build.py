@@ -60,7 +60,10 @@ def build(verbose: bool = False) -> str:
         # B) are measured wins over fewer waves without them; k_trmm32 (12 and
         # 76 bytes) keeps a few values there that it reloads once per row
         # tile, outside its k loop; k_norm_bwd with 1024 threads a row (12 bytes)
-        # has 128 registers and two constants too many
+        # has 128 registers and two constants too many, k_residual_fwd of fp32
+        # layer norms with as many (28) a few more; k_residual_bwd with 512
+        # threads of two chunks (52 to 76) keeps weights there, which it reads
+        # once a row
         name = None
         for line in r.stderr.splitlines():
             m = re.search(r"Function Name: (\S+)", line)

@@ -1,4 +1,4 @@
-// Dropout's mask on the device (dropout.hip, residual_fwd.hip, residual_bwd.hip): formed from a counter where it is
+// Dropout's mask on the device (dropout.hip, residual_fwd.h, residual_bwd.h): formed from a counter where it is
 // used, forward and backward, and never stored.
 //
 // Philox 4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", SC 2011): ten rounds of

@@ -9,11 +9,12 @@
 //   gated     y = act(x Wg^T + bg) (x Wu^T + bu)     a tile of C has half its columns from each
 //   hidden    da = dy W2, of which the epilogue forms dz = [da zu act'(zg), da act(zg)] and a = act(zg) zu
 //
-// Three kernels share one epilogue:
+// The kernels finish their sums alike (finish8 and the epilogues of product.h):
 //   k_product  16-bit operands on v_mfma_f32_16x16x32, tiles of C in registers,
-//              operand tiles copied from memory straight into LDS;
+//              operand tiles copied from memory straight into LDS (product.h);
 //   k_skinny   few rows of C: W streams through registers once, no LDS;
-//   k_finish   joins the K parts of a product that was split over work-groups.
+//   k_finish   joins the K parts of a product that was split over work-groups
+//              (k_finish_gated those of a gated layer).
 // Operands that the copies into LDS cannot take as they are (rows that do not start
 // 16-byte aligned, 8-bit copies, fp32) are laid out first in the workspace: fp32 as
 // three bf16 planes, hi + mid + lo, of whose nine products six are summed (|mid| is at most
@@ -391,7 +392,7 @@ size_t product_workspace_bytes(int dt, const Product& p) {
 hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws, hipStream_t st) {
     const Plan q = plan_of(dt, p);
     char* w = (char*)ws;
-    hipError_t err;
+    hipError_t err = hipSuccess;
     if (q.skinny) {
         const bool gated = p.gate == GATE_FORWARD;
         SkinnyArgs g{p.A, p.B, p.lda, p.ldb, p.M, gated ? p.N / 2 : p.N, p.K, 16, e};
@@ -423,7 +424,8 @@ hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws,
         }
         if (q.b.lay_out) {
             if (!p.bp.q) jobs[njobs++] = LayOut{p.B, p.ldb, q.b.rows, q.b.cols, w, q.b.ld};
-            else if ((err = launch_unpack8(dt == DT_F16 ? DT_F16 : DT_BF16, q.b.rows, q.b.cols, p.bp, w, q.b.ld, st)) != hipSuccess) return err;
+            else err = launch_unpack8(dt == DT_F16 ? DT_F16 : DT_BF16, q.b.rows, q.b.cols, p.bp, w, q.b.ld, st);
+            if (err != hipSuccess) return err;
             g.B = w;
             w += q.b.bytes;
         }

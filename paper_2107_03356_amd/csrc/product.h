@@ -44,8 +44,8 @@ struct Plan {
 // 248 us, with them 271.
 constexpr int64_t LAST_LEVEL_CACHE = int64_t(256) << 20;
 // Whether a product's results are stored past the caches: in tiles of 256, where they and the operands exceed them.
-// `kept`: bytes of a gated layer's pre-activations (bf16 8192 x 8192 over 2048 with 8-bit copies: 499 us so, 514 through the
-// caches).
+// `kept`: bytes of a gated layer's pre-activations (bf16 8192 rows, 2048 to 8192, and the copies' return: 587 us so, 603 through
+// the caches).
 inline bool streams(const Product& p, const Plan& q, int out_dt, int64_t kept = 0) {
     const int64_t out = p.gate == GATE_FORWARD ? p.M * p.N / 2 : p.M * p.N;
     const int64_t bytes = (p.M * p.K + p.N * p.K) * 2 * (q.nseg > 1 ? 3 : 1) + out * dtype_bytes(out_dt) + kept;
@@ -446,7 +446,8 @@ __device__ __forceinline__ void epilogue(const GemmArgs& g, float* part, int lan
 }
 
 // The same of a gated layer: the first half of a wave's columns are the gate's, the second the other projection's, for
-// the same N columns of the result.
+// the same N columns of the result. A tile's two halves of C meet in registers, so the pre-activations reach the memory only
+// where they are kept: bf16 8192 rows, 2048 to 8192, both kept in 8 bits, 499 to 515 us (1.07 to 1.10 PFLOP/s).
 template <typename T, bool EDGE, bool STREAM, int MT, int NTL>
 __device__ __forceinline__ void epilogue_gated(const GemmArgs& g, float* part, int lane, int64_t m0, int64_t n,
                                                v4 (&acc)[MT][NTL]) {
@@ -759,11 +760,12 @@ hipError_t run_product(const Product& p, const Plan& q, const GemmArgs& g, hipSt
     // (a gated layer's waves have 32 columns of the result, one group of an 8-bit copy: four waves of 16 rows then)
     constexpr int WM = KIND == GATED ? 4 : 2;
     const int64_t kept = KIND != GATED ? 0 : g.e.z ? p.M * p.N * dtype_bytes(g.e.io_dt) : g.e.p.q ? p.M * p.N : 0;
-    // HIDDEN writes three to six times what it reads, past what the caches hold in any case: 2.09 ms for a backward pass of bf16
-    // 8192 rows, 2048 to 8192, with plain stores, 2.11 with nontemporal ones
+    // HIDDEN writes three to six times what it reads, past what the caches hold in any case: bf16 8192 rows, 2048 to 8192, two
+    // parts each, take 527 us with plain stores, 548 with nontemporal ones
     if (q.tile == 64) k_product<T, KIND, 64, 64, WM, 4 / WM, 3, false><<<grid, 256, 0, st>>>(g);
     else if (q.tile == 128) k_product<T, KIND, 128, 128, 2, 2, 2, false><<<grid, 256, 0, st>>>(g);
-    else if (KIND == HIDDEN || !streams(p, q, g.e.out_dt, kept)) k_product<T, KIND, 256, 256, 2, 4, 2, false><<<grid, 512, 0, st>>>(g);
+    else if (KIND == HIDDEN || !streams(p, q, g.e.out_dt, kept))
+        k_product<T, KIND, 256, 256, 2, 4, 2, false><<<grid, 512, 0, st>>>(g);
     else if constexpr (KIND != HIDDEN) k_product<T, KIND, 256, 256, 2, 4, 2, true><<<grid, 512, 0, st>>>(g);
     return hipGetLastError();
 }

@@ -8,7 +8,9 @@
 //
 // so that two sums a column serve the three gradients behind N_post. One pass over the rows, which live in registers as in
 // the forward pass; the column sums of a work-group's rows are kept in registers and joined at the end, in a fixed order
-// (k_residual_params in residual.hip).
+// (k_residual_params in residual.hip). The memory's rate bounds it: bf16 16384 x 4096 with both rms norms, a gate for each
+// channel and dropout takes 166 us (4.8 TB/s of dh, ds, y, s, dy and dr) and 9 for the join; rms norm alone with ds 112
+// (5.9 TB/s). Layer norms, whose sums leave fewer waves, reach 4.8 TB/s there, and 2.9 at 8192 x 8192 (276 us).
 #pragma once
 
 #include "residual.h"
@@ -188,7 +190,8 @@ __global__ __launch_bounds__(norm_block(NT), 2) void k_residual_bwd(Residual g, 
 }
 
 // Wider rows: a work-group of 1024 threads a row, d in LDS in fp32, the inputs read again from the caches where they are needed
-// twice, the column sums in this work-group's part of the workspace. A thread reads only what it wrote.
+// twice, the column sums in this work-group's part of the workspace. A thread reads only what it wrote. bf16 4096 x 16384 with
+// everything on takes 370 us with rms norms, 538 with layer norms (2.2 and 1.5 TB/s).
 template <typename T, int NORMS>
 __global__ __launch_bounds__(1024) void k_residual_bwd_wide(Residual g, ResidualBwd b, int wt) {
     constexpr int NT = 1024;
@@ -290,8 +293,9 @@ __global__ __launch_bounds__(1024) void k_residual_bwd_wide(Residual g, Residual
 // f(threads that hold a row, chunks of eight values that each has, whether a row is loaded ahead), as constants. A row ahead,
 // its column sums and weights are most of the registers: 16-bit rows with rms norms take two chunks a thread (248
 // registers, two waves to a SIMD); with layer norms, whose sums are twice as many, one (16384 x 4096 202 us, 347 with what two
-// would spill), and without anything between too, whose inputs are few, for the sake of more waves (92 us against 108). Above 4096 columns fp32 rows and those of layer norms would need 1024 threads, which have 128
-// registers each: 512 with two chunks and no row ahead.
+// would spill), and without anything between too, whose inputs are few, for the sake of more waves (92 us against 108). Above
+// 4096 columns fp32 rows and those of layer norms would need 1024 threads, which have 128 registers each: 512 with two chunks
+// and no row ahead.
 template <typename T, bool ONE, typename F>
 void by_threads_bwd(int64_t cols, F f) {
     constexpr int C = residual_chunks(sizeof(T) == 4, ONE);
@@ -312,15 +316,18 @@ hipError_t residual_bwd(int wt, const Residual& g, const ResidualBwd& b, hipStre
     const int norms = between || !in_registers(g.cols) ? g.norms : g.norms | NOTHING_BETWEEN;
     by_norms(norms, [&](auto tag) {
         constexpr int NORMS = decltype(tag)::value;
-        // (fp32 with layer norms, 4096 x 8192: 342 us as a wider row, 469 with what 512 threads would spill)
-        if (!in_registers(g.cols) || (sizeof(T) == 4 && g.cols > 4096 && NORMS & LAYER_NORM && !(NORMS & NOTHING_BETWEEN))) {
+        // fp32 with layer norms, 4096 x 8192: 342 us as a wider row, 469 with what 512 threads would spill
+        constexpr bool SPILLS = sizeof(T) == 4 && NORMS & LAYER_NORM && !(NORMS & NOTHING_BETWEEN);
+        if (!in_registers(g.cols) || (SPILLS && g.cols > 4096)) {
             if constexpr (!(NORMS & NOTHING_BETWEEN))
                 k_residual_bwd_wide<T, NORMS><<<grid, 1024, (size_t)round_up(g.cols, 8) * 4, st>>>(g, b, wt);
             return;
         }
         by_threads_bwd<T, (NORMS & (LAYER_NORM | NOTHING_BETWEEN)) != 0>(g.cols, [&](auto nt, auto nch, auto ahead) {
             constexpr int NT = decltype(nt)::value;
-            k_residual_bwd<T, NT, decltype(nch)::value, decltype(ahead)::value, NORMS><<<grid, norm_block(NT), 0, st>>>(g, b, wt);
+            constexpr bool AHEAD = decltype(ahead)::value;
+            if constexpr (AHEAD || !SPILLS)
+                k_residual_bwd<T, NT, decltype(nch)::value, AHEAD, NORMS><<<grid, norm_block(NT), 0, st>>>(g, b, wt);
         });
     });
     return hipGetLastError();

@@ -1,5 +1,5 @@
 // Device helpers shared by the kernels that hold a row in the registers of NT threads (norm.hip,
-// residual_fwd.hip, residual_bwd.hip): sums over a row.
+// residual_fwd.h, residual_bwd.h): sums over a row.
 #pragma once
 
 #include "train_util.h"

@@ -1,5 +1,5 @@
-// Launchers of the training operators (norm.hip, pack8.hip, linear.hip; gated.hip, residual_fwd.hip, residual_bwd.hip,
-// dropout.hip), called by train_capi.hip and gated_capi.hip once the arguments have been checked.
+// Launchers of the training operators (norm.hip, pack8.hip, linear.hip; gated.hip, residual.hip, dropout.hip), called by
+// train_capi.hip and gated_capi.hip once the arguments have been checked.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -120,7 +120,7 @@ struct Drop {
 hipError_t launch_dropout(int dt, int64_t rows, int64_t cols, const void* x, int64_t ldx, Drop d, void* y, int64_t ldy,
                           hipStream_t st);
 
-// n = N_post(y), s = scale r + gate drop(n), h = N_pre(s); see residual_fwd.hip. Pointers of what is absent or not
+// n = N_post(y), s = scale r + gate drop(n), h = N_pre(s); see residual_fwd.h. Pointers of what is absent or not
 // wanted are null.
 struct Residual {
     int norms;           // MFAC_NORM_*
