@@ -61,10 +61,12 @@ __global__ __launch_bounds__(256) void k_gated_act_bwd(Strips s, const TA* da, i
             gate_slopes(e.act, a, u, d);
             sum_g += d[0];
             sum_u += u[0];
-            store_parts(e.out, e.out_part, e.parts, row * e.ldo, c, s.cols, d[0]);
-            store_parts(e.out, e.out_part, e.parts, row * e.ldo + s.cols, c, e.ldo - s.cols, u[0]);
-            if (c + 8 >= s.cols && c + 8 < e.ldo - s.cols)
-                store_parts(e.out, e.out_part, e.parts, row * e.ldo + s.cols, c + 8, e.ldo - s.cols, f8{});
+            if (e.out) {
+                store_parts(e.out, e.out_part, e.parts, row * e.ldo, c, s.cols, d[0]);
+                store_parts(e.out, e.out_part, e.parts, row * e.ldo + s.cols, c, e.ldo - s.cols, u[0]);
+                if (c + 8 >= s.cols && c + 8 < e.ldo - s.cols)
+                    store_parts(e.out, e.out_part, e.parts, row * e.ldo + s.cols, c + 8, e.ldo - s.cols, f8{});
+            }
             if (e.a) store_parts(e.a, e.a_part, e.parts, row * e.lda, c, e.lda, a[0]);
         }
     }

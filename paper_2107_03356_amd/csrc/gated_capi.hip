@@ -80,6 +80,7 @@ struct GatedBwd {
 
     bool da_given() const { return cout == 0; }
     bool sums() const { return db1 || (dw1 && beta); }
+    bool dz_wanted() const { return dx || dw1; }
     int64_t dy_part() const { return rows * lddy_in * 2; }
     int64_t dz_part() const { return rows * lddz * 2; }
     int64_t a_part() const { return rows * lda * 2; }
@@ -151,7 +152,7 @@ struct GatedBwd {
             if (dx) w1_in = take((size_t)hidden * ldw1_in * 12);
         }
         if (!da_given() && !fused) da = take((size_t)rows * hidden * 4);
-        dz = take((size_t)dz_part() * parts);
+        if (dz_wanted()) dz = take((size_t)dz_part() * parts);
         if (dw2) a = take((size_t)a_part() * parts);
         if (sums()) {
             db = take((size_t)hidden * 8);
@@ -284,7 +285,7 @@ MFAC_API mfac_status mfac_gated_bwd(mfac_dtype type, mfac_dtype gtype, mfac_act 
     e.ldz = ldz;
     e.p = packed(qg, ldqz, sg);
     e.p2 = packed(qu, ldqz, su);
-    e.out = ws + g.dz;
+    e.out = g.dz_wanted() ? ws + g.dz : nullptr;
     e.ldo = g.lddz;
     e.a = dw2 ? ws + g.a : nullptr;
     e.lda = g.lda;

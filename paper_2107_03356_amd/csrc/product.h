@@ -174,8 +174,10 @@ __device__ __forceinline__ void finish_hidden8(const Epilogue& e, int64_t N, boo
         if (e.parts == 1) return;
         store8_dt((char*)base + apart, e.out_dt, off, n, N, e.out_dt == DT_BF16 ? rest_of<bf16>(v) : rest_of<f16>(v));
     };
-    store(e.out, e.out_part, m * e.ldo, d[0]);
-    store(e.out, e.out_part, m * e.ldo + N, u[0]);
+    if (e.out) {
+        store(e.out, e.out_part, m * e.ldo, d[0]);
+        store(e.out, e.out_part, m * e.ldo + N, u[0]);
+    }
     if (e.a) store(e.a, e.a_part, m * e.lda, g[0]);
 }
 
@@ -586,8 +588,10 @@ __device__ __forceinline__ void epilogue_hidden(const GemmArgs& g, float* part, 
         gate_slopes(e.act, a, u, d);
 #pragma unroll
         for (int j = 0; j < H; ++j) {
-            store(e.out, e.out_part, m * e.ldo + n + j * 32, d[j]);
-            store(e.out, e.out_part, m * e.ldo + N + n + j * 32, u[j]);
+            if (e.out) {
+                store(e.out, e.out_part, m * e.ldo + n + j * 32, d[j]);
+                store(e.out, e.out_part, m * e.ldo + N + n + j * 32, u[j]);
+            }
             if (e.a) store(e.a, e.a_part, m * e.lda + n + j * 32, a[j]);
         }
     });

@@ -71,6 +71,7 @@ def test_gated_workspaces():
     every = B.MFAC_GATED_DX | B.MFAC_GATED_DW1 | B.MFAC_GATED_DW2
     assert need(B.MFAC_BF16, B.MFAC_GATED_DX) == dz                     # dz alone, from the product itself
     assert need(B.MFAC_BF16, every) == dz + a
+    assert need(B.MFAC_BF16, B.MFAC_GATED_DW2) == a and need(B.MFAC_BF16, B.MFAC_GATED_DB1) < da + dz
     assert need(B.MFAC_F32, every) == 2 * (dz + a)                      # in two parts
     assert need(B.MFAC_BF16, every | B.MFAC_GATED_DB1) >= dz + a + da   # da is stored where its sums are wanted
     assert need(B.MFAC_F32, every, type=B.MFAC_F32) >= 3 * (dz + a) + da
