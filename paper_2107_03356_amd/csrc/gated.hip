@@ -11,21 +11,6 @@
 namespace mfac {
 namespace {
 
-// v in 16-bit parts of type R, each what the rounding of those before it leaves: one or two of 16-bit data, three of fp32,
-// of which the first is cut at bf16's largest value (see k_lay_out_split in linear.hip). fp16's second: see rest_of.
-template <typename T, typename R>
-__device__ __forceinline__ void store_parts_as(void* base, int64_t part, int parts, int64_t off, int64_t c, int64_t cols, f8 v) {
-    typedef typename VecOf<R, 8>::plain V;
-    for (int p = 0; p < parts; ++p) {
-        f8 x = v;
-        if (sizeof(T) == 4 && p == 0)
-            x = __builtin_elementwise_min(__builtin_elementwise_max(x, f8(-0x1.fep127f)), f8(0x1.fep127f));
-        const f8 r = __builtin_convertvector(__builtin_convertvector(x, V), f8);
-        store8((R*)((char*)base + p * part) + off, c, cols, r);
-        v = (v - r) * REST_SCALE<R>;
-    }
-}
-
 template <typename T, typename TA, bool PACKED>
 __global__ __launch_bounds__(256) void k_gated_act_bwd(Strips s, const TA* da, int64_t ldda, Epilogue e, float* part) {
     __shared__ __attribute__((aligned(32))) float sums[2][256 * 8];
@@ -33,10 +18,6 @@ __global__ __launch_bounds__(256) void k_gated_act_bwd(Strips s, const TA* da, i
     const int lc = lane & ((1 << s.ll) - 1);
     const int64_t c = ((int64_t)blockIdx.x << (s.ll + 3)) + lc * 8, ngroups = (s.cols + 31) / 32;
     const int64_t sub = (int64_t)(threadIdx.x >> 6) * rpw + (lane >> s.ll), nsub = 4 * rpw;
-    using R = std::conditional_t<sizeof(T) == 4, bf16, T>;
-    auto store_parts = [](void* base, int64_t part, int parts, int64_t off, int64_t c, int64_t cols, f8 v) {
-        store_parts_as<T, R>(base, part, parts, off, c, cols, v);
-    };
     f8 sum_g = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, sum_u = sum_g;
     if (c < s.cols) {
         const int64_t step = gridDim.y * nsub;
@@ -61,13 +42,7 @@ __global__ __launch_bounds__(256) void k_gated_act_bwd(Strips s, const TA* da, i
             gate_slopes(e.act, a, u, d);
             sum_g += d[0];
             sum_u += u[0];
-            if (e.out) {
-                store_parts(e.out, e.out_part, e.parts, row * e.ldo, c, s.cols, d[0]);
-                store_parts(e.out, e.out_part, e.parts, row * e.ldo + s.cols, c, e.ldo - s.cols, u[0]);
-                if (c + 8 >= s.cols && c + 8 < e.ldo - s.cols)
-                    store_parts(e.out, e.out_part, e.parts, row * e.ldo + s.cols, c + 8, e.ldo - s.cols, f8{});
-            }
-            if (e.a) store_parts(e.a, e.a_part, e.parts, row * e.lda, c, e.lda, a[0]);
+            store_dz<T>(e, s.cols, row, c, d[0], u[0], a[0]);
         }
     }
     if (!part) return;

@@ -331,7 +331,7 @@ Plan plan_of(int dt, const Product& p) {
 template <typename T>
 hipError_t run_product(const Product& p, const Plan& q, const GemmArgs& g, hipStream_t st) {
     if (p.gate == GATE_FORWARD) return run_product<T, GATED>(p, q, g, st);
-    if (p.gate == GATE_HIDDEN) return run_product<T, HIDDEN>(p, q, g, st);
+    if (p.gate == GATE_HIDDEN && q.splits == 1) return run_product<T, HIDDEN>(p, q, g, st);   // else when its parts are joined
     if (p.a_col) return run_product<T, WEIGHT>(p, q, g, st);
     return p.b_col ? run_product<T, INPUT>(p, q, g, st) : run_product<T, FORWARD>(p, q, g, st);
 }
@@ -384,6 +384,7 @@ hipError_t launch_lay_out(int dt, int n, const LayOut* jobs, hipStream_t st) {
     return hipGetLastError();
 }
 
+int product_splits(int dt, const Product& p) { return plan_of(dt, p).splits; }
 size_t product_workspace_bytes(int dt, const Product& p) {
     const Plan q = plan_of(dt, p);
     return q.a.bytes + q.b.bytes + q.part_bytes;

@@ -156,7 +156,7 @@ __device__ __forceinline__ void finish_gated8(const Epilogue& e, int64_t N, bool
     act_apply(act_forward(e.act), one);
     store8_dt(e.out, e.out_dt, m * e.ldo, n, N, one[0] * u);
 }
-// And of the gradient of its output, c: dz and a, of 16-bit data.
+// And of the gradient of its output, c: dz and a.
 __device__ __forceinline__ void finish_hidden8(const Epilogue& e, int64_t N, bool in, int64_t m, int64_t n, f8 c) {
     if (!in || n >= N) return;
     f8 d[1] = {c}, g[1], u[1];
@@ -169,16 +169,9 @@ __device__ __forceinline__ void finish_hidden8(const Epilogue& e, int64_t N, boo
         u[0] = load8_dt(e.z2, e.io_dt, m * e.ldz, n, N);
     }
     gate_slopes(e.act, g, u, d);
-    auto store = [&](void* base, int64_t apart, int64_t off, f8 v) {
-        store8_dt(base, e.out_dt, off, n, N, v);
-        if (e.parts == 1) return;
-        store8_dt((char*)base + apart, e.out_dt, off, n, N, e.out_dt == DT_BF16 ? rest_of<bf16>(v) : rest_of<f16>(v));
-    };
-    if (e.out) {
-        store(e.out, e.out_part, m * e.ldo, d[0]);
-        store(e.out, e.out_part, m * e.ldo + N, u[0]);
-    }
-    if (e.a) store(e.a, e.a_part, m * e.lda, g[0]);
+    if (e.io_dt == DT_F32) store_dz<float>(e, N, m, n, d[0], u[0], g[0]);
+    else if (e.io_dt == DT_BF16) store_dz<bf16>(e, N, m, n, d[0], u[0], g[0]);
+    else store_dz<f16>(e, N, m, n, d[0], u[0], g[0]);
 }
 
 // Four sums at a time, as the matrix cores leave them: lane l has columns n .. n + 3, n = 4 (l / 16)
@@ -531,23 +524,13 @@ struct RawEight {
 // (HIDDEN_COLS), so a wave has them all or none: with checks for each column this code would be twice as long, and a wave runs
 // all of it once a tile.
 template <typename T, int MT, int NTL>
-__device__ __forceinline__ void epilogue_hidden(const GemmArgs& g, float* part, int lane, int64_t m0, int64_t n,
+__device__ __forceinline__ void epilogue_hidden(const GemmArgs& g, int lane, int64_t m0, int64_t n,
                                                 v4 (&acc)[MT][NTL]) {
     constexpr int H = NTL / 2;
     typedef typename VecOf<T, 8>::plain V;
     const Epilogue& e = g.e;
     const int64_t N = g.N;
     const bool packed = e.p.q;
-    if (part) {
-        for_each_index(std::make_integer_sequence<int, MT>(), [&](auto tag) {
-            constexpr int i = decltype(tag)::value;
-            const int64_t m = m0 + i * 16;
-            if (m >= g.M) return;
-#pragma unroll
-            for (int j = 0; j < NTL; ++j) store4<false, false>(part + m * N, n + j * 16, N, acc[i][j]);
-        });
-        return;
-    }
     n += (lane >> 4 & 1) * 12;   // an odd l / 16: 16 further, less 4
     RawEight<T> zg[H], zu[H];
     auto load = [&](int64_t m) {
@@ -741,7 +724,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
     float* part = g.splits > 1 ? g.part + (int64_t)k_part * g.M * g.N * (KIND == GATED ? 2 : 1) : nullptr;
     const int m = m0 + wm * (TM / WM) + (lane & 15), n = n0 + wn * (COLS / WN) + 4 * (lane >> 4);
     if constexpr (KIND == HIDDEN) {
-        if (n < g.N) epilogue_hidden<T>(g, part, lane, m, n, acc);
+        if (n < g.N) epilogue_hidden<T>(g, lane, m, n, acc);
         return;
     }
     auto finish = [&](auto edge) {

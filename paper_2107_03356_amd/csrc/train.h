@@ -94,6 +94,7 @@ struct Product {
     int64_t b_part;
 };
 size_t product_workspace_bytes(int dt, const Product& p);
+int product_splits(int dt, const Product& p);   // parts of K, of rows > 0
 // A matrix as the products take it: ld elements a row, a multiple of 8; of fp32 three parts, one after another.
 struct LayOut {
     const void* src;

@@ -356,6 +356,32 @@ __device__ __forceinline__ V rest_of(V v) {
     return (v - __builtin_convertvector(__builtin_convertvector(v, R), V)) * REST_SCALE<T>;
 }
 
+// v in 16-bit parts, each what the rounding of those before it leaves: one or two of 16-bit data, three bf16 ones of fp32,
+// of which the first is cut at bf16's largest value (see k_lay_out_split in linear.hip).
+template <typename T>
+__device__ __forceinline__ void store_parts(void* base, int64_t part, int parts, int64_t off, int64_t c, int64_t cols, f8 v) {
+    using R = std::conditional_t<sizeof(T) == 4, bf16, T>;
+    typedef typename VecOf<R, 8>::plain V;
+    for (int p = 0; p < parts; ++p) {
+        f8 x = v;
+        if (sizeof(T) == 4 && p == 0)
+            x = __builtin_elementwise_min(__builtin_elementwise_max(x, f8(-0x1.fep127f)), f8(0x1.fep127f));
+        const f8 r = __builtin_convertvector(__builtin_convertvector(x, V), f8);
+        store8((R*)((char*)base + p * part) + off, c, cols, r);
+        v = (v - r) * REST_SCALE<R>;
+    }
+}
+// Columns c .. c + 7 of row m of dz = [d u] and a (N columns each, d, u and a zeros past them), and zeros up to the rows' ends.
+template <typename T>
+__device__ __forceinline__ void store_dz(const Epilogue& e, int64_t N, int64_t m, int64_t c, f8 d, f8 u, f8 a) {
+    if (e.out) {
+        store_parts<T>(e.out, e.out_part, e.parts, m * e.ldo, c, N, d);
+        store_parts<T>(e.out, e.out_part, e.parts, m * e.ldo + N, c, e.ldo - N, u);
+        if (c + 8 >= N && c + 8 < e.ldo - N) store_parts<T>(e.out, e.out_part, e.parts, m * e.ldo + N, c + 8, e.ldo - N, f8{});
+    }
+    if (e.a) store_parts<T>(e.a, e.a_part, e.parts, m * e.lda, c, e.lda, a);
+}
+
 // ---------------------------------------------------------------- sums over a wave
 __device__ __forceinline__ float wave_sum(float v) {
     v += __uint_as_float(dpp<DPP_XOR1>(__float_as_uint(v)));

@@ -48,6 +48,7 @@ hipError_t launch_gated_act_bwd(int dt, int da_dt, int64_t rows, int64_t hidden,
     return launched();
 }
 hipError_t launch_zero_matrix(int, int64_t, int64_t, void*, int64_t, hipStream_t) { return launched(); }
+int product_splits(int, const Product& p) { return 1 + (p.M + p.N) % 2; }   // either, by the sizes
 size_t product_workspace_bytes(int, const Product& p) { return (size_t)(p.M + p.N + p.K); }
 hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws, hipStream_t) {
     CHECK((const char*)ws + product_workspace_bytes(dt, p) <= ws_to || !ws_from);
@@ -63,10 +64,11 @@ hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws,
     CHECK(p.a_parts * p.b_parts != 4);   // not both in two parts
     const int64_t width = p.gate == GATE_HIDDEN ? 2 * p.N : p.gate == GATE_FORWARD ? p.N / 2 : p.N;
     CHECK(e.ldo >= width);
-    range(e.out, ((p.M - 1) * e.ldo + width) * dtype_bytes(e.out_dt));
+    if (p.gate != GATE_HIDDEN) range(e.out, ((p.M - 1) * e.ldo + width) * dtype_bytes(e.out_dt));
     if (p.gate == GATE_HIDDEN) {
-        CHECK(dt != DT_F32 && p.N % 64 == 0 && (e.parts == 1 || e.parts == 2));
-        range(e.out, e.out_part * (e.parts - 1) + p.M * e.ldo * 2);
+        CHECK(product_splits(dt, p) > 1 || (dt != DT_F32 && p.N % 64 == 0));
+        CHECK(dt == DT_F32 ? e.parts == 3 : e.parts == 1 || e.parts == 2);
+        if (e.out) range(e.out, e.out_part * (e.parts - 1) + p.M * e.ldo * 2);
         if (e.a) range(e.a, e.a_part * (e.parts - 1) + p.M * e.lda * 2);
     }
     if (e.beta) CHECK(e.gamma && e.db);

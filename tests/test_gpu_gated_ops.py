@@ -183,12 +183,16 @@ def test_hidden_sizes_run_every_kernel(dev):
     from gated_cases import gated_plan
     seen = {gated_plan("bf16", True, r, c, h)[:2] for r, h, c in HIDDEN}
     assert {t for t, _ in seen} == {64, 128, 256} and any(s > 1 for _, s in seen), seen
+    # where parts of K are joined, dz and a are formed there, whatever the hidden size (test_gated_feed_forward_backward)
+    for dtype in ("f32", "bf16"):
+        assert all(gated_plan(dtype, True, r, c, h)[1] > 1 for r, c, h in ((260, 2056, 261), (70, 2056, 320)))
 
 
 @pytest.mark.parametrize("rows,hid,cout", HIDDEN)
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 def test_gated_backward_behind_the_next_layer(dev, dtype, rows, hid, cout):
-    """dz where da = dy w2, formed in that product (16-bit data, hidden a multiple of 64, no db) or from a stored da."""
+    """dz where da = dy w2, formed in that product (no db; parts of K joined, or 16-bit data and hidden a multiple of 64) or
+    from a stored da."""
     from paper_2107_03356_amd import nn
     say("gated backward behind the next layer", dtype, rows, hid, cout)
     tiny = TINY[dtype]
@@ -232,7 +236,7 @@ def test_gated_activation_formed_again(dev, dtype, rows, hid):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("rows,dim,hid", [(1, 64, 96), (130, 72, 200), (700, 264, 515)])
+@pytest.mark.parametrize("rows,dim,hid", [(1, 64, 96), (130, 72, 200), (700, 264, 515), (260, 2056, 261), (70, 2056, 320)])
 def test_gated_feed_forward_backward(dev, dtype, rows, dim, hid):
     """Against the formulas, with dz and a counted as the call rounds them: to the data's type for dx and for gradients
     of that type, in two parts for gradients in float32."""
