@@ -283,7 +283,7 @@ __device__ __forceinline__ float act_slope(float z, float* a) {
         const float e = __builtin_amdgcn_exp2f(z * fmaf(-0.10294323980544930f, z2, -2.30220819813644130f));
         const float p = __builtin_amdgcn_rcpf(1.f + e);
         *a = z * p;
-        return fmaf(p * (fminf(e, __FLT_MAX__) * p) * z, fmaf(0.21406444881780073f, z2, 1.59576912160573072f), p);
+        return fmaf(p * (fminf(e, __FLT_MAX__) * p) * z, fmaf(0.21406444881780073f, z2, 1.595769121605731f), p);
     }
     if constexpr (ACT == 4) {
         const float e = exp_fast(-z);
@@ -328,7 +328,7 @@ __device__ __forceinline__ void gate_slopes(int act, V (&g)[N], V (&u)[N], V (&d
     };
     const ActForward f = act_forward(act);
     if (f.formula == 1) {
-        const float r = act == 4 ? 1.f : 1.59576912160573072f, s = act == 4 ? 0.f : 0.21406444881780073f;
+        const float r = act == 4 ? 1.f : 1.595769121605731f, s = act == 4 ? 0.f : 0.21406444881780073f;
         each([&](float z, float& a) {
             const float z2 = fminf(z * z, 1e30f);
             const float e = __builtin_amdgcn_exp2f(z * fmaf(f.q, z2, f.p));
