@@ -58,7 +58,76 @@ __global__ __launch_bounds__(256) void k_gated_act_bwd(Strips s, const TA* da, i
     }
 }
 
+// The largest finite magnitude of four matrices: work-group (i, j) goes over its pieces of the j-th. With the factors 11 us for
+// 1537 rows, 520 to 1365; for 8192 rows, 2048 to 8192, 70 of the pass's 2450 (the pre-activations are read once more; of
+// copies their bytes s alone, 15 to 40).
+struct Range {
+    Magnitudes of[4];
+    Strips s[4];
+};
+__global__ __launch_bounds__(256) void k_magnitudes(Range r, float* part) {
+    __shared__ unsigned red[4];
+    const Magnitudes& m = r.of[blockIdx.y];
+    unsigned most = 0;
+    if (m.p)
+        for_strips(r.s[blockIdx.y], [&](int64_t row, int64_t c) {
+            if (row >= m.rows || c >= m.cols) return;
+            if (m.dt < 0) {   // 127 times the power of a group
+                const uint8_t* s = (const uint8_t*)m.p + row * m.ld;
+                for (int64_t i = c; i < min(c + 8, m.cols); ++i)
+                    if (s[i] != 255) most = max(most, __float_as_uint(127.f * unpack_scale(min((unsigned)s[i], 247u))));
+                return;
+            }
+            const f8 v = m.dt == DT_F32 ? load8((const float*)m.p + row * m.ld, c, m.cols) : load8((const f16*)m.p + row * m.ld, c, m.cols);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most = max(most, abs_bits(v[i]) < 0x7f800000u ? abs_bits(v[i]) : 0u);
+        });
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) most = max(most, (unsigned)__shfl_xor((int)most, step));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = most;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        part[blockIdx.y * RANGE_WGS + blockIdx.x] = __uint_as_float(max(max(red[0], red[1]), max(red[2], red[3])));
+}
+// The factors, 2^-k by which bounds of dz and a come below 2^15: |da| <= sums max|dy| max|w| (or is given), act's slope is
+// at most 1.13 and |act(z)| at most |z|. k is 0 for values of ordinary size. The two parts of a value are within 2^(k - 36)
+// of it (or 2^-22 of itself): the bound is below 2^(k + 15), so a value has all of its digits unless it is 2^29 times
+// smaller than the bound, which with normally distributed dy, W and z is 10^3 to 10^4 times dz's usual size.
+__global__ __launch_bounds__(RANGE_WGS) void k_range_factors(float* range, float sums) {
+    __shared__ float red[4][RANGE_WGS / 64];
+    for (int j = 0; j < 4; ++j) {
+        float v = range[4 + j * RANGE_WGS + threadIdx.x];
+#pragma unroll
+        for (int step = 1; step < 64; step *= 2) v = fmaxf(v, __shfl_xor(v, step));
+        if ((threadIdx.x & 63) == 0) red[j][threadIdx.x >> 6] = v;
+    }
+    __syncthreads();
+    if (threadIdx.x >= 2) return;
+    double m[4] = {0., 0., 0., 0.};
+    for (int j = 0; j < 4; ++j)
+        for (int i = 0; i < RANGE_WGS / 64; ++i) m[j] = fmax(m[j], (double)red[j][i]);
+    const double bound = threadIdx.x ? m[2] * m[3] : m[0] * (sums > 0.f ? sums * m[1] : 1.) * 1.13 * fmax(m[2], m[3]);
+    const int exponent = (int)(__double_as_longlong(bound) >> 52) - 1022;   // bound < 2^exponent
+    const unsigned k = (unsigned)max(0, min(exponent - 15, 126));
+    range[threadIdx.x] = __uint_as_float((127u - k) << 23);
+    range[2 + threadIdx.x] = __uint_as_float((127u + k) << 23);
+}
+
 }  // namespace
+
+hipError_t launch_gate_range(const Magnitudes& d, const Magnitudes& w, int64_t sums, int64_t rows, int64_t hidden, const Epilogue& e,
+                             hipStream_t st) {
+    const int64_t groups = ceil_div(hidden, 32);
+    auto pre = [&](const void* z, const Packed& p) {
+        return p.q ? Magnitudes{p.s, groups, rows, groups, -1} : Magnitudes{z, e.ldz, rows, hidden, DT_F16};
+    };
+    Range r{{e.out ? d : Magnitudes{}, e.out ? w : Magnitudes{}, pre(e.z, e.p), pre(e.z2, e.p2)}, {}};
+    for (int j = 0; j < 4; ++j)
+        if (r.of[j].p) r.s[j] = strips_of(r.of[j].rows, r.of[j].cols);
+    k_magnitudes<<<dim3(RANGE_WGS, 4), 256, 0, st>>>(r, e.range + 4);
+    k_range_factors<<<1, RANGE_WGS, 0, st>>>(e.range, w.p ? (float)sums : 0.f);
+    return hipGetLastError();
+}
 
 // As many as give about 2048 work-groups; one for up to eight rows to each of a work-group's, whose sums are then db without
 // a launch that joins parts.
@@ -66,6 +135,10 @@ int64_t gated_bwd_parts(int64_t rows, int64_t hidden) { return act_bwd_parts(row
 
 hipError_t launch_gated_act_bwd(int dt, int da_dt, int64_t rows, int64_t hidden, const void* da, int64_t ldda,
                                 const Epilogue& e, float* db, float* part, hipStream_t st) {
+    if (e.range && rows > 0) {
+        const hipError_t err = launch_gate_range({da, ldda, rows, hidden, da_dt}, {}, 0, rows, hidden, e, st);
+        if (err != hipSuccess) return err;
+    }
     const Strips s = strips_of(rows, hidden);
     const int64_t nparts = rows > 0 ? gated_bwd_parts(rows, hidden) : 0;
     if (!db) part = nullptr;

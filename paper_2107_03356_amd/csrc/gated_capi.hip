@@ -76,11 +76,12 @@ struct GatedBwd {
     bool fused;
     int parts;
     int64_t lddy_in, ldw2_in, ldx_in, ldw1_in, lddz, lda;
-    size_t dy_in, w2_in, x_in, w1_in, da, dz, a, db, db_part, product, total;
+    size_t dy_in, w2_in, x_in, w1_in, da, dz, a, db, db_part, range, product, total;
 
     bool da_given() const { return cout == 0; }
     bool sums() const { return db1 || (dw1 && beta); }
     bool dz_wanted() const { return dx || dw1; }
+    bool ranged() const { return type == MFAC_F16 && parts == 2; }   // dz and a may need factors to be in two parts
     int64_t dy_part() const { return rows * lddy_in * 2; }
     int64_t dz_part() const { return rows * lddz * 2; }
     int64_t a_part() const { return rows * lda * 2; }
@@ -132,7 +133,7 @@ struct GatedBwd {
         lddz = round_up(2 * hidden, 8);
         lda = ldw2_in = round_up(hidden, 8);
         ldx_in = ldw1_in = round_up(cin, 8);
-        dy_in = w2_in = x_in = w1_in = da = dz = a = db = db_part = product = total = 0;
+        dy_in = w2_in = x_in = w1_in = da = dz = a = db = db_part = range = product = total = 0;
         if (!(dx || dw1 || db1 || dw2)) return;
         // Gradients of 16-bit weights' data in fp32 are formed from dz and a in two parts: rounded to one, they leave
         // the gradient 2.3e-3 from 64 bits (relative, 2-norm), in two 3e-6. It doubles these two products.
@@ -160,6 +161,7 @@ struct GatedBwd {
             db = take((size_t)hidden * 8);
             db_part = take((size_t)gated_bwd_parts(std::max<int64_t>(rows, 1), hidden) * hidden * 8);
         }
+        if (ranged()) range = take(GATE_RANGE * 4);
         if (rows > 0) {   // one after another in the same place; addresses in the workspace are aligned, and not looked at
             if (!da_given()) need(da_product(dy_laid_out() ? nullptr : dy, nullptr));
             if (dx) need(dx_product(nullptr, nullptr));
@@ -294,6 +296,8 @@ MFAC_API mfac_status mfac_gated_bwd(mfac_dtype type, mfac_dtype gtype, mfac_act 
     e.parts = g.parts;
     e.out_part = g.dz_part();
     e.a_part = g.a_part();
+    float* const range = g.ranged() ? (float*)(ws + g.range) : nullptr;
+    e.range = range;
     float* db = db1 ? db1 : g.sums() ? (float*)(ws + g.db) : nullptr;
     if (g.fused) {
         err = launch_product(type, g.da_product(dy_at, ws), e, ws + g.product, stream);
@@ -309,8 +313,9 @@ MFAC_API mfac_status mfac_gated_bwd(mfac_dtype type, mfac_dtype gtype, mfac_act 
         if (err == hipSuccess)
             err = launch_gated_act_bwd(type, MFAC_F32, rows, hidden, ws + g.da, hidden, e, db, (float*)(ws + g.db_part), stream);
     }
-    auto product = [&](const Product& p, int out_dt, void* out, int64_t ldo, bool affine) {
+    auto product = [&](const Product& p, int out_dt, void* out, int64_t ldo, bool affine, int factor) {
         Epilogue o{};
+        o.times = range ? range + factor : nullptr;
         o.out_dt = out_dt;
         o.io_dt = type;
         o.out = out;
@@ -322,9 +327,9 @@ MFAC_API mfac_status mfac_gated_bwd(mfac_dtype type, mfac_dtype gtype, mfac_act 
         }
         if (err == hipSuccess) err = launch_product(type, p, o, ws + g.product, stream);
     };
-    if (dw2) product(g.dw2_product(dy_at, ws + g.a), gtype, dw2, lddw2, false);
-    if (dx) product(g.dx_product(ws + g.dz, ws), type, dx, lddx, false);
-    if (dw1) product(g.dw1_product(ws + g.dz, ws), gtype, dw1, lddw1, true);
+    if (dw2) product(g.dw2_product(dy_at, ws + g.a), gtype, dw2, lddw2, false, 3);
+    if (dx) product(g.dx_product(ws + g.dz, ws), type, dx, lddx, false, 2);
+    if (dw1) product(g.dw1_product(ws + g.dz, ws), gtype, dw1, lddw1, true, 2);
     return done(err);
 }
 

@@ -455,6 +455,11 @@ hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws,
         g.splits = q.splits;
         g.part = (float*)w;
         g.e = e;
+        if (p.gate == GATE_HIDDEN && e.range) {
+            const int64_t sums = p.K;
+            err = launch_gate_range({p.A, p.lda, p.M, p.K, DT_F16}, {p.B, p.ldb, sums, p.N, DT_F16}, sums, p.M, p.N, e, st);
+            if (err != hipSuccess) return err;
+        }
         err = dt == DT_F16 ? run_product<f16>(p, q, g, st) : run_product<bf16>(p, q, g, st);
     }
     if (err != hipSuccess || q.splits == 1) return err;

@@ -541,8 +541,15 @@ __device__ __forceinline__ void epilogue_hidden(const GemmArgs& g, int lane, int
             zu[j].load(e.z2, e.ldz, e.p2, m, n + j * 32, N);
         }
     };
-    auto store = [&](void* base, int64_t apart, int64_t off, f8 v) {
+    float dz_by = 1.f, a_by = 1.f;
+    if constexpr (std::is_same_v<T, f16>)
+        if (e.range) {
+            dz_by = e.range[0];
+            a_by = e.range[1];
+        }
+    auto store = [&](void* base, int64_t apart, int64_t off, f8 v, float by) {
         T* at = (T*)base + off;
+        if constexpr (std::is_same_v<T, f16>) v *= by;
         const V first = __builtin_convertvector(v, V);
         *reinterpret_cast<typename VecOf<T, 8>::type*>(at) = first;
         if (e.parts == 1) return;
@@ -572,10 +579,10 @@ __device__ __forceinline__ void epilogue_hidden(const GemmArgs& g, int lane, int
 #pragma unroll
         for (int j = 0; j < H; ++j) {
             if (e.out) {
-                store(e.out, e.out_part, m * e.ldo + n + j * 32, d[j]);
-                store(e.out, e.out_part, m * e.ldo + N + n + j * 32, u[j]);
+                store(e.out, e.out_part, m * e.ldo + n + j * 32, d[j], dz_by);
+                store(e.out, e.out_part, m * e.ldo + N + n + j * 32, u[j], dz_by);
             }
-            if (e.a) store(e.a, e.a_part, m * e.lda + n + j * 32, a[j]);
+            if (e.a) store(e.a, e.a_part, m * e.lda + n + j * 32, a[j], a_by);
         }
     });
 }
@@ -720,6 +727,15 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
 #pragma unroll
                 for (int j = 0; j < NTL; ++j) acc[i][j] *= 1.f / REST_SCALE<T>;
     }
+
+    if constexpr (std::is_same_v<T, f16> && (KIND == WEIGHT || KIND == INPUT))
+        if (g.e.times) {   // dz or a was stored times a factor
+            const float by = *g.e.times;
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NTL; ++j) acc[i][j] *= by;
+        }
 
     float* part = g.splits > 1 ? g.part + (int64_t)k_part * g.M * g.N * (KIND == GATED ? 2 : 1) : nullptr;
     const int m = m0 + wm * (TM / WM) + (lane & 15), n = n0 + wn * (COLS / WN) + 4 * (lane >> 4);

@@ -66,7 +66,23 @@ struct Epilogue {
     // out and a in this many 16-bit parts (1, 2; of fp32 3), each what the rounding of those before it leaves, bytes apart
     int parts;
     int64_t out_part, a_part;
+    // of fp16 data in two parts: GATE_RANGE floats for the factors that keep dz and a within fp16's range, formed before the
+    // pass (gated.hip); null: 1
+    float* range;
+    const float* times;  // an fp16 product's sums are multiplied by this one (null: 1)
 };
+
+// Of Epilogue::range: dz and a are stored times [0] and [1], and [2] and [3] take these out again (powers of two, at most
+// and at least 1); behind them the maxima they are formed from.
+constexpr int RANGE_WGS = 1024, GATE_RANGE = 4 + 4 * RANGE_WGS;
+struct Magnitudes {
+    const void* p;       // rows x cols, of type dt, or an 8-bit copy's bytes s (dt < 0)
+    int64_t ld, rows, cols;
+    int dt;
+};
+// d: dy, with w of `sums` rows (the next layer's weight), or da itself (w.p null)
+hipError_t launch_gate_range(const Magnitudes& d, const Magnitudes& w, int64_t sums, int64_t rows, int64_t hidden, const Epilogue& e,
+                             hipStream_t st);
 
 // What a product's N columns are.
 enum : int {

@@ -374,6 +374,12 @@ __device__ __forceinline__ void store_parts(void* base, int64_t part, int parts,
 // Columns c .. c + 7 of row m of dz = [d u] and a (N columns each, d, u and a zeros past them), and zeros up to the rows' ends.
 template <typename T>
 __device__ __forceinline__ void store_dz(const Epilogue& e, int64_t N, int64_t m, int64_t c, f8 d, f8 u, f8 a) {
+    if constexpr (std::is_same_v<T, f16>)
+        if (e.range) {
+            d *= e.range[0];
+            u *= e.range[0];
+            a *= e.range[1];
+        }
     if (e.out) {
         store_parts<T>(e.out, e.out_part, e.parts, m * e.ldo, c, N, d);
         store_parts<T>(e.out, e.out_part, e.parts, m * e.ldo + N, c, e.ldo - N, u);
