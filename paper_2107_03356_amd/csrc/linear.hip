@@ -37,6 +37,7 @@ extern template hipError_t run_product<bf16, INPUT>(const Product&, const Plan&,
 extern template hipError_t run_product<f16, INPUT>(const Product&, const Plan&, const GemmArgs&, hipStream_t);
 extern template hipError_t run_product<bf16, WEIGHT>(const Product&, const Plan&, const GemmArgs&, hipStream_t);
 extern template hipError_t run_product<f16, WEIGHT>(const Product&, const Plan&, const GemmArgs&, hipStream_t);
+extern template hipError_t run_product<f16, WEIGHT_PARTS>(const Product&, const Plan&, const GemmArgs&, hipStream_t);
 extern template hipError_t run_product<bf16, GATED>(const Product&, const Plan&, const GemmArgs&, hipStream_t);
 extern template hipError_t run_product<f16, GATED>(const Product&, const Plan&, const GemmArgs&, hipStream_t);
 extern template hipError_t run_product<bf16, HIDDEN>(const Product&, const Plan&, const GemmArgs&, hipStream_t);
@@ -332,6 +333,8 @@ template <typename T>
 hipError_t run_product(const Product& p, const Plan& q, const GemmArgs& g, hipStream_t st) {
     if (p.gate == GATE_FORWARD) return run_product<T, GATED>(p, q, g, st);
     if (p.gate == GATE_HIDDEN && q.splits == 1) return run_product<T, HIDDEN>(p, q, g, st);   // else when its parts are joined
+    if constexpr (std::is_same_v<T, f16>)
+        if (p.a_col && q.nseg == 2) return run_product<T, WEIGHT_PARTS>(p, q, g, st);
     if (p.a_col) return run_product<T, WEIGHT>(p, q, g, st);
     return p.b_col ? run_product<T, INPUT>(p, q, g, st) : run_product<T, FORWARD>(p, q, g, st);
 }

@@ -67,9 +67,12 @@ __device__ __forceinline__ void for_each_index(std::integer_sequence<int, I...>,
 
 // ---------------------------------------------------------------- epilogue
 // The products' epilogues; the fields of the others are unused.
-enum : int { FORWARD = 0, INPUT = 1, WEIGHT = 2, GATED = 3, HIDDEN = 4 };
-constexpr bool a_is_col(int kind) { return kind == WEIGHT; }
-constexpr bool b_is_col(int kind) { return kind == INPUT || kind == WEIGHT || kind == HIDDEN; }
+// WEIGHT_PARTS is WEIGHT of an fp16 operand in two parts: a kernel of its own, since its look at every K step for the end of
+// the second parts cost plain fp16 gradients 1 to 5% (2048 rows, 1024 to 1024: 16.8 us against 16.0).
+enum : int { FORWARD = 0, INPUT = 1, WEIGHT = 2, GATED = 3, HIDDEN = 4, WEIGHT_PARTS = 5 };
+constexpr bool is_weight(int kind) { return kind == WEIGHT || kind == WEIGHT_PARTS; }
+constexpr bool a_is_col(int kind) { return is_weight(kind); }
+constexpr bool b_is_col(int kind) { return kind == INPUT || is_weight(kind) || kind == HIDDEN; }
 constexpr int HIDDEN_COLS = 64;   // HIDDEN's N is a multiple of a wave's columns in every tile
 
 // What an epilogue reads for columns n .. n + 7, whichever the row.
@@ -387,7 +390,7 @@ __device__ __forceinline__ typename Frag<T>::type read_frag(const char* lds, int
 template <typename T, int KIND, bool EDGE, bool STREAM, int MT, int NTL>
 __device__ __forceinline__ void epilogue(const GemmArgs& g, float* part, int lane, int64_t m0, int64_t n,
                                          v4 (&acc)[MT][NTL]) {
-    constexpr bool FWD = KIND == FORWARD, WGT = KIND == WEIGHT;
+    constexpr bool FWD = KIND == FORWARD, WGT = is_weight(KIND);
     const Epilogue& e = g.e;
     const int64_t N = g.N;
     v4 bias[NTL], beta[WGT ? NTL : 1];   // bias, or gamma
@@ -698,8 +701,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
 
     const int steps = s_end - s_begin;
     // The second parts of fp16 come first, as stored: after their last step the sums lose their factor.
-    constexpr bool RESTS = KIND == WEIGHT && std::is_same_v<T, f16>;
-    const int rests = RESTS && g.nseg == 2 ? min(g.ksteps - s_begin, steps) : 0;
+    constexpr bool RESTS = KIND == WEIGHT_PARTS;
+    const int rests = RESTS ? min(g.ksteps - s_begin, steps) : 0;
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i)
         if (i < steps) issue(i);
@@ -728,7 +731,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_product(GemmArgs g) {
                 for (int j = 0; j < NTL; ++j) acc[i][j] *= 1.f / REST_SCALE<T>;
     }
 
-    if constexpr (std::is_same_v<T, f16> && (KIND == WEIGHT || KIND == INPUT))
+    if constexpr (KIND == WEIGHT_PARTS || (KIND == INPUT && std::is_same_v<T, f16>))
         if (g.e.times) {   // dz or a was stored times a factor
             const float by = *g.e.times;
 #pragma unroll
