@@ -627,10 +627,16 @@ mfac_status mfac_residual_norm_bwd(mfac_dtype type, mfac_dtype wtype, int32_t no
                                    int64_t lddgates, void* dpost_w, void* dpost_b, void* dgate, void* dpre_w,
                                    void* dpre_b, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
-/* How the products of a gated layer are run, as mfac_linear_plan: the layer itself, or with `hidden_bwd` != 0 the product of
- * mfac_gated_bwd that forms dz (cin is then its cout). */
-mfac_status mfac_gated_plan(mfac_dtype type, int32_t hidden_bwd, int64_t rows, int64_t cin, int64_t hidden,
-                            int32_t plan[3]);
+/* How the products of a gated layer are run, as mfac_linear_plan: the layer itself, by what it keeps, or the product of
+ * mfac_gated_bwd that forms da (cin is then its cout), by whether db1 or beta asks for column sums. */
+typedef enum {
+    MFAC_GATED_FORWARD = 0,        /* nothing kept */
+    MFAC_GATED_HIDDEN = 1,
+    MFAC_GATED_FORWARD_Z = 2,      /* the pre-activations kept */
+    MFAC_GATED_FORWARD_COPIES = 3, /* 8-bit copies of them */
+    MFAC_GATED_HIDDEN_SUMS = 4
+} mfac_gated_product;
+mfac_status mfac_gated_plan(mfac_dtype type, int32_t product, int64_t rows, int64_t cin, int64_t hidden, int32_t plan[3]);
 
 #ifdef __cplusplus
 }

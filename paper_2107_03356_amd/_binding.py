@@ -28,6 +28,7 @@ MFAC_STATIC_FP32 = 2
 MFAC_F32, MFAC_BF16, MFAC_F16 = 0, 1, 2
 MFAC_PRODUCT_FORWARD, MFAC_PRODUCT_INPUT, MFAC_PRODUCT_WEIGHT = range(3)
 MFAC_GATED_DX, MFAC_GATED_DW1, MFAC_GATED_DB1, MFAC_GATED_DW2, MFAC_GATED_BETA = 1, 2, 4, 8, 16
+MFAC_GATED_FORWARD, MFAC_GATED_HIDDEN, MFAC_GATED_FORWARD_Z, MFAC_GATED_FORWARD_COPIES, MFAC_GATED_HIDDEN_SUMS = range(5)
 MFAC_NORM_POST, MFAC_NORM_PRE, MFAC_NORM_LAYER = 1, 2, 4
 MFAC_ACT_NONE, MFAC_ACT_RELU, MFAC_ACT_GELU, MFAC_ACT_GELU_TANH, MFAC_ACT_SILU = range(5)
 

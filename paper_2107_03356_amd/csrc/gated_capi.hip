@@ -138,11 +138,10 @@ struct GatedBwd {
         // Gradients of 16-bit weights' data in fp32 are formed from dz and a in two parts: rounded to one, they leave
         // the gradient 2.3e-3 from 64 bits (relative, 2-norm), in two 3e-6. It doubles these two products.
         parts = type == MFAC_F32 ? 3 : gtype == MFAC_F32 && (dw1 || dw2) ? 2 : 1;
-        // dz straight from the product that forms da, without db, whose sums would have to be joined over the tiles: where
-        // its parts of K are joined, and in its epilogue of 16-bit data where a wave's columns are all there or none (fp32's
-        // epilogue would write 18 bytes a sum). Otherwise da is stored in fp32 and read again.
+        // dz straight from the product that forms da, without db, whose sums would have to be joined over the tiles.
+        // Otherwise da is stored in fp32 and read again.
         fused = !da_given() && !sums() && rows > 0;
-        fused = fused && (product_splits(type, da_product(nullptr, nullptr)) > 1 || (type != MFAC_F32 && hidden % 64 == 0));
+        fused = fused && hidden_fused(type, product_splits(type, da_product(nullptr, nullptr)), hidden);
         auto take = [&](size_t bytes) {
             const size_t at = total;
             total += (size_t)round_up((int64_t)bytes, 256);

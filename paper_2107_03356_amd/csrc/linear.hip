@@ -496,23 +496,27 @@ extern "C" __attribute__((visibility("default"))) mfac_status mfac_linear_plan(m
     return MFAC_OK;
 }
 
-extern "C" __attribute__((visibility("default"))) mfac_status mfac_gated_plan(mfac_dtype type, int32_t hidden_bwd,
-                                                                              int64_t rows, int64_t cin, int64_t hidden,
-                                                                              int32_t plan[3]) {
+extern "C" __attribute__((visibility("default"))) mfac_status mfac_gated_plan(mfac_dtype type, int32_t product, int64_t rows,
+                                                                              int64_t cin, int64_t hidden, int32_t plan[3]) {
     using namespace mfac;
     constexpr int64_t most = int64_t(1) << 21;
-    if (type < MFAC_F32 || type > MFAC_F16 || rows < 1 || rows > (int64_t(1) << 30) || cin < 1 || cin > most ||
-        hidden < 1 || hidden > most / 2 || !plan)
+    if (type < MFAC_F32 || type > MFAC_F16 || product < MFAC_GATED_FORWARD || product > MFAC_GATED_HIDDEN_SUMS || rows < 1 ||
+        rows > (int64_t(1) << 30) || cin < 1 || cin > most || hidden < 1 || hidden > most / 2 || !plan)
         return MFAC_EINVAL;
+    const bool backward = product == MFAC_GATED_HIDDEN || product == MFAC_GATED_HIDDEN_SUMS;
     Product p{};
     p.M = rows;
-    p.N = hidden_bwd ? hidden : 2 * hidden;
+    p.N = backward ? hidden : 2 * hidden;
     p.K = cin;
-    p.b_col = hidden_bwd != 0;
-    p.gate = hidden_bwd ? GATE_HIDDEN : GATE_FORWARD;
+    p.b_col = backward;
+    p.gate = backward ? GATE_HIDDEN : GATE_FORWARD;
     const Plan q = plan_of(type, p);
     plan[0] = q.tile;
     plan[1] = q.splits;
-    plan[2] = q.splits == 1 && streams(p, q, type);
+    if (backward)   // where dz is not formed in it, the product stores da in fp32
+        plan[2] = q.splits == 1 && !(product == MFAC_GATED_HIDDEN && hidden_fused(type, q.splits, hidden)) && streams(p, q, DT_F32);
+    else
+        plan[2] = q.splits == 1 &&
+                  streams(p, q, type, kept_bytes(p, product == MFAC_GATED_FORWARD_Z, product == MFAC_GATED_FORWARD_COPIES, type));
     return MFAC_OK;
 }

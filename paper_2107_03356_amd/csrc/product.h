@@ -51,6 +51,10 @@ inline bool streams(const Product& p, const Plan& q, int out_dt, int64_t kept = 
     const int64_t bytes = (p.M * p.K + p.N * p.K) * 2 * (q.nseg > 1 ? 3 : 1) + out * dtype_bytes(out_dt) + kept;
     return q.tile == 256 && bytes > LAST_LEVEL_CACHE;
 }
+// Bytes that a gated layer stores of its pre-activations, of type dt or as copies.
+inline int64_t kept_bytes(const Product& p, bool z, bool copies, int dt) {
+    return z ? p.M * p.N * dtype_bytes(dt) : copies ? p.M * p.N : 0;
+}
 
 // Launches the tiles of a product; compiled in the files named above.
 template <typename T, int KIND>
@@ -765,7 +769,7 @@ hipError_t run_product(const Product& p, const Plan& q, const GemmArgs& g, hipSt
     // 2048^3 against 27
     // (a gated layer's waves have 32 columns of the result, one group of an 8-bit copy: four waves of 16 rows then)
     constexpr int WM = KIND == GATED ? 4 : 2;
-    const int64_t kept = KIND != GATED ? 0 : g.e.z ? p.M * p.N * dtype_bytes(g.e.io_dt) : g.e.p.q ? p.M * p.N : 0;
+    const int64_t kept = KIND == GATED ? kept_bytes(p, g.e.z, g.e.p.q, g.e.io_dt) : 0;
     // HIDDEN writes three to six times what it reads, past what the caches hold in any case: bf16 8192 rows, 2048 to 8192, two
     // parts each, take 527 us with plain stores, 548 with nontemporal ones
     if (q.tile == 64) k_product<T, KIND, 64, 64, WM, 4 / WM, 3, false><<<grid, 256, 0, st>>>(g);

@@ -110,6 +110,10 @@ struct Product {
     int64_t b_part;
 };
 size_t product_workspace_bytes(int dt, const Product& p);
+// Whether dz and a come straight from the product that forms da, in so many parts of K (no column sums wanted): where its
+// parts are joined, and in its epilogue of 16-bit data where a wave's columns are all there or none (fp32's epilogue would
+// write 18 bytes a sum).
+inline bool hidden_fused(int dt, int splits, int64_t hidden) { return splits > 1 || (dt != DT_F32 && hidden % 64 == 0); }
 int product_splits(int dt, const Product& p);   // parts of K, of rows > 0
 // A matrix as the products take it: ld elements a row, a multiple of 8; of fp32 three parts, one after another.
 struct LayOut {
