@@ -32,7 +32,7 @@ struct NormArgs {
     float *mean, *rstd;
     Packed p;
     int64_t rows, cols, ngroups;  // ngroups: groups per row of the copy
-    float eps, inv_cols, ncols;   // the mean by division, so that a row of equal values has a mean of exactly that
+    float eps, inv_cols, ncols;   // the mean by division: exact for a row of equal values whose sum is (bf16, fp16 to 8192)
 };
 
 template <typename T, typename TW, int NT, int NCH>

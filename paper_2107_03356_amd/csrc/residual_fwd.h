@@ -19,7 +19,11 @@
 namespace mfac {
 namespace {
 
-// The row's mean (0 for rms norm) and 1 / sqrt(variance + eps) of values v, which become xhat; zeros past the end.
+// The row's mean (0 for rms norm) and 1 / sqrt(variance + eps) of values v, which become xhat; zeros past the end. The mean is
+// that of an fp32 sum, at most some 40 units of 2^-24 of the mean magnitude off. Where a row's values lie closer together than
+// that, xhat is what the mean's error leaves of them: values that are all 1000, with eps 1e-6, up to 0.08 instead of 0 (values
+// whose sum is exact, as bf16 ones, 0). Summing what the mean leaves beside the squares, to take it off as well, took 10%
+// longer (bf16 8192 x 4096 64.7 us, not 57.0; fp32 4096 x 8192 180, not 108).
 template <int NT, int NCH, bool LAYER>
 __device__ __forceinline__ void normalise(f8 (&v)[NCH], const Residual& g, int t, float* red, int& turn, float& mean,
                                           float& rstd) {
@@ -28,7 +32,7 @@ __device__ __forceinline__ void normalise(f8 (&v)[NCH], const Residual& g, int t
     if constexpr (LAYER) {
 #pragma unroll
         for (int j = 0; j < NCH; ++j) sum += sum8(v[j]);
-        mean = row_sum<NT>(sum, red, turn) / (float)g.cols;   // by division: a row of equal values has that mean
+        mean = row_sum<NT>(sum, red, turn) / (float)g.cols;   // by division: exact for equal values whose sum is
         sum = 0.f;
 #pragma unroll
         for (int j = 0; j < NCH; ++j) {
