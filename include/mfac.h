@@ -557,9 +557,10 @@ mfac_status mfac_gated_linear(mfac_dtype type, mfac_dtype btype, mfac_act act, i
  * those that are NULL are not formed, nor dz or a where they alone need it. da is not rounded. dz and a are rounded to `type`
  * for the products, so that fp16's past 65504 are infinite; for dw1 and dw2 of 16-bit data in fp32 (gtype) they are taken in
  * two parts, the second what the first's rounding leaves. The two parts of fp16 (dz's first serves dx too) are stored times
- * powers of two that keep them finite, which the products take out again. bf16 is infinite from 0x1.ffp127 on. x, or its 8-bit copy (q, s; x NULL), and W1 (w1) are needed for dw1 and dx. gamma and beta (cin fp32
- * values each; beta may be NULL) say that x stands for gamma x + beta in dw1. The workspace query takes, besides
- * addresses that are not read (x NULL: a copy), what is wanted as bits. */
+ * powers of two that keep them finite, which the products take out again. bf16 is infinite from 0x1.ffp127 on. x, or its
+ * 8-bit copy (q, s; x NULL), is needed for dw1, W1 (w1) for dx, W2 (w2) for all but dw2. gamma and beta (cin fp32 values
+ * each; beta may be NULL) say that x stands for gamma x + beta in dw1. The workspace query takes, besides addresses that are
+ * not read (x NULL: a copy), what is wanted as bits. */
 #define MFAC_GATED_DX 1u
 #define MFAC_GATED_DW1 2u
 #define MFAC_GATED_DB1 4u

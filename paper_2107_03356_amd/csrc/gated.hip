@@ -23,10 +23,10 @@ __global__ __launch_bounds__(256) void k_gated_act_bwd(Strips s, const TA* da, i
         const int64_t step = gridDim.y * nsub;
         int64_t row = blockIdx.y * nsub + sub;
         // the next row is on its way while this one is worked on
-        Raw8<TA> next;
+        Raw8<TA> next{};   // without da (a alone is formed) zeros
         std::conditional_t<PACKED, RawPacked8, Raw8<T>> zg, zu;
         auto load = [&](int64_t r) {
-            next.load(da + r * ldda, c, s.cols);
+            if (da) next.load(da + r * ldda, c, s.cols);
             if constexpr (PACKED) {
                 zg.load(e.p.q + r * e.p.ldq, e.p.s + r * ngroups, c, s.cols);
                 zu.load(e.p2.q + r * e.p2.ldq, e.p2.s + r * ngroups, c, s.cols);

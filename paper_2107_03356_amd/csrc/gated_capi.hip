@@ -81,6 +81,7 @@ struct GatedBwd {
     bool da_given() const { return cout == 0; }
     bool sums() const { return db1 || (dw1 && beta); }
     bool dz_wanted() const { return dx || dw1; }
+    bool da_wanted() const { return dz_wanted() || db1; }   // a is formed without it
     bool ranged() const { return type == MFAC_F16 && parts == 2; }   // dz and a may need factors to be in two parts
     int64_t dy_part() const { return rows * lddy_in * 2; }
     int64_t dz_part() const { return rows * lddz * 2; }
@@ -118,7 +119,7 @@ struct GatedBwd {
         int n = 0;
         if (dy_laid_out()) jobs[n++] = LayOut{dy, lddy, rows, cout, ws + dy_in, lddy_in};
         if (type != MFAC_F32) return n;
-        if (!da_given()) jobs[n++] = LayOut{w2, ldw2, cout, hidden, ws + w2_in, ldw2_in};
+        if (!da_given() && da_wanted()) jobs[n++] = LayOut{w2, ldw2, cout, hidden, ws + w2_in, ldw2_in};
         if (dw1 && x) jobs[n++] = LayOut{x, ldx, rows, cin, ws + x_in, ldx_in};
         if (dx) jobs[n++] = LayOut{w1, ldw1, 2 * hidden, cin, ws + w1_in, ldw1_in};
         return n;
@@ -140,7 +141,7 @@ struct GatedBwd {
         parts = type == MFAC_F32 ? 3 : gtype == MFAC_F32 && (dw1 || dw2) ? 2 : 1;
         // dz straight from the product that forms da, without db, whose sums would have to be joined over the tiles.
         // Otherwise da is stored in fp32 and read again.
-        fused = !da_given() && !sums() && rows > 0;
+        fused = !da_given() && da_wanted() && !sums() && rows > 0;
         fused = fused && hidden_fused(type, product_splits(type, da_product(nullptr, nullptr)), hidden);
         auto take = [&](size_t bytes) {
             const size_t at = total;
@@ -149,11 +150,11 @@ struct GatedBwd {
         };
         if (dy_laid_out()) dy_in = take((size_t)dy_part() * (type == MFAC_F32 ? 3 : 1));
         if (type == MFAC_F32) {
-            if (!da_given()) w2_in = take((size_t)cout * ldw2_in * 6);
+            if (!da_given() && da_wanted()) w2_in = take((size_t)cout * ldw2_in * 6);
             if (dw1 && x) x_in = take((size_t)rows * ldx_in * 6);
             if (dx) w1_in = take((size_t)hidden * ldw1_in * 12);
         }
-        if (!da_given() && !fused) da = take((size_t)rows * hidden * 4);
+        if (!da_given() && da_wanted() && !fused) da = take((size_t)rows * hidden * 4);
         if (dz_wanted()) dz = take((size_t)dz_part() * parts);
         if (dw2) a = take((size_t)a_part() * parts);
         if (sums()) {
@@ -162,7 +163,7 @@ struct GatedBwd {
         }
         if (ranged()) range = take(GATE_RANGE * 4);
         if (rows > 0) {   // one after another in the same place; addresses in the workspace are aligned, and not looked at
-            if (!da_given()) need(da_product(dy_laid_out() ? nullptr : dy, nullptr));
+            if (!da_given() && da_wanted()) need(da_product(dy_laid_out() ? nullptr : dy, nullptr));
             if (dx) need(dx_product(nullptr, nullptr));
             if (dw1) need(dw1_product(nullptr, nullptr));
             if (dw2) need(dw2_product(dy_laid_out() ? nullptr : dy, nullptr));
@@ -255,7 +256,7 @@ MFAC_API mfac_status mfac_gated_bwd(mfac_dtype type, mfac_dtype gtype, mfac_act 
     if (!dx && !dw1 && !db1 && !dw2) return MFAC_OK;
     if (rows > 0) {
         const bool copy = q || s;
-        if (!matrix_ok(dy, type, lddy, cout ? cout : hidden) || (cout && !matrix_ok(w2, type, ldw2, hidden)) ||
+        if (!matrix_ok(dy, type, lddy, cout ? cout : hidden) || (cout && (dx || dw1 || db1) && !matrix_ok(w2, type, ldw2, hidden)) ||
             !pair_ok(type, hidden, zg, zu, ldz, qg, sg, qu, su, ldqz, false) ||
             (dx && (!matrix_ok(w1, type, ldw1, cin) || !matrix_ok(dx, type, lddx, cin))))
             return MFAC_EINVAL;
@@ -298,7 +299,9 @@ MFAC_API mfac_status mfac_gated_bwd(mfac_dtype type, mfac_dtype gtype, mfac_act 
     float* const range = g.ranged() ? (float*)(ws + g.range) : nullptr;
     e.range = range;
     float* db = db1 ? db1 : g.sums() ? (float*)(ws + g.db) : nullptr;
-    if (g.fused) {
+    if (!g.da_wanted()) {
+        err = launch_gated_act_bwd(type, type, rows, hidden, nullptr, 0, e, nullptr, nullptr, stream);
+    } else if (g.fused) {
         err = launch_product(type, g.da_product(dy_at, ws), e, ws + g.product, stream);
     } else if (g.da_given()) {
         err = launch_gated_act_bwd(type, type, rows, hidden, dy, lddy, e, db, (float*)(ws + g.db_part), stream);

@@ -125,7 +125,7 @@ struct LayOut {
 hipError_t launch_lay_out(int dt, int n, const LayOut* jobs, hipStream_t st);   // n <= 4
 hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws, hipStream_t st);
 
-// The gate's part of a backward pass; da is of type da_dt, dt or fp32. Of the epilogue act, z, p, z2, p2, out (dz), a and
+// The gate's part of a backward pass; da is of type da_dt, dt or fp32, or null where out and db are (a alone is formed). Of the epilogue act, z, p, z2, p2, out (dz), a and
 // their parts are used; out and a are 16-bit (bf16 for fp32 data), ldo and lda multiples of 8, zeros past their columns.
 // part: gated_bwd_parts(rows, hidden) * 2 * hidden floats (unused if db is null)
 int64_t gated_bwd_parts(int64_t rows, int64_t hidden);

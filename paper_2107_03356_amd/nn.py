@@ -462,8 +462,15 @@ def _gate_pair(z, rows, n, like):
     return (zg.data_ptr(), zu.data_ptr(), _ld(zg)), (None, None, None, None, 0), (zg, zu)
 
 
-def _gated_backward(dy, x, w1, w2, z, act, affine, grad_dtype, need):
-    """(dx, dw1, db1, dw2), of a gated layer (w2 None), or of it and the layer that follows."""
+def _gate_width(z):
+    try:
+        return z[0].shape[-1]
+    except (TypeError, AttributeError, IndexError):
+        raise ValueError("gated: z is the pair (gate, other) of pre-activations") from None
+
+
+def _gated_backward(dy, x, w1, w2, z, act, affine, grad_dtype, need, behind=True):
+    """(dx, dw1, db1, dw2), of a gated layer, or of it and the layer w2 `behind` it (w2 None: dw2 alone is wanted)."""
     code = _act(act)
     dy2 = _rows(dy, "gated: dy")
     rows = dy2.shape[0]
@@ -472,11 +479,17 @@ def _gated_backward(dy, x, w1, w2, z, act, affine, grad_dtype, need):
         return None, None, None, None
     w2m, cout = (None, 0), 0
     n = dy2.shape[1]
-    if w2 is not None:
-        w2 = _weight(w2)
-        cout, n = dy2.shape[1], w2.shape[1]
-        _same("gated: w2", w2, dy2, (cout, n))
-        w2m = _mat(w2)
+    if behind:
+        cout = n
+        if w2 is not None:
+            w2 = _weight(w2)
+            n = w2.shape[1]
+            _same("gated: w2", w2, dy2, (cout, n))
+            w2m = _mat(w2)
+        elif need_x or need_w1 or need_b1:
+            raise ValueError("gated: only dw2 is formed without w2")
+        else:
+            n = _gate_width(z)
     zm, packed_z, held = _gate_pair(z, rows, n, dy2)
     xm, packed, cin, gamma, beta, w1m = (None, 0), _NO_COPY, 1, None, None, (None, 0)
     if need_x:
@@ -519,7 +532,7 @@ def gated_linear_backward(dy, x, weight, z, act="silu", affine=None, grad_dtype=
     """(dx, dweight, dbias) of y = act(zg) * zu, [zg, zu] = x weight^T + bias, from dy, the input x and the pre-activations z
     (a pair of tensors or of Packed8). ``affine``, ``grad_dtype``: see gated_feed_forward_backward. ``need``: which of the
     three to form; the others are None."""
-    return _gated_backward(dy, x, weight, None, z, act, affine, grad_dtype, (*map(bool, need), False))[:3]
+    return _gated_backward(dy, x, weight, None, z, act, affine, grad_dtype, (*map(bool, need), False), behind=False)[:3]
 
 
 def gated_feed_forward_backward(dy, x, w1, w2, z, act="silu", affine=None, grad_dtype=None, need=(True,) * 5):
@@ -528,7 +541,7 @@ def gated_feed_forward_backward(dy, x, w1, w2, z, act="silu", affine=None, grad_
     gamma * x + beta; dx is then the gradient of that. dw1 and dw2 are of ``grad_dtype`` (float32 or dy's type, the default);
     in float32 of 16-bit data they are those of dz and act(zg) * zu in two parts each, which doubles their products: rounded to
     one, these would leave them off by 2e-3. db1 and db2 are float32. ``need``: which of the five to form; the others are
-    None."""
+    None. w2 may be None where neither dx, dw1 nor db1 is."""
     need_x, need_w1, need_b1, need_w2, need_b2 = map(bool, need)
     dx, dw1, db1, dw2 = _gated_backward(dy, x, w1, w2, z, act, affine, grad_dtype, (need_x, need_w1, need_b1, need_w2))
     return dx, dw1, db1, dw2, act_backward(dy)[2] if need_b2 else None
@@ -915,7 +928,8 @@ class _GatedFeedForward(torch.autograd.Function):
         a, (zg, zu) = gated_linear_forward(x, c1, b1, act, "pack8" if copy8 else "z")
         y = linear_forward(a, c2, b2)
         ctx.act, ctx.types = act, tuple(None if p is None else p.dtype for p in (w1, b1, w2, b2))
-        _keep(ctx, x=(pack8(x) if copy8 else x) if need[1] else None, zg=zg, zu=zu, c1=c1 if need[0] else None, c2=c2)
+        _keep(ctx, x=(pack8(x) if copy8 else x) if need[1] else None, zg=zg, zu=zu, c1=c1 if need[0] else None,
+              c2=c2 if inner else None)
         return y
 
     @staticmethod
