@@ -914,22 +914,26 @@ class _GatedLinear(torch.autograd.Function):
 
 
 class _GatedFeedForward(torch.autograd.Function):
-    """y = (act(zg) * zu) W2^T + b2, [zg, zu] = x W1^T + b1. act(zg) * zu is formed again in the backward pass."""
+    """y = (act(zg) * zu) W2^T + b2, [zg, zu] = x W1^T + b1. act(zg) * zu is formed again in the backward pass. q and s: the
+    8-bit copy that the norm before the block keeps, of which x is gamma times that plus beta; kept for dW1 in place of a copy
+    of x."""
 
     @staticmethod
-    def forward(ctx, x, w1, b1, w2, b2, act, copy8, grad):
+    def forward(ctx, x, w1, b1, w2, b2, act, copy8, grad, q, s, gamma, beta):
         c1, c2 = w1.to(x.dtype), w2.to(x.dtype)
         need = [grad and n for n in ctx.needs_input_grad[:5]]
         inner = any(need[:3])   # whether a gradient passes through the gate
         if not (inner or need[3]):
             ctx.types = tuple(None if p is None else p.dtype for p in (w1, b1, w2, b2))
-            _keep(ctx, x=None, zg=None, zu=None, c1=None, c2=None)
+            _keep(ctx, x=None, zg=None, zu=None, c1=None, c2=None, gamma=None, beta=None)
             return linear_forward(gated_linear_forward(x, c1, b1, act), c2, b2)
         a, (zg, zu) = gated_linear_forward(x, c1, b1, act, "pack8" if copy8 else "z")
         y = linear_forward(a, c2, b2)
         ctx.act, ctx.types = act, tuple(None if p is None else p.dtype for p in (w1, b1, w2, b2))
-        _keep(ctx, x=(pack8(x) if copy8 else x) if need[1] else None, zg=zg, zu=zu, c1=c1 if need[0] else None,
-              c2=c2 if inner else None)
+        shared = q is not None and need[1]
+        kept = None if not need[1] else Packed8(q, s) if shared else pack8(x) if copy8 else x
+        _keep(ctx, x=kept, zg=zg, zu=zu, c1=c1 if need[0] else None, c2=c2 if inner else None, gamma=gamma if shared else None,
+              beta=beta if shared else None)
         return y
 
     @staticmethod
@@ -939,17 +943,18 @@ class _GatedFeedForward(torch.autograd.Function):
         t = ctx.types
         need = ctx.needs_input_grad[:5]
         if not any(need[:4]):
-            return None, None, None, None, _to(act_backward(dy)[2], t[3]), None, None, None
+            return (None, None, None, None, _to(act_backward(dy)[2], t[3])) + (None,) * 7
         # in float32 where either weight has neither its own type nor the data's
         grad = dy.dtype if t[0] == t[2] == dy.dtype else torch.float32
         dx, dw1, db1, dw2, db2 = gated_feed_forward_backward(dy, k["x"], k["c1"], k["c2"], (k["zg"], k["zu"]), ctx.act,
-                                                             grad_dtype=grad, need=need)
-        return dx, _to(dw1, t[0]), _to(db1, t[1]), _to(dw2, t[2]), _to(db2, t[3]), None, None, None
+                                                             None if k["gamma"] is None else (k["gamma"], k["beta"]), grad, need)
+        return (dx, _to(dw1, t[0]), _to(db1, t[1]), _to(dw2, t[2]), _to(db2, t[3])) + (None,) * 7
 
 
 class _Residual(torch.autograd.Function):
     @staticmethod
     def forward(ctx, y, residual, w1, b1, w2, b2, gate, post, pre, scale, p, at, kind, eps, copy8, grad):
+        """(s, h, the kept copy of N_pre's xhat as two tensors), s None where it is y."""
         ctx.set_materialize_grads(False)
         need = [grad and n for n in ctx.needs_input_grad[:7]]
         train = any(need)
@@ -963,13 +968,14 @@ class _Residual(torch.autograd.Function):
             m2, r2 = o.pre if pre else (None, None)
             _keep(ctx, y=y if post or need[6] else None, s=o.copy if o.copy is not None else o.s if pre else None, m1=m1, r1=r1,
                   m2=m2, r2=r2, w1=w1, b1=b1, w2=w2, b2=b2, gate=gate, at=at if p > 0 else None)
-        return o.h if plain else (o.s, o.h)
+        copy = (None, None) if o.copy is None else (o.copy.q, o.copy.s)
+        ctx.mark_non_differentiable(*(t for t in copy if t is not None))
+        return (None if plain else o.s, o.h, *copy)
 
     @staticmethod
     @once_differentiable
-    def backward(ctx, *grads):
+    def backward(ctx, ds, dh, *of_copy):
         post, pre, scale, p, kind = ctx.options
-        ds, dh = grads if len(grads) == 2 else (None, grads[0])
         if ds is None and dh is None:
             return (None,) * 16
         k = _kept(ctx)
@@ -1029,21 +1035,27 @@ def gated_linear(x, weight, bias=None, act="silu", copy8=False):
 def gated_feed_forward(x, w1, w2, b1=None, b2=None, act="silu", copy8=False):
     """gated_linear(x, w1, b1, act) w2^T + b2, differentiable. copy8: what the backward pass needs is kept in 8 bits."""
     _act(act)
-    return _GatedFeedForward.apply(x, w1, b1, w2, b2, act, copy8, torch.is_grad_enabled())
+    return _GatedFeedForward.apply(x, w1, b1, w2, b2, act, copy8, torch.is_grad_enabled(), None, None, None, None)
 
 
 def residual_norm(y, residual=None, post=None, pre=None, gate=None, scale=1.0, p=0.0, at=None, kind="rms", eps=1e-6,
                   copy8=False):
     """(s, h) of residual_norm_forward, differentiable; h is None without pre, and s is y where nothing lies between.
     ``at`` is drawn where p > 0 and none is given. copy8: keep N_pre's xhat in 8 bits for the backward pass instead of s."""
+    return _residual_norm(y, residual, post, pre, gate, scale, p, at, kind, eps, copy8)[:2]
+
+
+def _residual_norm(y, residual=None, post=None, pre=None, gate=None, scale=1.0, p=0.0, at=None, kind="rms", eps=1e-6,
+                   copy8=False):
+    """(s, h, and the kept copy of N_pre's xhat as two tensors, or None twice)"""
     if post is None and pre is None and gate is None and residual is None and p == 0:
-        return y, None
+        return y, None, None, None
     _between(_rows(y, "residual_norm: y"), post, pre, gate, kind)
     if p > 0 and at is None:
         at = dropout_at(y.device)
-    out = _Residual.apply(y, residual, *(post or (None, None)), *(pre or (None, None)), gate, post is not None,
-                          pre is not None, scale, p, at, kind, eps, copy8, torch.is_grad_enabled())
-    return out if isinstance(out, tuple) else (y, out)
+    s, *rest = _Residual.apply(y, residual, *(post or (None, None)), *(pre or (None, None)), gate, post is not None,
+                               pre is not None, scale, p, at, kind, eps, copy8, torch.is_grad_enabled())
+    return (y if s is None else s, *rest)
 
 
 def rms_norm(x, weight=None, eps=1e-6, copy8=False):
@@ -1169,16 +1181,30 @@ class GatedFeedForward(torch.nn.Module):
 
     def inner(self, h):
         """The block without its norms and skip connection."""
-        return gated_feed_forward(h, self.up.weight, self.down.weight, self.up.bias, self.down.bias, self.up.act, self.copy8)
+        return self._inner(h, None, None)
 
     def join(self, y, x, pre=None):
         """(s, h): the stream after the block, and its norm `pre` (the next block's; None: no h)."""
-        return residual_norm(y, x, _norm_of(self.post), _norm_of(pre), self.gate, self.scale, self.p if self.training else 0.0,
-                             kind=self.kind, eps=self.eps, copy8=self.copy8)
+        return self._join(y, x, pre)[:2]
+
+    def _inner(self, h, q, s):
+        """`inner` of self.norm's h, whose 8-bit copy (q, s) the norm keeps: one copy serves both backward passes."""
+        gamma, beta = (None if v is None else v.detach() for v in _norm_of(self.norm))
+        if not self.copy8 or q is None:
+            q = s = gamma = beta = None
+        return _GatedFeedForward.apply(h, self.up.weight, self.up.bias, self.down.weight, self.down.bias, self.up.act, self.copy8,
+                                       torch.is_grad_enabled(), q, s, gamma, beta)
+
+    def _join(self, y, x, pre):
+        return _residual_norm(y, x, _norm_of(self.post), _norm_of(pre), self.gate, self.scale, self.p if self.training else 0.0,
+                              kind=self.kind, eps=self.eps, copy8=self.copy8)
+
+    def _first(self, x):
+        """self.norm of x, with the copy that it keeps."""
+        return _residual_norm(x, pre=_norm_of(self.norm), kind=self.kind, eps=self.eps, copy8=self.copy8)[1:]
 
     def forward(self, x):
-        h = residual_norm(x, pre=_norm_of(self.norm), kind=self.kind, eps=self.eps, copy8=self.copy8)[1]
-        return self.join(self.inner(h), x)[0]
+        return self.join(self._inner(*self._first(x)), x)[0]
 
 
 def _norm_of(module):
@@ -1198,8 +1224,7 @@ class GatedStack(torch.nn.Module):
         self.norm = RMSNorm(dim, eps, device=device) if kind == "rms" else LayerNorm(dim, eps, device=device)
 
     def forward(self, x):
-        first = self.blocks[0]
-        h = residual_norm(x, pre=_norm_of(first.norm), kind=first.kind, eps=first.eps, copy8=first.copy8)[1]
+        h, *copy = self.blocks[0]._first(x)
         for block, norm in zip(self.blocks, [b.norm for b in self.blocks[1:]] + [self.norm]):
-            x, h = block.join(block.inner(h), x, norm)
+            x, h, *copy = block._join(block._inner(h, *copy), x, norm)
         return h
