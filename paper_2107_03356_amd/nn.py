@@ -598,6 +598,17 @@ def dropout_forward(x, p, at):
     return y
 
 
+def _pair(norm):
+    """(weight, bias) of a norm, None twice where there is none."""
+    if norm is None:
+        return None, None
+    try:
+        w, b = norm
+    except (TypeError, ValueError):
+        raise ValueError("residual_norm: a norm is None or a pair (weight, bias)") from None
+    return w, b
+
+
 def _between(y, post, pre, gate, kind):
     """(norms, type code of the parameters, post w, post b, pre w, pre b, gate, gates) for rows like y."""
     layer = KINDS.get(kind)
@@ -617,10 +628,7 @@ def _between(y, post, pre, gate, kind):
     for i, norm in ((0, post), (1, pre)):
         if norm is None:
             continue
-        try:
-            w, b = norm
-        except (TypeError, ValueError):
-            raise ValueError("residual_norm: a norm is None or a pair (weight, bias)") from None
+        w, b = _pair(norm)
         if w is not None:
             w, found = vector(w, found)
         if b is not None:
@@ -1050,11 +1058,11 @@ def _residual_norm(y, residual=None, post=None, pre=None, gate=None, scale=1.0, 
     """(s, h, and the kept copy of N_pre's xhat as two tensors, or None twice)"""
     if post is None and pre is None and gate is None and residual is None and p == 0:
         return y, None, None, None
-    _between(_rows(y, "residual_norm: y"), post, pre, gate, kind)
+    of_post, of_pre = _pair(post), _pair(pre)
     if p > 0 and at is None:
         at = dropout_at(y.device)
-    s, *rest = _Residual.apply(y, residual, *(post or (None, None)), *(pre or (None, None)), gate, post is not None,
-                               pre is not None, scale, p, at, kind, eps, copy8, torch.is_grad_enabled())
+    s, *rest = _Residual.apply(y, residual, *of_post, *of_pre, gate, post is not None, pre is not None, scale, p, at, kind, eps,
+                               copy8, torch.is_grad_enabled())
     return (y if s is None else s, *rest)
 
 

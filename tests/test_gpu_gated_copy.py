@@ -78,3 +78,36 @@ def test_its_gradients_are_those_of_the_passes(dev, kind, dtype, bias):
     assert torch.equal(x.grad, g.dy + dy)
     if bias:
         assert torch.equal(block.up.bias.grad, db1) and torch.equal(block.down.bias.grad, db2)
+
+
+def test_rows_without_unit_stride_are_copied_once(dev):
+    """Each input that has none is copied for the call, and not a second time to look at it."""
+    from paper_2107_03356_amd import nn
+    say("copied once")
+    rows, cols = 200, 320
+    y, r, g = (rand(dev, s, cols, rows).t() for s in (1, 2, 3))
+    w = rand(dev, 4, cols, at=1)
+
+    def allocations(*t):
+        with torch.no_grad():
+            torch.cuda.synchronize()
+            before = torch.cuda.memory_stats()["allocation.all.allocated"]
+            out = nn.residual_norm(t[0], t[1], pre=(w, None), gate=t[2])
+            return torch.cuda.memory_stats()["allocation.all.allocated"] - before, out
+
+    plain, want = allocations(*(t.contiguous() for t in (y, r, g)))
+    strided, got = allocations(y, r, g)
+    assert strided == plain + 3
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_refused_calls_of_residual_norm(dev):
+    from paper_2107_03356_amd import nn
+    say("refused")
+    x, w = rand(dev, 1, 5, 64), rand(dev, 2, 64)
+    for kw in (dict(kind="mean"), dict(pre=(w[:63], None)), dict(pre=w), dict(pre=(w, w)), dict(gate=w[:63]), dict(gate=x[:4]),
+               dict(residual=x[:4]), dict(p=1.5), dict(p=float("nan")), dict(pre=(w, None), residual=x.half())):
+        with pytest.raises(ValueError):
+            nn.residual_norm(x, **{**dict(residual=x), **kw})
+    with pytest.raises(ValueError):
+        nn.residual_norm(x.cpu(), x.cpu())
