@@ -5,41 +5,22 @@
 #include <algorithm>
 
 #include "../../include/mfac.h"
+#include "checks.h"
 #include "internal.h"
 #include "train.h"
-
-#define MFAC_API extern "C" __attribute__((visibility("default")))
 
 using namespace mfac;
 
 namespace {
 
-constexpr int64_t MOST = int64_t(1) << 30, MOST_WIDTH = int64_t(1) << 21, MOST_HELD = int64_t(1) << 15;
+constexpr int64_t MOST_HELD = int64_t(1) << 15;
 
-bool type_ok(int t) { return t == MFAC_F32 || t == MFAC_BF16 || t == MFAC_F16; }
-bool param_type_ok(int t, int data) { return t == MFAC_F32 || t == data; }
-bool act_ok(int a) { return a >= MFAC_ACT_NONE && a <= MFAC_ACT_SILU; }
 // hidden: 2 hidden rows of W are a layer's width
 bool gated_ok(int64_t rows, int64_t cin, int64_t hidden) {
-    return rows >= 0 && rows <= MOST && cin >= 1 && cin <= MOST_WIDTH && hidden >= 1 && hidden <= MOST_WIDTH / 2;
-}
-bool aligned(const void* p, int type) { return (uintptr_t)p % (type == MFAC_F32 ? 4 : 2) == 0; }
-bool matrix_ok(const void* p, int type, int64_t ld, int64_t cols) {
-    return p && ld >= cols && ld <= (int64_t(1) << 33) && aligned(p, type);
+    return size_ok(rows, cin) && cin <= MOST_WIDTH && hidden >= 1 && hidden <= MOST_WIDTH / 2;
 }
 bool matrix_or_none(const void* p, int type, int64_t ld, int64_t cols) { return !p || matrix_ok(p, type, ld, cols); }
-bool vector_ok(const void* p, int type) { return !p || aligned(p, type); }
-bool copy_ok(const void* q, int64_t ldq, const void* s, int64_t cols) {
-    return q && s && ldq >= cols && ldq <= (int64_t(1) << 33);
-}
-
-mfac_status done(hipError_t e) { return e == hipSuccess ? MFAC_OK : MFAC_EHIP; }
-
-mfac_status check_workspace(size_t need, const void* ws, size_t bytes) {
-    if (need == 0) return MFAC_OK;
-    if (bytes < need) return MFAC_EWORKSPACE;
-    return ws && ((uintptr_t)ws & 255) == 0 ? MFAC_OK : MFAC_EINVAL;
-}
+bool copy_ok(const void* q, int64_t ldq, const void* s, int64_t cols) { return packed_ok(q, ldq, s, cols, false); }
 
 Product gated_product(int64_t rows, int64_t cin, int64_t hidden, const void* x, int64_t ldx, const void* w, int64_t ldw) {
     return Product{rows, 2 * hidden, cin, x, ldx, false, w, ldw, false, Packed{}, GATE_FORWARD};
@@ -467,7 +448,7 @@ MFAC_API mfac_status mfac_residual_norm_bwd(mfac_dtype type, mfac_dtype wtype, i
 MFAC_API mfac_status mfac_dropout(mfac_dtype type, int64_t rows, int64_t cols, const void* x, int64_t ldx, double p,
                                   const int64_t* at, void* y, int64_t ldy, hipStream_t stream) {
     Drop d{};
-    if (!type_ok(type) || rows < 0 || rows > MOST || cols < 1 || cols > MOST || !drop_of(p, at, d)) return MFAC_EINVAL;
+    if (!type_ok(type) || !size_ok(rows, cols) || !drop_of(p, at, d)) return MFAC_EINVAL;
     if (rows == 0) return MFAC_OK;
     if (!matrix_ok(x, type, ldx, cols) || !matrix_ok(y, type, ldy, cols) || !at) return MFAC_EINVAL;
     return done(launch_dropout(type, rows, cols, x, ldx, d, y, ldy, stream));

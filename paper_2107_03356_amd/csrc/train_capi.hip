@@ -5,46 +5,16 @@
 #include <algorithm>
 
 #include "../../include/mfac.h"
+#include "checks.h"
 #include "internal.h"
 #include "train.h"
-
-#define MFAC_API extern "C" __attribute__((visibility("default")))
 
 using namespace mfac;
 
 namespace {
 
-constexpr int64_t MOST = int64_t(1) << 30;
-
-bool type_ok(int t) { return t == MFAC_F32 || t == MFAC_BF16 || t == MFAC_F16; }
-// Parameters come in fp32 or in the type of the data.
-bool param_type_ok(int t, int data) { return t == MFAC_F32 || t == data; }
-bool act_ok(int a) { return a >= MFAC_ACT_NONE && a <= MFAC_ACT_SILU; }
-bool size_ok(int64_t rows, int64_t cols) { return rows >= 0 && rows <= MOST && cols >= 1 && cols <= MOST; }
-// A layer's widths are at most 2^21: the products' copies address a tile of 256 rows in 32 bits.
 bool layer_ok(int64_t rows, int64_t cin, int64_t cout) {
-    return size_ok(rows, cin) && size_ok(rows, cout) && cin <= (int64_t(1) << 21) && cout <= (int64_t(1) << 21);
-}
-
-// A matrix of rows x cols with ld elements between rows.
-bool matrix_ok(const void* p, int type, int64_t ld, int64_t cols) {
-    return p && ld >= cols && ld <= (int64_t(1) << 33) && (uintptr_t)p % (type == MFAC_F32 ? 4 : 2) == 0;
-}
-bool vector_ok(const void* p, int type) { return !p || (uintptr_t)p % (type == MFAC_F32 ? 4 : 2) == 0; }
-// q and s both given, or (where it may be absent) neither.
-bool packed_ok(const void* q, int64_t ldq, const void* s, int64_t cols, bool absent_ok) {
-    if (!q && !s) return absent_ok;
-    return q && s && ldq >= cols && ldq <= (int64_t(1) << 33);
-}
-bool workspace_ok(const void* ws) { return ws && ((uintptr_t)ws & 255) == 0; }
-
-mfac_status done(hipError_t e) { return e == hipSuccess ? MFAC_OK : MFAC_EHIP; }
-
-// The workspace a call needs: MFAC_OK, or what is wrong with the one given.
-mfac_status check_workspace(size_t need, const void* ws, size_t bytes) {
-    if (need == 0) return MFAC_OK;
-    if (bytes < need) return MFAC_EWORKSPACE;
-    return workspace_ok(ws) ? MFAC_OK : MFAC_EINVAL;
+    return size_ok(rows, cin) && size_ok(rows, cout) && cin <= MOST_WIDTH && cout <= MOST_WIDTH;
 }
 
 Product forward_product(int64_t rows, int64_t cin, int64_t cout, const void* x, int64_t ldx, const void* w,
