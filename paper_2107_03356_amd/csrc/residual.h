@@ -11,6 +11,7 @@
 
 namespace mfac {
 
+int64_t residual_bwd_grid(int dt, int norms, int64_t rows, int64_t cols);   // work-groups, each with its column sums
 template <typename T>
 hipError_t residual_fwd(int wt, const Residual& g, hipStream_t st);
 template <typename T>

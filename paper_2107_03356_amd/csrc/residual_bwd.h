@@ -311,7 +311,7 @@ void by_threads_bwd(int64_t cols, F f) {
 template <typename T>
 hipError_t residual_bwd(int wt, const Residual& g, const ResidualBwd& b, hipStream_t st) {
     constexpr int DT = sizeof(T) == 4 ? DT_F32 : DT_BF16;
-    const unsigned grid = (unsigned)residual_bwd_parts(DT, g.norms, g.rows, g.cols);
+    const unsigned grid = (unsigned)residual_bwd_grid(DT, g.norms, g.rows, g.cols);
     const bool between = g.norms & POST_NORM || g.y || g.gate || g.gates || g.drop.threshold;
     const int norms = between || !in_registers(g.cols) ? g.norms : g.norms | NOTHING_BETWEEN;
     by_norms(norms, [&](auto tag) {

@@ -25,9 +25,10 @@ def test_rows_of_equal_values(dev, size, cols):
     say("rows of equal values", size, cols)
     eps = 1e-6
     x = (size * rand(dev, 1, 50, 1)).expand(50, cols).contiguous()
-    o = nn.residual_norm_forward(x, pre=(None, None), kind="layer", eps=eps)
     units = (ROW + 2) * E32 * x.abs().double()
-    assert (o.h.abs() <= units / eps ** 0.5).all() and ((o.pre[0] - x[:, 0]).abs() <= units[:, 0]).all()
-    x = x.to(torch.bfloat16)
-    o = nn.residual_norm_forward(x, pre=(None, None), kind="layer", eps=eps)
-    assert (o.h == 0).all() and torch.equal(o.pre[0], x[:, 0].float())
+    for residual in (None, 0 * x):
+        o = nn.residual_norm_forward(x, residual, pre=(None, None), kind="layer", eps=eps)
+        assert (o.h.abs() <= units / eps ** 0.5).all() and ((o.pre[0] - x[:, 0]).abs() <= units[:, 0]).all()
+        y, r = x.to(torch.bfloat16), None if residual is None else residual.to(torch.bfloat16)
+        o = nn.residual_norm_forward(y, r, pre=(None, None), kind="layer", eps=eps)
+        assert (o.h == 0).all() and torch.equal(o.pre[0], y[:, 0].float())
