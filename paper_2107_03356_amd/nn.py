@@ -1187,32 +1187,28 @@ class GatedFeedForward(torch.nn.Module):
         self.down = Linear(hidden, dim, bias, device=device)
         self.gate = None if gate is None else torch.nn.Parameter(torch.full((dim,), float(gate), device=device))
 
-    def inner(self, h):
-        """The block without its norms and skip connection."""
-        return self._inner(h, None, None)
-
-    def join(self, y, x, pre=None):
-        """(s, h): the stream after the block, and its norm `pre` (the next block's; None: no h)."""
-        return self._join(y, x, pre)[:2]
-
-    def _inner(self, h, q, s):
-        """`inner` of self.norm's h, whose 8-bit copy (q, s) the norm keeps: one copy serves both backward passes."""
-        gamma, beta = (None if v is None else v.detach() for v in _norm_of(self.norm))
-        if not self.copy8 or q is None:
-            q = s = gamma = beta = None
+    def inner(self, h, copy=None):
+        """The block without its norms and skip connection. copy: what self.norm kept of h, (q, s) or None (see join)."""
+        q, s, gamma, beta = None, None, None, None
+        if self.copy8 and copy is not None:
+            (q, s), (gamma, beta) = copy, (None if v is None else v.detach() for v in _norm_of(self.norm))
         return _GatedFeedForward.apply(h, self.up.weight, self.up.bias, self.down.weight, self.down.bias, self.up.act, self.copy8,
                                        torch.is_grad_enabled(), q, s, gamma, beta)
 
-    def _join(self, y, x, pre):
-        return _residual_norm(y, x, _norm_of(self.post), _norm_of(pre), self.gate, self.scale, self.p if self.training else 0.0,
-                              kind=self.kind, eps=self.eps, copy8=self.copy8)
+    def join(self, y, x, pre=None, want_copy=False):
+        """(s, h): the stream after the block, and its norm `pre` (the next block's; None: no h). want_copy: also the 8-bit copy
+        that the norm keeps of h's xhat, (q, s), or None where it keeps none: the next block's `inner` shares it."""
+        s, h, *copy = _residual_norm(y, x, _norm_of(self.post), _norm_of(pre), self.gate, self.scale,
+                                     self.p if self.training else 0.0, kind=self.kind, eps=self.eps, copy8=self.copy8)
+        return (s, h, copy if copy[0] is not None else None) if want_copy else (s, h)
 
-    def _first(self, x):
-        """self.norm of x, with the copy that it keeps."""
-        return _residual_norm(x, pre=_norm_of(self.norm), kind=self.kind, eps=self.eps, copy8=self.copy8)[1:]
+    def first(self, x):
+        """(h, copy): the norm before the block, of x, and what it keeps of it, as in join."""
+        _, h, *copy = _residual_norm(x, pre=_norm_of(self.norm), kind=self.kind, eps=self.eps, copy8=self.copy8)
+        return h, copy if copy[0] is not None else None
 
     def forward(self, x):
-        return self.join(self._inner(*self._first(x)), x)[0]
+        return self.join(self.inner(*self.first(x)), x)[0]
 
 
 def _norm_of(module):
@@ -1232,7 +1228,7 @@ class GatedStack(torch.nn.Module):
         self.norm = RMSNorm(dim, eps, device=device) if kind == "rms" else LayerNorm(dim, eps, device=device)
 
     def forward(self, x):
-        h, *copy = self.blocks[0]._first(x)
+        h, copy = self.blocks[0].first(x)
         for block, norm in zip(self.blocks, [b.norm for b in self.blocks[1:]] + [self.norm]):
-            x, h, *copy = block._join(block._inner(h, *copy), x, norm)
+            x, h, copy = block.join(block.inner(h, copy), x, norm, want_copy=True)
         return h
