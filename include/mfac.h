@@ -535,13 +535,11 @@ mfac_status mfac_linear_plan(mfac_dtype type, mfac_dtype otype, mfac_product pro
  * ----------------------------------------------------------------------
  * By the same rules as the calls above. */
 
-/* Gated layer: z = x W^T + b for W of 2 hidden rows (those of the gate, then those
- * of the other projection; bias likewise), y = act(zg) zu, for x (rows x cin), W
- * (2 hidden x cin), y (rows x hidden); hidden at most 2^20. Both projections, the
- * activation and the product are one kernel. bias (2 hidden values of btype) may be NULL. The
- * pre-activations zg and zu (rows x hidden each) may be kept for the backward
- * pass, as matrices of `type` with the same ldz (they may be the halves of one), or as
- * 8-bit copies (qg, sg) and (qu, su) with the same ldq; both or neither of the two. */
+/* Gated layer: z = x W^T + b for W of 2 hidden rows (those of the gate, then those of the other projection; bias likewise),
+ * y = act(zg) zu, for x (rows x cin), W (2 hidden x cin), y (rows x hidden); hidden at most 2^20. Both projections, the
+ * activation and the product are one kernel. bias (2 hidden values of btype) may be NULL. The pre-activations zg and zu
+ * (rows x hidden each) may be kept for the backward pass, as matrices of `type` with the same ldz (they may be the halves of
+ * one), or as 8-bit copies (qg, sg) and (qu, su) with the same ldq; both or neither of the two. */
 size_t mfac_gated_linear_workspace_bytes(mfac_dtype type, int64_t rows, int64_t cin, int64_t hidden, const void* x,
                                          int64_t ldx, const void* w, int64_t ldw);
 mfac_status mfac_gated_linear(mfac_dtype type, mfac_dtype btype, mfac_act act, int64_t rows, int64_t cin, int64_t hidden,
@@ -554,13 +552,13 @@ mfac_status mfac_gated_linear(mfac_dtype type, mfac_dtype btype, mfac_act act, i
  * copies), with da = dy W2, or dy,
  *   dz = [da zu act'(zg), da act(zg)], a = act(zg) zu,
  *   dx = dz W, dw1 = dz^T x (gtype), db1 = column sums of dz in fp32, dw2 = dy^T a (gtype);
- * those that are NULL are not formed, nor dz or a where they alone need it. da is not rounded. dz and a are rounded to `type`
- * for the products, so that fp16's past 65504 are infinite; for dw1 and dw2 of 16-bit data in fp32 (gtype) they are taken in
- * two parts, the second what the first's rounding leaves. The two parts of fp16 (dz's first serves dx too) are stored times
- * powers of two that keep them finite, which the products take out again. bf16 is infinite from 0x1.ffp127 on. x, or its
- * 8-bit copy (q, s; x NULL), is needed for dw1, W1 (w1) for dx, W2 (w2) for all but dw2. gamma and beta (cin fp32 values
- * each; beta may be NULL) say that x stands for gamma x + beta in dw1. The workspace query takes, besides addresses that are
- * not read (x NULL: a copy), what is wanted as bits. */
+ * those that are NULL are not formed, nor da, dz or a where they alone need it. da is not rounded. dz and a are rounded to
+ * `type` for the products, so that fp16's past 65504 are infinite; for dw1 and dw2 of 16-bit data in fp32 (gtype) they are
+ * taken in two parts, the second what the first's rounding leaves. The two parts of fp16 (dz's first serves dx too) are
+ * stored times powers of two that keep them finite, which the products take out again; bf16 is infinite from 0x1.ffp127 on.
+ * x, or its 8-bit copy (q, s; x NULL), is needed for dw1, W1 (w1) for dx, W2 (w2) for all but dw2. gamma and beta (cin fp32
+ * values each; beta may be NULL) say that x stands for gamma x + beta in dw1. The workspace query takes, besides addresses
+ * that are not read (x NULL: a copy), what is wanted as bits. */
 #define MFAC_GATED_DX 1u
 #define MFAC_GATED_DW1 2u
 #define MFAC_GATED_DB1 4u
@@ -578,27 +576,25 @@ mfac_status mfac_gated_bwd(mfac_dtype type, mfac_dtype gtype, mfac_act act, int6
                            void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* Dropout. at: two int64 in device memory, seed and offset, 8-byte aligned, read when the kernel runs (so a captured graph
- * takes what they hold when it is replayed). Element (row, c) of a matrix takes half-word c % 8 of the
- * Philox 4x32-10 block with counter (c / 8, row, offset mod 2^32, offset / 2^32) and key (seed mod 2^32, seed /
- * 2^32), both taken as unsigned; half-word i is the lower (i even) or upper half of word i / 2. It is kept
- * where the half-word is at least T = floor(65536 p + 1/2), and multiplied by 65536 / (65536 - T);
- * others become 0, infinities and NaN among them. 0 <= p <= 1; with T = 0 every value is kept, with
- * T = 65536 none. The mask depends on p, at and the place in the matrix alone, not on the type or strides: the
- * gradient is the same call on dy. y may be x. */
+ * takes what they hold when it is replayed). Element (row, c) of a matrix takes half-word c % 8 of the Philox 4x32-10 block
+ * with counter (c / 8, row, offset mod 2^32, offset / 2^32) and key (seed mod 2^32, seed / 2^32), both taken as unsigned;
+ * half-word i is the lower (i even) or upper half of word i / 2. It is kept where the half-word is at least
+ * T = floor(65536 p + 1/2), and multiplied by 65536 / (65536 - T); others become 0, infinities and NaN among them.
+ * 0 <= p <= 1; with T = 0 every value is kept, with T = 65536 none. The mask depends on p, at and the place in the matrix
+ * alone, not on the type or strides: the gradient is the same call on dy. y may be x. */
 mfac_status mfac_dropout(mfac_dtype type, int64_t rows, int64_t cols, const void* x, int64_t ldx, double p,
                          const int64_t* at, void* y, int64_t ldy, hipStream_t stream);
 
 /* What lies between two blocks of a network with a residual stream, row by row:
  *   n = N_post(y), s = scale res + gate drop(n), h = N_pre(s).
- * N is rms norm, x rstd w with rstd = 1 / sqrt(mean(x^2) + eps), or with
- * MFAC_NORM_LAYER layer norm as above, both of one kind; either may be absent (n = y;
- * no h). post_w, post_b, pre_w, pre_b (cols values of wtype) may be NULL (1 and 0); rms
- * norm has no b. The gate is one value for each channel (`gate`, cols values of wtype), one for each
- * element (`gates`, of `type`), or absent (1). drop is dropout with p and at (at may be NULL where T is 0). res and s
- * may be NULL (no residual; not wanted, where h is). h is formed from s before its rounding. Statistics
- * (rows fp32 values each) may be NULL; means are layer norm's. q and sq: the 8-bit copy of N_pre's xhat, or both
- * NULL. cols at most 2^15. eps >= 0 and scale finite. s may be y or res, and h may be y or res, but not s. With
- * MFAC_NORM_PRE alone and no residual, gate or dropout the call is h = N(y). */
+ * N is rms norm, x rstd w with rstd = 1 / sqrt(mean(x^2) + eps), or with MFAC_NORM_LAYER layer norm as above, both of one
+ * kind; either may be absent (n = y; no h). post_w, post_b, pre_w, pre_b (cols values of wtype) may be NULL (1 and 0); rms
+ * norm has no b. The gate is one value for each channel (`gate`, cols values of wtype), one for each element (`gates`, of
+ * `type`), or absent (1). drop is dropout with p and at (at may be NULL where T is 0). res and s may be NULL (no residual;
+ * not wanted, where h is). h is formed from s before its rounding. Statistics (rows fp32 values each) may be NULL; means are
+ * layer norm's. q and sq: the 8-bit copy of N_pre's xhat, or both NULL. cols at most 2^15. eps >= 0 and scale finite. s may
+ * be y or res, and h may be y or res, but not s. With MFAC_NORM_PRE alone and no residual, gate or dropout the call is
+ * h = N(y). */
 typedef enum {
     MFAC_NORM_POST = 1,
     MFAC_NORM_PRE = 2,
@@ -611,12 +607,12 @@ mfac_status mfac_residual_norm(mfac_dtype type, mfac_dtype wtype, int32_t norms,
                                void* h, int64_t ldh, float* post_mean, float* post_rstd, float* pre_mean,
                                float* pre_rstd, int8_t* q, int64_t ldq, uint8_t* sq, hipStream_t stream);
 
-/* Its gradients. ds is the gradient that reaches s from elsewhere (NULL: none; needed without MFAC_NORM_PRE), dh that of
- * h. With d = ds + the gradient of N_pre at dh,
+/* Its gradients. ds is the gradient that reaches s from elsewhere (NULL: none; needed without MFAC_NORM_PRE), dh that of h.
+ * With d = ds + the gradient of N_pre at dh,
  *   dres = scale d, dn = gate drop(d), dgate(s) = d drop(n), dy = the gradient of N_post at dn;
- * outputs may be NULL (not wanted); those of parameters (wtype) are sums over the rows. s, or the 8-bit copy of N_pre's xhat (then s
- * and pre_mean are NULL); y may be NULL where neither MFAC_NORM_POST nor a gate's gradient needs it. dy and dres may be
- * ds or dh, dy may be y. The workspace is needed for parameters' gradients. */
+ * outputs may be NULL (not wanted); those of parameters (wtype) are sums over the rows. s, or the 8-bit copy of N_pre's xhat
+ * (then s and pre_mean are NULL); y may be NULL where neither MFAC_NORM_POST nor a gate's gradient needs it. dy and dres may
+ * be ds or dh, dy may be y. The workspace is needed for parameters' gradients. */
 size_t mfac_residual_norm_bwd_workspace_bytes(mfac_dtype type, int32_t norms, int64_t rows, int64_t cols);
 mfac_status mfac_residual_norm_bwd(mfac_dtype type, mfac_dtype wtype, int32_t norms, int64_t rows, int64_t cols,
                                    const void* ds, int64_t ldds, const void* dh, int64_t lddh, const void* y,

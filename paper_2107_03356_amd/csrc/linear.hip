@@ -403,7 +403,9 @@ hipError_t launch_product(int dt, const Product& p, const Epilogue& e, void* ws,
         // Rows of W a work-group: the 32 columns of a group in one for an 8-bit copy of z; else so
         // that the work-groups are about as many as CUs. 1024 x 4096, 12 rows: fp32 14.6 us with 16,
         // 13.4 with 8 (a quarter of it the fp32 MFMAs); bf16 9.4 and 8.2. A gated layer has twice the rows of W to
-        // one: 8192 columns, bf16 over 2048, 13.7 us with 16, 14.7 with 32, 17.8 with 8.
+        // one: 8192 columns, bf16 over 2048, 13.5 us with 16, 14.7 with 32, 17.2 with 8. More work-groups than CUs are a second
+        // turn, so 8 end at 2048 columns: bf16 over 2048, one row, 2048 columns 5.6 with 8 and 6.8 with 16, 2304 8.8 and 6.9,
+        // 2816 8.9 and 7.0, 4096 9.3 and 7.0; fp32, 12 rows, 2048 10.6 and 13.0, 2816 17.9 and 13.1.
         if (e.p.q || (!gated && g.N > 16 * CUS)) g.rows = 32;
         else if (g.N <= 8 * CUS) g.rows = 8;
         const unsigned grid = (unsigned)ceil_div(g.N, g.rows);
