@@ -111,3 +111,49 @@ def test_refused_calls_of_residual_norm(dev):
             nn.residual_norm(x, **{**dict(residual=x), **kw})
     with pytest.raises(ValueError):
         nn.residual_norm(x.cpu(), x.cpu())
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_captured_and_checkpointed_steps_share_the_copy(dev, kind):
+    """A training step of blocks with copy8, captured and replayed, and with its blocks checkpointed."""
+    from torch.utils.checkpoint import checkpoint
+
+    from paper_2107_03356_amd import nn
+    say("captured step with copies", kind)
+    torch.manual_seed(7)
+    net = nn.GatedStack(72, 136, 2, kind=kind, copy8=True, post_norm=True, device=dev)
+    x, dy = rand(dev, 1, 40, 72, dtype=BF16), rand(dev, 2, 40, 72, dtype=BF16)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            net(x).backward(dy)
+    torch.cuda.current_stream().wait_stream(side)
+    for v in net.parameters():
+        v.grad = None
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = net(x)
+        y.backward(dy)
+    again = nn.GatedStack(72, 136, 2, kind=kind, copy8=True, post_norm=True, device=dev)
+    again.load_state_dict(net.state_dict())
+    for turn in range(3):
+        x.copy_(rand(dev, 10 + turn, 40, 72))
+        graph.replay()
+        torch.cuda.synchronize()
+        for v in again.parameters():
+            v.grad = None
+        want = again(x)
+        want.backward(dy)
+        assert torch.equal(y, want)
+        assert all(torch.equal(v.grad, u.grad) for v, u in zip(net.parameters(), again.parameters()))
+    block = again.blocks[0]
+    grads = []
+    for reentrant in (None, True, False):
+        leaf = x.clone().requires_grad_()
+        for v in block.parameters():
+            v.grad = None
+        out = block(leaf) if reentrant is None else checkpoint(block, leaf, use_reentrant=reentrant)
+        out.backward(dy)
+        grads.append([leaf.grad] + [v.grad for v in block.parameters()])
+    assert all(torch.equal(a, b) for other in grads[1:] for a, b in zip(grads[0], other))

@@ -126,3 +126,38 @@ def test_gated_feed_forward_backward_of_fp16(dev, rows, dim, hid):
     """The whole backward pass in fp16, against the formulas with dz and a counted as the call rounds them."""
     from test_gpu_gated_ops import test_gated_feed_forward_backward as of_type
     of_type(dev, F16, rows, dim, hid)
+
+
+def test_captured_factors_follow_their_inputs(dev):
+    """A captured pass takes the factors anew at each replay, from small inputs and from large ones."""
+    from paper_2107_03356_amd import nn
+    say("captured factors")
+    rows, dim, hid = 300, 72, 192
+    x, dy = (torch.empty(rows, dim, dtype=F16, device=dev) for _ in range(2))
+    w1, w2 = rand(dev, 1, 2 * hid, dim, dtype=F16, scale=2.0 ** -12), rand(dev, 2, dim, hid, dtype=F16)
+    z = tuple(torch.empty(rows, hid, dtype=F16, device=dev) for _ in range(2))
+
+    def fill(turn):
+        for i, t in enumerate((x, dy, *z)):
+            t.copy_(rand(dev, 10 * turn + i, *t.shape, scale=(1.0, 200.0, 2.0 ** -9, 1000.0)[turn]))
+
+    def run():
+        return nn.gated_feed_forward_backward(dy, x, w1, w2, z, grad_dtype=F32, need=(True, True, False, True, False))
+
+    fill(0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = run()
+    for turn in (1, 2, 3, 0, 3):
+        fill(turn)
+        graph.replay()
+        torch.cuda.synchronize()
+        got, want = [held[i].clone() for i in (0, 1, 3)], run()
+        assert all(torch.equal(a, want[i]) for a, i in zip(got, (0, 1, 3)))
+        # dx is of fp16: with values of 1000 its standard deviation is 8.5e3 * 1e3 * 0.6 * 2^-12 * sqrt(384) = 2.4e4
+        assert torch.isfinite(got[1]).all() and torch.isfinite(got[2]).all()
