@@ -1208,7 +1208,8 @@ class GatedFeedForward(torch.nn.Module):
         return h, copy if copy[0] is not None else None
 
     def forward(self, x):
-        return self.join(self.inner(*self.first(x)), x)[0]
+        h, copy = self.first(x)
+        return self.join(self.inner(h) if copy is None else self.inner(h, copy), x)[0]
 
 
 def _norm_of(module):
@@ -1230,5 +1231,7 @@ class GatedStack(torch.nn.Module):
     def forward(self, x):
         h, copy = self.blocks[0].first(x)
         for block, norm in zip(self.blocks, [b.norm for b in self.blocks[1:]] + [self.norm]):
-            x, h, copy = block.join(block.inner(h, copy), x, norm, want_copy=True)
+            y = block.inner(h) if copy is None else block.inner(h, copy)
+            x, h, *kept = block.join(y, x, norm, want_copy=True) if block.copy8 else block.join(y, x, norm)
+            copy = kept[0] if kept else None
         return h
